@@ -387,6 +387,171 @@ int externd_step_deflate(float* R, int64_t m, int64_t n, const int8_t* U, const 
                          const double* d, int32_t bb, double* colnorm2_out, double* fro2_out,
                          void* workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * Operators of decoding: what runs between and behind the projections that
+ * externd_apply evaluates.  Rotary positions turn q and k, a cache in 4 bits
+ * holds k and v, attention reads it, and the log probabilities of given
+ * tokens judge the result (perplexity).
+ *
+ * Conventions, besides those at the top: `dtype` is one of the codes below
+ * and holds for every array of that type in the call; strides count elements;
+ * the innermost dimension of every array is dense.  All calls are
+ * asynchronous on `stream`, allocate nothing and may be captured into a
+ * graph.  Device contents that the host cannot see (positions, lengths, page
+ * numbers, targets) never lead a kernel outside its arrays: what they would
+ * reach there is left out as each call says.  Outputs are bit-identical from
+ * run to run.
+ */
+#define EXTERND_F32  0
+#define EXTERND_BF16 1
+#define EXTERND_F16  2
+
+/* Rotary frequencies, on the host (no device work).  Pair i of rot_dim / 2
+ * turns by theta_i = base^(-2 i / rot_dim) radians a position.
+ *  scaling  EXTERND_ROPE_PLAIN: as above.
+ *           EXTERND_ROPE_LINEAR: theta_i / factor (positions interpolated).
+ *           EXTERND_ROPE_BASE: base * factor^(rot_dim / (rot_dim - 2)), so that
+ *           the slowest pair is interpolated and the fastest is not.
+ *           EXTERND_ROPE_PARTS: with r_i = original_length theta_i / 2 pi turns
+ *           in the trained context and g_i = clamp((r_i - beta_slow) /
+ *           (beta_fast - beta_slow), 0, 1): theta_i (g_i + (1 - g_i) / factor);
+ *           amplitude 0.1 ln(factor) + 1.
+ *  freqs    host, out: rot_dim / 2 words, theta_i in units of 2^-64 turns.
+ *  amplitude  host, out (may be NULL): the factor on the turned entries.
+ * rot_dim even, 2 .. 1024; base > 1; factor >= 1; original_length >= 1 and
+ * beta_fast > beta_slow for PARTS (ignored otherwise).  Any other word may be
+ * used as a frequency too: a position p turns pair i by p freqs[i] mod 2^64,
+ * which is exact at every position.                                       */
+#define EXTERND_ROPE_PLAIN  0
+#define EXTERND_ROPE_LINEAR 1
+#define EXTERND_ROPE_BASE   2
+#define EXTERND_ROPE_PARTS  3
+int externd_rotary_frequencies(int32_t rot_dim, double base, int32_t scaling, double factor,
+                               int64_t original_length, double beta_fast, double beta_slow, uint64_t* freqs,
+                               double* amplitude);
+
+/* Rotary positions of q and (k may be NULL) k: with phi = positions[t] theta_i,
+ *   a' = amplitude (a cos phi - b sin phi),  b' = amplitude (b cos phi + a sin phi)
+ * for the pairs (a, b) = entries (i, i + rot_dim / 2) of each head
+ * (interleaved = 0) or (2 i, 2 i + 1) (interleaved = 1), i < rot_dim / 2;
+ * entries from rot_dim on are copied.  inverse = 1 turns by -phi: the gradient
+ * of the same call.  The arithmetic is fp32, rounded once to dtype.
+ *  q, q_out   device, tokens x heads_q x head_dim with the given strides; q_out
+ *             may be q with the same strides (in place), and no other overlap.
+ *  positions  device int64[tokens], any value; freqs device uint64[rot_dim / 2].
+ * head_dim 2 .. 1024, rot_dim even, 2 .. head_dim; tokens 0 is a valid call;
+ * tokens < 2^31, heads <= 65535.                                          */
+int externd_rotary(const void* q, void* q_out, int64_t q_token_stride, int64_t q_head_stride,
+                   int64_t q_out_token_stride, int64_t q_out_head_stride, int32_t heads_q, const void* k,
+                   void* k_out, int64_t k_token_stride, int64_t k_head_stride, int64_t k_out_token_stride,
+                   int64_t k_out_head_stride, int32_t heads_k, int32_t dtype, int64_t tokens, int32_t head_dim,
+                   int32_t rot_dim, int32_t interleaved, int32_t inverse, const int64_t* positions,
+                   const uint64_t* freqs, float amplitude, void* stream);
+
+/*
+ * The cache in 4 bits.  Pages of page_tokens tokens (a power of two, 16 ..
+ * 1024); a page holds, for each of heads_kv heads, externd_kv4_page_bytes()
+ * bytes: with P = page_tokens, D = head_dim (64, 128 or 256), H = D / 2,
+ *   K codes  [P][H]          byte i: channel i (low nibble), i + H (high)
+ *   V codes  [P / 16][H][16] the same bytes, tokens of a block side by side
+ *   words    [P][2][D / 64]  uint16, K's then V's, one per 64 channels: an
+ *                            fp16 scale s whose low four bits hold the zero
+ *                            point z.  A value is s (code - z).
+ * For 64 values x with lo = min(x, 0), hi = max(x, 0): s is (hi - lo) / 15
+ * rounded up to seven significant bits (to a multiple of 2^-20 below 2^-14),
+ * at most 4352; z = round(-lo / s), code = round(x / s) + z in 0 .. 15.  Every
+ * value is exactly an fp16 number, and within s / 2 of x (s (1 + 2^-20) / 2
+ * with the rounding of x / s) while hi - lo <= 65280.  64 values with an
+ * infinity or a NaN among them are all held as NaN.
+ *
+ * Sequences: the cache belongs to `batch` sequences.  Device int32 lens[batch]
+ * is the number of tokens in each, the new ones of this step included; token
+ * position p of sequence b is in page table[b table_pages + p / P] at p % P.
+ * Device int32 starts[batch + 1] (rising from 0 to `tokens`) says where the
+ * new tokens of each sequence are in the call's arrays; NULL: one token each
+ * (tokens = batch).  The new tokens are the last ones: token i of a sequence's
+ * n new ones is at position lens - n + i.  Lengths above table_pages P count
+ * as that much, positions below 0 are in no sequence, and page numbers outside
+ * [0, num_pages) name pages without tokens.
+ */
+size_t externd_kv4_page_bytes(int32_t head_dim, int32_t page_tokens);  /* of one head; 0 on invalid arguments */
+
+/* Stores the new tokens' k and v (device, tokens x heads_kv x head_dim).
+ * Tokens whose position or page is none are not stored.  cache: device, 16-byte
+ * aligned, num_pages x heads_kv x externd_kv4_page_bytes() bytes.  Two tokens
+ * of one call must not share a place.  tokens, num_pages <= 2^31 - 1.     */
+int externd_kv4_append(void* cache, int64_t num_pages, int32_t heads_kv, int32_t head_dim, int32_t page_tokens,
+                       const void* k, const void* v, int32_t dtype, int64_t k_token_stride, int64_t k_head_stride,
+                       int64_t v_token_stride, int64_t v_head_stride, int64_t tokens, int32_t batch,
+                       const int32_t* starts, const int32_t* lens, const int32_t* table, int64_t table_pages,
+                       void* stream);
+
+/* The values held for the new tokens (with starts over whole sequences: for
+ * all tokens), dense, as dtype; 0 where a token has no place.             */
+int externd_kv4_read(const void* cache, int64_t num_pages, int32_t heads_kv, int32_t head_dim, int32_t page_tokens,
+                     void* k, void* v, int32_t dtype, int64_t tokens, int32_t batch, const int32_t* starts,
+                     const int32_t* lens, const int32_t* table, int64_t table_pages, void* stream);
+
+/* Attention of the new tokens over the cache: with the values k^, v^ held,
+ * for query head h (cache head h heads_kv / heads_q) of a token at position p,
+ *   x_j = scale q . k^_j,  out = sum_j softmax(x)_j v^_j,  lse = ln sum_j exp x_j
+ * over the positions j <= p, and j > p - window where window > 0.  No such j
+ * (an empty sequence, a position below 0, pages without tokens): out 0 and
+ * lse -infinity.
+ *  q          device, tokens x heads_q x head_dim; out device, dense, the same.
+ *  lse        device fp32, tokens x heads_q, or NULL.
+ *  max_new    the largest number of new tokens of one sequence, or more.
+ *  max_len    the largest length, or more; 0: not known.  Both only choose
+ *             the launch: results hold whatever they are.
+ *  heads_q a multiple of heads_kv, heads_q / heads_kv <= 64; scale finite;
+ *  window >= 0; batch <= 65535.
+ *  workspace  device, >= externd_kv4_attention_workspace_bytes() bytes for the
+ *             same sizes, 256-byte aligned (may be NULL where that is 0).
+ * A NaN or an infinity in q makes that row NaN; NaN values make those rows
+ * NaN that see them.                                                       */
+size_t externd_kv4_attention_workspace_bytes(int32_t heads_q, int32_t heads_kv, int32_t head_dim, int32_t dtype,
+                                             int64_t tokens, int32_t batch, int32_t max_new, int64_t max_len);
+int externd_kv4_attention(const void* cache, int64_t num_pages, int32_t heads_kv, int32_t head_dim,
+                          int32_t page_tokens, const void* q, int32_t dtype, int64_t q_token_stride,
+                          int64_t q_head_stride, int32_t heads_q, void* out, float* lse, int64_t tokens,
+                          int32_t batch, int32_t max_new, int64_t max_len, const int32_t* starts,
+                          const int32_t* lens, const int32_t* table, int64_t table_pages, float scale,
+                          int32_t window, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Log probabilities of given tokens: with z = scale x of each row,
+ *   lse = ln sum_v exp z_v,  logprob = z_target - lse,
+ *   entropy = lse - sum_v p_v z_v,  p = exp(z - lse),
+ * and the `top` largest logits, the lower index first among equal ones (a NaN
+ * with its sign clear counts above all): their indices and z - lse.
+ *  logits     device, rows x vocab, row_stride >= vocab.
+ *  targets    device int64[rows], or NULL with logprob NULL.  Below 0: no token
+ *             is asked for, logprob 0.  vocab or more: logprob NaN.
+ *  scale      finite, > 0 (1 / temperature).
+ *  top        0 .. EXTERND_LOGPROBS_MAX_TOP, at most vocab; top_logprobs device
+ *             fp32 and top_ids device int64, rows x top (NULL with top = 0).
+ *  entropy, lse  device fp32[rows], each may be NULL.
+ *  workspace  device, 256-byte aligned (may be NULL where no bytes are needed).
+ * A row of nothing but -infinity: lse and log probabilities -infinity, entropy
+ * 0.  A NaN or +infinity makes a row's lse, entropy and log probabilities NaN.
+ * Sums are fp32 over at most 2^31 - 1 entries a row.                        */
+#define EXTERND_LOGPROBS_MAX_TOP 64
+size_t externd_token_logprobs_workspace_bytes(int64_t rows, int64_t vocab, int32_t top);
+int externd_token_logprobs(const void* logits, int32_t dtype, int64_t rows, int64_t vocab, int64_t row_stride,
+                           const int64_t* targets, float scale, int32_t top, float* logprob, float* entropy,
+                           float* lse, float* top_logprobs, int64_t* top_ids, void* workspace,
+                           size_t workspace_bytes, void* stream);
+
+/* Gradient of the above for the logits:
+ *   grad_v = scale [ g_logprob ([v = target] - p_v) - g_entropy p_v (ln p_v + entropy) ]
+ * with the forward call's lse and entropy; g_logprob counts as 0 where a row
+ * has no target.  Either gradient may be NULL (0); entropy may be NULL with
+ * g_entropy.  grad: device, rows x vocab of dtype with its own row stride; it
+ * may be `logits` itself with the same stride.  Where p_v = 0 the entry is 0. */
+int externd_token_logprobs_backward(const void* logits, int32_t dtype, int64_t rows, int64_t vocab,
+                                    int64_t row_stride, const int64_t* targets, float scale, const float* lse,
+                                    const float* entropy, const float* g_logprob, const float* g_entropy,
+                                    void* grad, int64_t grad_row_stride, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

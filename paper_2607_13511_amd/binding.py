@@ -65,6 +65,27 @@ _SIGNATURES = {
                                           _c_ptr, _c_size, _c_ptr]),
     "externd_step_deflate": (ctypes.c_int, [_c_ptr, _c_i64, _c_i64, _c_ptr, _c_ptr, _c_ptr, _c_i32,
                                             _c_ptr, _c_ptr, _c_ptr, _c_size, _c_ptr]),
+    "externd_rotary_frequencies": (ctypes.c_int, [_c_i32, _c_dbl, _c_i32, _c_dbl, _c_i64, _c_dbl, _c_dbl, _c_ptr,
+                                                  _c_ptr]),
+    "externd_rotary": (ctypes.c_int, [_c_ptr, _c_ptr, _c_i64, _c_i64, _c_i64, _c_i64, _c_i32, _c_ptr, _c_ptr, _c_i64,
+                                      _c_i64, _c_i64, _c_i64, _c_i32, _c_i32, _c_i64, _c_i32, _c_i32, _c_i32, _c_i32,
+                                      _c_ptr, _c_ptr, ctypes.c_float, _c_ptr]),
+    "externd_kv4_page_bytes": (_c_size, [_c_i32, _c_i32]),
+    "externd_kv4_append": (ctypes.c_int, [_c_ptr, _c_i64, _c_i32, _c_i32, _c_i32, _c_ptr, _c_ptr, _c_i32, _c_i64,
+                                          _c_i64, _c_i64, _c_i64, _c_i64, _c_i32, _c_ptr, _c_ptr, _c_ptr, _c_i64,
+                                          _c_ptr]),
+    "externd_kv4_read": (ctypes.c_int, [_c_ptr, _c_i64, _c_i32, _c_i32, _c_i32, _c_ptr, _c_ptr, _c_i32, _c_i64,
+                                        _c_i32, _c_ptr, _c_ptr, _c_ptr, _c_i64, _c_ptr]),
+    "externd_kv4_attention_workspace_bytes": (_c_size, [_c_i32, _c_i32, _c_i32, _c_i32, _c_i64, _c_i32, _c_i32,
+                                                        _c_i64]),
+    "externd_kv4_attention": (ctypes.c_int, [_c_ptr, _c_i64, _c_i32, _c_i32, _c_i32, _c_ptr, _c_i32, _c_i64, _c_i64,
+                                             _c_i32, _c_ptr, _c_ptr, _c_i64, _c_i32, _c_i32, _c_i64, _c_ptr, _c_ptr,
+                                             _c_ptr, _c_i64, ctypes.c_float, _c_i32, _c_ptr, _c_size, _c_ptr]),
+    "externd_token_logprobs_workspace_bytes": (_c_size, [_c_i64, _c_i64, _c_i32]),
+    "externd_token_logprobs": (ctypes.c_int, [_c_ptr, _c_i32, _c_i64, _c_i64, _c_i64, _c_ptr, ctypes.c_float, _c_i32,
+                                              _c_ptr, _c_ptr, _c_ptr, _c_ptr, _c_ptr, _c_ptr, _c_size, _c_ptr]),
+    "externd_token_logprobs_backward": (ctypes.c_int, [_c_ptr, _c_i32, _c_i64, _c_i64, _c_i64, _c_ptr, ctypes.c_float,
+                                                       _c_ptr, _c_ptr, _c_ptr, _c_ptr, _c_ptr, _c_i64, _c_ptr]),
 }
 EXPORTED = tuple(_SIGNATURES)
 
@@ -457,6 +478,320 @@ def step_deflate(R, U, V, d, stream=None):
                                     _dev_ptr(fro), _dev_ptr(ws), ws.numel(), _stream_ptr(torch, stream))
     _check(st, "externd_step_deflate")
     return col, fro
+
+
+# ---------------------------------------------------------------------------
+# operators of decoding: rotary positions, the 4-bit cache and attention over
+# it, log probabilities of given tokens
+# ---------------------------------------------------------------------------
+ROPE_SCALINGS = ("plain", "linear", "base", "parts")   # EXTERND_ROPE_*
+LOGPROBS_MAX_TOP = 64                                  # EXTERND_LOGPROBS_MAX_TOP
+_dtype_codes = None   # torch dtype -> EXTERND_F32, _BF16, _F16
+
+
+def _dtype_code(torch, dtype, name) -> int:
+    global _dtype_codes
+    if _dtype_codes is None:
+        _dtype_codes = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+    code = _dtype_codes.get(dtype)
+    if code is None:
+        raise ValueError(f"{name}: expected float32, bfloat16 or float16, got {dtype}")
+    return code
+
+
+def _req_heads(t, dtype, tokens, name):
+    """A CUDA tensor (tokens, heads, channels) of dtype whose channels are dense; returns its token and head strides."""
+    if not (t.is_cuda and t.dtype is dtype and t.dim() == 3 and t.shape[0] == tokens):
+        raise ValueError(f"{name}: expected a {dtype} CUDA tensor of shape ({tokens}, heads, channels), "
+                         f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+    ts, hs, cs = t.stride()
+    if cs != 1 and t.shape[2] > 1:
+        raise ValueError(f"{name}: the channels of a head must be dense, got strides {t.stride()}")
+    return ts, hs
+
+
+def rotary_frequencies(rot_dim: int, base: float = 10000.0, scaling: str = "plain", factor: float = 1.0,
+                       original_length: int = 0, beta_fast: float = 32.0, beta_slow: float = 1.0):
+    """Frequencies of the rot_dim / 2 pairs as an int64 numpy array in units
+    of 2^-64 turns a position, and the amplitude of the turned entries
+    (externd_rotary_frequencies).  Needs no GPU."""
+    if scaling not in ROPE_SCALINGS:
+        raise ValueError(f"scaling: expected one of {ROPE_SCALINGS}, got {scaling!r}")
+    freqs = np.zeros(max(rot_dim // 2, 1), dtype=np.int64)
+    amplitude = ctypes.c_double(0.0)
+    _check(lib().externd_rotary_frequencies(rot_dim, base, ROPE_SCALINGS.index(scaling), factor, original_length,
+                                            beta_fast, beta_slow, freqs.ctypes.data, ctypes.byref(amplitude)),
+           "externd_rotary_frequencies")
+    return freqs, amplitude.value
+
+
+def _rotary(q, k, positions, freqs, interleaved, amplitude, inverse, out, stream):
+    torch = _torch()
+    if q.dim() != 3:
+        raise ValueError(f"q: expected (tokens, heads, channels), got shape {tuple(q.shape)}")
+    tokens, heads, dim = q.shape
+    code = _dtype_code(torch, q.dtype, "q")
+    qs = _req_heads(q, q.dtype, tokens, "q")
+    _req(positions, torch, torch.int64, (tokens,), "positions")
+    _req(freqs, torch, torch.int64, (freqs.numel(),), "freqs")
+    qo, ko = out if out is not None else (torch.empty((tokens, heads, dim), dtype=q.dtype, device=q.device), None)
+    qos = _req_heads(qo, q.dtype, tokens, "q out")
+    if qo.shape != q.shape:
+        raise ValueError(f"q out: expected shape {tuple(q.shape)}, got {tuple(qo.shape)}")
+    ks = kos = (0, 0)
+    kp = kop = None
+    kh = 0
+    if k is not None:
+        ks = _req_heads(k, q.dtype, tokens, "k")
+        kh = k.shape[1]
+        if k.shape[2] != dim:
+            raise ValueError(f"k: expected {dim} channels a head, got {k.shape[2]}")
+        if out is None:
+            ko = torch.empty((tokens, kh, dim), dtype=q.dtype, device=q.device)
+        elif ko is None or ko.shape != k.shape:
+            raise ValueError(f"k out: expected shape {tuple(k.shape)}")
+        kos = _req_heads(ko, q.dtype, tokens, "k out")
+        kp, kop = k.data_ptr(), ko.data_ptr()
+    if tokens:
+        st = lib().externd_rotary(q.data_ptr(), qo.data_ptr(), qs[0], qs[1], qos[0], qos[1], heads, kp, kop, ks[0],
+                                  ks[1], kos[0], kos[1], kh, code, tokens, dim, 2 * freqs.numel(), int(interleaved),
+                                  inverse, positions.data_ptr(), freqs.data_ptr(), amplitude,
+                                  _stream_ptr(torch, stream))
+        if st != OK:
+            raise ExterndError(st, "externd_rotary")
+    return qo, ko
+
+
+def rotary(q, k, positions, freqs, interleaved: bool = False, amplitude: float = 1.0, out=None, stream=None):
+    """q and k (tokens x heads x channels; k may be None) turned to their
+    int64 positions (externd_rotary).  ``freqs``: CUDA int64, as
+    ``rotary_frequencies`` gives them; the first 2 * len(freqs) channels of a
+    head are turned.  ``out``: (q_out, k_out), which may be (q, k) themselves.
+    Returns (q', k')."""
+    return _rotary(q, k, positions, freqs, interleaved, amplitude, 0, out, stream)
+
+
+def rotary_backward(grad_q, grad_k, positions, freqs, interleaved: bool = False, amplitude: float = 1.0, out=None,
+                    stream=None):
+    """Gradients for q and k from those of ``rotary``'s results: the inverse
+    turn with the same amplitude (externd_rotary)."""
+    return _rotary(grad_q, grad_k, positions, freqs, interleaved, amplitude, 1, out, stream)
+
+
+def kv4_cache(num_pages: int, heads_kv: int, head_dim: int, page_tokens: int, device="cuda"):
+    """An empty cache in 4 bits: uint8 (num_pages, heads_kv, bytes of a page
+    and head)."""
+    torch = _torch()
+    nbytes = lib().externd_kv4_page_bytes(head_dim, page_tokens)
+    if nbytes == 0:
+        raise ExterndError(EINVAL, "externd_kv4_page_bytes")
+    return torch.zeros((num_pages, heads_kv, nbytes), dtype=torch.uint8, device=device)
+
+
+def _kv4_args(torch, cache, head_dim, tokens, table, lens, starts):
+    """(num_pages, heads, page tokens, batch, starts pointer) of a call on a cache."""
+    if not (cache.is_cuda and cache.dtype is torch.uint8 and cache.dim() == 3 and cache.is_contiguous()):
+        raise ValueError(f"cache: expected a contiguous uint8 CUDA tensor (pages, heads, bytes), got {cache.dtype} "
+                         f"{tuple(cache.shape)} on {cache.device}")
+    pages, heads, nbytes = cache.shape
+    per = head_dim + head_dim // 16
+    if head_dim not in (64, 128, 256) or nbytes % per:
+        raise ValueError(f"cache: {nbytes} bytes a page and head are no whole number of tokens of {head_dim} channels")
+    batch = lens.numel()
+    _req(lens, torch, torch.int32, (batch,), "lens")
+    if not (table.is_cuda and table.dtype is torch.int32 and table.dim() == 2 and table.shape[0] == batch
+            and table.is_contiguous()):
+        raise ValueError(f"table: expected a contiguous int32 CUDA tensor ({batch}, pages), got {table.dtype} "
+                         f"{tuple(table.shape)} on {table.device}")
+    sp = None
+    if starts is not None:
+        _req(starts, torch, torch.int32, (batch + 1,), "starts")
+        sp = starts.data_ptr()
+    elif tokens != batch:
+        raise ValueError(f"without starts there is one new token a sequence: {tokens} tokens, {batch} sequences")
+    return pages, heads, nbytes // per, batch, sp
+
+
+def kv4_append(cache, k, v, table, lens, starts=None, stream=None):
+    """Stores k and v (new tokens x cache heads x channels) in the cache, in
+    place (externd_kv4_append).  ``lens`` int32: tokens of each sequence with
+    the new ones; ``table`` int32 (sequences, pages): their pages; ``starts``
+    int32 (sequences + 1): where each sequence's new tokens are, or None for
+    one each."""
+    torch = _torch()
+    if k.dim() != 3 or v.shape != k.shape:
+        raise ValueError(f"k, v: expected the same (tokens, heads, channels), got {tuple(k.shape)} and {tuple(v.shape)}")
+    tokens, heads, dim = k.shape
+    pages, kv, page, batch, sp = _kv4_args(torch, cache, dim, tokens, table, lens, starts)
+    if heads != kv:
+        raise ValueError(f"k, v: expected the cache's {kv} heads, got {heads}")
+    code = _dtype_code(torch, k.dtype, "k")
+    ks, vs = _req_heads(k, k.dtype, tokens, "k"), _req_heads(v, k.dtype, tokens, "v")
+    if tokens:
+        st = lib().externd_kv4_append(cache.data_ptr(), pages, kv, dim, page, k.data_ptr(), v.data_ptr(), code, ks[0],
+                                      ks[1], vs[0], vs[1], tokens, batch, sp, lens.data_ptr(), table.data_ptr(),
+                                      table.shape[1], _stream_ptr(torch, stream))
+        if st != OK:
+            raise ExterndError(st, "externd_kv4_append")
+
+
+def kv4_read(cache, table, lens, head_dim: int, starts=None, tokens=None, dtype=None, stream=None):
+    """K and V (tokens x cache heads x channels) as the cache holds them for
+    the new tokens that ``starts`` (and their number ``tokens``) names; with
+    starts over whole sequences, for all tokens (externd_kv4_read)."""
+    torch = _torch()
+    if tokens is None:
+        if starts is not None:
+            raise ValueError("tokens: their number is needed with starts")
+        tokens = lens.numel()
+    dtype = torch.float32 if dtype is None else dtype
+    pages, kv, page, batch, sp = _kv4_args(torch, cache, head_dim, tokens, table, lens, starts)
+    code = _dtype_code(torch, dtype, "dtype")
+    k = torch.empty((tokens, kv, head_dim), dtype=dtype, device=cache.device)
+    v = torch.empty((tokens, kv, head_dim), dtype=dtype, device=cache.device)
+    if tokens:
+        st = lib().externd_kv4_read(cache.data_ptr(), pages, kv, head_dim, page, k.data_ptr(), v.data_ptr(), code,
+                                    tokens, batch, sp, lens.data_ptr(), table.data_ptr(), table.shape[1],
+                                    _stream_ptr(torch, stream))
+        if st != OK:
+            raise ExterndError(st, "externd_kv4_read")
+    return k, v
+
+
+def kv4_attention_workspace_bytes(heads_q: int, heads_kv: int, head_dim: int, dtype, tokens: int, batch: int,
+                                  max_new: int = 1, max_len: int = 0) -> int:
+    return int(lib().externd_kv4_attention_workspace_bytes(heads_q, heads_kv, head_dim,
+                                                           _dtype_code(_torch(), dtype, "dtype"), tokens, batch,
+                                                           max_new, max_len))
+
+
+def kv4_attention(cache, q, table, lens, starts=None, max_new=None, max_len=None, scale=None, window: int = 0, out=None,
+                  stream=None, workspace=None):
+    """Attention of the new tokens' q (tokens x query heads x channels) over
+    the cache, causal, within ``window`` positions where that is above 0
+    (externd_kv4_attention).  ``max_new``, ``max_len``: the most new tokens
+    and the greatest length of a sequence where the caller knows them (they
+    choose the launch only); ``scale``: 1 / sqrt(channels) unless given.
+    Returns (out, lse): tokens x query heads x channels in q's type, and fp32
+    tokens x query heads."""
+    torch = _torch()
+    if q.dim() != 3:
+        raise ValueError(f"q: expected (tokens, heads, channels), got shape {tuple(q.shape)}")
+    tokens, heads, dim = q.shape
+    pages, kv, page, batch, sp = _kv4_args(torch, cache, dim, tokens, table, lens, starts)
+    code = _dtype_code(torch, q.dtype, "q")
+    qs = _req_heads(q, q.dtype, tokens, "q")
+    if out is None:
+        out = torch.empty((tokens, heads, dim), dtype=q.dtype, device=q.device)
+    else:
+        _req(out, torch, q.dtype, (tokens, heads, dim), "out")
+    lse = torch.empty((tokens, heads), dtype=torch.float32, device=q.device)
+    if not tokens:
+        return out, lse
+    if max_new is None:
+        max_new = 1 if sp is None else tokens
+    if max_len is None:
+        max_len = table.shape[1] * page
+    if scale is None:
+        scale = dim ** -0.5
+    L = lib()
+    nbytes = L.externd_kv4_attention_workspace_bytes(heads, kv, dim, code, tokens, batch, max_new, max_len)
+    wp = None
+    if workspace is not None:
+        wp, nbytes = workspace.data_ptr(), workspace.numel()
+    elif nbytes:
+        workspace = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
+        wp = workspace.data_ptr()
+    st = L.externd_kv4_attention(cache.data_ptr(), pages, kv, dim, page, q.data_ptr(), code, qs[0], qs[1], heads,
+                                 out.data_ptr(), lse.data_ptr(), tokens, batch, max_new, max_len, sp, lens.data_ptr(),
+                                 table.data_ptr(), table.shape[1], scale, window, wp, nbytes,
+                                 _stream_ptr(torch, stream))
+    if st != OK:
+        raise ExterndError(st, "externd_kv4_attention")
+    return out, lse
+
+
+@dataclass
+class TokenLogprobs:
+    logprob: "object"          # torch.float32 (rows,): of the targets; 0 where none is asked for
+    entropy: "object"          # torch.float32 (rows,)
+    lse: "object"              # torch.float32 (rows,)
+    top_logprobs: "object"     # torch.float32 (rows, top), the largest first
+    top_ids: "object"          # torch.int64 (rows, top)
+
+
+def _req_logits(torch, t, name):
+    if not (t.is_cuda and t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1)):
+        raise ValueError(f"{name}: expected a CUDA tensor (rows, vocabulary) with dense rows, got {t.dtype} "
+                         f"{tuple(t.shape)} {t.stride()} on {t.device}")
+    rows, vocab = t.shape
+    return rows, vocab, t.stride(0) if rows > 1 else vocab, _dtype_code(torch, t.dtype, name)
+
+
+def token_logprobs(logits, targets=None, top: int = 0, scale: float = 1.0, stream=None,
+                   workspace=None) -> TokenLogprobs:
+    """Log probabilities of the int64 ``targets`` (rows; below 0: none asked
+    for) under the softmax of ``scale * logits`` (rows x vocabulary), each
+    row's entropy, and its ``top`` most likely tokens, the lower index first
+    among equals (externd_token_logprobs).  Without targets logprob is None."""
+    torch = _torch()
+    rows, vocab, stride, code = _req_logits(torch, logits, "logits")
+    dev = logits.device
+    logprob = tp = lp = None
+    if targets is not None:
+        _req(targets, torch, torch.int64, (rows,), "targets")
+        logprob = torch.empty((rows,), dtype=torch.float32, device=dev)
+        tp, lp = targets.data_ptr(), logprob.data_ptr()
+    if not 0 <= top <= min(LOGPROBS_MAX_TOP, vocab):
+        raise ExterndError(EINVAL, "externd_token_logprobs")
+    entropy = torch.empty((rows,), dtype=torch.float32, device=dev)
+    lse = torch.empty((rows,), dtype=torch.float32, device=dev)
+    vals = torch.empty((rows, top), dtype=torch.float32, device=dev)
+    ids = torch.empty((rows, top), dtype=torch.int64, device=dev)
+    if rows:
+        L = lib()
+        nbytes = L.externd_token_logprobs_workspace_bytes(rows, vocab, top)
+        wp = None
+        if workspace is not None:
+            wp, nbytes = workspace.data_ptr(), workspace.numel()
+        elif nbytes:
+            workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+            wp = workspace.data_ptr()
+        st = L.externd_token_logprobs(logits.data_ptr(), code, rows, vocab, stride, tp, scale, top, lp,
+                                      entropy.data_ptr(), lse.data_ptr(), vals.data_ptr() if top else None,
+                                      ids.data_ptr() if top else None, wp, nbytes, _stream_ptr(torch, stream))
+        if st != OK:
+            raise ExterndError(st, "externd_token_logprobs")
+    return TokenLogprobs(logprob, entropy, lse, vals, ids)
+
+
+def token_logprobs_backward(logits, targets, lse, entropy, grad_logprob=None, grad_entropy=None, scale: float = 1.0,
+                            out=None, stream=None):
+    """Gradient for the logits from those of ``token_logprobs``'s logprob and
+    entropy (externd_token_logprobs_backward); ``out`` may be the logits
+    themselves.  Returns it (rows x vocabulary, the logits' type)."""
+    torch = _torch()
+    rows, vocab, stride, code = _req_logits(torch, logits, "logits")
+    ptrs = [None] * 5
+    for i, (t, dt, name) in enumerate(((targets, torch.int64, "targets"), (lse, torch.float32, "lse"),
+                                       (entropy, torch.float32, "entropy"),
+                                       (grad_logprob, torch.float32, "grad_logprob"),
+                                       (grad_entropy, torch.float32, "grad_entropy"))):
+        if t is not None:
+            _req(t, torch, dt, (rows,), name)
+            ptrs[i] = t.data_ptr()
+    if out is None:
+        out = torch.empty((rows, vocab), dtype=logits.dtype, device=logits.device)
+    orows, ovocab, ostride, _ = _req_logits(torch, out, "out")
+    if (orows, ovocab) != (rows, vocab) or out.dtype is not logits.dtype:
+        raise ValueError(f"out: expected {logits.dtype} of shape {(rows, vocab)}, got {out.dtype} {tuple(out.shape)}")
+    if rows:
+        st = lib().externd_token_logprobs_backward(logits.data_ptr(), code, rows, vocab, stride, ptrs[0], scale,
+                                                   ptrs[1], ptrs[2], ptrs[3], ptrs[4], out.data_ptr(), ostride,
+                                                   _stream_ptr(torch, stream))
+        if st != OK:
+            raise ExterndError(st, "externd_token_logprobs_backward")
+    return out
 
 
 # ---------------------------------------------------------------------------

@@ -15,7 +15,8 @@ CSRC = os.path.join(PKG_DIR, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB_NAME = "libexternd.so"
 LIB_PATH = os.path.join(PKG_DIR, LIB_NAME)
-SOURCES = ["externd_kernels.hip", "externd_api.hip", "externd_apply.hip", "externd_seq.hip"]
+SOURCES = ["externd_kernels.hip", "externd_api.hip", "externd_apply.hip", "externd_seq.hip", "externd_rotary.hip",
+           "externd_kv4.hip", "externd_kv4_attention.hip", "externd_logprobs.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"

@@ -1,0 +1,93 @@
+// What the decoding operators share: the three storage types, where a new
+// token is, and where a cache keeps it.
+#pragma once
+
+#include <hip/hip_fp16.h>
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "externd.h"
+
+namespace externd {
+
+inline bool dtype_ok(int32_t d) { return d == EXTERND_F32 || d == EXTERND_BF16 || d == EXTERND_F16; }
+inline int dtype_bytes(int32_t d) { return d == EXTERND_F32 ? 4 : 2; }
+
+// Storage type of a dtype code, widened to and rounded from fp32 (to nearest,
+// ties to even; a NaN stays one).
+template <int DT> struct Elem;
+template <> struct Elem<EXTERND_F32> {
+  typedef float T;
+  static __device__ __forceinline__ float load(float v) { return v; }
+  static __device__ __forceinline__ float store(float v) { return v; }
+};
+template <> struct Elem<EXTERND_F16> {
+  typedef _Float16 T;
+  static __device__ __forceinline__ float load(_Float16 v) { return (float)v; }
+  static __device__ __forceinline__ _Float16 store(float v) { return (_Float16)v; }
+};
+template <> struct Elem<EXTERND_BF16> {
+  typedef __bf16 T;
+  static __device__ __forceinline__ float load(__bf16 v) {
+    return __uint_as_float((unsigned)__builtin_bit_cast(uint16_t, v) << 16);
+  }
+  static __device__ __forceinline__ __bf16 store(float v) { return (__bf16)v; }
+};
+
+// The cache's layout for one page size and head width (include/externd.h).
+struct Kv4Shape {
+  int64_t num_pages;
+  int heads, dim, page_log2;
+  int64_t head_bytes;   // of one head of one page
+};
+constexpr int KV4_GROUP = 64;          // channels that share a scale
+constexpr float KV4_SCALE_MAX = 4352.f;
+constexpr unsigned KV4_NAN = 0x7E00u;  // word of a group that held a NaN or an infinity
+
+struct Kv4Sequences {
+  const int32_t* starts;
+  const int32_t* lens;
+  const int32_t* table;
+  int64_t table_pages, tokens;
+  int batch;
+};
+
+// The sequence of new token t: the last b with starts[b] <= t.
+__device__ __forceinline__ int sequence_of(const Kv4Sequences& s, int64_t t) {
+  if (!s.starts) return (int)t;
+  int lo = 0, hi = s.batch - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (s.starts[mid] <= t) lo = mid; else hi = mid - 1;
+  }
+  return lo;
+}
+
+// Position of new token t of sequence b; below 0: none.
+__device__ __forceinline__ int64_t position_of(const Kv4Sequences& s, int b, int64_t t) {
+  const int64_t end = s.starts ? s.starts[b + 1] : b + 1;
+  return (int64_t)s.lens[b] - (end - t);
+}
+
+// Page of position p of sequence b, or -1.
+__device__ __forceinline__ int64_t page_of(const Kv4Shape& c, const Kv4Sequences& s, int b, int64_t p) {
+  if (p < 0) return -1;
+  const int64_t i = p >> c.page_log2;
+  if (i >= s.table_pages) return -1;
+  const int64_t page = s.table[(int64_t)b * s.table_pages + i];
+  return page >= 0 && page < c.num_pages ? page : -1;
+}
+
+// Fills the shape; false where the arguments are not a cache's.
+inline bool kv4_shape(int64_t num_pages, int32_t heads, int32_t dim, int32_t page_tokens, Kv4Shape* c) {
+  const size_t bytes = externd_kv4_page_bytes(dim, page_tokens);
+  if (!bytes || num_pages < 1 || num_pages > INT32_MAX || heads < 1 || heads > 4096) return false;
+  c->num_pages = num_pages;
+  c->heads = heads;
+  c->dim = dim;
+  c->page_log2 = __builtin_ctz((unsigned)page_tokens);
+  c->head_bytes = (int64_t)bytes;
+  return true;
+}
+
+}  // namespace externd

@@ -1,0 +1,200 @@
+"""Host side of the decoding operators (no GPU needed): the rotary
+frequencies, the cache's sizes, refusals before any device work, and the
+oracle's own forms against brute force and differences."""
+import ctypes
+import math
+
+import numpy as np
+import pytest
+
+import oracle.decode_oracle as ref
+from paper_2607_13511_amd import binding
+
+D256 = ctypes.c_void_p(256)          # never dereferenced: validation fails first
+
+
+@pytest.mark.parametrize("rot,base,scaling,kw", [
+    (128, 1e4, "plain", {}), (64, 1e6, "linear", {"factor": 4.0}), (128, 5e5, "base", {"factor": 8.0}),
+    (96, 1e4, "parts", {"factor": 4.0, "original_length": 4096}), (2, 1e4, "plain", {}), (114, 1e4, "linear", {"factor": 1.0}),
+    (128, 1e4, "parts", {"factor": 16.0, "original_length": 8192, "beta_fast": 24.0, "beta_slow": 2.0})])
+def test_rotary_frequencies(rot, base, scaling, kw):
+    freqs, amplitude = binding.rotary_frequencies(rot, base, scaling, **kw)
+    theta, want = ref.rotary_theta(rot, base, scaling, **kw)
+    assert freqs.shape == (rot // 2,) and freqs.dtype == np.int64
+    # the words are whole numbers: half a unit of 2^-64 turns; fp64 powers of the reference: 1e-14 relative
+    assert np.allclose(freqs.astype(np.float64) / 2.0 ** 64 * 2 * math.pi, theta, rtol=1e-14, atol=math.pi * 2.0 ** -64)
+    assert amplitude == pytest.approx(want, rel=1e-15)
+
+
+def test_rotary_frequencies_refuses():
+    for args in [(0, 1e4), (3, 1e4), (1026, 1e4), (64, 1.0), (64, float("nan")), (64, float("inf"))]:
+        with pytest.raises(binding.ExterndError) as e:
+            binding.rotary_frequencies(*args)
+        assert e.value.status == binding.EINVAL
+    for kw in [dict(scaling="linear", factor=0.5), dict(scaling="base", factor=float("nan")),
+               dict(scaling="parts", factor=2.0), dict(scaling="parts", factor=2.0, original_length=8, beta_fast=1.0)]:
+        with pytest.raises(binding.ExterndError):
+            binding.rotary_frequencies(64, 1e4, **kw)
+    with pytest.raises(binding.ExterndError):
+        binding.rotary_frequencies(2, 1e4, scaling="base", factor=2.0)     # no slowest pair beside the fastest
+    with pytest.raises(ValueError):
+        binding.rotary_frequencies(64, 1e4, scaling="other")
+
+
+def test_page_bytes():
+    f = binding.lib().externd_kv4_page_bytes
+    for dim in (64, 128, 256):
+        for page in (16, 32, 256, 1024):
+            assert f(dim, page) == page * (dim // 2 * 2 + 2 * dim // 64 * 2)      # two codes a byte, a word per 64
+    for dim, page in [(96, 16), (0, 16), (128, 8), (128, 48), (128, 2048), (128, 0), (-64, 16)]:
+        assert f(dim, page) == 0
+
+
+def test_rotary_refuses_before_device_work():
+    f, d = binding.lib().externd_rotary, D256
+    good = dict(q=d, qo=d, hq=4, k=d, ko=d, hk=2, dt=1, tokens=3, dim=64, rot=32, il=0, inv=0, pos=d, fr=d, amp=1.0)
+
+    def call(**kw):
+        a = {**good, **kw}
+        return f(a["q"], a["qo"], 256, 64, 256, 64, a["hq"], a["k"], a["ko"], 128, 64, 128, 64, a["hk"], a["dt"], a["tokens"],
+                 a["dim"], a["rot"], a["il"], a["inv"], a["pos"], a["fr"], a["amp"], None)
+    for kw in [dict(q=None), dict(qo=None), dict(ko=None), dict(k=None), dict(pos=None), dict(fr=None), dict(hq=0), dict(hk=0),
+               dict(dt=3), dict(dt=-1), dict(tokens=-1), dict(rot=0), dict(rot=31), dict(rot=66), dict(dim=1), dict(il=2),
+               dict(inv=-1), dict(amp=float("nan")), dict(amp=float("inf"))]:
+        assert call(**kw) == binding.EINVAL, kw
+    assert call(dim=2048, rot=32) == binding.EUNSUPPORTED
+    assert call(hq=70000) == binding.EUNSUPPORTED and call(tokens=1 << 31) == binding.EUNSUPPORTED
+    assert call(tokens=0, q=None, qo=None, pos=None) == binding.OK
+
+
+def test_cache_calls_refuse_before_device_work():
+    L, d = binding.lib(), D256
+    good = dict(cache=d, pages=4, heads=2, dim=64, page=16, k=d, v=d, dt=0, tokens=3, batch=3, starts=None, lens=d, table=d, tp=2)
+
+    def append(**kw):
+        a = {**good, **kw}
+        return L.externd_kv4_append(a["cache"], a["pages"], a["heads"], a["dim"], a["page"], a["k"], a["v"], a["dt"], 128, 64,
+                                    128, 64, a["tokens"], a["batch"], a["starts"], a["lens"], a["table"], a["tp"], None)
+
+    def read(**kw):
+        a = {**good, **kw}
+        return L.externd_kv4_read(a["cache"], a["pages"], a["heads"], a["dim"], a["page"], a["k"], a["v"], a["dt"], a["tokens"],
+                                  a["batch"], a["starts"], a["lens"], a["table"], a["tp"], None)
+    for f in (append, read):
+        for kw in [dict(cache=None), dict(cache=ctypes.c_void_p(264)), dict(pages=0), dict(heads=0), dict(dim=80), dict(page=24),
+                   dict(page=8), dict(k=None), dict(v=None), dict(dt=5), dict(tokens=-1), dict(tokens=4), dict(batch=0),
+                   dict(lens=None), dict(table=None), dict(tp=0)]:
+            assert f(**kw) == binding.EINVAL, kw
+        assert f(tokens=1 << 31, starts=d) == binding.EUNSUPPORTED
+        assert f(tokens=0, starts=d, k=None, v=None) == binding.OK
+
+
+def test_attention_refuses_before_device_work():
+    L, d = binding.lib(), D256
+    good = dict(cache=d, pages=4, kv=2, dim=64, page=16, q=d, dt=0, hq=4, out=d, lse=d, tokens=3, batch=3, mn=1, ml=32, starts=None,
+                lens=d, table=d, tp=2, scale=0.125, window=0, ws=d, wsb=1 << 40)
+
+    def call(**kw):
+        a = {**good, **kw}
+        return L.externd_kv4_attention(a["cache"], a["pages"], a["kv"], a["dim"], a["page"], a["q"], a["dt"], 256, 64, a["hq"],
+                                       a["out"], a["lse"], a["tokens"], a["batch"], a["mn"], a["ml"], a["starts"], a["lens"],
+                                       a["table"], a["tp"], a["scale"], a["window"], a["ws"], a["wsb"], None)
+    for kw in [dict(cache=None), dict(cache=ctypes.c_void_p(8)), dict(pages=0), dict(kv=0), dict(dim=32), dict(page=17),
+               dict(q=None), dict(out=None), dict(dt=7), dict(hq=3), dict(hq=1), dict(hq=130), dict(tokens=-1), dict(tokens=5),
+               dict(batch=0), dict(mn=0), dict(ml=-1), dict(lens=None), dict(table=None), dict(tp=0), dict(window=-1),
+               dict(scale=float("nan")), dict(scale=float("inf"))]:
+        assert call(**kw) == binding.EINVAL, kw
+    assert call(tokens=70000, batch=70000) == binding.EUNSUPPORTED
+    wsb = L.externd_kv4_attention_workspace_bytes
+    need = wsb(32, 8, 128, 1, 1, 1, 1, 131072)
+    if need:
+        for ws, n in [(d, need - 1), (None, need), (ctypes.c_void_p(264), need)]:
+            assert call(kv=8, hq=32, dim=128, dt=1, tokens=1, batch=1, ml=131072, ws=ws, wsb=n) == binding.EWORKSPACE
+    assert wsb(32, 8, 96, 1, 1, 1, 1, 131072) == 0 and wsb(33, 8, 128, 1, 1, 1, 1, 131072) == 0
+
+
+def test_logprobs_refuse_before_device_work():
+    L, d = binding.lib(), D256
+    good = dict(x=d, dt=0, rows=3, vocab=50, stride=50, y=d, scale=1.0, top=4, lp=d, h=d, lse=d, tl=d, ti=d, ws=d, wsb=1 << 40)
+
+    def call(**kw):
+        a = {**good, **kw}
+        return L.externd_token_logprobs(a["x"], a["dt"], a["rows"], a["vocab"], a["stride"], a["y"], a["scale"], a["top"], a["lp"],
+                                        a["h"], a["lse"], a["tl"], a["ti"], a["ws"], a["wsb"], None)
+    for kw in [dict(x=None), dict(dt=3), dict(rows=-1), dict(vocab=0), dict(stride=49), dict(y=None), dict(scale=0.0),
+               dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")), dict(top=-1), dict(top=65), dict(top=51),
+               dict(tl=None), dict(ti=None)]:
+        assert call(**kw) == binding.EINVAL, kw
+    assert call(rows=1 << 31) == binding.EUNSUPPORTED and call(vocab=1 << 31, stride=1 << 31) == binding.EUNSUPPORTED
+    assert call(rows=0, x=None) == binding.OK
+    need = L.externd_token_logprobs_workspace_bytes(1, 131072, 20)
+    if need:
+        for ws, n in [(d, need - 1), (None, need), (ctypes.c_void_p(264), need)]:
+            assert call(rows=1, vocab=131072, stride=131072, top=20, ws=ws, wsb=n) == binding.EWORKSPACE
+
+    def back(**kw):
+        a = {**good, "g": d, "ge": d, "out": d, "os": 50, **kw}
+        return L.externd_token_logprobs_backward(a["x"], a["dt"], a["rows"], a["vocab"], a["stride"], a["y"], a["scale"], a["lse"],
+                                                 a["h"], a["g"], a["ge"], a["out"], a["os"], None)
+    for kw in [dict(x=None), dict(out=None), dict(lse=None), dict(y=None), dict(h=None), dict(os=49), dict(stride=49),
+               dict(scale=0.0), dict(dt=9), dict(vocab=0), dict(rows=-1)]:
+        assert back(**kw) == binding.EINVAL, kw
+    assert back(rows=0, x=None, out=None, lse=None) == binding.OK
+
+
+def test_oracle_quantization_error_is_half_a_step():
+    rng = np.random.default_rng(0)
+    for size in (1e-7, 1e-3, 1.0, 300.0, 6e4):
+        x = size * rng.standard_t(4, size=(40, 128))
+        x = np.clip(x, -30000, 30000)
+        x[0] = np.abs(x[0])
+        x[1] = -np.abs(x[1])
+        x[2] = 0.0
+        x[3, :64] = x[3, 0]
+        c, s, z = ref.kv4_quantize(x)
+        v = ref.kv4_values(x)
+        assert np.all(np.abs(v - x).reshape(40, 2, 64) <= s[..., None] * (0.5 + 1e-12) + 0.0)
+        assert np.array_equal(v.astype(np.float16).astype(np.float64), v)          # every value is an fp16 number
+        # the step is at most 1/64 above the span's fifteenth, or 2^-20 above it
+        span = (np.maximum(x.reshape(40, 2, 64).max(-1), 0) - np.minimum(x.reshape(40, 2, 64).min(-1), 0)) / 15
+        assert np.all(s <= np.maximum(span * (1 + 1 / 64), span + 2.0 ** -20)) and np.all(s >= span)
+
+
+def test_oracle_pages_roundtrip():
+    rng = np.random.default_rng(1)
+    for dim, page in ((64, 16), (128, 32), (256, 16)):
+        n, heads = 37, 2
+        k, v = rng.standard_normal((n, heads, dim)), rng.standard_normal((n, heads, dim))
+        cache = rng.integers(0, 256, (5, heads, page * (dim + dim // 16)), dtype=np.uint8)
+        table = np.array([3, 1, 4])
+        ref.kv4_encode(cache, page, k, v, table, 0, heads)
+        for h in range(heads):
+            K, V, there = ref.kv4_decode(cache, page, dim, table, n, h)
+            assert there.all()
+            assert np.array_equal(K, ref.kv4_values(k)[:, h]) and np.array_equal(V, ref.kv4_values(v)[:, h])
+
+
+def test_oracle_gradients_against_differences():
+    rng = np.random.default_rng(2)
+    x, y = rng.standard_normal((3, 11)), np.array([4, -1, 10])
+    g, ge = rng.standard_normal(3), rng.standard_normal(3)
+
+    def loss(x):
+        lp, h, *_ = ref.logprobs(x, y, 1.7, 0)
+        return (g * lp).sum() + (ge * h).sum()
+    d = ref.logprobs_backward(x, y, 1.7, g, ge)
+    for i in np.ndindex(x.shape):
+        e = np.zeros_like(x)
+        e[i] = 1e-5
+        # central differences: truncation of order 1e-10 times third derivatives of order 10
+        assert abs((loss(x + e) - loss(x - e)) / 2e-5 - d[i]) < 1e-8
+    # rotary: <R x, w> = <x, R^T w>, the inverse turn
+    freqs = ref_words(8)
+    a, w, pos = rng.standard_normal((5, 2, 20)), rng.standard_normal((5, 2, 20)), rng.integers(0, 1 << 40, 5)
+    for il in (False, True):
+        assert np.vdot(ref.rotary(a, pos, freqs, il, 1.3)[..., :16], w[..., :16]) == pytest.approx(
+            np.vdot(a[..., :16], ref.rotary(w, pos, freqs, il, 1.3, inverse=True)[..., :16]), rel=1e-12)
+
+
+def ref_words(half):
+    return np.array([int(2.0 ** 64 / (2 * math.pi) * 1e4 ** (-i / half)) for i in range(half)], dtype=np.int64)
