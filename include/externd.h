@@ -504,7 +504,7 @@ int externd_kv4_read(const void* cache, int64_t num_pages, int32_t heads_kv, int
  *  max_len    the largest length, or more; 0: not known.  Both only choose
  *             the launch: results hold whatever they are.
  *  heads_q a multiple of heads_kv, heads_q / heads_kv <= 64; scale finite;
- *  window >= 0; batch <= 65535.
+ *  window >= 0; batch <= 65535, tokens heads_q < 2^31.
  *  workspace  device, >= externd_kv4_attention_workspace_bytes() bytes for the
  *             same sizes, 256-byte aligned (may be NULL where that is 0).
  * A NaN or an infinity in q makes that row NaN; NaN values make those rows

@@ -66,7 +66,7 @@ __device__ __forceinline__ int sequence_of(const Kv4Sequences& s, int64_t t) {
 // Position of new token t of sequence b; below 0: none.
 __device__ __forceinline__ int64_t position_of(const Kv4Sequences& s, int b, int64_t t) {
   const int64_t end = s.starts ? s.starts[b + 1] : b + 1;
-  return (int64_t)s.lens[b] - (end - t);
+  return (int64_t)max(s.lens[b], 0) - (end - t);
 }
 
 // Page of position p of sequence b, or -1.
