@@ -24,72 +24,291 @@ __device__ __forceinline__ uint64_t order_key(float x, unsigned index) {
   return (uint64_t)((unsigned)b ^ 0x80000000u) << 32 | (0xFFFFFFFFu - index);
 }
 
-template <typename V, typename F>
-__device__ __forceinline__ V block_reduce(V v, V* lds, F f) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  for (int d = 32; d; d >>= 1) v = f(v, (V)__shfl_xor(v, d));
-  __syncthreads();
-  if (lane == 0) lds[wave] = v;
-  __syncthreads();
-  v = lds[0];
-  for (int i = 1; i < (int)(blockDim.x >> 6); i++) v = f(v, lds[i]);
+__device__ __forceinline__ float value_of(uint64_t key) {
+  int b = (int)((unsigned)(key >> 32) ^ 0x80000000u);
+  return __int_as_float(b < 0 ? b ^ 0x7FFFFFFF : b);
+}
+__device__ __forceinline__ int64_t index_of(uint64_t key) { return (int64_t)(0xFFFFFFFFu - (unsigned)key); }
+
+typedef unsigned v4u __attribute__((ext_vector_type(4)));
+
+// A larger of two that is a NaN where one of them is.
+__device__ __forceinline__ float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+
+template <int DT> struct Vec {
+  static constexpr int E = DT == EXTERND_F32 ? 4 : 8;      // entries of 16 bytes
+  static __device__ __forceinline__ void unpack(v4u v, float* x) {
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      if constexpr (DT == EXTERND_F32) x[i] = __uint_as_float(v[i]);
+      else if constexpr (DT == EXTERND_BF16) {
+        x[2 * i] = __uint_as_float(v[i] << 16);
+        x[2 * i + 1] = __uint_as_float(v[i] & 0xFFFF0000u);
+      } else {
+        x[2 * i] = (float)__builtin_bit_cast(_Float16, (uint16_t)v[i]);
+        x[2 * i + 1] = (float)__builtin_bit_cast(_Float16, (uint16_t)(v[i] >> 16));
+      }
+    }
+  }
+  static __device__ __forceinline__ v4u pack(const float* x) {
+    v4u v;
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      if constexpr (DT == EXTERND_F32) v[i] = __float_as_uint(x[i]);
+      else
+        v[i] = (unsigned)__builtin_bit_cast(uint16_t, Elem<DT>::store(x[2 * i])) |
+               (unsigned)__builtin_bit_cast(uint16_t, Elem<DT>::store(x[2 * i + 1])) << 16;
+    }
+    return v;
+  }
+};
+
+// Entries of a row before its first 16-byte boundary.
+template <int DT>
+__device__ __forceinline__ int64_t row_head(const void* p, int64_t n) {
+  constexpr int B = DT == EXTERND_F32 ? 4 : 2;
+  const int64_t h = (int64_t)((16 - ((uintptr_t)p & 15)) & 15) / B;
+  return h < n ? h : n;
+}
+
+__device__ __forceinline__ uint64_t shfl_xor64(uint64_t v, int d) {
+  const unsigned lo = __shfl_xor((unsigned)v, d), hi = __shfl_xor((unsigned)(v >> 32), d);
+  return (uint64_t)hi << 32 | lo;
+}
+__device__ __forceinline__ float wave_sum(float v) {
+  for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
+  return v;
+}
+__device__ __forceinline__ float wave_max(float v) {
+  for (int d = 32; d; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
   return v;
 }
 
-// One workgroup per row: the maximum, then the sums, then the largest logits
-// one after another.
-template <int DT>
-__global__ __launch_bounds__(256) void k_logprobs(LogprobArgs a) {
-  typedef typename Elem<DT>::T T;
-  __shared__ float lf[4];
-  __shared__ unsigned long long lk[4];
-  const int64_t r = blockIdx.x;
-  const T* x = (const T*)a.logits + r * a.stride;
-  const int n = (int)a.vocab;
-  float m = -INFINITY, nan = 0.f;
-  for (int i = threadIdx.x; i < n; i += 256) {
-    const float z = Elem<DT>::load(x[i]) * a.scale;
-    m = fmaxf(m, z);
-    nan = z == z && z < INFINITY ? nan : NAN;
+// The largest keys that a wave has seen, lane i the i-th, and those not sorted in yet.
+struct Best {
+  uint64_t key;          // 0: none
+  uint64_t* waiting;     // LDS, 128 keys
+  int count;             // of them
+  int top;
+  float bar;             // entries not above it are out; a NaN (nothing compares) while fewer than `top` are known
+
+  __device__ __forceinline__ void init(uint64_t* lds, int k) {
+    key = 0;
+    waiting = lds;
+    count = 0;
+    top = k;
+    bar = NAN;
   }
-  m = block_reduce(m, lf, [](float p, float q) { return fmaxf(p, q); });
-  float sum = 0.f, mean = 0.f;
-  if (m > -INFINITY)
-    for (int i = threadIdx.x; i < n; i += 256) {
-      const float z = Elem<DT>::load(x[i]) * a.scale - m, e = expf(z);
-      sum += e;
-      mean += z == -INFINITY ? 0.f : e * z;
+  // Sorts the first (at most 64) waiting keys in.
+  __device__ __forceinline__ void merge() {
+    const int lane = threadIdx.x & 63;
+    uint64_t k = lane < count ? waiting[lane] : 0;
+    for (int size = 2; size <= 64; size <<= 1)        // ascending over the wave
+      for (int d = size >> 1; d; d >>= 1) {
+        const uint64_t o = shfl_xor64(k, d);
+        const bool low = !(lane & d), up = size == 64 || !(lane & size);
+        k = (low == up) == (k < o) ? k : o;
+      }
+    key = key > k ? key : k;                          // the 64 largest of both, rising then falling
+    for (int d = 32; d; d >>= 1) {
+      const uint64_t o = shfl_xor64(key, d);
+      key = !(lane & d) == (key > o) ? key : o;
     }
-  const auto plus = [](float p, float q) { return p + q; };
-  sum = block_reduce(sum, lf, plus);
-  mean = block_reduce(mean, lf, plus);
-  nan = block_reduce(nan, lf, plus);
-  const float lse = m == -INFINITY ? nan == 0.f ? -INFINITY : NAN : m + logf(sum) + nan;
-  if (threadIdx.x == 0) {
+    const int left = count - 64;
+    if (left > 0 && lane < left) waiting[lane] = waiting[64 + lane];
+    count = left > 0 ? left : 0;
+    const uint64_t last = (uint64_t)(unsigned)__builtin_amdgcn_readlane((unsigned)(key >> 32), top - 1) << 32 |
+                          (unsigned)__builtin_amdgcn_readlane((unsigned)key, top - 1);
+    bar = last ? value_of(last) : NAN;
+  }
+  // `in`: this lane's x may be among the largest.
+  __device__ __forceinline__ void offer(bool in, float x, unsigned index) {
+    const uint64_t mask = __ballot(in);
+    if (!mask) return;
+    const int lane = threadIdx.x & 63;
+    if (in) waiting[count + __popcll(mask & ((1ull << lane) - 1))] = order_key(x, index);
+    count += __popcll(mask);
+    if (count >= 64) merge();
+  }
+};
+
+// Sums of a row (or a part of it) of one lane: with y = (x - ref) scale log2(e),
+// s = sum 2^y and t = sum 2^y y.  `ref` is the same in a wave: the largest entry
+// of the first ones, and moved only when one is 2^8 larger, so that entries
+// need no maximum of their own.
+struct Sums {
+  float ref, s, t;
+  __device__ __forceinline__ void move(float to, float c) {
+    const float d = fmaxf((ref - to) * c, -1e9f), f = __builtin_amdgcn_exp2f(d);
+    t = s > 0.f ? fmaf(s, d, t) * f : s;      // s is 0 or NaN otherwise
+    s *= f;
+    ref = to;
+  }
+};
+
+// Wave-wide: E entries of every lane (present: whether the lane has any).
+template <int E>
+__device__ __forceinline__ void take(const float* x, bool present, unsigned index, float c, Sums& a, Best& best, bool first) {
+  float big = x[0];
+#pragma unroll
+  for (int e = 1; e < E; e++) big = larger(big, x[e]);
+  big = present ? big : -INFINITY;
+  if (first) a.ref = fmaxf(wave_max(big), -3.402823466e38f);
+  else if (__any((big - a.ref) * c > 8.f)) a.move(wave_max(big), c);
+  if (best.top && __any(present && !(big <= best.bar))) {
+    // earlier entries have lower indices, so what equals their bar is out; what these ones raise it to is not
+    const float bar = best.bar;
+#pragma unroll
+    for (int e = 0; e < E; e++) best.offer(present && !(x[e] <= bar) && !(x[e] < best.bar), x[e], index + e);
+  }
+  float s[2] = {0.f, 0.f}, t[2] = {0.f, 0.f};
+#pragma unroll
+  for (int e = 0; e < E; e++) {
+    const float y = larger((x[e] - a.ref) * c, -200.f), w = __builtin_amdgcn_exp2f(y);      // 2^-200 is 0
+    s[e & 1] += w;
+    t[e & 1] = fmaf(w, y, t[e & 1]);
+  }
+  a.s += present ? s[0] + s[1] : 0.f;
+  a.t += present ? t[0] + t[1] : 0.f;
+}
+
+struct RowPart {
+  float ref, s, t;
+  int pad;
+};
+
+struct LogprobSplit {
+  int parts;
+  int64_t each;        // 16-byte vectors of a part, a multiple of 64
+  RowPart* sums;       // rows x parts
+  uint64_t* keys;      // rows x parts x top
+};
+
+// What a row's sums say (lane 0) and the largest logits (lanes below top).
+template <int DT>
+__device__ __forceinline__ void write_row(const LogprobArgs& a, int64_t r, float ref, float s, float t, uint64_t key) {
+  typedef typename Elem<DT>::T T;
+  const T* x = (const T*)a.logits + r * a.stride;
+  const int lane = threadIdx.x & 63;
+  const float ln2 = 0.69314718055994530942f, l2 = log2f(s);
+  const bool none = s == 0.f;      // nothing but -infinity
+  const float lse = none ? -INFINITY : fmaf(ln2, l2, ref * a.scale);
+  if (lane == 0) {
     if (a.lse) a.lse[r] = lse;
-    if (a.entropy) a.entropy[r] = lse == -INFINITY ? 0.f : logf(sum) - mean / sum + nan;
+    if (a.entropy) a.entropy[r] = none ? 0.f : ln2 * (l2 - t / s);
     if (a.logprob) {
       const int64_t y = a.targets[r];
-      const float z = y >= 0 && y < n ? Elem<DT>::load(x[y]) * a.scale : 0.f;
-      a.logprob[r] = y < 0 ? 0.f : y >= n ? NAN : z == -INFINITY && !(lse != lse) ? -INFINITY : z - lse;
+      const float z = y >= 0 && y < a.vocab ? Elem<DT>::load(x[y]) * a.scale : 0.f;
+      a.logprob[r] = y < 0 ? 0.f : y >= a.vocab ? NAN : none ? -INFINITY : z - lse;
     }
   }
-  uint64_t last = ~0ull;
-  for (int j = 0; j < a.top; j++) {
-    unsigned long long best = 0;
-    for (int i = threadIdx.x; i < n; i += 256) {
-      const uint64_t key = order_key(Elem<DT>::load(x[i]), (unsigned)i);
-      if (key < last && key > best) best = key;
-    }
-    best = block_reduce(best, lk, [](unsigned long long p, unsigned long long q) { return p > q ? p : q; });
-    last = best;
-    if (threadIdx.x == 0) {
-      const int i = (int)(0xFFFFFFFFu - (unsigned)best);
-      const float z = Elem<DT>::load(x[i]) * a.scale;
-      a.top_ids[r * a.top + j] = i;
-      a.top_logprobs[r * a.top + j] = z == -INFINITY && !(lse != lse) ? -INFINITY : z - lse;
-    }
+  if (lane < a.top) {
+    a.top_ids[r * a.top + lane] = index_of(key);
+    a.top_logprobs[r * a.top + lane] = none ? -INFINITY : value_of(key) * a.scale - lse;
   }
+}
+
+// One wave per row, or per part of one: a single pass over its entries with
+// four 16-byte loads of every lane in flight ahead of those in work.
+template <int DT>
+__global__ __launch_bounds__(256) void k_logprobs(LogprobArgs a, LogprobSplit sp) {
+  typedef typename Elem<DT>::T T;
+  constexpr int E = Vec<DT>::E, U = 4;
+  __shared__ uint64_t waiting[4][128];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t unit = (int64_t)blockIdx.x * 4 + wave;
+  if (unit >= a.rows * sp.parts) return;
+  const int64_t r = unit / sp.parts;
+  const int part = (int)(unit - r * sp.parts);
+  const T* x = (const T*)a.logits + r * a.stride;
+  const int64_t head = row_head<DT>(x, a.vocab), nv = (a.vocab - head) / E, tail = head + nv * E;
+  const int64_t v0 = min((int64_t)part * sp.each, nv), v1 = part == sp.parts - 1 ? nv : min(v0 + sp.each, nv);
+  const v4u* v = (const v4u*)(x + head);
+  const float c = a.scale * 1.44269504088896340736f;
+  Sums sum = {0.f, 0.f, 0.f};
+  Best best;
+  best.init(waiting[wave], a.top);
+  bool first = true;
+  v4u now[U], next[U];
+  int64_t i = v0;
+  const int64_t blocks = (v1 - v0) / (64 * U);
+  if (blocks > 0)
+#pragma unroll
+    for (int u = 0; u < U; u++) now[u] = v[i + u * 64 + lane];
+  if (part == 0 && head) {
+    float one = -INFINITY;
+    if (lane < head) one = Elem<DT>::load(x[lane]);
+    take<1>(&one, lane < head, (unsigned)lane, c, sum, best, first);
+    first = false;
+  }
+  for (int64_t k = 0; k < blocks; k++, i += 64 * U) {
+    if (k + 1 < blocks)
+#pragma unroll
+      for (int u = 0; u < U; u++) next[u] = v[i + (U + u) * 64 + lane];
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+      float y[E];
+      Vec<DT>::unpack(now[u], y);
+      take<E>(y, true, (unsigned)(head + (i + u * 64 + lane) * E), c, sum, best, first);
+      first = false;
+    }
+#pragma unroll
+    for (int u = 0; u < U; u++) now[u] = next[u];
+  }
+  for (; i < v1; i += 64) {
+    const bool in = i + lane < v1;
+    float y[E];
+    Vec<DT>::unpack(v[in ? i + lane : v1 - 1], y);
+    take<E>(y, in, (unsigned)(head + (i + lane) * E), c, sum, best, first);
+    first = false;
+  }
+  if (part == sp.parts - 1 && tail < a.vocab) {
+    const bool in = tail + lane < a.vocab;
+    float one = -INFINITY;
+    if (in) one = Elem<DT>::load(x[tail + lane]);
+    take<1>(&one, in, (unsigned)(tail + lane), c, sum, best, first);
+    first = false;
+  }
+  if (a.top && best.count) best.merge();
+  const float s = wave_sum(sum.s), t = wave_sum(sum.t);
+  if (sp.parts == 1) {
+    write_row<DT>(a, r, sum.ref, s, t, best.key);
+    return;
+  }
+  if (lane == 0) sp.sums[unit] = {first ? -3.402823466e38f : sum.ref, s, t, 0};
+  if (lane < a.top) sp.keys[unit * a.top + lane] = best.key;
+}
+
+// Joins a row's parts: one wave per row.
+template <int DT>
+__global__ __launch_bounds__(64) void k_logprobs_join(LogprobArgs a, LogprobSplit sp) {
+  __shared__ uint64_t waiting[128];
+  const int64_t r = blockIdx.x;
+  const int lane = threadIdx.x;
+  const RowPart* p = sp.sums + r * sp.parts;
+  const float c = a.scale * 1.44269504088896340736f;
+  float ref = -3.402823466e38f;
+  for (int i = lane; i < sp.parts; i += 64) ref = fmaxf(ref, p[i].s > 0.f ? p[i].ref : ref);
+  ref = wave_max(ref);
+  float s = 0.f, t = 0.f;
+  for (int i = lane; i < sp.parts; i += 64) {
+    Sums one = {p[i].ref, p[i].s, p[i].t};
+    if (one.s != 0.f) one.move(ref, c);
+    s += one.s;
+    t += one.t;
+  }
+  s = wave_sum(s);
+  t = wave_sum(t);
+  Best best;
+  best.init(waiting, a.top);
+  const uint64_t* keys = sp.keys + r * sp.parts * a.top;
+  const int n = sp.parts * a.top;
+  for (int i = 0; i < n; i += 64) {
+    const uint64_t key = i + lane < n ? keys[i + lane] : 0;
+    best.offer(key && !(value_of(key) < best.bar), value_of(key), (unsigned)index_of(key));
+  }
+  if (a.top && best.count) best.merge();
+  write_row<DT>(a, r, ref, s, t, best.key);
 }
 
 struct LogprobGradArgs {
@@ -99,24 +318,86 @@ struct LogprobGradArgs {
   const int64_t* targets;
   float scale;
   const float *lse, *entropy, *g_logprob, *g_entropy;
+  int64_t first;      // row of the grid's first
 };
 
+// One workgroup per row and stretch of it: 16-byte loads and stores where a
+// row of both arrays starts at the same place within 16 bytes, else one by one.
 template <int DT>
 __global__ __launch_bounds__(256) void k_logprobs_grad(LogprobGradArgs a) {
   typedef typename Elem<DT>::T T;
-  const int64_t r = blockIdx.x;
+  constexpr int E = Vec<DT>::E, U = 4;
+  const int64_t r = a.first + blockIdx.y;
   const T* x = (const T*)a.logits + r * a.stride;
   T* d = (T*)a.grad + r * a.grad_stride;
-  const int n = (int)a.vocab;
   const int64_t y = a.targets ? a.targets[r] : -1;
   const float lse = a.lse[r], g = a.g_logprob && y >= 0 ? a.g_logprob[r] : 0.f;
   const float ge = a.g_entropy ? a.g_entropy[r] : 0.f, h = a.g_entropy ? a.entropy[r] : 0.f;
-  for (int i = threadIdx.x; i < n; i += 256) {
-    const float lp = lse == -INFINITY ? lse : Elem<DT>::load(x[i]) * a.scale - lse, p = expf(lp);
-    float v = p == 0.f ? 0.f : -p * (g + ge * (lp + h));
-    if (i == y) v += g;
-    d[i] = Elem<DT>::store(v * a.scale);
+  const float scale = a.scale;
+  // grad = scale ([v = y] g - p (g + ge (lp + h))), lp = ln p
+  auto entry = [&](float v, int64_t i) -> float {
+    const float lp = fmaf(v, scale, -lse), p = __builtin_amdgcn_exp2f(lp * 1.44269504088896340736f);
+    float o = p > 0.f ? -p * fmaf(ge, lp + h, g) : p == 0.f || lse == -INFINITY ? 0.f : p;
+    if (i == y) o += g;
+    return o * scale;
+  };
+  const int64_t stretch = (int64_t)256 * U * E;
+  const int64_t head = row_head<DT>(x, a.vocab), nv = (a.vocab - head) / E, tail = head + nv * E;
+  if ((((uintptr_t)x ^ (uintptr_t)d) & 15) != 0) {
+    const int64_t end = min((int64_t)(blockIdx.x + 1) * stretch, a.vocab);
+    for (int64_t i = (int64_t)blockIdx.x * stretch + threadIdx.x; i < end; i += 256)
+      d[i] = Elem<DT>::store(entry(Elem<DT>::load(x[i]), i));
+    return;
   }
+  const int64_t v0 = (int64_t)blockIdx.x * (256 * U) + threadIdx.x;
+  const v4u* from = (const v4u*)(x + head);
+  v4u* to = (v4u*)(d + head);
+  v4u in[U];
+#pragma unroll
+  for (int u = 0; u < U; u++)
+    if (v0 + u * 256 < nv) in[u] = from[v0 + u * 256];
+#pragma unroll
+  for (int u = 0; u < U; u++)
+    if (v0 + u * 256 < nv) {
+      float f[E];
+      Vec<DT>::unpack(in[u], f);
+      const int64_t i = head + (v0 + u * 256) * E;
+#pragma unroll
+      for (int e = 0; e < E; e++) f[e] = entry(f[e], i + e);
+      to[v0 + u * 256] = Vec<DT>::pack(f);
+    }
+  if (blockIdx.x == 0) {      // what is off the 16-byte boundaries: fewer than 2 E entries
+    const int64_t i = (int64_t)threadIdx.x < head ? threadIdx.x : tail + threadIdx.x - head;
+    if (i < a.vocab) d[i] = Elem<DT>::store(entry(Elem<DT>::load(x[i]), i));
+  }
+}
+
+// Parts of a row: one wave each, so that few rows still fill the chip (2048
+// waves, eight a CU), but not below 2048 entries.
+static LogprobSplit split_of(int64_t rows, int64_t vocab) {
+  LogprobSplit sp = {};
+  int64_t parts = (2048 + rows - 1) / rows;
+  const int64_t most = (vocab + 2047) / 2048;
+  parts = parts > most ? most : parts;
+  sp.parts = (int)parts;
+  return sp;
+}
+static size_t split_bytes(int64_t rows, int parts, int top) {
+  return ((size_t)rows * parts * (sizeof(RowPart) + (size_t)top * 8) + 255) & ~(size_t)255;
+}
+
+static void launch_logprobs_grad(LogprobGradArgs a, int32_t dtype, int64_t r0, int64_t rows, int64_t stretches, hipStream_t s) {
+  a.first = r0;
+  const dim3 grid((unsigned)stretches, (unsigned)rows);
+  if (dtype == EXTERND_F32) k_logprobs_grad<EXTERND_F32><<<grid, 256, 0, s>>>(a);
+  else if (dtype == EXTERND_BF16) k_logprobs_grad<EXTERND_BF16><<<grid, 256, 0, s>>>(a);
+  else k_logprobs_grad<EXTERND_F16><<<grid, 256, 0, s>>>(a);
+}
+
+template <int DT>
+static void launch_logprobs(const LogprobArgs& a, const LogprobSplit& sp, hipStream_t s) {
+  k_logprobs<DT><<<dim3((unsigned)((a.rows * sp.parts + 3) / 4)), 256, 0, s>>>(a, sp);
+  if (sp.parts > 1) k_logprobs_join<DT><<<dim3((unsigned)a.rows), 64, 0, s>>>(a, sp);
 }
 
 static bool logprob_sizes_ok(int64_t rows, int64_t vocab, int32_t top) {
@@ -130,8 +411,9 @@ using namespace externd;
 extern "C" {
 
 size_t externd_token_logprobs_workspace_bytes(int64_t rows, int64_t vocab, int32_t top) {
-  if (!logprob_sizes_ok(rows, vocab, top)) return 0;
-  return 0;
+  if (!logprob_sizes_ok(rows, vocab, top) || !rows) return 0;
+  const int parts = split_of(rows, vocab).parts;
+  return parts == 1 ? 0 : split_bytes(rows, parts, top);
 }
 
 int externd_token_logprobs(const void* logits, int32_t dtype, int64_t rows, int64_t vocab, int64_t row_stride,
@@ -146,11 +428,15 @@ int externd_token_logprobs(const void* logits, int32_t dtype, int64_t rows, int6
   if (need && (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 255))) return EXTERND_EWORKSPACE;
   if (!rows) return EXTERND_OK;
   const LogprobArgs a = {logits, rows, vocab, row_stride, targets, scale, top, logprob, entropy, lse, top_logprobs, top_ids};
+  LogprobSplit sp = split_of(rows, vocab);
+  const int per = dtype == EXTERND_F32 ? 4 : 8;      // entries of a vector
+  sp.each = ((vocab / per + sp.parts - 1) / sp.parts + 63) & ~(int64_t)63;
+  sp.sums = (RowPart*)workspace;
+  sp.keys = (uint64_t*)(sp.sums + rows * sp.parts);
   const hipStream_t s = (hipStream_t)stream;
-  const dim3 grid((unsigned)rows);
-  if (dtype == EXTERND_F32) k_logprobs<EXTERND_F32><<<grid, 256, 0, s>>>(a);
-  else if (dtype == EXTERND_BF16) k_logprobs<EXTERND_BF16><<<grid, 256, 0, s>>>(a);
-  else k_logprobs<EXTERND_F16><<<grid, 256, 0, s>>>(a);
+  if (dtype == EXTERND_F32) launch_logprobs<EXTERND_F32>(a, sp, s);
+  else if (dtype == EXTERND_BF16) launch_logprobs<EXTERND_BF16>(a, sp, s);
+  else launch_logprobs<EXTERND_F16>(a, sp, s);
   return hipGetLastError() == hipSuccess ? EXTERND_OK : EXTERND_EHIP;
 }
 
@@ -165,12 +451,12 @@ int externd_token_logprobs_backward(const void* logits, int32_t dtype, int64_t r
   if (rows > INT32_MAX || vocab > INT32_MAX) return EXTERND_EUNSUPPORTED;
   if (!rows) return EXTERND_OK;
   const LogprobGradArgs a = {logits, grad, rows, vocab, row_stride, grad_row_stride, targets, scale, lse, entropy,
-                             g_logprob, g_entropy};
+                             g_logprob, g_entropy, 0};
   const hipStream_t s = (hipStream_t)stream;
-  const dim3 grid((unsigned)rows);
-  if (dtype == EXTERND_F32) k_logprobs_grad<EXTERND_F32><<<grid, 256, 0, s>>>(a);
-  else if (dtype == EXTERND_BF16) k_logprobs_grad<EXTERND_BF16><<<grid, 256, 0, s>>>(a);
-  else k_logprobs_grad<EXTERND_F16><<<grid, 256, 0, s>>>(a);
+  const int64_t stretch = 256 * 4 * (dtype == EXTERND_F32 ? 4 : 8);
+  for (int64_t r0 = 0; r0 < rows; r0 += 65535) {      // rows are the grid's second dimension
+    launch_logprobs_grad(a, dtype, r0, rows - r0 < 65535 ? rows - r0 : 65535, (vocab + stretch - 1) / stretch, s);
+  }
   return hipGetLastError() == hipSuccess ? EXTERND_OK : EXTERND_EHIP;
 }
 
