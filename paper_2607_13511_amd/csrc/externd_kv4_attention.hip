@@ -1,4 +1,5 @@
 // Attention over the cache in 4 bits.
+#include <limits.h>
 #include <math.h>
 
 #include "externd_decode.hpp"
@@ -8,6 +9,10 @@ namespace externd {
 typedef int v4i __attribute__((ext_vector_type(4)));
 typedef unsigned v4u __attribute__((ext_vector_type(4)));
 typedef unsigned v2u __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 struct AttnArgs {
   const uint8_t* cache;
@@ -22,7 +27,7 @@ struct AttnArgs {
   int window, dtype;
   int nsplit, chunk;      // parts of a sequence (grid x), and the least tokens of a part (a multiple of 256)
   int row_blocks;         // row blocks a launch starts per sequence and cache head
-  float* part;            // per (row, part): DIM sums, then the maximum and the sum of weights
+  float* part;            // per (row, part): DIM sums, the maximum and the sum of weights, two unused
 };
 
 __device__ __forceinline__ float load_any(const void* p, int64_t i, int dtype) {
@@ -468,7 +473,7 @@ __global__ __launch_bounds__(256, DIM * RT <= 128 ? 3 : 2) void k_attention_spli
         store_any(a.out, to * DIM + d, none ? 0.f : o / sum, a.dtype);
         if (a.lse && d == 0) a.lse[to] = none ? -INFINITY : (top + log2f(sum)) * 0.69314718055994530942f;
       } else {
-        float* part = a.part + (to * a.nsplit + sp) * (DIM + 2);
+        float* part = a.part + (to * a.nsplit + sp) * (DIM + 4);
         part[d] = o;
         if (d == 0) {
           part[DIM] = top;
@@ -477,6 +482,362 @@ __global__ __launch_bounds__(256, DIM * RT <= 128 ? 3 : 2) void k_attention_spli
       }
     }
     __syncthreads();
+  }
+}
+
+// Attention of 256 rows over one part of a sequence, for 16-bit queries: the
+// codes become fp16 values in LDS, shared by eight waves of 32 rows each, and
+//   S^T = K Q^T  and  O^T += V^T P^T  on v_mfma_f32_32x32x16_f16.
+// Every value s (code - z) is exactly an fp16 number and a query row enters as
+// fp16 with its largest entry near 2^15 (exact for bf16 entries within 2^-29
+// of it), so the scores are fp32 sums of exact products; only the softmax weights are
+// rounded (to 11 bits, for the second product; their sum takes them as they are).  S^T leaves a row's scores in two
+// lanes, whose registers, rounded, are the second product's operand as they
+// are: token order within 16 is free, so V is stored in the order that S^T has.
+//
+// A tile of TT tokens is converted once (4 operations for 2 codes: mask to
+// 1024 + code, subtract 1024 + z, times s) while the tile before is in work;
+// one barrier a tile.  The weights are taken against a running reference that
+// moves only when a row's maximum passes it by 2^8, so O is rarely rescaled.
+template <int DIM>
+__global__ __launch_bounds__(512, 2) void k_attention_chunk(AttnArgs a) {
+  constexpr int NG = DIM / KV4_GROUP, HALF = DIM / 2, ROWS = 256;
+  constexpr int TT = DIM == 256 ? 32 : 64;          // tokens of a tile
+  constexpr int NS = TT / 32, KS = DIM / 16, PS = TT / 16, CT = DIM / 32;
+  constexpr int KU = DIM / 8, VU = TT / 8;          // 16-byte units of a row of K (a token) and of V (a channel)
+  constexpr int WB = 8 / PS;                        // waves of a 16-token block
+  __shared__ __align__(16) _Float16 kt[2][TT * DIM], vt[2][DIM * TT];
+  __shared__ __align__(8) uint8_t flags[2][8];      // of each wave's 8 values' tokens: 1 there, 3 some NaN among them
+  __shared__ uint8_t nans[2][8][NG];                // which of them
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, half = lane >> 5;
+  const int h = blockIdx.x % a.c.heads, sp = blockIdx.x / a.c.heads, b = blockIdx.z;
+  const int P = 1 << a.c.page_log2;
+  const int block = wave / WB;                      // the 16-token block of a tile that this wave converts
+  const int vhalf = WB == 2 ? wave & 1 : (wave >> 1) & 1;      // of it, tokens 4 vhalf + {0..3, 8..11}
+  const int vcol = WB == 2 ? lane : (wave & 1) * 64 + lane;    // byte column of V
+  const bool vin = DIM > 64 || lane < 32;
+  const int ktok = DIM == 256 ? wave * 4 + (lane >> 4) : DIM == 128 ? wave * 8 + (lane >> 3) : wave * 8 + ((lane & 31) >> 2);
+  const int kunit = DIM == 256 ? lane & 15 : DIM == 128 ? lane & 7 : lane & 3;
+  // 16-byte units are permuted within a row so that 16 rows' same unit spans all banks
+  auto kat = [](int tok, int u) { return (tok * KU + (DIM == 64 ? u ^ ((tok >> 1) & 7) : u ^ (tok & 15))) * 8; };
+  auto vat = [](int ch, int u) { return (ch * VU + (TT == 64 ? u ^ ((ch >> 1) & 7) : u ^ ((ch >> 2) & 3))) * 8; };
+
+  for (int rb = a.row_blocks - 1 - (int)blockIdx.y;; rb += a.row_blocks) {
+    const RowBlock R = row_block<ROWS>(a, b, rb);
+    if (rb * ROWS >= R.rows) break;
+    const int row = rb * ROWS + wave * 32 + l32;
+    const int64_t to = (R.t0 + row / a.each) * a.heads_q + h * a.each + row % a.each;
+    if (R.parts == 0 && sp == 0 && row < R.rows) {      // rows that see nothing
+      for (int d = half; d < DIM; d += 2) store_any(a.out, to * DIM + d, 0.f, a.dtype);
+      if (a.lse && !half) a.lse[to] = -INFINITY;
+    }
+    if (sp >= R.parts) continue;
+    const int c0 = R.lo + sp * R.part, c1 = (int)min((int64_t)R.hi, (int64_t)c0 + R.part);
+
+    // ---- this lane's half of its row's query, as fp16 ----
+    f16x8 Q[KS];
+    float factor;
+    {
+      float x[KS][8], top = 0.f;
+      bool bad = false;
+#pragma unroll
+      for (int k = 0; k < KS; k++)
+#pragma unroll
+        for (int j = 0; j < 8; j++) {
+          x[k][j] = 0.f;
+          if (row < R.rows) {
+            const int64_t at = (R.t0 + row / a.each) * a.q_ts + (h * a.each + row % a.each) * a.q_hs;
+            x[k][j] = load_any(a.q, at + k * 16 + half * 8 + j, a.dtype);
+          }
+          bad |= !__builtin_isfinite(x[k][j]);
+          top = fmaxf(top, fabsf(x[k][j]));
+        }
+      top = fmaxf(top, __shfl_xor(top, 32));
+      bad |= __shfl_xor((int)bad, 32) != 0;
+      int e = 0;
+      frexpf(top, &e);                  // top < 2^e
+      const float sign = a.scale < 0.f ? -1.f : 1.f;
+#pragma unroll
+      for (int k = 0; k < KS; k++)
+#pragma unroll
+        for (int j = 0; j < 8; j++) {
+          constexpr int order[8] = {0, 2, 1, 3, 4, 6, 5, 7};      // as two codes come out of one mask
+          Q[k][j] = (_Float16)(bad ? 0.f : ldexpf(sign * x[k][order[j]], 15 - e));
+        }
+      factor = bad ? NAN : ldexpf(fabsf(a.scale) * 1.44269504088896340736f, e - 15);
+    }
+    const int pos = R.first + row / a.each;
+    const int last = row < R.rows ? min(pos, c1 - 1) : -1;
+    const int least = a.window > 0 ? pos - a.window + 1 : 0;
+    // over the wave: where every row sees every token, and past which none does
+    int all_from = row < R.rows ? least : INT_MIN, all_to = row < R.rows ? last : INT_MAX, none_from = last;
+    for (int d = 16; d; d >>= 1) {
+      all_from = max(all_from, __shfl_xor(all_from, d));
+      all_to = min(all_to, __shfl_xor(all_to, d));
+      none_from = max(none_from, __shfl_xor(none_from, d));
+    }
+    all_from = __builtin_amdgcn_readfirstlane(all_from);
+    all_to = __builtin_amdgcn_readfirstlane(all_to);
+    none_from = __builtin_amdgcn_readfirstlane(none_from);
+
+    f32x16 O[CT];
+#pragma unroll
+    for (int c = 0; c < CT; c++)
+#pragma unroll
+      for (int i = 0; i < 16; i++) O[c][i] = 0.f;
+    float ref = -INFINITY, l = 0.f, poison[NG];
+#pragma unroll
+    for (int g = 0; g < NG; g++) poison[g] = 0.f;
+
+    const int ntiles = (c1 - c0 + TT - 1) / TT;
+    v2u kraw;
+    unsigned vraw[2], kword[(NG + 1) / 2], vword[8][(NG + 1) / 2];
+    int page_now = -1;       // of the loaded tile's block
+    auto lookup = [&](int tile) -> int {
+      const int tok = c0 + tile * TT + block * 16;
+      if (tile >= ntiles || tok >= c1) return -1;
+      const int page = a.s.table[(int64_t)b * a.s.table_pages + (tok >> a.c.page_log2)];
+      return page >= 0 && page < a.c.num_pages ? page : -1;
+    };
+    auto load = [&](int tile, int page) {
+      page_now = __builtin_amdgcn_readfirstlane(page);
+      const uint8_t* base = a.cache + ((int64_t)max(page_now, 0) * a.c.heads + h) * a.c.head_bytes;
+      const int o = (c0 + tile * TT + block * 16) & (P - 1);      // the block's place in its page
+      const uint8_t* words = base + (unsigned)P * DIM;
+      const int kt0 = o + (ktok & 15);
+      kraw = *(const v2u*)(base + kt0 * HALF + kunit * 8);
+#pragma unroll
+      for (int g = 0; g < (NG + 1) / 2; g++) kword[g] = ((const unsigned*)(words + kt0 * (4 * NG)))[g];
+      const unsigned* vp = (const unsigned*)(base + (unsigned)P * HALF + (o >> 4) * (HALF * 16) + (vin ? vcol : 0) * 16);
+      vraw[0] = vp[vhalf];
+      vraw[1] = vp[2 + vhalf];
+#pragma unroll
+      for (int j = 0; j < 8; j++) {
+        const int tok = o + 4 * vhalf + (j & 3) + (j >> 2) * 8;
+        const unsigned* w = (const unsigned*)(words + tok * (4 * NG));
+#pragma unroll
+        for (int g = 0; g < (NG + 1) / 2; g++) vword[j][g] = NG == 1 ? w[0] >> 16 : w[NG / 2 + g];
+      }
+    };
+    // one dword of codes to four pairs of values: bytes (0, 2), (1, 3) of the low nibbles, then of the high ones
+    auto pair = [](unsigned w, unsigned minus, unsigned scale) -> unsigned {
+      const f16x2 c = __builtin_bit_cast(f16x2, (w & 0x000F000Fu) | 0x64006400u);
+      return __builtin_bit_cast(unsigned, (c + __builtin_bit_cast(f16x2, minus)) * __builtin_bit_cast(f16x2, scale));
+    };
+    auto convert = [&](int buf, int tile) {
+      {
+        // K: the low nibbles are unit kunit, the high ones unit kunit + KU / 2
+        unsigned out[2][4];
+#pragma unroll
+        for (int s = 0; s < 2; s++) {
+          // groups of byte column 8 kunit: below D / 2, and D / 2 further
+          const int g = DIM == 256 ? 2 * s : DIM == 128 ? s : 0;
+          unsigned w = DIM == 256 ? kword[s] : kword[0];
+          w = DIM == 256 ? (kunit >= 8 ? w >> 16 : w & 0xFFFFu) : g & 1 ? w >> 16 : w & 0xFFFFu;
+          w |= w << 16;
+          const unsigned scale = w & 0xFFF0FFF0u, minus = (w & 0x000F000Fu) | 0xE400E400u;
+#pragma unroll
+          for (int j = 0; j < 2; j++) {
+            out[s][2 * j] = pair(kraw[j] >> (4 * s), minus, scale);
+            out[s][2 * j + 1] = pair(kraw[j] >> (4 * s + 8), minus, scale);
+          }
+        }
+        if (vin) {
+          *(v4u*)&kt[buf][kat(ktok, kunit)] = v4u{out[0][0], out[0][1], out[0][2], out[0][3]};
+          *(v4u*)&kt[buf][kat(ktok, kunit + KU / 2)] = v4u{out[1][0], out[1][1], out[1][2], out[1][3]};
+        }
+      }
+      {
+        // V: words of tokens that are not there count as 0, NaN ones too (kept as bits)
+        const int tok = c0 + tile * TT + block * 16 + 4 * vhalf;
+        unsigned mask[NG], flag = page_now >= 0 ? 1 : 0;
+#pragma unroll
+        for (int g = 0; g < NG; g++) mask[g] = 0;
+#pragma unroll
+        for (int j = 0; j < 8; j++) {
+          const bool in = page_now >= 0 && tok + (j & 3) + (j >> 2) * 8 < c1;
+#pragma unroll
+          for (int g = 0; g < (NG + 1) / 2; g++) {
+            unsigned w = in ? __builtin_amdgcn_readfirstlane(vword[j][g]) : 0u;
+            if ((w & 0x7C00u) == 0x7C00u) {
+              mask[2 * g] |= 1u << j;
+              w &= 0xFFFF0000u;
+            }
+            if (NG > 1 && (w & 0x7C000000u) == 0x7C000000u) {
+              mask[NG > 1 ? 2 * g + 1 : 0] |= 1u << j;
+              w &= 0xFFFFu;
+            }
+            vword[j][g] = w;
+          }
+        }
+        unsigned out[2][4];
+#pragma unroll
+        for (int s = 0; s < 2; s++) {
+          const int wi = DIM == 256 ? s : 0;
+          const bool top = DIM == 256 ? wave & 1 : DIM == 128 ? s == 1 : false;      // group's half of the word
+#pragma unroll
+          for (int j = 0; j < 2; j++)
+#pragma unroll
+            for (int q = 0; q < 2; q++) {
+              const unsigned w0 = vword[4 * j + q][wi], w1 = vword[4 * j + q + 2][wi];
+              const unsigned w = top ? (w0 >> 16) | (w1 & 0xFFFF0000u) : (w0 & 0xFFFFu) | (w1 << 16);
+              out[s][2 * j + q] = pair(vraw[j] >> (4 * s + 8 * q), (w & 0x000F000Fu) | 0xE400E400u, w & 0xFFF0FFF0u);
+            }
+        }
+        const int u = block * 2 + vhalf;
+        if (vin) {
+          *(v4u*)&vt[buf][vat(vcol, u)] = v4u{out[0][0], out[0][1], out[0][2], out[0][3]};
+          *(v4u*)&vt[buf][vat(HALF + vcol, u)] = v4u{out[1][0], out[1][1], out[1][2], out[1][3]};
+        }
+#pragma unroll
+        for (int g = 0; g < NG; g++)
+          if (mask[g]) flag |= 2;
+        if (lane == 0) {
+          flags[buf][wave] = (uint8_t)flag;
+          if (flag & 2)
+#pragma unroll
+            for (int g = 0; g < NG; g++) nans[buf][wave][g] = (uint8_t)mask[g];
+        }
+      }
+    };
+
+    auto compute = [&](int buf, int tile) {
+      const int tok0 = c0 + tile * TT;
+      if (tok0 > none_from) return;
+      const v2u fl = *(const v2u*)flags[buf];
+      const unsigned f0 = __builtin_amdgcn_readfirstlane(fl[0]), f1 = __builtin_amdgcn_readfirstlane(fl[1]);
+      f32x16 S[NS];
+#pragma unroll
+      for (int s = 0; s < NS; s++) {
+#pragma unroll
+        for (int i = 0; i < 16; i++) S[s][i] = 0.f;
+#pragma unroll
+        for (int k = 0; k < KS; k++) {
+          const f16x8 A = *(const f16x8*)&kt[buf][kat(s * 32 + l32, 2 * k + half)];
+          S[s] = __builtin_amdgcn_mfma_f32_32x32x16_f16(A, Q[k], S[s], 0, 0, 0);
+        }
+      }
+      const bool plain = f0 == 0x01010101u && f1 == 0x01010101u && tok0 >= all_from && tok0 + TT - 1 <= all_to;
+      float top = -INFINITY;
+      if (plain) {
+#pragma unroll
+        for (int s = 0; s < NS; s++)
+#pragma unroll
+          for (int i = 0; i < 16; i++) top = fmaxf(top, S[s][i]);
+      } else {
+#pragma unroll
+        for (int s = 0; s < NS; s++)
+#pragma unroll
+          for (int i = 0; i < 16; i++) {
+            const int t = s * 32 + 8 * (i / 4) + 4 * half + i % 4, p = tok0 + t;
+            const int w = t / 16 * WB;      // a wave that converted the token's block
+            const unsigned f = (w < 4 ? f0 >> (8 * w) : f1 >> (8 * (w - 4))) & 1;
+            const bool seen = f && p <= last && p >= least;
+            top = fmaxf(top, seen ? S[s][i] : -INFINITY);
+          }
+      }
+      const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+      top = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * factor;
+      if (__any(top > ref + 8.f)) {
+        const float to = fmaxf(ref, top), keep = ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref - to);
+        ref = to;
+        l *= keep;
+#pragma unroll
+        for (int c = 0; c < CT; c++)
+#pragma unroll
+          for (int i = 0; i < 16; i++) O[c][i] *= keep;
+      }
+      const float at = ref == -INFINITY ? 0.f : ref;
+      f16x8 B[PS];
+      float sum[2] = {0.f, 0.f};
+#pragma unroll
+      for (int s = 0; s < NS; s++)
+#pragma unroll
+        for (int i = 0; i < 16; i++) S[s][i] = fmaf(S[s][i], factor, -at);
+      if (!plain) {
+#pragma unroll
+        for (int s = 0; s < NS; s++)
+#pragma unroll
+          for (int i = 0; i < 16; i++) {
+            const int t = s * 32 + 8 * (i / 4) + 4 * half + i % 4, p = tok0 + t;
+            const int w = t / 16 * WB + (WB == 2 ? half : 2 * half);      // the wave that converted the token's values
+            const unsigned f = (w < 4 ? f0 >> (8 * (w & 3)) : f1 >> (8 * (w & 3)));
+            const bool seen = (f & 1) && p <= last && p >= least;
+            S[s][i] = seen ? S[s][i] : -INFINITY;
+            if (f & 2 && seen) {
+              const int bit = i % 4 + (i / 4 & 1) * 4;
+#pragma unroll
+              for (int g = 0; g < NG; g++)
+                if (nans[buf][w][g] >> bit & 1) poison[g] = NAN;
+            }
+          }
+      }
+#pragma unroll
+      for (int k = 0; k < PS; k++) {
+        const int s = k / 2, i0 = (k & 1) * 8;
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+          const int i = i0 + (j >> 1) * 4 + (j & 1);
+          const float p0 = __builtin_amdgcn_exp2f(S[s][i]), p1 = __builtin_amdgcn_exp2f(S[s][i + 2]);
+          sum[0] += p0;
+          sum[1] += p1;
+          B[k][2 * j] = (_Float16)p0;
+          B[k][2 * j + 1] = (_Float16)p1;
+        }
+      }
+      l += sum[0] + sum[1];
+#pragma unroll
+      for (int k = 0; k < PS; k++)
+#pragma unroll
+        for (int c = 0; c < CT; c++) {
+          const f16x8 A = *(const f16x8*)&vt[buf][vat(c * 32 + l32, 2 * k + half)];
+          O[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(A, B[k], O[c], 0, 0, 0);
+        }
+    };
+
+    load(0, lookup(0));
+    int page = lookup(1);
+    convert(0, 0);
+    load(1, page);
+    page = lookup(2);
+    __syncthreads();
+    for (int tile = 0; tile < ntiles; tile++) {
+      if (tile + 1 < ntiles) {
+        convert((tile + 1) & 1, tile + 1);
+        load(tile + 2, page);
+        page = lookup(tile + 3);
+      }
+      compute(tile & 1, tile);
+      __syncthreads();
+    }
+
+    const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
+    l = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+#pragma unroll
+    for (int g = 0; g < NG; g++) poison[g] += __shfl_xor(poison[g], 32);
+    if (row < R.rows) {
+      const bool whole = R.parts == 1, none = l == 0.f;
+      const float by = whole ? none ? 0.f : 1.f / l : 1.f;
+      float* part = a.part + (to * a.nsplit + sp) * (DIM + 4);
+#pragma unroll
+      for (int c = 0; c < CT; c++)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+          const int d = c * 32 + 2 * i + 4 * half;
+          float o[4];
+#pragma unroll
+          for (int j = 0; j < 4; j++) o[j] = (O[c][i + j] + poison[c / 2]) * by;
+          if (!whole) *(f32x4*)(part + d) = f32x4{o[0], o[1], o[2], o[3]};
+          else
+#pragma unroll
+            for (int j = 0; j < 4; j++) store_any(a.out, to * DIM + d + j, o[j], a.dtype);
+        }
+      if (whole && a.lse && !half) a.lse[to] = none ? -INFINITY : (ref + log2f(l)) * 0.69314718055994530942f;
+      if (!whole && !half) {
+        part[DIM] = ref;
+        part[DIM + 1] = l;
+      }
+    }
   }
 }
 
@@ -493,15 +854,15 @@ __global__ __launch_bounds__(DIM) void k_attention_join(AttnArgs a) {
   const RowBlock R = row_block<ROWS>(a, b, row / ROWS);
   if (R.parts < 2) return;      // written by k_attention_split
   const int64_t to = t * a.heads_q + hq;
-  const float* part = a.part + to * a.nsplit * (DIM + 2);
+  const float* part = a.part + to * a.nsplit * (DIM + 4);
   float top = -INFINITY;
-  for (int p = 0; p < R.parts; p++) top = fmaxf(top, part[p * (DIM + 2) + DIM]);
+  for (int p = 0; p < R.parts; p++) top = fmaxf(top, part[p * (DIM + 4) + DIM]);
   const float at = top == -INFINITY ? 0.f : top;
   float o = 0.f, sum = 0.f;
   for (int p = 0; p < R.parts; p++) {
-    const float f = __builtin_amdgcn_exp2f(part[p * (DIM + 2) + DIM] - at);
-    o = fmaf(part[p * (DIM + 2) + d], f, o);
-    sum = fmaf(part[p * (DIM + 2) + DIM + 1], f, sum);
+    const float f = __builtin_amdgcn_exp2f(part[p * (DIM + 4) + DIM] - at);
+    o = fmaf(part[p * (DIM + 4) + d], f, o);
+    sum = fmaf(part[p * (DIM + 4) + DIM + 1], f, sum);
   }
   const bool none = sum == 0.f;
   store_any(a.out, to * DIM + d, none ? 0.f : o / sum, a.dtype);
@@ -511,20 +872,23 @@ __global__ __launch_bounds__(DIM) void k_attention_join(AttnArgs a) {
 // Row tiles of four that a workgroup takes (registers allow two at 256 channels).
 static int row_tiles(int rows, int dim) { return rows <= 4 ? 1 : rows <= 8 || dim == 256 ? 2 : 4; }
 
+constexpr int CHUNK_ROWS = 64;
+
 struct SplitPlan {
-  int rt, row_blocks, nsplit, chunk;
+  int rt, row_blocks, nsplit, chunk;      // rt 0: k_attention_chunk
 };
 // Parts of about equal size: enough workgroups to fill the chip (two of four
 // waves a CU resident, in one pass), a part no shorter than four waves' tile each.
-static SplitPlan split_plan(int each, int heads_kv, int dim, int batch, int64_t max_new, int64_t max_len) {
+static SplitPlan split_plan(int each, int heads_kv, int dim, int dtype, int batch, int64_t max_new, int64_t max_len) {
   SplitPlan p;
   const int64_t rows = max_new * each;
-  p.rt = row_tiles((int)(rows > 64 ? 64 : rows), dim);
-  const int64_t blocks = (rows + 4 * p.rt - 1) / (4 * p.rt);
+  p.rt = dtype != EXTERND_F32 && rows >= CHUNK_ROWS ? 0 : row_tiles((int)(rows > 64 ? 64 : rows), dim);
+  const int per = p.rt ? 4 * p.rt : 256;
+  const int64_t blocks = (rows + per - 1) / per;
   p.row_blocks = (int)(blocks > 16384 / heads_kv ? (16384 / heads_kv > 0 ? 16384 / heads_kv : 1) : blocks);
   const int64_t units = (int64_t)batch * heads_kv * p.row_blocks;
   const int64_t len = max_len < 1 ? 65536 : max_len;
-  int64_t n = (512 + units - 1) / units;
+  int64_t n = ((p.rt ? 512 : 256) + units - 1) / units;
   const int64_t most = (len + 255) / 256;
   n = n > most ? most : n;
   n = n > 256 ? 256 : n < 1 ? 1 : n;
@@ -546,7 +910,11 @@ static void launch_split(const AttnArgs& a, hipStream_t s) {
 }
 template <int DIM>
 static void launch_split(const AttnArgs& a, int rt, hipStream_t s) {
-  if (rt == 1) launch_split<DIM, 1>(a, s);
+  if (rt == 0) {
+    const dim3 grid((unsigned)(a.nsplit * a.c.heads), (unsigned)a.row_blocks, (unsigned)a.s.batch);
+    k_attention_chunk<DIM><<<grid, 512, 0, s>>>(a);
+    if (a.nsplit > 1) k_attention_join<DIM, 256><<<dim3((unsigned)a.s.tokens, (unsigned)a.heads_q), DIM, 0, s>>>(a);
+  } else if (rt == 1) launch_split<DIM, 1>(a, s);
   else if (rt == 2) launch_split<DIM, 2>(a, s);
   else if constexpr (DIM != 256) launch_split<DIM, 4>(a, s);
 }
@@ -568,9 +936,9 @@ extern "C" {
 size_t externd_kv4_attention_workspace_bytes(int32_t heads_q, int32_t heads_kv, int32_t head_dim, int32_t dtype,
                                              int64_t tokens, int32_t batch, int32_t max_new, int64_t max_len) {
   if (!attention_sizes_ok(heads_q, heads_kv, head_dim, dtype, tokens, batch, max_new, max_len)) return 0;
-  const SplitPlan p = split_plan(heads_q / heads_kv, heads_kv, head_dim, batch, max_new, max_len);
+  const SplitPlan p = split_plan(heads_q / heads_kv, heads_kv, head_dim, dtype, batch, max_new, max_len);
   if (p.nsplit == 1) return 0;
-  return ((size_t)tokens * heads_q * p.nsplit * (head_dim + 2) * 4 + 255) & ~(size_t)255;
+  return ((size_t)tokens * heads_q * p.nsplit * (head_dim + 4) * 4 + 255) & ~(size_t)255;
 }
 
 int externd_kv4_attention(const void* cache, int64_t num_pages, int32_t heads_kv, int32_t head_dim,
@@ -602,7 +970,7 @@ int externd_kv4_attention(const void* cache, int64_t num_pages, int32_t heads_kv
   a.scale = scale;
   a.window = window;
   a.dtype = dtype;
-  const SplitPlan p = split_plan(a.each, heads_kv, head_dim, batch, max_new, max_len);
+  const SplitPlan p = split_plan(a.each, heads_kv, head_dim, dtype, batch, max_new, max_len);
   a.nsplit = p.nsplit;
   a.chunk = p.chunk;
   a.row_blocks = p.row_blocks;
