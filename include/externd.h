@@ -440,7 +440,7 @@ int externd_rotary_frequencies(int32_t rot_dim, double base, int32_t scaling, do
  *             may be q with the same strides (in place), and no other overlap.
  *  positions  device int64[tokens], any value; freqs device uint64[rot_dim / 2].
  * head_dim 2 .. 1024, rot_dim even, 2 .. head_dim; tokens 0 is a valid call;
- * tokens < 2^31, heads <= 65535.                                          */
+ * tokens < 2^31, heads_q + heads_k <= 65535.                                */
 int externd_rotary(const void* q, void* q_out, int64_t q_token_stride, int64_t q_head_stride,
                    int64_t q_out_token_stride, int64_t q_out_head_stride, int32_t heads_q, const void* k,
                    void* k_out, int64_t k_token_stride, int64_t k_head_stride, int64_t k_out_token_stride,
@@ -487,7 +487,8 @@ int externd_kv4_append(void* cache, int64_t num_pages, int32_t heads_kv, int32_t
                        void* stream);
 
 /* The values held for the new tokens (with starts over whole sequences: for
- * all tokens), dense, as dtype; 0 where a token has no place.             */
+ * all tokens), dense and 16-byte aligned, as dtype; 0 where a token has no
+ * place.                                                                   */
 int externd_kv4_read(const void* cache, int64_t num_pages, int32_t heads_kv, int32_t head_dim, int32_t page_tokens,
                      void* k, void* v, int32_t dtype, int64_t tokens, int32_t batch, const int32_t* starts,
                      const int32_t* lens, const int32_t* table, int64_t table_pages, void* stream);

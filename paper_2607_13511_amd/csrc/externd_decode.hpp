@@ -34,6 +34,66 @@ template <> struct Elem<EXTERND_BF16> {
   static __device__ __forceinline__ __bf16 store(float v) { return (__bf16)v; }
 };
 
+typedef unsigned v4u __attribute__((ext_vector_type(4)));
+typedef unsigned v2u __attribute__((ext_vector_type(2)));
+
+// 16 bytes of a type.
+template <int DT> struct Vec {
+  static constexpr int E = DT == EXTERND_F32 ? 4 : 8;      // entries
+  static __device__ __forceinline__ void unpack(v4u v, float* x) {
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      if constexpr (DT == EXTERND_F32) x[i] = __uint_as_float(v[i]);
+      else if constexpr (DT == EXTERND_BF16) {
+        x[2 * i] = __uint_as_float(v[i] << 16);
+        x[2 * i + 1] = __uint_as_float(v[i] & 0xFFFF0000u);
+      } else {
+        x[2 * i] = (float)__builtin_bit_cast(_Float16, (uint16_t)v[i]);
+        x[2 * i + 1] = (float)__builtin_bit_cast(_Float16, (uint16_t)(v[i] >> 16));
+      }
+    }
+  }
+  static __device__ __forceinline__ v4u pack(const float* x) {
+    v4u v;
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      if constexpr (DT == EXTERND_F32) v[i] = __float_as_uint(x[i]);
+      else
+        v[i] = (unsigned)__builtin_bit_cast(uint16_t, Elem<DT>::store(x[2 * i])) |
+               (unsigned)__builtin_bit_cast(uint16_t, Elem<DT>::store(x[2 * i + 1])) << 16;
+    }
+    return v;
+  }
+};
+
+// N entries at p, in 16-byte loads or stores where VEC (p is 16-byte aligned then).
+template <int DT, int N, bool VEC>
+__device__ __forceinline__ void load_n(const typename Elem<DT>::T* p, float* x) {
+  constexpr int E = Vec<DT>::E;
+  if constexpr (VEC) {
+#pragma unroll
+    for (int i = 0; i < N / E; i++) Vec<DT>::unpack(((const v4u*)p)[i], x + i * E);
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; i++) x[i] = Elem<DT>::load(p[i]);
+  }
+}
+template <int DT, int N, bool VEC>
+__device__ __forceinline__ void store_n(typename Elem<DT>::T* p, const float* x) {
+  constexpr int E = Vec<DT>::E;
+  if constexpr (VEC) {
+#pragma unroll
+    for (int i = 0; i < N / E; i++) ((v4u*)p)[i] = Vec<DT>::pack(x + i * E);
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; i++) p[i] = Elem<DT>::store(x[i]);
+  }
+}
+// Whether every head of an array starts at a multiple of 16 bytes.
+inline bool rows_aligned(const void* p, int64_t token_stride, int64_t head_stride, int bytes) {
+  return !(((uintptr_t)p | (uint64_t)(token_stride * bytes) | (uint64_t)(head_stride * bytes)) & 15);
+}
+
 // The cache's layout for one page size and head width (include/externd.h).
 struct Kv4Shape {
   int64_t num_pages;

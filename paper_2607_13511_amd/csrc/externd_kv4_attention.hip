@@ -7,8 +7,6 @@
 namespace externd {
 
 typedef int v4i __attribute__((ext_vector_type(4)));
-typedef unsigned v4u __attribute__((ext_vector_type(4)));
-typedef unsigned v2u __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -148,6 +146,79 @@ __global__ __launch_bounds__(256, DIM * RT <= 128 ? 3 : 2) void k_attention_spli
     if (sp >= R.parts) continue;
     const int c0 = R.lo + sp * R.part, c1 = (int)min((int64_t)R.hi, (int64_t)c0 + R.part);
 
+    uint8_t* const pbuf = lds + SHARED_Q + wave * (NG * (16 * PROW + 64));
+    uint8_t* const zbuf = pbuf + NG * 16 * PROW;
+
+    const int ntiles = (c1 - c0 + 63) >> 6;
+    constexpr int NW = NG == 1 ? 1 : NG / 2;    // 32-bit loads of a token's K words (V's likewise; one for both at 64)
+    v4u kr[4][NU], vr[NC];
+    unsigned kw[4][NW], vw[4][NW];
+    unsigned ok = 0;        // bit t: block t of the tile has a page
+    // page of this lane's block (seg) of a tile, or -1
+    auto lookup = [&](int tile) -> int {
+      const int tok = c0 + tile * 64 + seg * 16;
+      if (tile >= ntiles || tok >= c1) return -1;
+      const int page = a.s.table[(int64_t)b * a.s.table_pages + (tok >> a.c.page_log2)];
+      return page >= 0 && page < a.c.num_pages ? page : -1;
+    };
+    auto base_of = [&](uint64_t off, int t) -> const uint8_t* {
+      const unsigned lo = __builtin_amdgcn_readlane((unsigned)off, 16 * t);
+      const unsigned hi = __builtin_amdgcn_readlane((unsigned)(off >> 32), 16 * t);
+      return a.cache + ((uint64_t)hi << 32 | lo);
+    };
+    auto offset_of = [&](int page) -> uint64_t {
+      return (uint64_t)((int64_t)max(page, 0) * a.c.heads + h) * (uint64_t)a.c.head_bytes;
+    };
+    auto load_k = [&](int tile, int page) {
+      const uint64_t off = offset_of(page);
+#pragma unroll
+      for (int t = 0; t < 4; t++) {
+        const uint8_t* base = base_of(off, t);
+        const unsigned o = (unsigned)((c0 + tile * 64 + 16 * t) & (P - 1)) + l16;
+        const uint8_t* kp = base + o * HALF + seg * (DIM == 64 ? 8 : 16);
+        if constexpr (DIM == 64) {
+          const v2u x = *(const v2u*)kp;
+          kr[t][0] = v4u{x[0], x[1], 0, 0};
+        } else {
+#pragma unroll
+          for (int u = 0; u < NU; u++) kr[t][u] = *(const v4u*)(kp + 64 * u);
+        }
+        const unsigned* wp = (const unsigned*)(base + (unsigned)P * DIM + o * (4 * NG));
+#pragma unroll
+        for (int g = 0; g < NW; g++) kw[t][g] = wp[g];
+      }
+    };
+    auto load_v = [&](int tile, int page) {
+      const uint64_t off = offset_of(page);
+      const int tok = c0 + tile * 64;
+      ok = 0;
+#pragma unroll
+      for (int t = 0; t < 4; t++) {
+        if constexpr (NG > 1) {
+          const unsigned o = (unsigned)((tok + 16 * t) & (P - 1)) + l16;
+          const unsigned* wp = (const unsigned*)(base_of(off, t) + (unsigned)P * DIM + o * (4 * NG)) + NW;
+#pragma unroll
+          for (int g = 0; g < NW; g++) vw[t][g] = wp[g];
+        }
+        ok |= (unsigned)(__builtin_amdgcn_readlane(page, 16 * t) >= 0) << t;
+      }
+      const uint8_t* vp = a.cache + off + (unsigned)P * HALF + ((unsigned)((tok + 16 * seg) & (P - 1)) >> 4) * (HALF * 16) + l16 * 16;
+#pragma unroll
+      for (int c = 0; c < NC; c++) vr[c] = *(const v4u*)(vp + c * 256);
+    };
+    auto k_word = [&](int t, int g) -> unsigned { return g & 1 ? kw[t][g / 2] >> 16 : kw[t][g / 2] & 0xFFFFu; };
+    auto v_word = [&](int t, int g) -> unsigned {
+      if (NG == 1) return vw[t][0] >> 16;
+      return g & 1 ? vw[t][g / 2] >> 16 : vw[t][g / 2] & 0xFFFFu;
+    };
+
+    // the first tile's loads are in flight while the queries are taken apart
+    int page = lookup(wave);
+    if (wave < ntiles) {
+      load_k(wave, page);
+      load_v(wave, page);
+    }
+
     // ---- the rows' digits, one wave per row ----
     for (int r = wave; r < ROWS; r += 4) {
       const int row = rb * ROWS + r;
@@ -217,72 +288,6 @@ __global__ __launch_bounds__(256, DIM * RT <= 128 ? 3 : 2) void k_attention_spli
 #pragma unroll
       for (int i = 0; i < 2 * NC; i++) O[p][i] = 0.f;
     }
-    uint8_t* const pbuf = lds + SHARED_Q + wave * (NG * (16 * PROW + 64));
-    uint8_t* const zbuf = pbuf + NG * 16 * PROW;
-
-    const int ntiles = (c1 - c0 + 63) >> 6;
-    constexpr int NW = NG == 1 ? 1 : NG / 2;    // 32-bit loads of a token's K words (V's likewise; one for both at 64)
-    v4u kr[4][NU], vr[NC];
-    unsigned kw[4][NW], vw[4][NW];
-    unsigned ok = 0;        // bit t: block t of the tile has a page
-    // page of this lane's block (seg) of a tile, or -1
-    auto lookup = [&](int tile) -> int {
-      const int tok = c0 + tile * 64 + seg * 16;
-      if (tile >= ntiles || tok >= c1) return -1;
-      const int page = a.s.table[(int64_t)b * a.s.table_pages + (tok >> a.c.page_log2)];
-      return page >= 0 && page < a.c.num_pages ? page : -1;
-    };
-    auto base_of = [&](uint64_t off, int t) -> const uint8_t* {
-      const unsigned lo = __builtin_amdgcn_readlane((unsigned)off, 16 * t);
-      const unsigned hi = __builtin_amdgcn_readlane((unsigned)(off >> 32), 16 * t);
-      return a.cache + ((uint64_t)hi << 32 | lo);
-    };
-    auto offset_of = [&](int page) -> uint64_t {
-      return (uint64_t)((int64_t)max(page, 0) * a.c.heads + h) * (uint64_t)a.c.head_bytes;
-    };
-    auto load_k = [&](int tile, int page) {
-      const uint64_t off = offset_of(page);
-#pragma unroll
-      for (int t = 0; t < 4; t++) {
-        const uint8_t* base = base_of(off, t);
-        const unsigned o = (unsigned)((c0 + tile * 64 + 16 * t) & (P - 1)) + l16;
-        const uint8_t* kp = base + o * HALF + seg * (DIM == 64 ? 8 : 16);
-        if constexpr (DIM == 64) {
-          const v2u x = *(const v2u*)kp;
-          kr[t][0] = v4u{x[0], x[1], 0, 0};
-        } else {
-#pragma unroll
-          for (int u = 0; u < NU; u++) kr[t][u] = *(const v4u*)(kp + 64 * u);
-        }
-        const unsigned* wp = (const unsigned*)(base + (unsigned)P * DIM + o * (4 * NG));
-#pragma unroll
-        for (int g = 0; g < NW; g++) kw[t][g] = wp[g];
-      }
-    };
-    auto load_v = [&](int tile, int page) {
-      const uint64_t off = offset_of(page);
-      const int tok = c0 + tile * 64;
-      ok = 0;
-#pragma unroll
-      for (int t = 0; t < 4; t++) {
-        if constexpr (NG > 1) {
-          const unsigned o = (unsigned)((tok + 16 * t) & (P - 1)) + l16;
-          const unsigned* wp = (const unsigned*)(base_of(off, t) + (unsigned)P * DIM + o * (4 * NG)) + NW;
-#pragma unroll
-          for (int g = 0; g < NW; g++) vw[t][g] = wp[g];
-        }
-        ok |= (unsigned)(__builtin_amdgcn_readlane(page, 16 * t) >= 0) << t;
-      }
-      const uint8_t* vp = a.cache + off + (unsigned)P * HALF + ((unsigned)((tok + 16 * seg) & (P - 1)) >> 4) * (HALF * 16) + l16 * 16;
-#pragma unroll
-      for (int c = 0; c < NC; c++) vr[c] = *(const v4u*)(vp + c * 256);
-    };
-    auto k_word = [&](int t, int g) -> unsigned { return g & 1 ? kw[t][g / 2] >> 16 : kw[t][g / 2] & 0xFFFFu; };
-    auto v_word = [&](int t, int g) -> unsigned {
-      if (NG == 1) return vw[t][0] >> 16;
-      return g & 1 ? vw[t][g / 2] >> 16 : vw[t][g / 2] & 0xFFFFu;
-    };
-
     // One tile: K's registers are free once the scores are there and take the
     // next tile's K then; V's likewise at the end.
     auto compute = [&](int tile, int next_page) {
@@ -419,11 +424,6 @@ __global__ __launch_bounds__(256, DIM * RT <= 128 ? 3 : 2) void k_attention_spli
       if (more) load_v(tile + 4, next_page);
     };
 
-    int page = lookup(wave);
-    if (wave < ntiles) {
-      load_k(wave, page);
-      load_v(wave, page);
-    }
     page = lookup(wave + 4);
     for (int tile = wave; tile < ntiles; tile += 4) {
       const int after = lookup(tile + 8);
@@ -841,32 +841,56 @@ __global__ __launch_bounds__(512, 2) void k_attention_chunk(AttnArgs a) {
   }
 }
 
-// Joins the parts of a row: one workgroup of DIM threads per new token and
-// query head.
+// Joins the parts of a row (at most 256): one workgroup per new token and query
+// head, four channels a thread and 1024 / DIM parts side by side.
 template <int DIM, int ROWS>
-__global__ __launch_bounds__(DIM) void k_attention_join(AttnArgs a) {
+__global__ __launch_bounds__(256) void k_attention_join(AttnArgs a) {
+  constexpr int TH = DIM / 4, GR = 256 / TH;
+  __shared__ float weight[256], red[8];
+  __shared__ f32x4 acc[GR][TH];
   const int64_t t = blockIdx.x;
-  const int hq = blockIdx.y, d = threadIdx.x;
+  const int hq = blockIdx.y, tid = threadIdx.x;
   const int b = sequence_of(a.s, t);
   const int64_t t0 = a.s.starts ? a.s.starts[b] : b;
   const int row = (int)(t - t0) * a.each + hq % a.each;
   if (row < 0) return;
   const RowBlock R = row_block<ROWS>(a, b, row / ROWS);
-  if (R.parts < 2) return;      // written by k_attention_split
+  if (R.parts < 2) return;      // written by the kernel before
   const int64_t to = t * a.heads_q + hq;
   const float* part = a.part + to * a.nsplit * (DIM + 4);
-  float top = -INFINITY;
-  for (int p = 0; p < R.parts; p++) top = fmaxf(top, part[p * (DIM + 4) + DIM]);
+  const float m = tid < R.parts ? part[(size_t)tid * (DIM + 4) + DIM] : -INFINITY;
+  const float l = tid < R.parts ? part[(size_t)tid * (DIM + 4) + DIM + 1] : 0.f;
+  float top = m;
+  for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+  if ((tid & 63) == 0) red[tid >> 6] = top;
+  __syncthreads();
+  top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
   const float at = top == -INFINITY ? 0.f : top;
-  float o = 0.f, sum = 0.f;
-  for (int p = 0; p < R.parts; p++) {
-    const float f = __builtin_amdgcn_exp2f(part[p * (DIM + 4) + DIM] - at);
-    o = fmaf(part[p * (DIM + 4) + d], f, o);
-    sum = fmaf(part[p * (DIM + 4) + DIM + 1], f, sum);
+  const float w = __builtin_amdgcn_exp2f(m - at);
+  weight[tid] = w;
+  float sum = tid < R.parts ? w * l : 0.f;
+  for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
+  if ((tid & 63) == 0) red[4 + (tid >> 6)] = sum;
+  __syncthreads();
+  sum = (red[4] + red[5]) + (red[6] + red[7]);
+  const int g = tid / TH, c = tid % TH;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int p = g; p < R.parts; p += GR) {
+    const f32x4 x = *(const f32x4*)(part + (size_t)p * (DIM + 4) + 4 * c);
+    const float f = weight[p];
+#pragma unroll
+    for (int j = 0; j < 4; j++) o[j] = fmaf(x[j], f, o[j]);
   }
+  acc[g][c] = o;
+  __syncthreads();
+  if (tid >= DIM) return;
+  float out = 0.f;
+#pragma unroll
+  for (int i = 0; i < GR; i++) out += acc[i][tid >> 2][tid & 3];
   const bool none = sum == 0.f;
-  store_any(a.out, to * DIM + d, none ? 0.f : o / sum, a.dtype);
-  if (a.lse && d == 0) a.lse[to] = none ? -INFINITY : (top + log2f(sum)) * 0.69314718055994530942f;
+  store_any(a.out, to * DIM + tid, none ? 0.f : out / sum, a.dtype);
+  if (a.lse && tid == 0) a.lse[to] = none ? -INFINITY : (top + log2f(sum)) * 0.69314718055994530942f;
 }
 
 // Row tiles of four that a workgroup takes (registers allow two at 256 channels).
@@ -906,14 +930,14 @@ static void launch_split(const AttnArgs& a, hipStream_t s) {
   if (a.dtype == EXTERND_F32) k_attention_split<DIM, RT, true><<<grid, 256, 0, s>>>(a);
   else k_attention_split<DIM, RT, false><<<grid, 256, 0, s>>>(a);
   if (a.nsplit > 1)
-    k_attention_join<DIM, 4 * RT><<<dim3((unsigned)a.s.tokens, (unsigned)a.heads_q), DIM, 0, s>>>(a);
+    k_attention_join<DIM, 4 * RT><<<dim3((unsigned)a.s.tokens, (unsigned)a.heads_q), 256, 0, s>>>(a);
 }
 template <int DIM>
 static void launch_split(const AttnArgs& a, int rt, hipStream_t s) {
   if (rt == 0) {
     const dim3 grid((unsigned)(a.nsplit * a.c.heads), (unsigned)a.row_blocks, (unsigned)a.s.batch);
     k_attention_chunk<DIM><<<grid, 512, 0, s>>>(a);
-    if (a.nsplit > 1) k_attention_join<DIM, 256><<<dim3((unsigned)a.s.tokens, (unsigned)a.heads_q), DIM, 0, s>>>(a);
+    if (a.nsplit > 1) k_attention_join<DIM, 256><<<dim3((unsigned)a.s.tokens, (unsigned)a.heads_q), 256, 0, s>>>(a);
   } else if (rt == 1) launch_split<DIM, 1>(a, s);
   else if (rt == 2) launch_split<DIM, 2>(a, s);
   else if constexpr (DIM != 256) launch_split<DIM, 4>(a, s);

@@ -30,38 +30,8 @@ __device__ __forceinline__ float value_of(uint64_t key) {
 }
 __device__ __forceinline__ int64_t index_of(uint64_t key) { return (int64_t)(0xFFFFFFFFu - (unsigned)key); }
 
-typedef unsigned v4u __attribute__((ext_vector_type(4)));
-
 // A larger of two that is a NaN where one of them is.
 __device__ __forceinline__ float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }
-
-template <int DT> struct Vec {
-  static constexpr int E = DT == EXTERND_F32 ? 4 : 8;      // entries of 16 bytes
-  static __device__ __forceinline__ void unpack(v4u v, float* x) {
-#pragma unroll
-    for (int i = 0; i < 4; i++) {
-      if constexpr (DT == EXTERND_F32) x[i] = __uint_as_float(v[i]);
-      else if constexpr (DT == EXTERND_BF16) {
-        x[2 * i] = __uint_as_float(v[i] << 16);
-        x[2 * i + 1] = __uint_as_float(v[i] & 0xFFFF0000u);
-      } else {
-        x[2 * i] = (float)__builtin_bit_cast(_Float16, (uint16_t)v[i]);
-        x[2 * i + 1] = (float)__builtin_bit_cast(_Float16, (uint16_t)(v[i] >> 16));
-      }
-    }
-  }
-  static __device__ __forceinline__ v4u pack(const float* x) {
-    v4u v;
-#pragma unroll
-    for (int i = 0; i < 4; i++) {
-      if constexpr (DT == EXTERND_F32) v[i] = __float_as_uint(x[i]);
-      else
-        v[i] = (unsigned)__builtin_bit_cast(uint16_t, Elem<DT>::store(x[2 * i])) |
-               (unsigned)__builtin_bit_cast(uint16_t, Elem<DT>::store(x[2 * i + 1])) << 16;
-    }
-    return v;
-  }
-};
 
 // Entries of a row before its first 16-byte boundary.
 template <int DT>

@@ -38,32 +38,87 @@ __device__ __forceinline__ void sincos_turns(uint64_t phase, float* s, float* c)
   *c = (quarter + 1) & 2 ? -v : v;
 }
 
-// One workgroup per token and side: its threads go over the heads' entries,
-// a pair (or an entry that is only copied) at a time.
-template <int DT>
-__global__ __launch_bounds__(256) void k_rotary(RotaryArgs a) {
+// A workgroup takes TW tokens and `span` heads of q and k side by side: sin and
+// cos of its tokens' pairs once, in LDS, then units of N entries (of both
+// partners, N each), the unit index running through a head first.  Bound by
+// memory: 8191 tokens of 40 heads of 128 in bf16, 168 MB.
+template <int DT, int N, bool VEC>
+__global__ __launch_bounds__(256) void k_rotary(RotaryArgs a, int tw, int span) {
   typedef typename Elem<DT>::T T;
-  const int64_t t = blockIdx.x;
-  const RotarySide sd = a.side[blockIdx.y];
-  const int half = a.rot / 2, rest = a.dim - a.rot, per = half + rest;
-  const uint64_t pos = (uint64_t)a.positions[t];
-  for (int e = threadIdx.x; e < sd.heads * per; e += 256) {
-    const int h = e / per, i = e - h * per;
-    const T* in = (const T*)sd.in + t * sd.its + h * sd.ihs;
-    T* out = (T*)sd.out + t * sd.ots + h * sd.ohs;
-    if (i >= half) {
-      out[a.rot + i - half] = in[a.rot + i - half];
-      continue;
-    }
-    const int p = a.interleaved ? 2 * i : i, q = a.interleaved ? 2 * i + 1 : i + half;
+  extern __shared__ float2 turn[];      // tw x rot / 2: cos, sin
+  const int half = a.rot / 2, heads = a.side[0].heads + a.side[1].heads;
+  const int64_t t0 = (int64_t)blockIdx.x * tw;
+  const int nt = (int)min((int64_t)tw, a.tokens - t0);
+  const int h0 = blockIdx.y * span, nh = min(span, heads - h0);
+  for (int e = threadIdx.x; e < nt * half; e += 256) {
+    const int t = e / half;
     float s, c;
-    sincos_turns(pos * a.freqs[i], &s, &c);
-    s *= a.sign * a.amplitude;
-    c *= a.amplitude;
-    const float x = Elem<DT>::load(in[p]), y = Elem<DT>::load(in[q]);
-    out[p] = Elem<DT>::store(x * c - y * s);
-    out[q] = Elem<DT>::store(y * c + x * s);
+    sincos_turns((uint64_t)a.positions[t0 + t] * a.freqs[e - t * half], &s, &c);
+    turn[e] = make_float2(c * a.amplitude, s * a.sign * a.amplitude);
   }
+  __syncthreads();
+  const int pairs = (a.interleaved ? a.rot : half) / N;      // units that turn
+  constexpr int RN = VEC ? N : 1;      // entries of a unit that is only copied
+  const int units = pairs + (a.dim - a.rot) / RN;
+  for (int e = threadIdx.x; e < nt * nh * units; e += 256) {
+    const int th = e / units, u = e - th * units, t = th / nh, h = h0 + th - t * nh;
+    const RotarySide& sd = h < a.side[0].heads ? a.side[0] : a.side[1];
+    const int hh = h < a.side[0].heads ? h : h - a.side[0].heads;
+    const T* in = (const T*)sd.in + (t0 + t) * sd.its + hh * sd.ihs;
+    T* out = (T*)sd.out + (t0 + t) * sd.ots + hh * sd.ohs;
+    const float2* cs = turn + t * half;
+    if (u >= pairs) {                     // entries behind the turned ones
+      const int d = a.rot + (u - pairs) * RN;
+      if (in == out) continue;
+      float x[RN];
+      load_n<DT, RN, VEC>(in + d, x);
+      store_n<DT, RN, VEC>(out + d, x);
+    } else if (a.interleaved) {
+      const int d = u * N;
+      float x[N], y[N];
+      load_n<DT, N, VEC>(in + d, x);
+#pragma unroll
+      for (int i = 0; i < N; i += 2) {
+        const float2 w = cs[d / 2 + i / 2];
+        y[i] = x[i] * w.x - x[i + 1] * w.y;
+        y[i + 1] = x[i + 1] * w.x + x[i] * w.y;
+      }
+      store_n<DT, N, VEC>(out + d, y);
+    } else {
+      const int d = u * N;
+      float x[N], y[N], p[N], q[N];
+      load_n<DT, N, VEC>(in + d, x);
+      load_n<DT, N, VEC>(in + half + d, y);
+#pragma unroll
+      for (int i = 0; i < N; i++) {
+        const float2 w = cs[d + i];
+        p[i] = x[i] * w.x - y[i] * w.y;
+        q[i] = y[i] * w.x + x[i] * w.y;
+      }
+      store_n<DT, N, VEC>(out + d, p);
+      store_n<DT, N, VEC>(out + half + d, q);
+    }
+  }
+}
+
+template <int DT>
+static void launch_rotary(const RotaryArgs& a, bool vec, hipStream_t s) {
+  constexpr int E = Vec<DT>::E;
+  const int half = a.rot / 2, heads = a.side[0].heads + a.side[1].heads;
+  const int n = vec ? E : a.interleaved || !(half & 1) ? 2 : 1;
+  const int units = (a.interleaved ? a.rot : half) / n + (a.dim - a.rot) / (vec ? n : 1);
+  // a workgroup's work: about eight units a thread, fewer where that leaves CUs without any (512 workgroups wanted)
+  int64_t per = a.tokens * heads * units / 512;
+  per = per > 2048 ? 2048 : per < 256 ? 256 : per;
+  int tw = (int)(per / (heads * units));
+  tw = tw < 1 ? 1 : tw * half > 4096 ? (4096 / half > 1 ? 4096 / half : 1) : tw;
+  int span = tw > 1 ? heads : (int)(per / units);
+  span = span < 1 ? 1 : span > heads ? heads : span;
+  const dim3 grid((unsigned)((a.tokens + tw - 1) / tw), (unsigned)((heads + span - 1) / span));
+  const size_t lds = (size_t)tw * half * sizeof(float2);
+  if (vec) k_rotary<DT, E, true><<<grid, 256, lds, s>>>(a, tw, span);
+  else if (n == 2) k_rotary<DT, 2, false><<<grid, 256, lds, s>>>(a, tw, span);
+  else k_rotary<DT, 1, false><<<grid, 256, lds, s>>>(a, tw, span);
 }
 
 }  // namespace externd
@@ -110,7 +165,7 @@ int externd_rotary(const void* q, void* q_out, int64_t q_token_stride, int64_t q
     return EXTERND_EINVAL;
   if (!freqs || (tokens && (!q || !q_out || !positions)) || (k != nullptr) != (k_out != nullptr) || (k && heads_k < 1))
     return EXTERND_EINVAL;
-  if (head_dim > 1024 || heads_q > 65535 || (k && heads_k > 65535) || tokens > INT32_MAX) return EXTERND_EUNSUPPORTED;
+  if (head_dim > 1024 || (int64_t)heads_q + (k ? heads_k : 0) > 65535 || tokens > INT32_MAX) return EXTERND_EUNSUPPORTED;
   if (!tokens) return EXTERND_OK;
   RotaryArgs a;
   a.side[0] = {q, q_out, q_token_stride, q_head_stride, q_out_token_stride, q_out_head_stride, heads_q};
@@ -123,11 +178,17 @@ int externd_rotary(const void* q, void* q_out, int64_t q_token_stride, int64_t q
   a.interleaved = interleaved;
   a.amplitude = amplitude;
   a.sign = inverse ? -1.f : 1.f;
-  const dim3 grid((unsigned)tokens, k ? 2 : 1);
+  if (!k) a.side[1].heads = 0;
+  const int es = dtype_bytes(dtype), e = 16 / es;
+  // 16-byte units: no unit may straddle the halves, the turned part or the head
+  bool vec = !((interleaved ? rot_dim : rot_dim / 2) % e) && !((head_dim - rot_dim) % e);
+  for (int i = 0; i < (k ? 2 : 1); i++)
+    vec = vec && rows_aligned(a.side[i].in, a.side[i].its, a.side[i].ihs, es) &&
+          rows_aligned(a.side[i].out, a.side[i].ots, a.side[i].ohs, es);
   const hipStream_t s = (hipStream_t)stream;
-  if (dtype == EXTERND_F32) k_rotary<EXTERND_F32><<<grid, 256, 0, s>>>(a);
-  else if (dtype == EXTERND_BF16) k_rotary<EXTERND_BF16><<<grid, 256, 0, s>>>(a);
-  else k_rotary<EXTERND_F16><<<grid, 256, 0, s>>>(a);
+  if (dtype == EXTERND_F32) launch_rotary<EXTERND_F32>(a, vec, s);
+  else if (dtype == EXTERND_BF16) launch_rotary<EXTERND_BF16>(a, vec, s);
+  else launch_rotary<EXTERND_F16>(a, vec, s);
   return hipGetLastError() == hipSuccess ? EXTERND_OK : EXTERND_EHIP;
 }
 
