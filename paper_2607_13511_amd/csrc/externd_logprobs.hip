@@ -41,10 +41,52 @@ __device__ __forceinline__ int64_t row_head(const void* p, int64_t n) {
   return h < n ? h : n;
 }
 
-__device__ __forceinline__ uint64_t shfl_xor64(uint64_t v, int d) {
-  const unsigned lo = __shfl_xor((unsigned)v, d), hi = __shfl_xor((unsigned)(v >> 32), d);
-  return (uint64_t)hi << 32 | lo;
+// The value of lane ^ D, without LDS: DPP within 16 lanes, row swaps beyond.
+template <int D>
+__device__ __forceinline__ unsigned xor_lane(unsigned v) {
+  if constexpr (D == 1) return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xF, 0xF, true);
+  else if constexpr (D == 2) return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xF, 0xF, true);
+  else if constexpr (D == 4) {      // mirrored within 8 lanes (^ 7), then within 4 (^ 3)
+    const int m = __builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xF, 0xF, true);
+    return (unsigned)__builtin_amdgcn_update_dpp(0, m, 0x1B, 0xF, 0xF, true);
+  } else if constexpr (D == 8) return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x128, 0xF, 0xF, true);
+  else if constexpr (D == 16) {
+    const auto s = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    return threadIdx.x & 16 ? s[0] : s[1];
+  } else {
+    const auto s = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return threadIdx.x & 32 ? s[0] : s[1];
+  }
 }
+template <int D>
+__device__ __forceinline__ uint64_t xor_lane64(uint64_t v) {
+  return (uint64_t)xor_lane<D>((unsigned)(v >> 32)) << 32 | xor_lane<D>((unsigned)v);
+}
+// One step of a bitonic network: the lower lane of a pair keeps the smaller key where `up`.
+template <int D>
+__device__ __forceinline__ uint64_t order_pair(uint64_t k, bool up) {
+  const uint64_t o = xor_lane64<D>(k);
+  const bool low = !(threadIdx.x & D);
+  return (low == up) == (k < o) ? k : o;
+}
+template <int SIZE, int D>
+__device__ __forceinline__ uint64_t order_steps(uint64_t k, bool up) {
+  k = order_pair<D>(k, up);
+  if constexpr (D > 1) return order_steps<SIZE, D / 2>(k, up);
+  else return k;
+}
+// Rising over the wave.
+template <int SIZE = 2>
+__device__ __forceinline__ uint64_t sort_rising(uint64_t k) {
+  k = order_steps<SIZE, SIZE / 2>(k, SIZE == 64 || !(threadIdx.x & SIZE));
+  if constexpr (SIZE < 64) return sort_rising<SIZE * 2>(k);
+  else return k;
+}
+// The 64 largest of a falling and a rising list, falling.
+__device__ __forceinline__ uint64_t merge_lists(uint64_t falling, uint64_t rising) {
+  return order_steps<64, 32>(falling > rising ? falling : rising, false);
+}
+
 __device__ __forceinline__ float wave_sum(float v) {
   for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
   return v;
@@ -55,9 +97,12 @@ __device__ __forceinline__ float wave_max(float v) {
 }
 
 // The largest keys that a wave has seen, lane i the i-th, and those not sorted in yet.
+constexpr int BEST_WORDS = 128 + 128 + 8;      // 64-bit words of LDS
 struct Best {
   uint64_t key;          // 0: none
   uint64_t* waiting;     // LDS, 128 keys
+  float* some;           // LDS, 16 lanes' entries, and where each lane's begin
+  unsigned* whose;
   int count;             // of them
   int top;
   float bar;             // entries not above it are out; a NaN (nothing compares) while fewer than `top` are known
@@ -65,6 +110,8 @@ struct Best {
   __device__ __forceinline__ void init(uint64_t* lds, int k) {
     key = 0;
     waiting = lds;
+    some = (float*)(lds + 128);
+    whose = (unsigned*)(some + 256);
     count = 0;
     top = k;
     bar = NAN;
@@ -72,18 +119,7 @@ struct Best {
   // Sorts the first (at most 64) waiting keys in.
   __device__ __forceinline__ void merge() {
     const int lane = threadIdx.x & 63;
-    uint64_t k = lane < count ? waiting[lane] : 0;
-    for (int size = 2; size <= 64; size <<= 1)        // ascending over the wave
-      for (int d = size >> 1; d; d >>= 1) {
-        const uint64_t o = shfl_xor64(k, d);
-        const bool low = !(lane & d), up = size == 64 || !(lane & size);
-        k = (low == up) == (k < o) ? k : o;
-      }
-    key = key > k ? key : k;                          // the 64 largest of both, rising then falling
-    for (int d = 32; d; d >>= 1) {
-      const uint64_t o = shfl_xor64(key, d);
-      key = !(lane & d) == (key > o) ? key : o;
-    }
+    key = merge_lists(key, sort_rising(lane < count ? waiting[lane] : 0));
     const int left = count - 64;
     if (left > 0 && lane < left) waiting[lane] = waiting[64 + lane];
     count = left > 0 ? left : 0;
@@ -100,12 +136,40 @@ struct Best {
     count += __popcll(mask);
     if (count >= 64) merge();
   }
+  // The lanes of `may` have one at least.  Sixteen of them at a time put all of
+  // theirs side by side, so that 64 are looked at together.
+  template <int E, int G>
+  __device__ __forceinline__ void search(const float (*x)[E], uint64_t may, unsigned index) {
+    constexpr int S = E * G;
+    const int lane = threadIdx.x & 63, rank = __popcll(may & ((1ull << lane) - 1)), n = __popcll(may);
+    const bool mine = may >> lane & 1;
+    // earlier entries have lower indices, so what equals their bar is out; what these ones raise it to is not
+    const float was = bar;
+    for (int r0 = 0; r0 < n; r0 += 16) {
+      __builtin_amdgcn_wave_barrier();      // the wave's own LDS, in order
+      if (mine && rank >= r0 && rank < r0 + 16) {
+#pragma unroll
+        for (int g = 0; g < G; g++)
+#pragma unroll
+          for (int e = 0; e < E; e++) some[(rank - r0) * S + g * E + e] = x[g][e];
+        whose[rank - r0] = index;
+      }
+      __builtin_amdgcn_wave_barrier();
+      const int m = min(16, n - r0) * S;
+      for (int j = lane; j - lane < m; j += 64) {
+        const int at = j < m ? j : 0, slot = at % S;
+        const float v = some[at];
+        const unsigned i = whose[at / S] + (slot / E) * (64 * E) + slot % E;
+        offer(j < m && !(v <= was) && !(v < bar), v, i);
+      }
+    }
+  }
 };
 
 // Sums of a row (or a part of it) of one lane: with y = (x - ref) scale log2(e),
 // s = sum 2^y and t = sum 2^y y.  `ref` is the same in a wave: the largest entry
 // of the first ones, and moved only when one is 2^8 larger, so that entries
-// need no maximum of their own.
+// need no maximum of their own, and y is one fused multiply-add.
 struct Sums {
   float ref, s, t;
   __device__ __forceinline__ void move(float to, float c) {
@@ -116,30 +180,43 @@ struct Sums {
   }
 };
 
-// Wave-wide: E entries of every lane (present: whether the lane has any).
-template <int E>
-__device__ __forceinline__ void take(const float* x, bool present, unsigned index, float c, Sums& a, Best& best, bool first) {
-  float big = x[0];
+// Wave-wide: G times E entries of every lane (present: whether the lane has
+// any), those of g from index + 64 E g on.
+template <int E, int G>
+__device__ __forceinline__ void take(const float (*x)[E], bool present, unsigned index, float c, Sums& a, Best& best, bool first) {
+  float big = x[0][0];
 #pragma unroll
-  for (int e = 1; e < E; e++) big = larger(big, x[e]);
+  for (int g = 0; g < G; g++)
+#pragma unroll
+    for (int e = 0; e < E; e++) big = larger(big, x[g][e]);
   big = present ? big : -INFINITY;
   if (first) a.ref = fmaxf(wave_max(big), -3.402823466e38f);
   else if (__any((big - a.ref) * c > 8.f)) a.move(wave_max(big), c);
-  if (best.top && __any(present && !(big <= best.bar))) {
-    // earlier entries have lower indices, so what equals their bar is out; what these ones raise it to is not
-    const float bar = best.bar;
+  const uint64_t may = best.top ? __ballot(present && !(big <= best.bar)) : 0;
+  if (may) best.search<E, G>(x, may, index);
+  float s[4] = {0.f, 0.f, 0.f, 0.f}, t[4] = {0.f, 0.f, 0.f, 0.f};
+  const float from = a.ref * c;
+  if (fabsf(from) < 1e30f) {
 #pragma unroll
-    for (int e = 0; e < E; e++) best.offer(present && !(x[e] <= bar) && !(x[e] < best.bar), x[e], index + e);
-  }
-  float s[2] = {0.f, 0.f}, t[2] = {0.f, 0.f};
+    for (int g = 0; g < G; g++)
 #pragma unroll
-  for (int e = 0; e < E; e++) {
-    const float y = larger((x[e] - a.ref) * c, -200.f), w = __builtin_amdgcn_exp2f(y);      // 2^-200 is 0
-    s[e & 1] += w;
-    t[e & 1] = fmaf(w, y, t[e & 1]);
+      for (int e = 0; e < E; e++) {
+        const float y = larger(fmaf(x[g][e], c, -from), -200.f), w = __builtin_amdgcn_exp2f(y);      // 2^-200 is 0
+        s[e & 3] += w;
+        t[e & 3] = fmaf(w, y, t[e & 3]);
+      }
+  } else {                             // the product alone may overflow: the difference first
+#pragma unroll
+    for (int g = 0; g < G; g++)
+#pragma unroll
+      for (int e = 0; e < E; e++) {
+        const float y = larger((x[g][e] - a.ref) * c, -200.f), w = __builtin_amdgcn_exp2f(y);
+        s[e & 3] += w;
+        t[e & 3] = fmaf(w, y, t[e & 3]);
+      }
   }
-  a.s += present ? s[0] + s[1] : 0.f;
-  a.t += present ? t[0] + t[1] : 0.f;
+  a.s += present ? (s[0] + s[1]) + (s[2] + s[3]) : 0.f;
+  a.t += present ? (t[0] + t[1]) + (t[2] + t[3]) : 0.f;
 }
 
 struct RowPart {
@@ -149,8 +226,8 @@ struct RowPart {
 
 struct LogprobSplit {
   int parts;
-  int64_t each;        // 16-byte vectors of a part, a multiple of 64
-  RowPart* sums;       // rows x parts
+  int64_t each;        // a multiple of 64
+  RowPart* sums;       // rows x parts; `each`: 16-byte vectors of a wave
   uint64_t* keys;      // rows x parts x top
 };
 
@@ -178,81 +255,106 @@ __device__ __forceinline__ void write_row(const LogprobArgs& a, int64_t r, float
   }
 }
 
-// One wave per row, or per part of one: a single pass over its entries with
-// four 16-byte loads of every lane in flight ahead of those in work.
+constexpr int MAX_WAVES = 16;
+
+// One workgroup per row, or per part of one: its waves take equal stretches, in
+// a single pass with four 16-byte loads of every lane in flight ahead of those
+// in work, and are joined in LDS.
 template <int DT>
-__global__ __launch_bounds__(256) void k_logprobs(LogprobArgs a, LogprobSplit sp) {
+__global__ __launch_bounds__(64 * MAX_WAVES) void k_logprobs(LogprobArgs a, LogprobSplit sp) {
   typedef typename Elem<DT>::T T;
   constexpr int E = Vec<DT>::E, U = 4;
-  __shared__ uint64_t waiting[4][128];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t unit = (int64_t)blockIdx.x * 4 + wave;
-  if (unit >= a.rows * sp.parts) return;
-  const int64_t r = unit / sp.parts;
-  const int part = (int)(unit - r * sp.parts);
+  extern __shared__ uint64_t waiting[];      // BEST_WORDS a wave
+  __shared__ Sums sums[MAX_WAVES];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  const int64_t r = blockIdx.x / sp.parts;
+  const int part = (int)(blockIdx.x - r * sp.parts);
+  const int64_t unit = (int64_t)part * waves + wave, units = (int64_t)sp.parts * waves;
   const T* x = (const T*)a.logits + r * a.stride;
   const int64_t head = row_head<DT>(x, a.vocab), nv = (a.vocab - head) / E, tail = head + nv * E;
-  const int64_t v0 = min((int64_t)part * sp.each, nv), v1 = part == sp.parts - 1 ? nv : min(v0 + sp.each, nv);
+  const int64_t v0 = min(unit * sp.each, nv), v1 = unit == units - 1 ? nv : min(v0 + sp.each, nv);
   const v4u* v = (const v4u*)(x + head);
   const float c = a.scale * 1.44269504088896340736f;
-  Sums sum = {0.f, 0.f, 0.f};
+  Sums sum = {-3.402823466e38f, 0.f, 0.f};
   Best best;
-  best.init(waiting[wave], a.top);
+  best.init(waiting + wave * BEST_WORDS, a.top);
   bool first = true;
-  v4u now[U], next[U];
   int64_t i = v0;
   const int64_t blocks = (v1 - v0) / (64 * U);
-  if (blocks > 0)
+  v4u A[U], B[U];
+  auto load = [&](v4u* d, int64_t at) {
 #pragma unroll
-    for (int u = 0; u < U; u++) now[u] = v[i + u * 64 + lane];
-  if (part == 0 && head) {
-    float one = -INFINITY;
-    if (lane < head) one = Elem<DT>::load(x[lane]);
-    take<1>(&one, lane < head, (unsigned)lane, c, sum, best, first);
-    first = false;
-  }
-  for (int64_t k = 0; k < blocks; k++, i += 64 * U) {
-    if (k + 1 < blocks)
+    for (int u = 0; u < U; u++) d[u] = v[at + u * 64 + lane];
+  };
+  auto work = [&](const v4u* d, int64_t at) {
 #pragma unroll
-      for (int u = 0; u < U; u++) next[u] = v[i + (U + u) * 64 + lane];
-#pragma unroll
-    for (int u = 0; u < U; u++) {
-      float y[E];
-      Vec<DT>::unpack(now[u], y);
-      take<E>(y, true, (unsigned)(head + (i + u * 64 + lane) * E), c, sum, best, first);
+    for (int u = 0; u < U; u += 2) {
+      float y[2][E];
+      Vec<DT>::unpack(d[u], y[0]);
+      Vec<DT>::unpack(d[u + 1], y[1]);
+      take<E, 2>(y, true, (unsigned)(head + (at + u * 64 + lane) * E), c, sum, best, first);
       first = false;
     }
-#pragma unroll
-    for (int u = 0; u < U; u++) now[u] = next[u];
+  };
+  if (blocks > 0) load(A, i);
+  if (unit == 0 && head) {
+    float one[1][1] = {{-INFINITY}};
+    if (lane < head) one[0][0] = Elem<DT>::load(x[lane]);
+    take<1, 1>(one, lane < head, (unsigned)lane, c, sum, best, first);
+    first = false;
   }
-  for (; i < v1; i += 64) {
+  for (int64_t k = 0; k < blocks; k += 2, i += 2 * 64 * U) {
+    if (k + 1 < blocks) load(B, i + 64 * U);
+    work(A, i);
+    if (k + 1 >= blocks) break;
+    if (k + 2 < blocks) load(A, i + 2 * 64 * U);
+    work(B, i + 64 * U);
+  }
+  for (i = v0 + blocks * 64 * U; i < v1; i += 64) {
     const bool in = i + lane < v1;
-    float y[E];
-    Vec<DT>::unpack(v[in ? i + lane : v1 - 1], y);
-    take<E>(y, in, (unsigned)(head + (i + lane) * E), c, sum, best, first);
+    float y[1][E];
+    Vec<DT>::unpack(v[in ? i + lane : v1 - 1], y[0]);
+    take<E, 1>(y, in, (unsigned)(head + (i + lane) * E), c, sum, best, first);
     first = false;
   }
-  if (part == sp.parts - 1 && tail < a.vocab) {
+  if (unit == units - 1 && tail < a.vocab) {
     const bool in = tail + lane < a.vocab;
-    float one = -INFINITY;
-    if (in) one = Elem<DT>::load(x[tail + lane]);
-    take<1>(&one, in, (unsigned)(tail + lane), c, sum, best, first);
-    first = false;
+    float one[1][1] = {{-INFINITY}};
+    if (in) one[0][0] = Elem<DT>::load(x[tail + lane]);
+    take<1, 1>(one, in, (unsigned)(tail + lane), c, sum, best, first);
   }
   if (a.top && best.count) best.merge();
-  const float s = wave_sum(sum.s), t = wave_sum(sum.t);
+  sum.s = wave_sum(sum.s);
+  sum.t = wave_sum(sum.t);
+  if (waves > 1) {
+    // sums: wave 0, a wave's in each lane; lists: by halves, the upper half's turned round
+    if (lane == 0) sums[wave] = sum;
+    __syncthreads();
+    if (wave == 0) {
+      Sums one = lane < waves ? sums[lane] : Sums{-3.402823466e38f, 0.f, 0.f};
+      const float ref = wave_max(one.s > 0.f ? one.ref : -3.402823466e38f);
+      if (one.s != 0.f) one.move(ref, c);
+      sum = {ref, wave_sum(one.s), wave_sum(one.s != 0.f ? one.t : 0.f)};
+    }
+    if (a.top)
+      for (int d = 1; d < waves; d *= 2) {
+        if ((wave & (2 * d - 1)) == d) waiting[wave * BEST_WORDS + lane] = best.key;
+        __syncthreads();
+        if (!(wave & (2 * d - 1)) && wave + d < waves) best.key = merge_lists(best.key, waiting[(wave + d) * BEST_WORDS + 63 - lane]);
+      }
+    if (wave) return;
+  }
   if (sp.parts == 1) {
-    write_row<DT>(a, r, sum.ref, s, t, best.key);
+    write_row<DT>(a, r, sum.ref, sum.s, sum.t, best.key);
     return;
   }
-  if (lane == 0) sp.sums[unit] = {first ? -3.402823466e38f : sum.ref, s, t, 0};
-  if (lane < a.top) sp.keys[unit * a.top + lane] = best.key;
+  if (lane == 0) sp.sums[blockIdx.x] = {sum.ref, sum.s, sum.t, 0};
+  if (lane < a.top) sp.keys[(int64_t)blockIdx.x * a.top + lane] = best.key;
 }
 
 // Joins a row's parts: one wave per row.
 template <int DT>
 __global__ __launch_bounds__(64) void k_logprobs_join(LogprobArgs a, LogprobSplit sp) {
-  __shared__ uint64_t waiting[128];
   const int64_t r = blockIdx.x;
   const int lane = threadIdx.x;
   const RowPart* p = sp.sums + r * sp.parts;
@@ -263,22 +365,19 @@ __global__ __launch_bounds__(64) void k_logprobs_join(LogprobArgs a, LogprobSpli
   float s = 0.f, t = 0.f;
   for (int i = lane; i < sp.parts; i += 64) {
     Sums one = {p[i].ref, p[i].s, p[i].t};
-    if (one.s != 0.f) one.move(ref, c);
-    s += one.s;
-    t += one.t;
+    if (one.s != 0.f) {
+      one.move(ref, c);
+      s += one.s;
+      t += one.t;
+    }
   }
-  s = wave_sum(s);
-  t = wave_sum(t);
-  Best best;
-  best.init(waiting, a.top);
-  const uint64_t* keys = sp.keys + r * sp.parts * a.top;
-  const int n = sp.parts * a.top;
-  for (int i = 0; i < n; i += 64) {
-    const uint64_t key = i + lane < n ? keys[i + lane] : 0;
-    best.offer(key && !(value_of(key) < best.bar), value_of(key), (unsigned)index_of(key));
-  }
-  if (a.top && best.count) best.merge();
-  write_row<DT>(a, r, ref, s, t, best.key);
+  uint64_t key = 0;
+  if (a.top)
+    for (int i = 0; i < sp.parts; i++) {      // each falling: turned round
+      const int j = 63 - lane;
+      key = merge_lists(key, j < a.top ? sp.keys[(r * sp.parts + i) * a.top + j] : 0);
+    }
+  write_row<DT>(a, r, ref, wave_sum(s), wave_sum(t), key);
 }
 
 struct LogprobGradArgs {
@@ -342,14 +441,22 @@ __global__ __launch_bounds__(256) void k_logprobs_grad(LogprobGradArgs a) {
   }
 }
 
-// Parts of a row: one wave each, so that few rows still fill the chip (2048
-// waves, eight a CU), but not below 2048 entries.
-static LogprobSplit split_of(int64_t rows, int64_t vocab) {
+// Waves of a workgroup and workgroups (parts) of a row: 4096 waves where there
+// is work for them, sixteen a CU, a wave not below 2048 entries; the row's
+// waves in one workgroup up to sixteen, which needs no second launch, and in
+// several only where sixteen would take over 16384 entries each.
+static LogprobSplit split_of(int64_t rows, int64_t vocab, int* waves) {
   LogprobSplit sp = {};
-  int64_t parts = (2048 + rows - 1) / rows;
+  int64_t want = (4096 + rows - 1) / rows;
   const int64_t most = (vocab + 2047) / 2048;
-  parts = parts > most ? most : parts;
-  sp.parts = (int)parts;
+  want = want > most ? most : want;
+  int w = 1;
+  while (w < want && w < MAX_WAVES) w *= 2;
+  int64_t parts = 1;
+  if (w == MAX_WAVES && vocab > MAX_WAVES * 16384) parts = want / MAX_WAVES;
+  if (parts > 64) parts = 64;
+  sp.parts = (int)(parts < 1 ? 1 : parts);
+  *waves = w;
   return sp;
 }
 static size_t split_bytes(int64_t rows, int parts, int top) {
@@ -365,8 +472,9 @@ static void launch_logprobs_grad(LogprobGradArgs a, int32_t dtype, int64_t r0, i
 }
 
 template <int DT>
-static void launch_logprobs(const LogprobArgs& a, const LogprobSplit& sp, hipStream_t s) {
-  k_logprobs<DT><<<dim3((unsigned)((a.rows * sp.parts + 3) / 4)), 256, 0, s>>>(a, sp);
+static void launch_logprobs(const LogprobArgs& a, const LogprobSplit& sp, int waves, hipStream_t s) {
+  const size_t lds = a.top ? (size_t)waves * BEST_WORDS * sizeof(uint64_t) : 0;
+  k_logprobs<DT><<<dim3((unsigned)(a.rows * sp.parts)), 64 * waves, lds, s>>>(a, sp);
   if (sp.parts > 1) k_logprobs_join<DT><<<dim3((unsigned)a.rows), 64, 0, s>>>(a, sp);
 }
 
@@ -382,7 +490,8 @@ extern "C" {
 
 size_t externd_token_logprobs_workspace_bytes(int64_t rows, int64_t vocab, int32_t top) {
   if (!logprob_sizes_ok(rows, vocab, top) || !rows) return 0;
-  const int parts = split_of(rows, vocab).parts;
+  int waves;
+  const int parts = split_of(rows, vocab, &waves).parts;
   return parts == 1 ? 0 : split_bytes(rows, parts, top);
 }
 
@@ -398,15 +507,16 @@ int externd_token_logprobs(const void* logits, int32_t dtype, int64_t rows, int6
   if (need && (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 255))) return EXTERND_EWORKSPACE;
   if (!rows) return EXTERND_OK;
   const LogprobArgs a = {logits, rows, vocab, row_stride, targets, scale, top, logprob, entropy, lse, top_logprobs, top_ids};
-  LogprobSplit sp = split_of(rows, vocab);
+  int waves;
+  LogprobSplit sp = split_of(rows, vocab, &waves);
   const int per = dtype == EXTERND_F32 ? 4 : 8;      // entries of a vector
-  sp.each = ((vocab / per + sp.parts - 1) / sp.parts + 63) & ~(int64_t)63;
+  sp.each = ((vocab / per + sp.parts * waves - 1) / (sp.parts * waves) + 63) & ~(int64_t)63;
   sp.sums = (RowPart*)workspace;
   sp.keys = (uint64_t*)(sp.sums + rows * sp.parts);
   const hipStream_t s = (hipStream_t)stream;
-  if (dtype == EXTERND_F32) launch_logprobs<EXTERND_F32>(a, sp, s);
-  else if (dtype == EXTERND_BF16) launch_logprobs<EXTERND_BF16>(a, sp, s);
-  else launch_logprobs<EXTERND_F16>(a, sp, s);
+  if (dtype == EXTERND_F32) launch_logprobs<EXTERND_F32>(a, sp, waves, s);
+  else if (dtype == EXTERND_BF16) launch_logprobs<EXTERND_BF16>(a, sp, waves, s);
+  else launch_logprobs<EXTERND_F16>(a, sp, waves, s);
   return hipGetLastError() == hipSuccess ? EXTERND_OK : EXTERND_EHIP;
 }
 
