@@ -533,28 +533,35 @@ def _rotary(q, k, positions, freqs, interleaved, amplitude, inverse, out, stream
     code = _dtype_code(torch, q.dtype, "q")
     qs = _req_heads(q, q.dtype, tokens, "q")
     _req(positions, torch, torch.int64, (tokens,), "positions")
-    _req(freqs, torch, torch.int64, (freqs.numel(),), "freqs")
-    qo, ko = out if out is not None else (torch.empty((tokens, heads, dim), dtype=q.dtype, device=q.device), None)
-    qos = _req_heads(qo, q.dtype, tokens, "q out")
-    if qo.shape != q.shape:
-        raise ValueError(f"q out: expected shape {tuple(q.shape)}, got {tuple(qo.shape)}")
+    half = freqs.numel()
+    _req(freqs, torch, torch.int64, (half,), "freqs")
     ks = kos = (0, 0)
-    kp = kop = None
+    ko = kp = kop = None
     kh = 0
     if k is not None:
         ks = _req_heads(k, q.dtype, tokens, "k")
         kh = k.shape[1]
         if k.shape[2] != dim:
             raise ValueError(f"k: expected {dim} channels a head, got {k.shape[2]}")
-        if out is None:
-            ko = torch.empty((tokens, kh, dim), dtype=q.dtype, device=q.device)
-        elif ko is None or ko.shape != k.shape:
-            raise ValueError(f"k out: expected shape {tuple(k.shape)}")
-        kos = _req_heads(ko, q.dtype, tokens, "k out")
-        kp, kop = k.data_ptr(), ko.data_ptr()
+        kp = k.data_ptr()
+    if out is None:
+        qo, qos = q.new_empty((tokens, heads, dim)), (heads * dim, dim)
+        if kh:
+            ko, kos = q.new_empty((tokens, kh, dim)), (kh * dim, dim)
+    else:
+        qo, ko = out
+        qos = _req_heads(qo, q.dtype, tokens, "q out")
+        if qo.shape != q.shape:
+            raise ValueError(f"q out: expected shape {tuple(q.shape)}, got {tuple(qo.shape)}")
+        if kh:
+            if ko is None or ko.shape != k.shape:
+                raise ValueError(f"k out: expected shape {tuple(k.shape)}")
+            kos = _req_heads(ko, q.dtype, tokens, "k out")
+    if kh:
+        kop = ko.data_ptr()
     if tokens:
         st = lib().externd_rotary(q.data_ptr(), qo.data_ptr(), qs[0], qs[1], qos[0], qos[1], heads, kp, kop, ks[0],
-                                  ks[1], kos[0], kos[1], kh, code, tokens, dim, 2 * freqs.numel(), int(interleaved),
+                                  ks[1], kos[0], kos[1], kh, code, tokens, dim, 2 * half, int(interleaved),
                                   inverse, positions.data_ptr(), freqs.data_ptr(), amplitude,
                                   _stream_ptr(torch, stream))
         if st != OK:
@@ -647,8 +654,8 @@ def kv4_read(cache, table, lens, head_dim: int, starts=None, tokens=None, dtype=
     dtype = torch.float32 if dtype is None else dtype
     pages, kv, page, batch, sp = _kv4_args(torch, cache, head_dim, tokens, table, lens, starts)
     code = _dtype_code(torch, dtype, "dtype")
-    k = torch.empty((tokens, kv, head_dim), dtype=dtype, device=cache.device)
-    v = torch.empty((tokens, kv, head_dim), dtype=dtype, device=cache.device)
+    k = cache.new_empty((tokens, kv, head_dim), dtype=dtype)
+    v = cache.new_empty((tokens, kv, head_dim), dtype=dtype)
     if tokens:
         st = lib().externd_kv4_read(cache.data_ptr(), pages, kv, head_dim, page, k.data_ptr(), v.data_ptr(), code,
                                     tokens, batch, sp, lens.data_ptr(), table.data_ptr(), table.shape[1],
@@ -682,10 +689,10 @@ def kv4_attention(cache, q, table, lens, starts=None, max_new=None, max_len=None
     code = _dtype_code(torch, q.dtype, "q")
     qs = _req_heads(q, q.dtype, tokens, "q")
     if out is None:
-        out = torch.empty((tokens, heads, dim), dtype=q.dtype, device=q.device)
+        out = q.new_empty((tokens, heads, dim))
     else:
         _req(out, torch, q.dtype, (tokens, heads, dim), "out")
-    lse = torch.empty((tokens, heads), dtype=torch.float32, device=q.device)
+    lse = q.new_empty((tokens, heads), dtype=torch.float32)
     if not tokens:
         return out, lse
     if max_new is None:
@@ -700,7 +707,7 @@ def kv4_attention(cache, q, table, lens, starts=None, max_new=None, max_len=None
     if workspace is not None:
         wp, nbytes = workspace.data_ptr(), workspace.numel()
     elif nbytes:
-        workspace = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
+        workspace = cache.new_empty((nbytes,))
         wp = workspace.data_ptr()
     st = L.externd_kv4_attention(cache.data_ptr(), pages, kv, dim, page, q.data_ptr(), code, qs[0], qs[1], heads,
                                  out.data_ptr(), lse.data_ptr(), tokens, batch, max_new, max_len, sp, lens.data_ptr(),
@@ -736,18 +743,18 @@ def token_logprobs(logits, targets=None, top: int = 0, scale: float = 1.0, strea
     among equals (externd_token_logprobs).  Without targets logprob is None."""
     torch = _torch()
     rows, vocab, stride, code = _req_logits(torch, logits, "logits")
-    dev = logits.device
-    logprob = tp = lp = None
-    if targets is not None:
-        _req(targets, torch, torch.int64, (rows,), "targets")
-        logprob = torch.empty((rows,), dtype=torch.float32, device=dev)
-        tp, lp = targets.data_ptr(), logprob.data_ptr()
     if not 0 <= top <= min(LOGPROBS_MAX_TOP, vocab):
         raise ExterndError(EINVAL, "externd_token_logprobs")
-    entropy = torch.empty((rows,), dtype=torch.float32, device=dev)
-    lse = torch.empty((rows,), dtype=torch.float32, device=dev)
-    vals = torch.empty((rows, top), dtype=torch.float32, device=dev)
-    ids = torch.empty((rows, top), dtype=torch.int64, device=dev)
+    # one buffer for the three numbers of each row
+    entropy, lse, logprob = logits.new_empty((3, rows), dtype=torch.float32).unbind(0)
+    tp = lp = None
+    if targets is not None:
+        _req(targets, torch, torch.int64, (rows,), "targets")
+        tp, lp = targets.data_ptr(), logprob.data_ptr()
+    else:
+        logprob = None
+    vals = logits.new_empty((rows, top), dtype=torch.float32)
+    ids = logits.new_empty((rows, top), dtype=torch.int64)
     if rows:
         L = lib()
         nbytes = L.externd_token_logprobs_workspace_bytes(rows, vocab, top)
@@ -755,7 +762,7 @@ def token_logprobs(logits, targets=None, top: int = 0, scale: float = 1.0, strea
         if workspace is not None:
             wp, nbytes = workspace.data_ptr(), workspace.numel()
         elif nbytes:
-            workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+            workspace = logits.new_empty((nbytes,), dtype=torch.uint8)
             wp = workspace.data_ptr()
         st = L.externd_token_logprobs(logits.data_ptr(), code, rows, vocab, stride, tp, scale, top, lp,
                                       entropy.data_ptr(), lse.data_ptr(), vals.data_ptr() if top else None,
@@ -781,7 +788,7 @@ def token_logprobs_backward(logits, targets, lse, entropy, grad_logprob=None, gr
             _req(t, torch, dt, (rows,), name)
             ptrs[i] = t.data_ptr()
     if out is None:
-        out = torch.empty((rows, vocab), dtype=logits.dtype, device=logits.device)
+        out = logits.new_empty((rows, vocab))
     orows, ovocab, ostride, _ = _req_logits(torch, out, "out")
     if (orows, ovocab) != (rows, vocab) or out.dtype is not logits.dtype:
         raise ValueError(f"out: expected {logits.dtype} of shape {(rows, vocab)}, got {out.dtype} {tuple(out.shape)}")

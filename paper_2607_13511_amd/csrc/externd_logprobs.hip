@@ -30,6 +30,8 @@ __device__ __forceinline__ float value_of(uint64_t key) {
 }
 __device__ __forceinline__ int64_t index_of(uint64_t key) { return (int64_t)(0xFFFFFFFFu - (unsigned)key); }
 
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
 // A larger of two that is a NaN where one of them is.
 __device__ __forceinline__ float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 
@@ -82,6 +84,19 @@ __device__ __forceinline__ uint64_t sort_rising(uint64_t k) {
   if constexpr (SIZE < 64) return sort_rising<SIZE * 2>(k);
   else return k;
 }
+template <int SIZE, int D>
+__device__ __forceinline__ unsigned order_steps32(unsigned k, bool up) {
+  const unsigned o = xor_lane<D>(k);
+  k = (!(threadIdx.x & D) == up) ? min(k, o) : max(k, o);
+  if constexpr (D > 1) return order_steps32<SIZE, D / 2>(k, up);
+  else return k;
+}
+template <int SIZE = 2>
+__device__ __forceinline__ unsigned sort_rising32(unsigned k) {
+  k = order_steps32<SIZE, SIZE / 2>(k, SIZE == 64 || !(threadIdx.x & SIZE));
+  if constexpr (SIZE < 64) return sort_rising32<SIZE * 2>(k);
+  else return k;
+}
 // The 64 largest of a falling and a rising list, falling.
 __device__ __forceinline__ uint64_t merge_lists(uint64_t falling, uint64_t rising) {
   return order_steps<64, 32>(falling > rising ? falling : rising, false);
@@ -125,7 +140,7 @@ struct Best {
     count = left > 0 ? left : 0;
     const uint64_t last = (uint64_t)(unsigned)__builtin_amdgcn_readlane((unsigned)(key >> 32), top - 1) << 32 |
                           (unsigned)__builtin_amdgcn_readlane((unsigned)key, top - 1);
-    bar = last ? value_of(last) : NAN;
+    bar = last ? value_of(last) : bar;
   }
   // `in`: this lane's x may be among the largest.
   __device__ __forceinline__ void offer(bool in, float x, unsigned index) {
@@ -136,22 +151,31 @@ struct Best {
     count += __popcll(mask);
     if (count >= 64) merge();
   }
+  // First entries: with `top` lanes or more, the top-th largest of their
+  // maxima is a bar already (as many entries are not below it), where sorting
+  // in all of them would take eight rounds.
+  __device__ __forceinline__ void start(float big, bool present) {
+    if (__popcll(__ballot(present)) < top) return;
+    const unsigned k = sort_rising32(present ? (unsigned)(order_key(big, 0) >> 32) : 0u);
+    bar = value_of((uint64_t)(unsigned)__builtin_amdgcn_readlane(k, 64 - top) << 32);
+  }
   // The lanes of `may` have one at least.  Sixteen of them at a time put all of
   // theirs side by side, so that 64 are looked at together.
   template <int E, int G>
-  __device__ __forceinline__ void search(const float (*x)[E], uint64_t may, unsigned index) {
+  __device__ __forceinline__ void search(const float (*x)[E], uint64_t may, unsigned index, float was) {
     constexpr int S = E * G;
     const int lane = threadIdx.x & 63, rank = __popcll(may & ((1ull << lane) - 1)), n = __popcll(may);
     const bool mine = may >> lane & 1;
-    // earlier entries have lower indices, so what equals their bar is out; what these ones raise it to is not
-    const float was = bar;
     for (int r0 = 0; r0 < n; r0 += 16) {
       __builtin_amdgcn_wave_barrier();      // the wave's own LDS, in order
       if (mine && rank >= r0 && rank < r0 + 16) {
+        if constexpr (E >= 4) {
 #pragma unroll
-        for (int g = 0; g < G; g++)
+          for (int g = 0; g < G; g++)
 #pragma unroll
-          for (int e = 0; e < E; e++) some[(rank - r0) * S + g * E + e] = x[g][e];
+            for (int e = 0; e < E; e += 4)
+              *(f32x4*)(some + (rank - r0) * S + g * E + e) = f32x4{x[g][e], x[g][e + 1], x[g][e + 2], x[g][e + 3]};
+        } else some[rank - r0] = x[0][0];
         whose[rank - r0] = index;
       }
       __builtin_amdgcn_wave_barrier();
@@ -192,8 +216,13 @@ __device__ __forceinline__ void take(const float (*x)[E], bool present, unsigned
   big = present ? big : -INFINITY;
   if (first) a.ref = fmaxf(wave_max(big), -3.402823466e38f);
   else if (__any((big - a.ref) * c > 8.f)) a.move(wave_max(big), c);
-  const uint64_t may = best.top ? __ballot(present && !(big <= best.bar)) : 0;
-  if (may) best.search<E, G>(x, may, index);
+  if (best.top) {
+    // earlier entries have lower indices, so what equals their bar is out; what these ones raise it to is not
+    const float was = best.bar;
+    if (was != was && E * G > 1) best.start(big, present);
+    const uint64_t may = __ballot(present && !(big <= was) && !(big < best.bar));
+    if (may) best.search<E, G>(x, may, index, was);
+  }
   float s[4] = {0.f, 0.f, 0.f, 0.f}, t[4] = {0.f, 0.f, 0.f, 0.f};
   const float from = a.ref * c;
   if (fabsf(from) < 1e30f) {
@@ -264,8 +293,10 @@ template <int DT>
 __global__ __launch_bounds__(64 * MAX_WAVES) void k_logprobs(LogprobArgs a, LogprobSplit sp) {
   typedef typename Elem<DT>::T T;
   constexpr int E = Vec<DT>::E, U = 4;
-  extern __shared__ uint64_t waiting[];      // BEST_WORDS a wave
+  extern __shared__ uint64_t waiting[];      // BEST_WORDS a wave, then the pool: 128 a wave
   __shared__ Sums sums[MAX_WAVES];
+  __shared__ float bars[MAX_WAVES];
+  __shared__ int pooled;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
   const int64_t r = blockIdx.x / sp.parts;
   const int part = (int)(blockIdx.x - r * sp.parts);
@@ -323,26 +354,38 @@ __global__ __launch_bounds__(64 * MAX_WAVES) void k_logprobs(LogprobArgs a, Logp
     if (in) one[0][0] = Elem<DT>::load(x[tail + lane]);
     take<1, 1>(one, in, (unsigned)(tail + lane), c, sum, best, first);
   }
-  if (a.top && best.count) best.merge();
   sum.s = wave_sum(sum.s);
   sum.t = wave_sum(sum.t);
-  if (waves > 1) {
-    // sums: wave 0, a wave's in each lane; lists: by halves, the upper half's turned round
-    if (lane == 0) sums[wave] = sum;
-    __syncthreads();
-    if (wave == 0) {
-      Sums one = lane < waves ? sums[lane] : Sums{-3.402823466e38f, 0.f, 0.f};
-      const float ref = wave_max(one.s > 0.f ? one.ref : -3.402823466e38f);
-      if (one.s != 0.f) one.move(ref, c);
-      sum = {ref, wave_sum(one.s), wave_sum(one.s != 0.f ? one.t : 0.f)};
+  if (waves == 1) {
+    if (best.count) best.merge();
+  } else {
+    if (lane == 0) {
+      sums[wave] = sum;
+      bars[wave] = best.bar;
+      if (wave == 0) pooled = 0;
     }
-    if (a.top)
-      for (int d = 1; d < waves; d *= 2) {
-        if ((wave & (2 * d - 1)) == d) waiting[wave * BEST_WORDS + lane] = best.key;
-        __syncthreads();
-        if (!(wave & (2 * d - 1)) && wave + d < waves) best.key = merge_lists(best.key, waiting[(wave + d) * BEST_WORDS + 63 - lane]);
-      }
+    __syncthreads();
+    if (a.top) {
+      // what is not below any wave's bar goes into one pool, a little over `top` keys, which wave 0 sorts
+      uint64_t* const pool = waiting + waves * BEST_WORDS;
+      float bar = -INFINITY;
+      for (int w = 0; w < waves; w++) bar = fmaxf(bar, bars[w]);      // passes over NaN: none yet
+      const auto give = [&](uint64_t key) {
+        if (key && !(value_of(key) < bar)) pool[atomicAdd(&pooled, 1)] = key;
+      };
+      give(best.key);
+      if (lane < best.count) give(best.waiting[lane]);
+      __syncthreads();
+    }
     if (wave) return;
+    Sums one = lane < waves ? sums[lane] : Sums{-3.402823466e38f, 0.f, 0.f};
+    const float ref = wave_max(one.s > 0.f ? one.ref : -3.402823466e38f);
+    if (one.s != 0.f) one.move(ref, c);
+    sum = {ref, wave_sum(one.s), wave_sum(one.s != 0.f ? one.t : 0.f)};
+    best.key = 0;
+    if (a.top)
+      for (int k = 0; k < pooled; k += 64)
+        best.key = merge_lists(best.key, sort_rising(k + lane < pooled ? waiting[waves * BEST_WORDS + k + lane] : 0));
   }
   if (sp.parts == 1) {
     write_row<DT>(a, r, sum.ref, sum.s, sum.t, best.key);
@@ -473,7 +516,7 @@ static void launch_logprobs_grad(LogprobGradArgs a, int32_t dtype, int64_t r0, i
 
 template <int DT>
 static void launch_logprobs(const LogprobArgs& a, const LogprobSplit& sp, int waves, hipStream_t s) {
-  const size_t lds = a.top ? (size_t)waves * BEST_WORDS * sizeof(uint64_t) : 0;
+  const size_t lds = a.top ? (size_t)waves * (BEST_WORDS + 128) * sizeof(uint64_t) : 0;
   k_logprobs<DT><<<dim3((unsigned)(a.rows * sp.parts)), 64 * waves, lds, s>>>(a, sp);
   if (sp.parts > 1) k_logprobs_join<DT><<<dim3((unsigned)a.rows), 64, 0, s>>>(a, sp);
 }
