@@ -23,9 +23,11 @@ struct AttnArgs {
   float* lse;
   float scale;
   int window, dtype;
-  int nsplit, chunk;      // parts of a sequence (grid x), and the least tokens of a part (a multiple of 256)
-  int row_blocks;         // row blocks a launch starts per sequence and cache head
-  float* part;            // per (row, part): DIM sums, the maximum and the sum of weights, two unused
+  int q_vec;              // every query starts at a multiple of 16 bytes
+  int whole;              // a workgroup per row block and cache head, nothing to join
+  int blocks;             // numbers of row blocks (below)
+  float* part;            // per workgroup two row blocks' parts; a row: DIM sums, the maximum and the sum of weights, two unused
+  int2* parts;            // per row block and cache head: the first workgroup and the number of them
 };
 
 __device__ __forceinline__ float load_any(const void* p, int64_t i, int dtype) {
@@ -41,11 +43,12 @@ __device__ __forceinline__ void store_any(void* p, int64_t i, float v, int dtype
 
 // The queries of one sequence and cache head are rows: row r is new token
 // r / each, query head r % each of the cache head.  A row block (ROWS rows)
-// sees the tokens lo .. hi - 1 among it, in `parts` parts of `part` tokens.
+// sees the tokens lo .. hi - 1 among it, in tiles of 64.
 struct RowBlock {
   int64_t t0;          // first new token of the sequence
   int rows, first;     // rows of the sequence; position of its first new token
-  int lo, hi, part, parts;
+  int r0;              // the block's first row
+  int lo, hi, tiles;
 };
 template <int ROWS>
 __device__ __forceinline__ RowBlock row_block(const AttnArgs& a, int b, int rb) {
@@ -59,14 +62,161 @@ __device__ __forceinline__ RowBlock row_block(const AttnArgs& a, int b, int rb) 
   r.first = len - (int)(t1 - t0);
   const int64_t room = a.s.table_pages << a.c.page_log2;
   const int held = len > room ? (int)room : len;
-  const int r0 = rb * ROWS, r1 = min(r.rows, r0 + ROWS) - 1;
+  r.r0 = rb * ROWS;
+  const int r1 = min(r.rows, r.r0 + ROWS) - 1;
   r.hi = min(held, r.first + (r1 < 0 ? 0 : r1 / a.each) + 1);
-  r.lo = a.window > 0 ? max(0, r.first + r0 / a.each - a.window + 1) & ~63 : 0;
-  const int total = max(0, r.hi - r.lo);
-  const int each = (total + a.nsplit - 1) / a.nsplit;
-  r.part = max(a.chunk, (each + 255) & ~255);
-  r.parts = (total + r.part - 1) / r.part;
+  r.lo = a.window > 0 ? max(0, r.first + r.r0 / a.each - a.window + 1) & ~63 : 0;
+  r.tiles = (max(0, r.hi - r.lo) + 63) >> 6;
   return r;
+}
+
+// Row blocks are numbered through the call: those of sequence b from
+// starts[b] each / ROWS + b on (some numbers name no block), or evenly with one
+// token each.  A workgroup's share is a stretch of the list of all tiles, block
+// by block and cache head by cache head, as long as every other's, so lengths
+// need not be alike; the first and the last row block of a stretch may be
+// shared with neighbours, whose parts are joined by k_attention_join.  A row
+// block that sees nothing counts as one tile.
+template <int ROWS>
+__device__ __forceinline__ int64_t first_number(const AttnArgs& a, int b) {
+  return (int64_t)max(a.s.starts[b], 0) * a.each / ROWS + b;
+}
+template <int ROWS>
+__device__ __forceinline__ bool numbered_block(const AttnArgs& a, int number, RowBlock* r, int* b) {
+  int rb;
+  if (!a.s.starts) {
+    const int per = (a.each + ROWS - 1) / ROWS;
+    *b = number / per;
+    rb = number - *b * per;
+  } else {
+    int lo = 0, hi = a.s.batch - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (first_number<ROWS>(a, mid) <= number) lo = mid; else hi = mid - 1;
+    }
+    *b = lo;
+    rb = number - (int)first_number<ROWS>(a, lo);
+  }
+  if (rb < 0) return false;
+  *r = row_block<ROWS>(a, *b, rb);
+  return r->r0 < r->rows;
+}
+
+struct Walk {
+  int64_t at, end, base, total;      // this workgroup's stretch, where the current row block's tiles begin, all tiles
+  int number, b, groups;
+  RowBlock R;
+};
+__device__ __forceinline__ int64_t uniform64(int64_t v) {
+  return (int64_t)((uint64_t)(unsigned)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32 |
+                   (unsigned)__builtin_amdgcn_readfirstlane((int)v));
+}
+// In scalar registers: the same for all threads.
+__device__ __forceinline__ void walk_uniform(Walk& w) {
+  w.b = __builtin_amdgcn_readfirstlane(w.b);
+  w.R.t0 = uniform64(w.R.t0);
+  w.R.rows = __builtin_amdgcn_readfirstlane(w.R.rows);
+  w.R.first = __builtin_amdgcn_readfirstlane(w.R.first);
+  w.R.r0 = __builtin_amdgcn_readfirstlane(w.R.r0);
+  w.R.lo = __builtin_amdgcn_readfirstlane(w.R.lo);
+  w.R.hi = __builtin_amdgcn_readfirstlane(w.R.hi);
+  w.R.tiles = __builtin_amdgcn_readfirstlane(w.R.tiles);
+}
+// The next row block that is one, from `number` on.
+template <int ROWS>
+__device__ __forceinline__ void walk_to(const AttnArgs& a, Walk& w, int number) {
+  while (!numbered_block<ROWS>(a, number, &w.R, &w.b) && number < a.blocks - 1) number++;
+  w.number = number;
+  walk_uniform(w);
+}
+template <int ROWS, int NT>
+__device__ __forceinline__ bool walk_begin(const AttnArgs& a, Walk& w) {
+  __shared__ int64_t sums[NT / 64 + 1], found_base;
+  __shared__ int found;
+  const int tid = threadIdx.x;
+  if (a.whole) {
+    if (!numbered_block<ROWS>(a, blockIdx.x / a.c.heads, &w.R, &w.b)) return false;
+    walk_uniform(w);
+    const int n = max(w.R.tiles, 1);
+    w.base = 0;
+    w.at = (int64_t)(blockIdx.x % a.c.heads) * n;
+    w.end = w.at + n;
+    return true;
+  }
+  const int each = (a.blocks + NT - 1) / NT, n0 = min(tid * each, a.blocks), n1 = min(n0 + each, a.blocks);
+  int64_t mine = 0;
+  RowBlock r;
+  int b;
+  for (int n = n0; n < n1; n++)
+    if (numbered_block<ROWS>(a, n, &r, &b)) mine += (int64_t)max(r.tiles, 1) * a.c.heads;
+  int64_t to = mine;      // inclusive sum
+  for (int d = 1; d < 64; d <<= 1) {
+    const int64_t o = __shfl_up(to, d);
+    if ((tid & 63) >= d) to += o;
+  }
+  if ((tid & 63) == 63) sums[tid >> 6] = to;
+  __syncthreads();
+  int64_t before = 0, total = 0;
+  for (int i = 0; i < NT / 64; i++) {
+    if (i < tid >> 6) before += sums[i];
+    total += sums[i];
+  }
+  to += before;
+  w.total = uniform64(total);
+  w.groups = (int)min((int64_t)gridDim.x, w.total);
+  if ((int)blockIdx.x >= w.groups) return false;
+  w.at = w.total * blockIdx.x / w.groups;
+  w.end = w.total * (blockIdx.x + 1) / w.groups;
+  if (to - mine <= w.at && w.at < to) {      // one thread: its own row blocks again
+    int64_t base = to - mine;
+    for (int n = n0; n < n1; n++)
+      if (numbered_block<ROWS>(a, n, &r, &b)) {
+        const int64_t size = (int64_t)max(r.tiles, 1) * a.c.heads;
+        if (w.at < base + size) {
+          found = n;
+          found_base = base;
+          break;
+        }
+        base += size;
+      }
+  }
+  __syncthreads();
+  w.base = uniform64(found_base);
+  walk_to<ROWS>(a, w, __builtin_amdgcn_readfirstlane(found));
+  return true;
+}
+// Past `done` tiles; false at the stretch's end.
+template <int ROWS>
+__device__ __forceinline__ bool walk_on(const AttnArgs& a, Walk& w, int done) {
+  w.at += done;
+  if (w.at >= w.end) return false;
+  const int64_t size = (int64_t)max(w.R.tiles, 1) * a.c.heads;
+  if (w.at == w.base + size) {
+    w.base = w.at;
+    walk_to<ROWS>(a, w, w.number + 1);
+  }
+  return true;
+}
+// The row block's tiles of this turn: cache head, first and last tile, and where its part goes (null: it is whole).
+struct Turn {
+  int h, tile0, tile1;
+  float* part;
+};
+template <int ROWS, int DIM>
+__device__ __forceinline__ Turn walk_turn(const AttnArgs& a, const Walk& w) {
+  Turn u;
+  const int n = max(w.R.tiles, 1), off = (int)(w.at - w.base);
+  u.h = off / n;
+  u.tile0 = off - u.h * n;
+  u.tile1 = (int)min((int64_t)n, u.tile0 + (w.end - w.at));
+  const bool whole = u.tile0 == 0 && u.tile1 == n;
+  u.part = whole ? nullptr : a.part + ((int64_t)(2 * blockIdx.x + (u.tile0 == 0)) * ROWS) * (DIM + 4);
+  if (!a.whole && u.tile0 == 0 && threadIdx.x == 0) {
+    const int64_t last = w.base + (int64_t)u.h * n + n - 1;
+    const int count = whole ? 1 : (int)(((last + 1) * w.groups - 1) / w.total) - (int)blockIdx.x + 1;
+    a.parts[(w.R.t0 * a.each + w.R.r0) * a.c.heads + u.h] = make_int2((int)blockIdx.x, count);
+  }
+  return u;
 }
 
 template <int CTRL>
@@ -126,51 +276,50 @@ __global__ __launch_bounds__(256, DIM * RT <= 128 ? 3 : 2) void k_attention_spli
   __shared__ __align__(16) uint8_t lds[SHARED];
   __shared__ float row_factor[ROWS];
   __shared__ int row_sums[ROWS][NG][2];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, seg = lane >> 4;
-  const int b = blockIdx.z, h = blockIdx.y % a.c.heads;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, seg = lane >> 4;
   const int P = 1 << a.c.page_log2;
+  Walk W;
+  if (!walk_begin<ROWS, 256>(a, W)) return;
 
-  for (int rb = blockIdx.y / a.c.heads;; rb += a.row_blocks) {
-    const RowBlock R = row_block<ROWS>(a, b, rb);
-    if (rb * ROWS >= R.rows) break;
-    const int sp = blockIdx.x;
-    if (R.parts == 0 && sp == 0) {      // rows that see nothing
+  while (true) {
+    const RowBlock& R = W.R;
+    const Turn turn = walk_turn<ROWS, DIM>(a, W);
+    const int b = W.b, h = turn.h;
+    if (R.tiles == 0) {      // rows that see nothing
       for (int i = threadIdx.x; i < ROWS * DIM; i += 256) {
-        const int r = rb * ROWS + i / DIM;
+        const int r = R.r0 + i / DIM;
         if (r >= R.rows) break;
         const int64_t o = (R.t0 + r / a.each) * a.heads_q + h * a.each + r % a.each;
         store_any(a.out, o * DIM + i % DIM, 0.f, a.dtype);
         if (a.lse && i % DIM == 0) a.lse[o] = -INFINITY;
       }
+      if (!walk_on<ROWS>(a, W, 1)) return;
+      continue;
     }
-    if (sp >= R.parts) continue;
-    const int c0 = R.lo + sp * R.part, c1 = (int)min((int64_t)R.hi, (int64_t)c0 + R.part);
-
+    const int c0 = R.lo + 64 * turn.tile0, c1 = (int)min((int64_t)R.hi, (int64_t)R.lo + 64 * (int64_t)turn.tile1);
+    const int ntiles = turn.tile1 - turn.tile0;
     uint8_t* const pbuf = lds + SHARED_Q + wave * (NG * (16 * PROW + 64));
     uint8_t* const zbuf = pbuf + NG * 16 * PROW;
-
-    const int ntiles = (c1 - c0 + 63) >> 6;
     constexpr int NW = NG == 1 ? 1 : NG / 2;    // 32-bit loads of a token's K words (V's likewise; one for both at 64)
     v4u kr[4][NU], vr[NC];
     unsigned kw[4][NW], vw[4][NW];
-    unsigned ok = 0;        // bit t: block t of the tile has a page
-    // page of this lane's block (seg) of a tile, or -1
-    auto lookup = [&](int tile) -> int {
-      const int tok = c0 + tile * 64 + seg * 16;
-      if (tile >= ntiles || tok >= c1) return -1;
-      const int page = a.s.table[(int64_t)b * a.s.table_pages + (tok >> a.c.page_log2)];
-      return page >= 0 && page < a.c.num_pages ? page : -1;
+    uint64_t ok = 0;        // bit 16 t: block t of the tile has a page (as lanes say)
+    // table entry of this lane's block (seg) of a tile; only read here, so that nothing waits for it yet
+    auto entry = [&](int tile) -> int {
+      const unsigned tok = min((unsigned)c0 + (unsigned)(tile * 64 + seg * 16), (unsigned)(c1 - 1));
+      return a.s.table[(int64_t)b * a.s.table_pages + (tok >> a.c.page_log2)];
+    };
+    // its page's place in the cache; `has`: whether there is one (a page for no tokens reads page 0)
+    auto place = [&](int tile, int page, bool* has) -> uint64_t {
+      *has = (unsigned)c0 + (unsigned)(tile * 64 + seg * 16) < (unsigned)c1 && page >= 0 && page < a.c.num_pages;
+      return (uint64_t)((int64_t)(*has ? page : 0) * a.c.heads + h) * (uint64_t)a.c.head_bytes;
     };
     auto base_of = [&](uint64_t off, int t) -> const uint8_t* {
       const unsigned lo = __builtin_amdgcn_readlane((unsigned)off, 16 * t);
       const unsigned hi = __builtin_amdgcn_readlane((unsigned)(off >> 32), 16 * t);
       return a.cache + ((uint64_t)hi << 32 | lo);
     };
-    auto offset_of = [&](int page) -> uint64_t {
-      return (uint64_t)((int64_t)max(page, 0) * a.c.heads + h) * (uint64_t)a.c.head_bytes;
-    };
-    auto load_k = [&](int tile, int page) {
-      const uint64_t off = offset_of(page);
+    auto load_k = [&](int tile, uint64_t off) {
 #pragma unroll
       for (int t = 0; t < 4; t++) {
         const uint8_t* base = base_of(off, t);
@@ -188,10 +337,8 @@ __global__ __launch_bounds__(256, DIM * RT <= 128 ? 3 : 2) void k_attention_spli
         for (int g = 0; g < NW; g++) kw[t][g] = wp[g];
       }
     };
-    auto load_v = [&](int tile, int page) {
-      const uint64_t off = offset_of(page);
+    auto load_v = [&](int tile, uint64_t off) {
       const int tok = c0 + tile * 64;
-      ok = 0;
 #pragma unroll
       for (int t = 0; t < 4; t++) {
         if constexpr (NG > 1) {
@@ -200,7 +347,6 @@ __global__ __launch_bounds__(256, DIM * RT <= 128 ? 3 : 2) void k_attention_spli
 #pragma unroll
           for (int g = 0; g < NW; g++) vw[t][g] = wp[g];
         }
-        ok |= (unsigned)(__builtin_amdgcn_readlane(page, 16 * t) >= 0) << t;
       }
       const uint8_t* vp = a.cache + off + (unsigned)P * HALF + ((unsigned)((tok + 16 * seg) & (P - 1)) >> 4) * (HALF * 16) + l16 * 16;
 #pragma unroll
@@ -213,15 +359,19 @@ __global__ __launch_bounds__(256, DIM * RT <= 128 ? 3 : 2) void k_attention_spli
     };
 
     // the first tile's loads are in flight while the queries are taken apart
-    int page = lookup(wave);
-    if (wave < ntiles) {
-      load_k(wave, page);
-      load_v(wave, page);
+    const int here = entry(wave);
+    int ahead = entry(wave + 4);
+    {
+      bool has = false;
+      const uint64_t off = place(wave, here, &has);
+      ok = __ballot(has);
+      load_k(wave, off);
+      load_v(wave, off);
     }
 
     // ---- the rows' digits, one wave per row ----
     for (int r = wave; r < ROWS; r += 4) {
-      const int row = rb * ROWS + r;
+      const int row = R.r0 + r;
       float x[NG], top = 0.f;
       bool bad = false;
 #pragma unroll
@@ -271,12 +421,12 @@ __global__ __launch_bounds__(256, DIM * RT <= 128 ? 3 : 2) void k_attention_spli
     float O[RT][2 * NC], poison[RT][NG];
 #pragma unroll
     for (int p = 0; p < RT; p++) {
-      const int r = p * 4 + seg, row = rb * ROWS + r;
+      const int r = p * 4 + seg, row = R.r0 + r;
 #pragma unroll
       for (int g = 0; g < NG; g++) {
         Q[p][g] = *(const v4i*)(lds + ((p * NG + g) * 16 + l16) * QROW + seg * 16);
-        qhi[p][g] = row_sums[r][g][0];
-        qlo[p][g] = row_sums[r][g][1];
+        qhi[p][g] = -row_sums[r][g][0];
+        qlo[p][g] = -row_sums[r][g][1];
         poison[p][g] = 0.f;
       }
       factor[p] = row_factor[r];
@@ -290,7 +440,7 @@ __global__ __launch_bounds__(256, DIM * RT <= 128 ? 3 : 2) void k_attention_spli
     }
     // One tile: K's registers are free once the scores are there and take the
     // next tile's K then; V's likewise at the end.
-    auto compute = [&](int tile, int next_page) {
+    auto compute = [&](int tile, int next_entry) {
       const int tok = c0 + tile * 64 + l16;
       const v4i zero = {0, 0, 0, 0};
       float x[RT][4];
@@ -316,8 +466,8 @@ __global__ __launch_bounds__(256, DIM * RT <= 128 ? 3 : 2) void k_attention_spli
             const unsigned word = k_word(t, g);
             const v4i r = __builtin_amdgcn_mfma_i32_16x16x64_i8(Q[p][g], kop[g], zero, 0, 0, 0);
             const int z = (int)(word & 15);
-            const int hi = (r[3] << 8) + r[2] - __mul24(z, qhi[p][g]);
-            const int lo = (r[1] << 8) + r[0] - __mul24(z, qlo[p][g]);
+            const int hi = __mul24(z, qhi[p][g]) + ((r[3] << 8) + r[2]);
+            const int lo = __mul24(z, qlo[p][g]) + ((r[1] << 8) + r[0]);
             sum = fmaf(scale_of(word), fmaf((float)hi, 65536.f, (float)lo), sum);
           }
           x[p][t] = sum * factor[p];
@@ -328,8 +478,13 @@ __global__ __launch_bounds__(256, DIM * RT <= 128 ? 3 : 2) void k_attention_spli
 #pragma unroll
         for (int t = 0; t < 4; t++) vw[t][0] = kw[t][0];
       }
-      const bool more = tile + 4 < ntiles;
-      if (more) load_k(tile + 4, next_page);
+      // always loaded, so that the number of loads in flight is known where they are waited for: past the part's end
+      // a few lines of page 0, the same for all
+      bool has = false;
+      const uint64_t next = place(tile + 4, next_entry, &has);
+      const uint64_t next_ok = __ballot(has);
+      __builtin_amdgcn_sched_barrier(0);
+      load_k(tile + 4, next);
       // ---- zero points of the values, negated, for the accumulators' start ----
 #pragma unroll
       for (int t = 0; t < 4; t++)
@@ -344,7 +499,7 @@ __global__ __launch_bounds__(256, DIM * RT <= 128 ? 3 : 2) void k_attention_spli
 #pragma unroll
         for (int t = 0; t < 4; t++) {
           const int pos = tok + 16 * t;
-          seen[t] = (ok >> t & 1) && pos <= last[p] && pos >= least[p];
+          seen[t] = (bool)(ok >> (16 * t) & 1) & (pos <= last[p]) & (pos >= least[p]);
           x[p][t] = seen[t] ? x[p][t] : -INFINITY;
           top = fmaxf(top, x[p][t]);
         }
@@ -421,14 +576,18 @@ __global__ __launch_bounds__(256, DIM * RT <= 128 ? 3 : 2) void k_attention_spli
         }
         if constexpr (RT > 1) __builtin_amdgcn_sched_barrier(0);      // one row tile's registers at a time
       }
-      if (more) load_v(tile + 4, next_page);
+      __builtin_amdgcn_sched_barrier(0);      // into the registers that this tile's have left
+      load_v(tile + 4, next);
+      ok = next_ok;
     };
 
-    page = lookup(wave + 4);
-    for (int tile = wave; tile < ntiles; tile += 4) {
-      const int after = lookup(tile + 8);
-      compute(tile, page);
-      page = after;
+    // by two, so that no register is copied (and its load waited for) at the loop's end
+    for (int tile = wave; tile < ntiles; tile += 8) {
+      const int after = entry(tile + 8);
+      compute(tile, ahead);
+      if (tile + 4 >= ntiles) break;
+      ahead = entry(tile + 12);
+      compute(tile + 4, after);
     }
 
     // ---- join the four waves: lane (row, channel) sums of each, then by the row's maximum ----
@@ -451,9 +610,8 @@ __global__ __launch_bounds__(256, DIM * RT <= 128 ? 3 : 2) void k_attention_spli
       }
     }
     __syncthreads();
-    const bool whole = R.parts == 1;
     for (int i = threadIdx.x; i < ROWS * DIM; i += 256) {
-      const int r = i / DIM, d = i % DIM, row = rb * ROWS + r;
+      const int r = i / DIM, d = i % DIM, row = R.r0 + r;
       if (row >= R.rows) break;
       float top = -INFINITY;
 #pragma unroll
@@ -468,12 +626,12 @@ __global__ __launch_bounds__(256, DIM * RT <= 128 ? 3 : 2) void k_attention_spli
         sum = fmaf(from[DIM + 1], f, sum);
       }
       const int64_t to = (R.t0 + row / a.each) * a.heads_q + h * a.each + row % a.each;
-      if (whole) {
+      if (!turn.part) {
         const bool none = sum == 0.f;
         store_any(a.out, to * DIM + d, none ? 0.f : o / sum, a.dtype);
         if (a.lse && d == 0) a.lse[to] = none ? -INFINITY : (top + log2f(sum)) * 0.69314718055994530942f;
       } else {
-        float* part = a.part + (to * a.nsplit + sp) * (DIM + 4);
+        float* part = turn.part + r * (DIM + 4);
         part[d] = o;
         if (d == 0) {
           part[DIM] = top;
@@ -481,6 +639,7 @@ __global__ __launch_bounds__(256, DIM * RT <= 128 ? 3 : 2) void k_attention_spli
         }
       }
     }
+    if (!walk_on<ROWS>(a, W, ntiles)) return;
     __syncthreads();
   }
 }
@@ -499,8 +658,9 @@ __global__ __launch_bounds__(256, DIM * RT <= 128 ? 3 : 2) void k_attention_spli
 // 1024 + code, subtract 1024 + z, times s) while the tile before is in work;
 // one barrier a tile.  The weights are taken against a running reference that
 // moves only when a row's maximum passes it by 2^8, so O is rarely rescaled.
-template <int DIM>
+template <int DIM, int DT>
 __global__ __launch_bounds__(512, 2) void k_attention_chunk(AttnArgs a) {
+  typedef typename Elem<DT>::T T;
   constexpr int NG = DIM / KV4_GROUP, HALF = DIM / 2, ROWS = 256;
   constexpr int TT = DIM == 256 ? 32 : 64;          // tokens of a tile
   constexpr int NS = TT / 32, KS = DIM / 16, PS = TT / 16, CT = DIM / 32;
@@ -508,9 +668,8 @@ __global__ __launch_bounds__(512, 2) void k_attention_chunk(AttnArgs a) {
   constexpr int WB = 8 / PS;                        // waves of a 16-token block
   __shared__ __align__(16) _Float16 kt[2][TT * DIM], vt[2][DIM * TT];
   __shared__ __align__(8) uint8_t flags[2][8];      // of each wave's 8 values' tokens: 1 there, 3 some NaN among them
-  __shared__ uint8_t nans[2][8][NG];                // which of them
+  __shared__ uint16_t nans[2][8][NG];               // which of the block's tokens
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, half = lane >> 5;
-  const int h = blockIdx.x % a.c.heads, sp = blockIdx.x / a.c.heads, b = blockIdx.z;
   const int P = 1 << a.c.page_log2;
   const int block = wave / WB;                      // the 16-token block of a tile that this wave converts
   const int vhalf = WB == 2 ? wave & 1 : (wave >> 1) & 1;      // of it, tokens 4 vhalf + {0..3, 8..11}
@@ -522,17 +681,23 @@ __global__ __launch_bounds__(512, 2) void k_attention_chunk(AttnArgs a) {
   auto kat = [](int tok, int u) { return (tok * KU + (DIM == 64 ? u ^ ((tok >> 1) & 7) : u ^ (tok & 15))) * 8; };
   auto vat = [](int ch, int u) { return (ch * VU + (TT == 64 ? u ^ ((ch >> 1) & 7) : u ^ ((ch >> 2) & 3))) * 8; };
 
-  for (int rb = a.row_blocks - 1 - (int)blockIdx.y;; rb += a.row_blocks) {
-    const RowBlock R = row_block<ROWS>(a, b, rb);
-    if (rb * ROWS >= R.rows) break;
-    const int row = rb * ROWS + wave * 32 + l32;
+  Walk W;
+  if (!walk_begin<ROWS, 512>(a, W)) return;
+  while (true) {
+    const RowBlock& R = W.R;
+    const Turn turn = walk_turn<ROWS, DIM>(a, W);
+    const int b = W.b, h = turn.h;
+    const int row = R.r0 + wave * 32 + l32;
     const int64_t to = (R.t0 + row / a.each) * a.heads_q + h * a.each + row % a.each;
-    if (R.parts == 0 && sp == 0 && row < R.rows) {      // rows that see nothing
-      for (int d = half; d < DIM; d += 2) store_any(a.out, to * DIM + d, 0.f, a.dtype);
-      if (a.lse && !half) a.lse[to] = -INFINITY;
+    if (R.tiles == 0) {      // rows that see nothing
+      if (row < R.rows) {
+        for (int d = half; d < DIM; d += 2) ((T*)a.out)[to * DIM + d] = Elem<DT>::store(0.f);
+        if (a.lse && !half) a.lse[to] = -INFINITY;
+      }
+      if (!walk_on<ROWS>(a, W, 1)) return;
+      continue;
     }
-    if (sp >= R.parts) continue;
-    const int c0 = R.lo + sp * R.part, c1 = (int)min((int64_t)R.hi, (int64_t)c0 + R.part);
+    const int c0 = R.lo + 64 * turn.tile0, c1 = (int)min((int64_t)R.hi, (int64_t)R.lo + 64 * (int64_t)turn.tile1);
 
     // ---- this lane's half of its row's query, as fp16 ----
     f16x8 Q[KS];
@@ -540,15 +705,17 @@ __global__ __launch_bounds__(512, 2) void k_attention_chunk(AttnArgs a) {
     {
       float x[KS][8], top = 0.f;
       bool bad = false;
+      const T* q = (const T*)a.q + (R.t0 + min(row, R.rows - 1) / a.each) * a.q_ts + (h * a.each + row % a.each) * a.q_hs + half * 8;
+      if (a.q_vec)
+#pragma unroll
+        for (int k = 0; k < KS; k++) load_n<DT, 8, true>(q + k * 16, x[k]);
+      else
+#pragma unroll
+        for (int k = 0; k < KS; k++) load_n<DT, 8, false>(q + k * 16, x[k]);
 #pragma unroll
       for (int k = 0; k < KS; k++)
 #pragma unroll
         for (int j = 0; j < 8; j++) {
-          x[k][j] = 0.f;
-          if (row < R.rows) {
-            const int64_t at = (R.t0 + row / a.each) * a.q_ts + (h * a.each + row % a.each) * a.q_hs;
-            x[k][j] = load_any(a.q, at + k * 16 + half * 8 + j, a.dtype);
-          }
           bad |= !__builtin_isfinite(x[k][j]);
           top = fmaxf(top, fabsf(x[k][j]));
         }
@@ -564,7 +731,8 @@ __global__ __launch_bounds__(512, 2) void k_attention_chunk(AttnArgs a) {
           constexpr int order[8] = {0, 2, 1, 3, 4, 6, 5, 7};      // as two codes come out of one mask
           Q[k][j] = (_Float16)(bad ? 0.f : ldexpf(sign * x[k][order[j]], 15 - e));
         }
-      factor = bad ? NAN : ldexpf(fabsf(a.scale) * 1.44269504088896340736f, e - 15);
+      // above 0, so that a masked score of -infinity stays one
+      factor = bad ? NAN : fmaxf(ldexpf(fabsf(a.scale) * 1.44269504088896340736f, e - 15), 1.17549435e-38f);
     }
     const int pos = R.first + row / a.each;
     const int last = row < R.rows ? min(pos, c1 - 1) : -1;
@@ -591,16 +759,18 @@ __global__ __launch_bounds__(512, 2) void k_attention_chunk(AttnArgs a) {
 
     const int ntiles = (c1 - c0 + TT - 1) / TT;
     v2u kraw;
-    unsigned vraw[2], kword[(NG + 1) / 2], vword[8][(NG + 1) / 2];
+    unsigned vraw[2], kword[(NG + 1) / 2], vword[(NG + 1) / 2];      // vword: of the token that lane % 8 stands for
+    const int vtok = 4 * vhalf + (lane & 3) + (lane & 4) * 2;
     int page_now = -1;       // of the loaded tile's block
-    auto lookup = [&](int tile) -> int {
-      const int tok = c0 + tile * TT + block * 16;
-      if (tile >= ntiles || tok >= c1) return -1;
-      const int page = a.s.table[(int64_t)b * a.s.table_pages + (tok >> a.c.page_log2)];
-      return page >= 0 && page < a.c.num_pages ? page : -1;
+    // table entry of this wave's block of a tile; only read here, so that nothing waits for it yet
+    auto entry = [&](int tile) -> int {
+      const unsigned tok = min((unsigned)c0 + (unsigned)(tile * TT + block * 16), (unsigned)(c1 - 1));
+      return a.s.table[(int64_t)b * a.s.table_pages + (tok >> a.c.page_log2)];
     };
+    // always all loads, past the part's end from page 0: their number in flight is known where they are waited for
     auto load = [&](int tile, int page) {
-      page_now = __builtin_amdgcn_readfirstlane(page);
+      page = __builtin_amdgcn_readfirstlane(page);
+      page_now = (unsigned)c0 + (unsigned)(tile * TT + block * 16) < (unsigned)c1 && page >= 0 && page < a.c.num_pages ? page : -1;
       const uint8_t* base = a.cache + ((int64_t)max(page_now, 0) * a.c.heads + h) * a.c.head_bytes;
       const int o = (c0 + tile * TT + block * 16) & (P - 1);      // the block's place in its page
       const uint8_t* words = base + (unsigned)P * DIM;
@@ -611,13 +781,9 @@ __global__ __launch_bounds__(512, 2) void k_attention_chunk(AttnArgs a) {
       const unsigned* vp = (const unsigned*)(base + (unsigned)P * HALF + (o >> 4) * (HALF * 16) + (vin ? vcol : 0) * 16);
       vraw[0] = vp[vhalf];
       vraw[1] = vp[2 + vhalf];
+      const unsigned* w = (const unsigned*)(words + (o + vtok) * (4 * NG));
 #pragma unroll
-      for (int j = 0; j < 8; j++) {
-        const int tok = o + 4 * vhalf + (j & 3) + (j >> 2) * 8;
-        const unsigned* w = (const unsigned*)(words + tok * (4 * NG));
-#pragma unroll
-        for (int g = 0; g < (NG + 1) / 2; g++) vword[j][g] = NG == 1 ? w[0] >> 16 : w[NG / 2 + g];
-      }
+      for (int g = 0; g < (NG + 1) / 2; g++) vword[g] = NG == 1 ? w[0] >> 16 : w[NG / 2 + g];
     };
     // one dword of codes to four pairs of values: bytes (0, 2), (1, 3) of the low nibbles, then of the high ones
     auto pair = [](unsigned w, unsigned minus, unsigned scale) -> unsigned {
@@ -649,26 +815,17 @@ __global__ __launch_bounds__(512, 2) void k_attention_chunk(AttnArgs a) {
       }
       {
         // V: words of tokens that are not there count as 0, NaN ones too (kept as bits)
-        const int tok = c0 + tile * TT + block * 16 + 4 * vhalf;
-        unsigned mask[NG], flag = page_now >= 0 ? 1 : 0;
+        const bool in = page_now >= 0 && c0 + tile * TT + block * 16 + vtok < c1;
+        unsigned mask[NG], flag = page_now >= 0 ? 1 : 0, word[8][(NG + 1) / 2];
 #pragma unroll
-        for (int g = 0; g < NG; g++) mask[g] = 0;
+        for (int g = 0; g < (NG + 1) / 2; g++) {
+          unsigned w = in ? vword[g] : 0u;
+          const bool lo = (w & 0x7C00u) == 0x7C00u, hi = NG > 1 && (w & 0x7C000000u) == 0x7C000000u;
+          mask[2 * g] = (unsigned)__ballot(lo) & 0xFF;
+          if (NG > 1) mask[NG > 1 ? 2 * g + 1 : 0] = (unsigned)__ballot(hi) & 0xFF;
+          w &= (lo ? 0xFFFF0000u : ~0u) & (hi ? 0xFFFFu : ~0u);
 #pragma unroll
-        for (int j = 0; j < 8; j++) {
-          const bool in = page_now >= 0 && tok + (j & 3) + (j >> 2) * 8 < c1;
-#pragma unroll
-          for (int g = 0; g < (NG + 1) / 2; g++) {
-            unsigned w = in ? __builtin_amdgcn_readfirstlane(vword[j][g]) : 0u;
-            if ((w & 0x7C00u) == 0x7C00u) {
-              mask[2 * g] |= 1u << j;
-              w &= 0xFFFF0000u;
-            }
-            if (NG > 1 && (w & 0x7C000000u) == 0x7C000000u) {
-              mask[NG > 1 ? 2 * g + 1 : 0] |= 1u << j;
-              w &= 0xFFFFu;
-            }
-            vword[j][g] = w;
-          }
+          for (int j = 0; j < 8; j++) word[j][g] = __builtin_amdgcn_readlane(w, j);
         }
         unsigned out[2][4];
 #pragma unroll
@@ -679,7 +836,7 @@ __global__ __launch_bounds__(512, 2) void k_attention_chunk(AttnArgs a) {
           for (int j = 0; j < 2; j++)
 #pragma unroll
             for (int q = 0; q < 2; q++) {
-              const unsigned w0 = vword[4 * j + q][wi], w1 = vword[4 * j + q + 2][wi];
+              const unsigned w0 = word[4 * j + q][wi], w1 = word[4 * j + q + 2][wi];
               const unsigned w = top ? (w0 >> 16) | (w1 & 0xFFFF0000u) : (w0 & 0xFFFFu) | (w1 << 16);
               out[s][2 * j + q] = pair(vraw[j] >> (4 * s + 8 * q), (w & 0x000F000Fu) | 0xE400E400u, w & 0xFFF0FFF0u);
             }
@@ -692,11 +849,12 @@ __global__ __launch_bounds__(512, 2) void k_attention_chunk(AttnArgs a) {
 #pragma unroll
         for (int g = 0; g < NG; g++)
           if (mask[g]) flag |= 2;
-        if (lane == 0) {
-          flags[buf][wave] = (uint8_t)flag;
-          if (flag & 2)
+        if (lane == 0) flags[buf][wave] = (uint8_t)flag;
+        if (flag & 2 && lane < NG) {
+          unsigned m = mask[0];
 #pragma unroll
-            for (int g = 0; g < NG; g++) nans[buf][wave][g] = (uint8_t)mask[g];
+          for (int g = 1; g < NG; g++) m = lane == g ? mask[g] : m;
+          nans[buf][wave][lane] = (uint16_t)((m & 15) << (4 * vhalf) | (m >> 4) << (8 + 4 * vhalf));
         }
       }
     };
@@ -717,25 +875,38 @@ __global__ __launch_bounds__(512, 2) void k_attention_chunk(AttnArgs a) {
           S[s] = __builtin_amdgcn_mfma_f32_32x32x16_f16(A, Q[k], S[s], 0, 0, 0);
         }
       }
-      const bool plain = f0 == 0x01010101u && f1 == 0x01010101u && tok0 >= all_from && tok0 + TT - 1 <= all_to;
-      float top = -INFINITY;
-      if (plain) {
+      if (f0 != 0x01010101u || f1 != 0x01010101u || tok0 < all_from || tok0 + TT - 1 > all_to) {
+        // the tile's tokens that this lane's row sees, a bit each
+        const int from = max(least - tok0, 0), to = min(last - tok0, TT - 1);
+        uint64_t there = 0;      // blocks that have a page
 #pragma unroll
-        for (int s = 0; s < NS; s++)
+        for (int k = 0; k < PS; k++)
+          if ((k * WB < 4 ? f0 >> (8 * k * WB) : f1 >> (8 * (k * WB - 4))) & 1) there |= 0xFFFFull << (16 * k);
+        const uint64_t see = to < from ? 0 : there & (~0ull >> (63 - to)) & (~0ull << from);
+        if ((f0 | f1) & 0x02020202u)      // a NaN among the values: for the rows that see it, in its group
+          for (int g = 0; g < NG; g++) {
+            uint64_t nan = 0;
+            for (int w = 0; w < 8; w++)
+              if ((w < 4 ? f0 >> (8 * w) : f1 >> (8 * (w - 4))) & 2) nan |= (uint64_t)nans[buf][w][g] << (16 * (w / WB));
+            if (nan & see)
 #pragma unroll
-          for (int i = 0; i < 16; i++) top = fmaxf(top, S[s][i]);
-      } else {
+              for (int i = 0; i < NG; i++) poison[i] = i == g ? NAN : poison[i];
+          }
 #pragma unroll
-        for (int s = 0; s < NS; s++)
+        for (int s = 0; s < NS; s++) {
+          const unsigned bits = (unsigned)(see >> (32 * s)) >> (4 * half);
 #pragma unroll
           for (int i = 0; i < 16; i++) {
-            const int t = s * 32 + 8 * (i / 4) + 4 * half + i % 4, p = tok0 + t;
-            const int w = t / 16 * WB;      // a wave that converted the token's block
-            const unsigned f = (w < 4 ? f0 >> (8 * w) : f1 >> (8 * (w - 4))) & 1;
-            const bool seen = f && p <= last && p >= least;
-            top = fmaxf(top, seen ? S[s][i] : -INFINITY);
+            const int m = (int)(bits << (31 - (8 * (i / 4) + i % 4))) >> 31;
+            S[s][i] = __int_as_float((__float_as_int(S[s][i]) & m) | ((int)0xFF800000 & ~m));
           }
+        }
       }
+      float top = S[0][0];
+#pragma unroll
+      for (int s = 0; s < NS; s++)
+#pragma unroll
+        for (int i = 0; i < 16; i++) top = fmaxf(top, S[s][i]);
       const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
       top = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * factor;
       if (__any(top > ref + 8.f)) {
@@ -754,24 +925,6 @@ __global__ __launch_bounds__(512, 2) void k_attention_chunk(AttnArgs a) {
       for (int s = 0; s < NS; s++)
 #pragma unroll
         for (int i = 0; i < 16; i++) S[s][i] = fmaf(S[s][i], factor, -at);
-      if (!plain) {
-#pragma unroll
-        for (int s = 0; s < NS; s++)
-#pragma unroll
-          for (int i = 0; i < 16; i++) {
-            const int t = s * 32 + 8 * (i / 4) + 4 * half + i % 4, p = tok0 + t;
-            const int w = t / 16 * WB + (WB == 2 ? half : 2 * half);      // the wave that converted the token's values
-            const unsigned f = (w < 4 ? f0 >> (8 * (w & 3)) : f1 >> (8 * (w & 3)));
-            const bool seen = (f & 1) && p <= last && p >= least;
-            S[s][i] = seen ? S[s][i] : -INFINITY;
-            if (f & 2 && seen) {
-              const int bit = i % 4 + (i / 4 & 1) * 4;
-#pragma unroll
-              for (int g = 0; g < NG; g++)
-                if (nans[buf][w][g] >> bit & 1) poison[g] = NAN;
-            }
-          }
-      }
 #pragma unroll
       for (int k = 0; k < PS; k++) {
         const int s = k / 2, i0 = (k & 1) * 8;
@@ -795,19 +948,23 @@ __global__ __launch_bounds__(512, 2) void k_attention_chunk(AttnArgs a) {
         }
     };
 
-    load(0, lookup(0));
-    int page = lookup(1);
+    int e0 = entry(0), e1 = entry(1), e2 = entry(2);
+    load(0, e0);
     convert(0, 0);
-    load(1, page);
-    page = lookup(2);
+    load(1, e1);
     __syncthreads();
-    for (int tile = 0; tile < ntiles; tile++) {
-      if (tile + 1 < ntiles) {
-        convert((tile + 1) & 1, tile + 1);
-        load(tile + 2, page);
-        page = lookup(tile + 3);
-      }
-      compute(tile & 1, tile);
+    // by two: no register is copied, and its load waited for, at the loop's end
+    for (int tile = 0; tile < ntiles; tile += 2) {
+      e1 = entry(tile + 3);
+      convert(1, tile + 1);
+      load(tile + 2, e2);
+      compute(0, tile);
+      __syncthreads();
+      if (tile + 1 >= ntiles) break;
+      e2 = entry(tile + 4);
+      convert(0, tile + 2);
+      load(tile + 3, e1);
+      compute(1, tile + 1);
       __syncthreads();
     }
 
@@ -816,9 +973,9 @@ __global__ __launch_bounds__(512, 2) void k_attention_chunk(AttnArgs a) {
 #pragma unroll
     for (int g = 0; g < NG; g++) poison[g] += __shfl_xor(poison[g], 32);
     if (row < R.rows) {
-      const bool whole = R.parts == 1, none = l == 0.f;
+      const bool whole = !turn.part, none = l == 0.f;
       const float by = whole ? none ? 0.f : 1.f / l : 1.f;
-      float* part = a.part + (to * a.nsplit + sp) * (DIM + 4);
+      float* part = turn.part + (wave * 32 + l32) * (DIM + 4);
 #pragma unroll
       for (int c = 0; c < CT; c++)
 #pragma unroll
@@ -828,9 +985,14 @@ __global__ __launch_bounds__(512, 2) void k_attention_chunk(AttnArgs a) {
 #pragma unroll
           for (int j = 0; j < 4; j++) o[j] = (O[c][i + j] + poison[c / 2]) * by;
           if (!whole) *(f32x4*)(part + d) = f32x4{o[0], o[1], o[2], o[3]};
-          else
+          else {
+            v2u w;
 #pragma unroll
-            for (int j = 0; j < 4; j++) store_any(a.out, to * DIM + d + j, o[j], a.dtype);
+            for (int j = 0; j < 2; j++)
+              w[j] = (unsigned)__builtin_bit_cast(uint16_t, Elem<DT>::store(o[2 * j])) |
+                     (unsigned)__builtin_bit_cast(uint16_t, Elem<DT>::store(o[2 * j + 1])) << 16;
+            *(v2u*)((T*)a.out + to * DIM + d) = w;
+          }
         }
       if (whole && a.lse && !half) a.lse[to] = none ? -INFINITY : (ref + log2f(l)) * 0.69314718055994530942f;
       if (!whole && !half) {
@@ -838,37 +1000,45 @@ __global__ __launch_bounds__(512, 2) void k_attention_chunk(AttnArgs a) {
         part[DIM + 1] = l;
       }
     }
+    if (!walk_on<ROWS>(a, W, turn.tile1 - turn.tile0)) return;
   }
 }
 
-// Joins the parts of a row (at most 256): one workgroup per new token and query
-// head, four channels a thread and 1024 / DIM parts side by side.
+// Joins the parts of a row: one workgroup per new token and query head, four
+// channels a thread and 1024 / DIM parts side by side.
+constexpr int MAX_GROUPS = 768;      // workgroups of a launch that are joined
 template <int DIM, int ROWS>
 __global__ __launch_bounds__(256) void k_attention_join(AttnArgs a) {
   constexpr int TH = DIM / 4, GR = 256 / TH;
-  __shared__ float weight[256], red[8];
+  __shared__ float weight[MAX_GROUPS], red[8];
   __shared__ f32x4 acc[GR][TH];
   const int64_t t = blockIdx.x;
   const int hq = blockIdx.y, tid = threadIdx.x;
-  const int b = sequence_of(a.s, t);
-  const int64_t t0 = a.s.starts ? a.s.starts[b] : b;
+  const int64_t t0 = a.s.starts ? a.s.starts[sequence_of(a.s, t)] : t;
   const int row = (int)(t - t0) * a.each + hq % a.each;
-  if (row < 0) return;
-  const RowBlock R = row_block<ROWS>(a, b, row / ROWS);
-  if (R.parts < 2) return;      // written by the kernel before
-  const int64_t to = t * a.heads_q + hq;
-  const float* part = a.part + to * a.nsplit * (DIM + 4);
-  const float m = tid < R.parts ? part[(size_t)tid * (DIM + 4) + DIM] : -INFINITY;
-  const float l = tid < R.parts ? part[(size_t)tid * (DIM + 4) + DIM + 1] : 0.f;
-  float top = m;
+  if (t0 < 0 || row < 0) return;
+  const int2 parts = a.parts[(t0 * a.each + row / ROWS * ROWS) * a.c.heads + hq / a.each];
+  const int n = min(parts.y, MAX_GROUPS);
+  if (n < 2) return;      // written by the kernel before
+  // a row block's first part is its workgroup's last, its others their workgroups' first
+  const auto part = [&](int p) {
+    return a.part + ((int64_t)(p ? 2 * (parts.x + p) : 2 * parts.x + 1) * ROWS + row % ROWS) * (DIM + 4);
+  };
+  float top = -INFINITY;
+  for (int p = tid; p < n; p += 256) {
+    weight[p] = part(p)[DIM];
+    top = fmaxf(top, weight[p]);
+  }
   for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
   if ((tid & 63) == 0) red[tid >> 6] = top;
   __syncthreads();
   top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
   const float at = top == -INFINITY ? 0.f : top;
-  const float w = __builtin_amdgcn_exp2f(m - at);
-  weight[tid] = w;
-  float sum = tid < R.parts ? w * l : 0.f;
+  float sum = 0.f;
+  for (int p = tid; p < n; p += 256) {
+    weight[p] = __builtin_amdgcn_exp2f(weight[p] - at);
+    sum = fmaf(weight[p], part(p)[DIM + 1], sum);
+  }
   for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
   if ((tid & 63) == 0) red[4 + (tid >> 6)] = sum;
   __syncthreads();
@@ -876,8 +1046,8 @@ __global__ __launch_bounds__(256) void k_attention_join(AttnArgs a) {
   const int g = tid / TH, c = tid % TH;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-  for (int p = g; p < R.parts; p += GR) {
-    const f32x4 x = *(const f32x4*)(part + (size_t)p * (DIM + 4) + 4 * c);
+  for (int p = g; p < n; p += GR) {
+    const f32x4 x = *(const f32x4*)(part(p) + 4 * c);
     const float f = weight[p];
 #pragma unroll
     for (int j = 0; j < 4; j++) o[j] = fmaf(x[j], f, o[j]);
@@ -889,6 +1059,7 @@ __global__ __launch_bounds__(256) void k_attention_join(AttnArgs a) {
 #pragma unroll
   for (int i = 0; i < GR; i++) out += acc[i][tid >> 2][tid & 3];
   const bool none = sum == 0.f;
+  const int64_t to = t * a.heads_q + hq;
   store_any(a.out, to * DIM + tid, none ? 0.f : out / sum, a.dtype);
   if (a.lse && tid == 0) a.lse[to] = none ? -INFINITY : (top + log2f(sum)) * 0.69314718055994530942f;
 }
@@ -897,50 +1068,59 @@ __global__ __launch_bounds__(256) void k_attention_join(AttnArgs a) {
 static int row_tiles(int rows, int dim) { return rows <= 4 ? 1 : rows <= 8 || dim == 256 ? 2 : 4; }
 
 constexpr int CHUNK_ROWS = 64;
+constexpr int WHOLE_TILES = 16;
 
-struct SplitPlan {
-  int rt, row_blocks, nsplit, chunk;      // rt 0: k_attention_chunk
+struct Plan {
+  int rt, rows;              // row tiles of k_attention_split (0: k_attention_chunk), rows of a row block
+  int whole, blocks, groups; // AttnArgs::whole, ::blocks; workgroups
+  int64_t parts;             // entries of AttnArgs::parts
 };
-// Parts of about equal size: enough workgroups to fill the chip (two of four
-// waves a CU resident, in one pass), a part no shorter than four waves' tile each.
-static SplitPlan split_plan(int each, int heads_kv, int dim, int dtype, int batch, int64_t max_new, int64_t max_len) {
-  SplitPlan p;
+// One workgroup per row block and cache head where lengths are short; else as
+// many as are resident at once (three of four waves a CU where 168 registers
+// do, two elsewhere, one of eight for k_attention_chunk), but not below four
+// tiles each.
+static bool attention_plan(int heads_q, int heads_kv, int dim, int dtype, int64_t tokens, int batch, bool starts,
+                           int64_t max_new, int64_t max_len, Plan* p) {
+  const int each = heads_q / heads_kv;
   const int64_t rows = max_new * each;
-  p.rt = dtype != EXTERND_F32 && rows >= CHUNK_ROWS ? 0 : row_tiles((int)(rows > 64 ? 64 : rows), dim);
-  const int per = p.rt ? 4 * p.rt : 256;
-  const int64_t blocks = (rows + per - 1) / per;
-  p.row_blocks = (int)(blocks > 16384 / heads_kv ? (16384 / heads_kv > 0 ? 16384 / heads_kv : 1) : blocks);
-  const int64_t units = (int64_t)batch * heads_kv * p.row_blocks;
-  const int64_t len = max_len < 1 ? 65536 : max_len;
-  int64_t n = ((p.rt ? 512 : 256) + units - 1) / units;
-  const int64_t most = (len + 255) / 256;
-  n = n > most ? most : n;
-  n = n > 256 ? 256 : n < 1 ? 1 : n;
-  int64_t chunk = ((len + n - 1) / n + 255) & ~(int64_t)255;
-  if (chunk > (1 << 30)) chunk = 1 << 30;
-  p.chunk = (int)chunk;
-  p.nsplit = (int)((len + chunk - 1) / chunk);
-  if (p.nsplit < 1) p.nsplit = 1;
-  return p;
+  p->rt = dtype != EXTERND_F32 && rows >= CHUNK_ROWS ? 0 : row_tiles((int)(rows > 64 ? 64 : rows), dim);
+  p->rows = p->rt ? 4 * p->rt : 256;
+  const int64_t blocks = starts ? tokens * each / p->rows + batch : (int64_t)batch * ((each + p->rows - 1) / p->rows);
+  if (blocks * heads_kv > INT32_MAX) return false;
+  p->blocks = (int)blocks;
+  p->parts = tokens * heads_q;
+  const int64_t tiles = max_len > 0 ? (max_len + 63) / 64 : 1 << 20;
+  p->whole = tiles <= WHOLE_TILES;
+  if (p->whole) {
+    p->groups = (int)(blocks * heads_kv);
+    return true;
+  }
+  int64_t most = !p->rt ? 256 : dim * p->rt <= 128 ? 768 : 512;
+  const int64_t fit = (blocks * heads_kv * tiles + 3) / 4;
+  p->groups = (int)(most < fit ? most : fit);
+  return true;
+}
+static size_t plan_bytes(const Plan& p, int dim) {
+  if (p.whole) return 0;
+  const size_t parts = (size_t)p.groups * 2 * p.rows * (dim + 4) * sizeof(float);
+  return parts + (((size_t)p.parts * sizeof(int2) + 255) & ~(size_t)255);
 }
 
 template <int DIM, int RT>
-static void launch_split(const AttnArgs& a, hipStream_t s) {
-  const dim3 grid((unsigned)a.nsplit, (unsigned)(a.c.heads * a.row_blocks), (unsigned)a.s.batch);
-  if (a.dtype == EXTERND_F32) k_attention_split<DIM, RT, true><<<grid, 256, 0, s>>>(a);
-  else k_attention_split<DIM, RT, false><<<grid, 256, 0, s>>>(a);
-  if (a.nsplit > 1)
-    k_attention_join<DIM, 4 * RT><<<dim3((unsigned)a.s.tokens, (unsigned)a.heads_q), 256, 0, s>>>(a);
+static void launch_split(const AttnArgs& a, int groups, hipStream_t s) {
+  if (a.dtype == EXTERND_F32) k_attention_split<DIM, RT, true><<<groups, 256, 0, s>>>(a);
+  else k_attention_split<DIM, RT, false><<<groups, 256, 0, s>>>(a);
+  if (!a.whole) k_attention_join<DIM, 4 * RT><<<dim3((unsigned)a.s.tokens, (unsigned)a.heads_q), 256, 0, s>>>(a);
 }
 template <int DIM>
-static void launch_split(const AttnArgs& a, int rt, hipStream_t s) {
-  if (rt == 0) {
-    const dim3 grid((unsigned)(a.nsplit * a.c.heads), (unsigned)a.row_blocks, (unsigned)a.s.batch);
-    k_attention_chunk<DIM><<<grid, 512, 0, s>>>(a);
-    if (a.nsplit > 1) k_attention_join<DIM, 256><<<dim3((unsigned)a.s.tokens, (unsigned)a.heads_q), 256, 0, s>>>(a);
-  } else if (rt == 1) launch_split<DIM, 1>(a, s);
-  else if (rt == 2) launch_split<DIM, 2>(a, s);
-  else if constexpr (DIM != 256) launch_split<DIM, 4>(a, s);
+static void launch_split(const AttnArgs& a, const Plan& p, hipStream_t s) {
+  if (p.rt == 0) {
+    if (a.dtype == EXTERND_BF16) k_attention_chunk<DIM, EXTERND_BF16><<<p.groups, 512, 0, s>>>(a);
+    else k_attention_chunk<DIM, EXTERND_F16><<<p.groups, 512, 0, s>>>(a);
+    if (!a.whole) k_attention_join<DIM, 256><<<dim3((unsigned)a.s.tokens, (unsigned)a.heads_q), 256, 0, s>>>(a);
+  } else if (p.rt == 1) launch_split<DIM, 1>(a, p.groups, s);
+  else if (p.rt == 2) launch_split<DIM, 2>(a, p.groups, s);
+  else if constexpr (DIM != 256) launch_split<DIM, 4>(a, p.groups, s);
 }
 
 // Heads, types and counts of an attention call.
@@ -960,9 +1140,15 @@ extern "C" {
 size_t externd_kv4_attention_workspace_bytes(int32_t heads_q, int32_t heads_kv, int32_t head_dim, int32_t dtype,
                                              int64_t tokens, int32_t batch, int32_t max_new, int64_t max_len) {
   if (!attention_sizes_ok(heads_q, heads_kv, head_dim, dtype, tokens, batch, max_new, max_len)) return 0;
-  const SplitPlan p = split_plan(heads_q / heads_kv, heads_kv, head_dim, dtype, batch, max_new, max_len);
-  if (p.nsplit == 1) return 0;
-  return ((size_t)tokens * heads_q * p.nsplit * (head_dim + 4) * 4 + 255) & ~(size_t)255;
+  Plan p;
+  // either form of the call (starts or none) fits
+  size_t most = 0;
+  for (int starts = 0; starts < 2; starts++) {
+    if (!attention_plan(heads_q, heads_kv, head_dim, dtype, tokens, batch, starts, max_new, max_len, &p)) return 0;
+    const size_t n = plan_bytes(p, head_dim);
+    most = n > most ? n : most;
+  }
+  return most;
 }
 
 int externd_kv4_attention(const void* cache, int64_t num_pages, int32_t heads_kv, int32_t head_dim,
@@ -994,15 +1180,18 @@ int externd_kv4_attention(const void* cache, int64_t num_pages, int32_t heads_kv
   a.scale = scale;
   a.window = window;
   a.dtype = dtype;
-  const SplitPlan p = split_plan(a.each, heads_kv, head_dim, dtype, batch, max_new, max_len);
-  a.nsplit = p.nsplit;
-  a.chunk = p.chunk;
-  a.row_blocks = p.row_blocks;
+  a.q_vec = rows_aligned(q, q_token_stride, q_head_stride, dtype_bytes(dtype));
+  Plan p;
+  if (!attention_plan(heads_q, heads_kv, head_dim, dtype, tokens, batch, starts != nullptr, max_new, max_len, &p))
+    return EXTERND_EUNSUPPORTED;
+  a.whole = p.whole;
+  a.blocks = p.blocks;
   a.part = (float*)workspace;
+  a.parts = p.whole ? nullptr : (int2*)(a.part + (size_t)p.groups * 2 * p.rows * (head_dim + 4));
   const hipStream_t s = (hipStream_t)stream;
-  if (head_dim == 64) launch_split<64>(a, p.rt, s);
-  else if (head_dim == 128) launch_split<128>(a, p.rt, s);
-  else launch_split<256>(a, p.rt, s);
+  if (head_dim == 64) launch_split<64>(a, p, s);
+  else if (head_dim == 128) launch_split<128>(a, p, s);
+  else launch_split<256>(a, p, s);
   return hipGetLastError() == hipSuccess ? EXTERND_OK : EXTERND_EHIP;
 }
 
