@@ -12,6 +12,12 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
+// A row block that a workgroup begins and others go on with.
+struct AttnShare {
+  int64_t t0;             // RowBlock's
+  int rows, r0, h, count; // cache head; workgroups (below 2: none to join)
+};
+
 struct AttnArgs {
   const uint8_t* cache;
   Kv4Shape c;
@@ -27,7 +33,7 @@ struct AttnArgs {
   int whole;              // a workgroup per row block and cache head, nothing to join
   int blocks;             // numbers of row blocks (below)
   float* part;            // per workgroup two row blocks' parts; a row: DIM sums, the maximum and the sum of weights, two unused
-  int2* parts;            // per row block and cache head: the first workgroup and the number of them
+  AttnShare* shares;      // per workgroup
 };
 
 __device__ __forceinline__ float load_any(const void* p, int64_t i, int dtype) {
@@ -143,6 +149,7 @@ __device__ __forceinline__ bool walk_begin(const AttnArgs& a, Walk& w) {
     w.end = w.at + n;
     return true;
   }
+  if (tid == 0) a.shares[blockIdx.x].count = 0;      // until walk_turn finds one
   const int each = (a.blocks + NT - 1) / NT, n0 = min(tid * each, a.blocks), n1 = min(n0 + each, a.blocks);
   int64_t mine = 0;
   RowBlock r;
@@ -211,10 +218,10 @@ __device__ __forceinline__ Turn walk_turn(const AttnArgs& a, const Walk& w) {
   u.tile1 = (int)min((int64_t)n, u.tile0 + (w.end - w.at));
   const bool whole = u.tile0 == 0 && u.tile1 == n;
   u.part = whole ? nullptr : a.part + ((int64_t)(2 * blockIdx.x + (u.tile0 == 0)) * ROWS) * (DIM + 4);
-  if (!a.whole && u.tile0 == 0 && threadIdx.x == 0) {
+  if (!whole && u.tile0 == 0 && threadIdx.x == 0) {
     const int64_t last = w.base + (int64_t)u.h * n + n - 1;
-    const int count = whole ? 1 : (int)(((last + 1) * w.groups - 1) / w.total) - (int)blockIdx.x + 1;
-    a.parts[(w.R.t0 * a.each + w.R.r0) * a.c.heads + u.h] = make_int2((int)blockIdx.x, count);
+    const int count = (int)(((last + 1) * w.groups - 1) / w.total) - (int)blockIdx.x + 1;
+    a.shares[blockIdx.x] = {w.R.t0, w.R.rows, w.R.r0, u.h, count};
   }
   return u;
 }
@@ -666,9 +673,10 @@ __global__ __launch_bounds__(512, 2) void k_attention_chunk(AttnArgs a) {
   constexpr int NS = TT / 32, KS = DIM / 16, PS = TT / 16, CT = DIM / 32;
   constexpr int KU = DIM / 8, VU = TT / 8;          // 16-byte units of a row of K (a token) and of V (a channel)
   constexpr int WB = 8 / PS;                        // waves of a 16-token block
-  __shared__ __align__(16) _Float16 kt[2][TT * DIM], vt[2][DIM * TT];
-  __shared__ __align__(8) uint8_t flags[2][8];      // of each wave's 8 values' tokens: 1 there, 3 some NaN among them
-  __shared__ uint16_t nans[2][8][NG];               // which of the block's tokens
+  constexpr int AHEAD = 4;
+  __shared__ __align__(16) _Float16 kt[3][TT * DIM], vt[3][DIM * TT];
+  __shared__ __align__(8) uint8_t flags[3][8];      // of each wave's 8 values' tokens: 1 there, 3 some NaN among them
+  __shared__ uint16_t nans[3][8][NG];               // which of the block's tokens
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, half = lane >> 5;
   const int P = 1 << a.c.page_log2;
   const int block = wave / WB;                      // the 16-token block of a tile that this wave converts
@@ -703,50 +711,56 @@ __global__ __launch_bounds__(512, 2) void k_attention_chunk(AttnArgs a) {
     f16x8 Q[KS];
     float factor;
     {
-      float x[KS][8], top = 0.f;
-      bool bad = false;
+      v4u raw[KS];
       const T* q = (const T*)a.q + (R.t0 + min(row, R.rows - 1) / a.each) * a.q_ts + (h * a.each + row % a.each) * a.q_hs + half * 8;
-      if (a.q_vec)
 #pragma unroll
-        for (int k = 0; k < KS; k++) load_n<DT, 8, true>(q + k * 16, x[k]);
-      else
+      for (int k = 0; k < KS; k++) {
+        if (a.q_vec) raw[k] = *(const v4u*)(q + k * 16);
+        else {
+          const uint16_t* u = (const uint16_t*)(q + k * 16);
 #pragma unroll
-        for (int k = 0; k < KS; k++) load_n<DT, 8, false>(q + k * 16, x[k]);
+          for (int i = 0; i < 4; i++) raw[k][i] = (unsigned)u[2 * i] | (unsigned)u[2 * i + 1] << 16;
+        }
+      }
+      float top = 0.f;
+      bool bad = false;
 #pragma unroll
-      for (int k = 0; k < KS; k++)
+      for (int k = 0; k < KS; k++) {
+        float x[8];
+        Vec<DT>::unpack(raw[k], x);
 #pragma unroll
         for (int j = 0; j < 8; j++) {
-          bad |= !__builtin_isfinite(x[k][j]);
-          top = fmaxf(top, fabsf(x[k][j]));
+          bad |= !__builtin_isfinite(x[j]);
+          top = fmaxf(top, fabsf(x[j]));
         }
+      }
       top = fmaxf(top, __shfl_xor(top, 32));
       bad |= __shfl_xor((int)bad, 32) != 0;
       int e = 0;
       frexpf(top, &e);                  // top < 2^e
       const float sign = a.scale < 0.f ? -1.f : 1.f;
 #pragma unroll
-      for (int k = 0; k < KS; k++)
+      for (int k = 0; k < KS; k++) {
+        constexpr int order[8] = {0, 2, 1, 3, 4, 6, 5, 7};      // as two codes come out of one mask
+        float x[8];
+        Vec<DT>::unpack(raw[k], x);
 #pragma unroll
-        for (int j = 0; j < 8; j++) {
-          constexpr int order[8] = {0, 2, 1, 3, 4, 6, 5, 7};      // as two codes come out of one mask
-          Q[k][j] = (_Float16)(bad ? 0.f : ldexpf(sign * x[k][order[j]], 15 - e));
-        }
+        for (int j = 0; j < 8; j++) Q[k][j] = (_Float16)(bad ? 0.f : ldexpf(sign * x[order[j]], 15 - e));
+      }
       // above 0, so that a masked score of -infinity stays one
       factor = bad ? NAN : fmaxf(ldexpf(fabsf(a.scale) * 1.44269504088896340736f, e - 15), 1.17549435e-38f);
     }
     const int pos = R.first + row / a.each;
     const int last = row < R.rows ? min(pos, c1 - 1) : -1;
     const int least = a.window > 0 ? pos - a.window + 1 : 0;
-    // over the wave: where every row sees every token, and past which none does
-    int all_from = row < R.rows ? least : INT_MIN, all_to = row < R.rows ? last : INT_MAX, none_from = last;
+    // over the wave: where every row sees every token
+    int all_from = row < R.rows ? least : INT_MIN, all_to = row < R.rows ? last : INT_MAX;
     for (int d = 16; d; d >>= 1) {
       all_from = max(all_from, __shfl_xor(all_from, d));
       all_to = min(all_to, __shfl_xor(all_to, d));
-      none_from = max(none_from, __shfl_xor(none_from, d));
     }
     all_from = __builtin_amdgcn_readfirstlane(all_from);
     all_to = __builtin_amdgcn_readfirstlane(all_to);
-    none_from = __builtin_amdgcn_readfirstlane(none_from);
 
     f32x16 O[CT];
 #pragma unroll
@@ -758,87 +772,120 @@ __global__ __launch_bounds__(512, 2) void k_attention_chunk(AttnArgs a) {
     for (int g = 0; g < NG; g++) poison[g] = 0.f;
 
     const int ntiles = (c1 - c0 + TT - 1) / TT;
-    v2u kraw;
-    unsigned vraw[2], kword[(NG + 1) / 2], vword[(NG + 1) / 2];      // vword: of the token that lane % 8 stands for
+    struct KRaw {
+      v2u codes;
+      unsigned words[(NG + 1) / 2];
+    };
+    struct VRaw {
+      unsigned codes[2], words[(NG + 1) / 2];      // words: of the token that lane % 8 stands for
+    };
     const int vtok = 4 * vhalf + (lane & 3) + (lane & 4) * 2;
-    int page_now = -1;       // of the loaded tile's block
     // table entry of this wave's block of a tile; only read here, so that nothing waits for it yet
     auto entry = [&](int tile) -> int {
       const unsigned tok = min((unsigned)c0 + (unsigned)(tile * TT + block * 16), (unsigned)(c1 - 1));
       return a.s.table[(int64_t)b * a.s.table_pages + (tok >> a.c.page_log2)];
     };
-    // always all loads, past the part's end from page 0: their number in flight is known where they are waited for
-    auto load = [&](int tile, int page) {
+    // where the block is; no page (past the part's end as well): page 0, so that all loads are always issued and their
+    // number in flight is known where they are waited for
+    struct Place {
+      const uint8_t* base;
+      bool there;
+    };
+    const int64_t page_bytes = a.c.heads * a.c.head_bytes;
+    const uint8_t* const head_base = a.cache + h * a.c.head_bytes;
+    auto place_at = [&](int tile, int page) -> Place {
       page = __builtin_amdgcn_readfirstlane(page);
-      page_now = (unsigned)c0 + (unsigned)(tile * TT + block * 16) < (unsigned)c1 && page >= 0 && page < a.c.num_pages ? page : -1;
-      const uint8_t* base = a.cache + ((int64_t)max(page_now, 0) * a.c.heads + h) * a.c.head_bytes;
-      const int o = (c0 + tile * TT + block * 16) & (P - 1);      // the block's place in its page
-      const uint8_t* words = base + (unsigned)P * DIM;
-      const int kt0 = o + (ktok & 15);
-      kraw = *(const v2u*)(base + kt0 * HALF + kunit * 8);
+      const bool there = (unsigned)c0 + (unsigned)(tile * TT + block * 16) < (unsigned)c1 && (unsigned)page < (unsigned)a.c.num_pages;
+      return {head_base + (there ? page : 0) * page_bytes, there};
+    };
+    auto load_k = [&](KRaw& r, int tile, const Place& pl) {
+      const uint8_t* base = pl.base;
+      const int t = ((c0 + tile * TT + block * 16) & (P - 1)) + (ktok & 15);
+      r.codes = *(const v2u*)(base + t * HALF + kunit * 8);
 #pragma unroll
-      for (int g = 0; g < (NG + 1) / 2; g++) kword[g] = ((const unsigned*)(words + kt0 * (4 * NG)))[g];
+      for (int g = 0; g < (NG + 1) / 2; g++) r.words[g] = ((const unsigned*)(base + (unsigned)P * DIM + t * (4 * NG)))[g];
+    };
+    auto load_v = [&](VRaw& r, int tile, const Place& pl) {
+      const uint8_t* base = pl.base;
+      const int o = (c0 + tile * TT + block * 16) & (P - 1);
       const unsigned* vp = (const unsigned*)(base + (unsigned)P * HALF + (o >> 4) * (HALF * 16) + (vin ? vcol : 0) * 16);
-      vraw[0] = vp[vhalf];
-      vraw[1] = vp[2 + vhalf];
-      const unsigned* w = (const unsigned*)(words + (o + vtok) * (4 * NG));
+      r.codes[0] = vp[vhalf];
+      r.codes[1] = vp[2 + vhalf];
+      const unsigned* w = (const unsigned*)(base + (unsigned)P * DIM + (o + vtok) * (4 * NG));
 #pragma unroll
-      for (int g = 0; g < (NG + 1) / 2; g++) vword[g] = NG == 1 ? w[0] >> 16 : w[NG / 2 + g];
+      for (int g = 0; g < (NG + 1) / 2; g++) r.words[g] = NG == 1 ? w[0] >> 16 : w[NG / 2 + g];
     };
     // one dword of codes to four pairs of values: bytes (0, 2), (1, 3) of the low nibbles, then of the high ones
-    auto pair = [](unsigned w, unsigned minus, unsigned scale) -> unsigned {
-      const f16x2 c = __builtin_bit_cast(f16x2, (w & 0x000F000Fu) | 0x64006400u);
+    unsigned magic = 0x64006400u;      // in a register: mask and magic are one operation then
+    asm("" : "+v"(magic));
+    auto pair = [&](unsigned w, unsigned minus, unsigned scale) -> unsigned {
+      const f16x2 c = __builtin_bit_cast(f16x2, (w & 0x000F000Fu) | magic);
       return __builtin_bit_cast(unsigned, (c + __builtin_bit_cast(f16x2, minus)) * __builtin_bit_cast(f16x2, scale));
     };
-    auto convert = [&](int buf, int tile) {
-      {
+    auto convert_k = [&](int buf, const KRaw& raw) {
         // K: the low nibbles are unit kunit, the high ones unit kunit + KU / 2
         unsigned out[2][4];
 #pragma unroll
         for (int s = 0; s < 2; s++) {
           // groups of byte column 8 kunit: below D / 2, and D / 2 further
           const int g = DIM == 256 ? 2 * s : DIM == 128 ? s : 0;
-          unsigned w = DIM == 256 ? kword[s] : kword[0];
+          unsigned w = DIM == 256 ? raw.words[s] : raw.words[0];
           w = DIM == 256 ? (kunit >= 8 ? w >> 16 : w & 0xFFFFu) : g & 1 ? w >> 16 : w & 0xFFFFu;
           w |= w << 16;
           const unsigned scale = w & 0xFFF0FFF0u, minus = (w & 0x000F000Fu) | 0xE400E400u;
 #pragma unroll
           for (int j = 0; j < 2; j++) {
-            out[s][2 * j] = pair(kraw[j] >> (4 * s), minus, scale);
-            out[s][2 * j + 1] = pair(kraw[j] >> (4 * s + 8), minus, scale);
+            out[s][2 * j] = pair(raw.codes[j] >> (4 * s), minus, scale);
+            out[s][2 * j + 1] = pair(raw.codes[j] >> (4 * s + 8), minus, scale);
           }
         }
         if (vin) {
           *(v4u*)&kt[buf][kat(ktok, kunit)] = v4u{out[0][0], out[0][1], out[0][2], out[0][3]};
           *(v4u*)&kt[buf][kat(ktok, kunit + KU / 2)] = v4u{out[1][0], out[1][1], out[1][2], out[1][3]};
         }
-      }
-      {
+    };
+    auto convert_v = [&](int buf, int tile, bool there, const VRaw& raw) {
         // V: words of tokens that are not there count as 0, NaN ones too (kept as bits)
-        const bool in = page_now >= 0 && c0 + tile * TT + block * 16 + vtok < c1;
-        unsigned mask[NG], flag = page_now >= 0 ? 1 : 0, word[8][(NG + 1) / 2];
+        const bool in = there && c0 + tile * TT + block * 16 + vtok < c1;
+        unsigned flag = there, bad[(NG + 1) / 2], scale[NG][4], minus[NG][4];
 #pragma unroll
         for (int g = 0; g < (NG + 1) / 2; g++) {
-          unsigned w = in ? vword[g] : 0u;
+          unsigned w = in ? raw.words[g] : 0u;
           const bool lo = (w & 0x7C00u) == 0x7C00u, hi = NG > 1 && (w & 0x7C000000u) == 0x7C000000u;
-          mask[2 * g] = (unsigned)__ballot(lo) & 0xFF;
-          if (NG > 1) mask[NG > 1 ? 2 * g + 1 : 0] = (unsigned)__ballot(hi) & 0xFF;
-          w &= (lo ? 0xFFFF0000u : ~0u) & (hi ? 0xFFFFu : ~0u);
+          bad[g] = 0;
+          if (__any(lo || hi)) {
+            bad[g] = (unsigned)(__ballot(lo) & 0xFF) | (unsigned)(__ballot(hi) & 0xFF) << 8;
+            w &= (lo ? 0xFFFF0000u : ~0u) & (hi ? 0xFFFFu : ~0u);
+            flag = 3;
+          }
+          // tokens j and j + 2 side by side, one word per group, in the lanes of j = 0, 1, 4, 5
+          const unsigned w2 = dppu<0xEE>(w);
+          const unsigned p0 = __builtin_amdgcn_perm(w2, w, 0x05040100u), p1 = __builtin_amdgcn_perm(w2, w, 0x07060302u);
+          const unsigned s0 = p0 & 0xFFF0FFF0u, s1 = p1 & 0xFFF0FFF0u;
+          const unsigned m0 = (p0 & 0x000F000Fu) | 0xE400E400u, m1 = (p1 & 0x000F000Fu) | 0xE400E400u;
 #pragma unroll
-          for (int j = 0; j < 8; j++) word[j][g] = __builtin_amdgcn_readlane(w, j);
+          for (int j = 0; j < 4; j++) {
+            const int at = (j >> 1) * 4 + (j & 1);
+            scale[2 * g][j] = __builtin_amdgcn_readlane(s0, at);
+            minus[2 * g][j] = __builtin_amdgcn_readlane(m0, at);
+            if (NG > 1) {
+              scale[NG > 1 ? 2 * g + 1 : 0][j] = __builtin_amdgcn_readlane(s1, at);
+              minus[NG > 1 ? 2 * g + 1 : 0][j] = __builtin_amdgcn_readlane(m1, at);
+            }
+          }
         }
         unsigned out[2][4];
 #pragma unroll
         for (int s = 0; s < 2; s++) {
-          const int wi = DIM == 256 ? s : 0;
-          const bool top = DIM == 256 ? wave & 1 : DIM == 128 ? s == 1 : false;      // group's half of the word
+          // the column's group: below D / 2, and D / 2 further
+          const int g0 = DIM == 256 ? 2 * s : DIM == 128 ? s : 0, g1 = DIM == 256 ? 2 * s + 1 : g0;
 #pragma unroll
           for (int j = 0; j < 2; j++)
 #pragma unroll
             for (int q = 0; q < 2; q++) {
-              const unsigned w0 = word[4 * j + q][wi], w1 = word[4 * j + q + 2][wi];
-              const unsigned w = top ? (w0 >> 16) | (w1 & 0xFFFF0000u) : (w0 & 0xFFFFu) | (w1 << 16);
-              out[s][2 * j + q] = pair(vraw[j] >> (4 * s + 8 * q), (w & 0x000F000Fu) | 0xE400E400u, w & 0xFFF0FFF0u);
+              const unsigned sc = DIM == 256 && (wave & 1) ? scale[g1][2 * j + q] : scale[g0][2 * j + q];
+              const unsigned mi = DIM == 256 && (wave & 1) ? minus[g1][2 * j + q] : minus[g0][2 * j + q];
+              out[s][2 * j + q] = pair(raw.codes[j] >> (4 * s + 8 * q), mi, sc);
             }
         }
         const int u = block * 2 + vhalf;
@@ -846,35 +893,44 @@ __global__ __launch_bounds__(512, 2) void k_attention_chunk(AttnArgs a) {
           *(v4u*)&vt[buf][vat(vcol, u)] = v4u{out[0][0], out[0][1], out[0][2], out[0][3]};
           *(v4u*)&vt[buf][vat(HALF + vcol, u)] = v4u{out[1][0], out[1][1], out[1][2], out[1][3]};
         }
-#pragma unroll
-        for (int g = 0; g < NG; g++)
-          if (mask[g]) flag |= 2;
         if (lane == 0) flags[buf][wave] = (uint8_t)flag;
         if (flag & 2 && lane < NG) {
-          unsigned m = mask[0];
+          unsigned m = bad[0];
 #pragma unroll
-          for (int g = 1; g < NG; g++) m = lane == g ? mask[g] : m;
+          for (int g = 1; g < (NG + 1) / 2; g++) m = lane >> 1 == g ? bad[g] : m;
+          m = m >> (8 * (lane & 1)) & 0xFF;
           nans[buf][wave][lane] = (uint16_t)((m & 15) << (4 * vhalf) | (m >> 4) << (8 + 4 * vhalf));
+        }
+    };
+
+    f32x16 S[NS];
+    f16x8 B[PS];
+    // The matrix products of a step: the last tile's weights times its values, and this tile's scores.
+    auto values = [&](const _Float16* vb) {
+#pragma unroll
+      for (int k = 0; k < PS; k++)
+#pragma unroll
+        for (int c = 0; c < CT; c++) {
+          const f16x8 A = *(const f16x8*)&vb[vat(c * 32 + l32, 2 * k + half)];
+          O[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(A, B[k], O[c], 0, 0, 0);
+        }
+    };
+    auto scores = [&](const _Float16* kb) {
+#pragma unroll
+      for (int s = 0; s < NS; s++) {
+        const f32x16 zero = {};
+#pragma unroll
+        for (int k = 0; k < KS; k++) {
+          const f16x8 A = *(const f16x8*)&kb[kat(s * 32 + l32, 2 * k + half)];
+          S[s] = __builtin_amdgcn_mfma_f32_32x32x16_f16(A, Q[k], k ? S[s] : zero, 0, 0, 0);
         }
       }
     };
-
-    auto compute = [&](int buf, int tile) {
+    // This tile's scores to weights.
+    auto weights = [&](int buf, int tile) {
       const int tok0 = c0 + tile * TT;
-      if (tok0 > none_from) return;
       const v2u fl = *(const v2u*)flags[buf];
       const unsigned f0 = __builtin_amdgcn_readfirstlane(fl[0]), f1 = __builtin_amdgcn_readfirstlane(fl[1]);
-      f32x16 S[NS];
-#pragma unroll
-      for (int s = 0; s < NS; s++) {
-#pragma unroll
-        for (int i = 0; i < 16; i++) S[s][i] = 0.f;
-#pragma unroll
-        for (int k = 0; k < KS; k++) {
-          const f16x8 A = *(const f16x8*)&kt[buf][kat(s * 32 + l32, 2 * k + half)];
-          S[s] = __builtin_amdgcn_mfma_f32_32x32x16_f16(A, Q[k], S[s], 0, 0, 0);
-        }
-      }
       if (f0 != 0x01010101u || f1 != 0x01010101u || tok0 < all_from || tok0 + TT - 1 > all_to) {
         // the tile's tokens that this lane's row sees, a bit each
         const int from = max(least - tok0, 0), to = min(last - tok0, TT - 1);
@@ -919,7 +975,6 @@ __global__ __launch_bounds__(512, 2) void k_attention_chunk(AttnArgs a) {
           for (int i = 0; i < 16; i++) O[c][i] *= keep;
       }
       const float at = ref == -INFINITY ? 0.f : ref;
-      f16x8 B[PS];
       float sum[2] = {0.f, 0.f};
 #pragma unroll
       for (int s = 0; s < NS; s++)
@@ -939,34 +994,65 @@ __global__ __launch_bounds__(512, 2) void k_attention_chunk(AttnArgs a) {
         }
       }
       l += sum[0] + sum[1];
-#pragma unroll
-      for (int k = 0; k < PS; k++)
-#pragma unroll
-        for (int c = 0; c < CT; c++) {
-          const f16x8 A = *(const f16x8*)&vt[buf][vat(c * 32 + l32, 2 * k + half)];
-          O[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(A, B[k], O[c], 0, 0, 0);
-        }
+      __builtin_amdgcn_sched_barrier(0);      // the sums here, not beside the products: their registers
     };
 
-    int e0 = entry(0), e1 = entry(1), e2 = entry(2);
-    load(0, e0);
-    convert(0, 0);
-    load(1, e1);
-    __syncthreads();
-    // by two: no register is copied, and its load waited for, at the loop's end
-    for (int tile = 0; tile < ntiles; tile += 2) {
-      e1 = entry(tile + 3);
-      convert(1, tile + 1);
-      load(tile + 2, e2);
-      compute(0, tile);
-      __syncthreads();
-      if (tile + 1 >= ntiles) break;
-      e2 = entry(tile + 4);
-      convert(0, tile + 2);
-      load(tile + 3, e1);
-      compute(1, tile + 1);
-      __syncthreads();
+    // Two groups of four waves, one of each on a SIMD, half a step apart: while one runs its products, the other
+    // turns scores into weights and converts a later tile (K two tiles ahead, V one, in three buffers each).
+    KRaw kr;
+    VRaw vr;
+    int e1 = entry(1), e2 = entry(2), e = entry(0);
+    const Place first = place_at(0, e);
+    load_k(kr, 0, first);
+    load_v(vr, 0, first);
+    e = entry(3);
+    Place vplace = place_at(1, e1), kplace = place_at(2, e2);
+    {
+      KRaw k1;
+      load_k(k1, 1, vplace);
+      convert_k(0, kr);
+      convert_v(0, 0, first.there, vr);
+      load_v(vr, 1, vplace);
+      load_k(kr, 2, kplace);
+      convert_k(1, k1);
     }
+    __syncthreads();
+    if (wave >= 4) __syncthreads();
+    int b0 = 0, b1 = 1, b2 = 2;      // buffers of tiles n, n + 1, n + 2 (and n - 1)
+    scores(kt[0]);
+    for (int n = 0;; n++) {
+      __builtin_amdgcn_s_setprio(0);
+      __syncthreads();
+      weights(b0, n);
+      convert_k(b2, kr);
+      convert_v(b1, n + 1, vplace.there, vr);
+      __builtin_amdgcn_sched_barrier(0);      // into the registers that these have left
+      load_v(vr, n + 2, kplace);
+      vplace = kplace;
+      kplace = place_at(n + 3, e);
+      load_k(kr, n + 3, kplace);
+      e = entry(n + 4);
+      __syncthreads();
+      __builtin_amdgcn_s_setprio(1);
+      values(vt[b0]);
+      scores(kt[b1]);      // of no tile after the last one: not used then
+      // LDS operands AHEAD products ahead
+      __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
+#pragma unroll
+      for (int i = 0; i < PS * CT + NS * KS - AHEAD; i++) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, 0);
+      if (n + 1 >= ntiles) break;
+      const int b = b0;
+      b0 = b1;
+      b1 = b2;
+      b2 = b;
+    }
+    __builtin_amdgcn_s_setprio(0);
+    if (wave < 4) __syncthreads();
+    __syncthreads();      // the next row block's tiles may be written
 
     const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
     l = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
@@ -1004,64 +1090,136 @@ __global__ __launch_bounds__(512, 2) void k_attention_chunk(AttnArgs a) {
   }
 }
 
-// Joins the parts of a row: one workgroup per new token and query head, four
-// channels a thread and 1024 / DIM parts side by side.
-constexpr int MAX_GROUPS = 768;      // workgroups of a launch that are joined
+// Joins the parts of the row blocks that several workgroups share: a row's four
+// channels a thread, and SL threads of every SL-th part each for a row of more
+// than four parts, joined in LDS.  An item is as many rows as 256 threads hold;
+// each workgroup finds all row blocks that have parts and takes its stretch of
+// their items, since a workgroup for every possible one costs more than the
+// join itself (8192 of them take 20 us to end at once).
+constexpr int MAX_GROUPS = 768;
 template <int DIM, int ROWS>
-__global__ __launch_bounds__(256) void k_attention_join(AttnArgs a) {
-  constexpr int TH = DIM / 4, GR = 256 / TH;
-  __shared__ float weight[MAX_GROUPS], red[8];
+__global__ __launch_bounds__(256) void k_attention_join(AttnArgs a, int groups) {
+  constexpr int TH = DIM / 4, GR = 256 / TH, B = 4, EACH = MAX_GROUPS / 256;
+  __shared__ int ends[MAX_GROUPS], waves[4];
   __shared__ f32x4 acc[GR][TH];
-  const int64_t t = blockIdx.x;
-  const int hq = blockIdx.y, tid = threadIdx.x;
-  const int64_t t0 = a.s.starts ? a.s.starts[sequence_of(a.s, t)] : t;
-  const int row = (int)(t - t0) * a.each + hq % a.each;
-  if (t0 < 0 || row < 0) return;
-  const int2 parts = a.parts[(t0 * a.each + row / ROWS * ROWS) * a.c.heads + hq / a.each];
-  const int n = min(parts.y, MAX_GROUPS);
-  if (n < 2) return;      // written by the kernel before
-  // a row block's first part is its workgroup's last, its others their workgroups' first
-  const auto part = [&](int p) {
-    return a.part + ((int64_t)(p ? 2 * (parts.x + p) : 2 * parts.x + 1) * ROWS + row % ROWS) * (DIM + 4);
+  __shared__ float tops[GR], sums[GR];
+  const int tid = threadIdx.x, g = tid / TH, c = tid % TH;
+  const auto slices = [](int n) {
+    int s = 1;
+    while (s < GR && 4 * s < n) s *= 2;
+    return s;
   };
-  float top = -INFINITY;
-  for (int p = tid; p < n; p += 256) {
-    weight[p] = part(p)[DIM];
-    top = fmaxf(top, weight[p]);
-  }
-  for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-  if ((tid & 63) == 0) red[tid >> 6] = top;
-  __syncthreads();
-  top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-  const float at = top == -INFINITY ? 0.f : top;
-  float sum = 0.f;
-  for (int p = tid; p < n; p += 256) {
-    weight[p] = __builtin_amdgcn_exp2f(weight[p] - at);
-    sum = fmaf(weight[p], part(p)[DIM + 1], sum);
-  }
-  for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
-  if ((tid & 63) == 0) red[4 + (tid >> 6)] = sum;
-  __syncthreads();
-  sum = (red[4] + red[5]) + (red[6] + red[7]);
-  const int g = tid / TH, c = tid % TH;
-  f32x4 o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-  for (int p = g; p < n; p += GR) {
-    const f32x4 x = *(const f32x4*)(part(p) + 4 * c);
-    const float f = weight[p];
+  int count[EACH], mine = 0;
 #pragma unroll
-    for (int j = 0; j < 4; j++) o[j] = fmaf(x[j], f, o[j]);
+  for (int i = 0; i < EACH; i++) {
+    const int at = tid * EACH + i;
+    count[i] = 0;
+    if (at < groups) {
+      const AttnShare sh = a.shares[at];
+      const int per = GR / slices(sh.count);
+      if (sh.count >= 2) count[i] = (min(ROWS, sh.rows - sh.r0) + per - 1) / per;
+    }
+    mine += count[i];
   }
-  acc[g][c] = o;
+  int to = mine;
+  for (int d = 1; d < 64; d <<= 1) {
+    const int o = __shfl_up(to, d);
+    if ((tid & 63) >= d) to += o;
+  }
+  if ((tid & 63) == 63) waves[tid >> 6] = to;
   __syncthreads();
-  if (tid >= DIM) return;
-  float out = 0.f;
+  int total = 0;
 #pragma unroll
-  for (int i = 0; i < GR; i++) out += acc[i][tid >> 2][tid & 3];
-  const bool none = sum == 0.f;
-  const int64_t to = t * a.heads_q + hq;
-  store_any(a.out, to * DIM + tid, none ? 0.f : out / sum, a.dtype);
-  if (a.lse && tid == 0) a.lse[to] = none ? -INFINITY : (top + log2f(sum)) * 0.69314718055994530942f;
+  for (int i = 0; i < 4; i++) {
+    if (i < tid >> 6) to += waves[i];
+    total += waves[i];
+  }
+  to -= mine;
+#pragma unroll
+  for (int i = 0; i < EACH; i++) ends[tid * EACH + i] = to += count[i];
+  __syncthreads();
+
+  int item = (int)((int64_t)total * blockIdx.x / gridDim.x);
+  const int last = (int)((int64_t)total * (blockIdx.x + 1) / gridDim.x);
+  if (item >= last) return;
+  int first = 0;      // the first row block that ends past `item`
+  for (int hi = groups - 1; first < hi;) {
+    const int mid = (first + hi) >> 1;
+    if (ends[mid] > item) hi = mid; else first = mid + 1;
+  }
+  for (; item < last; item++) {
+    while (ends[first] <= item) first++;
+    const AttnShare sh = a.shares[first];
+    const int n = sh.count, SL = slices(n), per = GR / SL, s = g / per;
+    const int r = (item - (first ? ends[first - 1] : 0)) * per + g % per, row = sh.r0 + r;
+    const bool in = r < ROWS && row < sh.rows;
+    // a row block's first part is its workgroup's last, its others their workgroups' first
+    const auto part = [&](int p) {
+      return a.part + ((int64_t)(p ? 2 * (first + p) : 2 * first + 1) * ROWS + r) * (DIM + 4);
+    };
+    float top = -INFINITY, sum = 0.f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    const auto add = [&](float m, float l, const f32x4& x) {
+      const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+      sum = fmaf(l, f, sum);
+#pragma unroll
+      for (int j = 0; j < 4; j++) o[j] = fmaf(x[j], f, o[j]);
+    };
+    if (in)
+      for (int p0 = s; p0 < n; p0 += B * SL) {
+        f32x4 x[B];
+        float m[B], l[B];
+#pragma unroll
+        for (int i = 0; i < B; i++) {
+          const float* p = part(min(p0 + i * SL, n - 1));
+          m[i] = p[DIM];
+          l[i] = p[DIM + 1];
+          x[i] = *(const f32x4*)(p + 4 * c);
+        }
+        const float was = top;
+#pragma unroll
+        for (int i = 0; i < B; i++)
+          if (p0 + i * SL < n) top = fmaxf(top, m[i]);
+        const float keep = was == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(was - top);
+        if (p0 != s) {
+          sum *= keep;
+#pragma unroll
+          for (int j = 0; j < 4; j++) o[j] *= keep;
+        }
+#pragma unroll
+        for (int i = 0; i < B; i++)
+          if (p0 + i * SL < n) add(m[i], l[i], x[i]);
+      }
+    if (SL > 1) {
+      acc[g][c] = o;
+      if (c == 0) {
+        tops[g] = top;
+        sums[g] = sum;
+      }
+      __syncthreads();
+      if (s == 0) {
+        for (int i = 1; i < SL; i++) top = fmaxf(top, tops[i * per + g]);
+        const f32x4 x = o;
+        const float l = sum;
+        sum = 0.f;
+        o = f32x4{0.f, 0.f, 0.f, 0.f};
+        add(tops[g], l, x);
+        for (int i = 1; i < SL; i++) add(tops[i * per + g], sums[i * per + g], acc[i * per + g][c]);
+      }
+      __syncthreads();      // before the next item's
+    }
+    if (s || !in) continue;
+    const bool none = sum == 0.f;
+    const int64_t at = (sh.t0 + row / a.each) * a.heads_q + sh.h * a.each + row % a.each;
+#pragma unroll
+    for (int j = 0; j < 4; j++) store_any(a.out, at * DIM + 4 * c + j, none ? 0.f : o[j] / sum, a.dtype);
+    if (a.lse && c == 0) a.lse[at] = none ? -INFINITY : (top + log2f(sum)) * 0.69314718055994530942f;
+  }
+}
+template <int DIM, int ROWS>
+static void launch_join(const AttnArgs& a, int groups, hipStream_t s) {
+  const int items = (groups * ROWS + 1024 / DIM - 1) / (1024 / DIM);
+  k_attention_join<DIM, ROWS><<<items < 1024 ? items : 1024, 256, 0, s>>>(a, groups);
 }
 
 // Row tiles of four that a workgroup takes (registers allow two at 256 channels).
@@ -1073,7 +1231,6 @@ constexpr int WHOLE_TILES = 16;
 struct Plan {
   int rt, rows;              // row tiles of k_attention_split (0: k_attention_chunk), rows of a row block
   int whole, blocks, groups; // AttnArgs::whole, ::blocks; workgroups
-  int64_t parts;             // entries of AttnArgs::parts
 };
 // One workgroup per row block and cache head where lengths are short; else as
 // many as are resident at once (three of four waves a CU where 168 registers
@@ -1088,7 +1245,6 @@ static bool attention_plan(int heads_q, int heads_kv, int dim, int dtype, int64_
   const int64_t blocks = starts ? tokens * each / p->rows + batch : (int64_t)batch * ((each + p->rows - 1) / p->rows);
   if (blocks * heads_kv > INT32_MAX) return false;
   p->blocks = (int)blocks;
-  p->parts = tokens * heads_q;
   const int64_t tiles = max_len > 0 ? (max_len + 63) / 64 : 1 << 20;
   p->whole = tiles <= WHOLE_TILES;
   if (p->whole) {
@@ -1102,22 +1258,21 @@ static bool attention_plan(int heads_q, int heads_kv, int dim, int dtype, int64_
 }
 static size_t plan_bytes(const Plan& p, int dim) {
   if (p.whole) return 0;
-  const size_t parts = (size_t)p.groups * 2 * p.rows * (dim + 4) * sizeof(float);
-  return parts + (((size_t)p.parts * sizeof(int2) + 255) & ~(size_t)255);
+  return ((size_t)p.groups * (2 * p.rows * (dim + 4) * sizeof(float) + sizeof(AttnShare)) + 255) & ~(size_t)255;
 }
 
 template <int DIM, int RT>
 static void launch_split(const AttnArgs& a, int groups, hipStream_t s) {
   if (a.dtype == EXTERND_F32) k_attention_split<DIM, RT, true><<<groups, 256, 0, s>>>(a);
   else k_attention_split<DIM, RT, false><<<groups, 256, 0, s>>>(a);
-  if (!a.whole) k_attention_join<DIM, 4 * RT><<<dim3((unsigned)a.s.tokens, (unsigned)a.heads_q), 256, 0, s>>>(a);
+  if (!a.whole) launch_join<DIM, 4 * RT>(a, groups, s);
 }
 template <int DIM>
 static void launch_split(const AttnArgs& a, const Plan& p, hipStream_t s) {
   if (p.rt == 0) {
     if (a.dtype == EXTERND_BF16) k_attention_chunk<DIM, EXTERND_BF16><<<p.groups, 512, 0, s>>>(a);
     else k_attention_chunk<DIM, EXTERND_F16><<<p.groups, 512, 0, s>>>(a);
-    if (!a.whole) k_attention_join<DIM, 256><<<dim3((unsigned)a.s.tokens, (unsigned)a.heads_q), 256, 0, s>>>(a);
+    if (!a.whole) launch_join<DIM, 256>(a, p.groups, s);
   } else if (p.rt == 1) launch_split<DIM, 1>(a, p.groups, s);
   else if (p.rt == 2) launch_split<DIM, 2>(a, p.groups, s);
   else if constexpr (DIM != 256) launch_split<DIM, 4>(a, p.groups, s);
@@ -1187,7 +1342,7 @@ int externd_kv4_attention(const void* cache, int64_t num_pages, int32_t heads_kv
   a.whole = p.whole;
   a.blocks = p.blocks;
   a.part = (float*)workspace;
-  a.parts = p.whole ? nullptr : (int2*)(a.part + (size_t)p.groups * 2 * p.rows * (head_dim + 4));
+  a.shares = p.whole ? nullptr : (AttnShare*)(a.part + (size_t)p.groups * 2 * p.rows * (head_dim + 4));
   const hipStream_t s = (hipStream_t)stream;
   if (head_dim == 64) launch_split<64>(a, p, s);
   else if (head_dim == 128) launch_split<128>(a, p, s);
