@@ -82,7 +82,19 @@ __device__ __forceinline__ RowBlock row_block(const AttnArgs& a, int b, int rb) 
 // by block and cache head by cache head, as long as every other's, so lengths
 // need not be alike; the first and the last row block of a stretch may be
 // shared with neighbours, whose parts are joined by k_attention_join.  A row
-// block that sees nothing counts as one tile.
+// block and head counts as its tiles (one, where it sees nothing) and a few
+// units before them, for what a workgroup does besides tiles; a stretch that
+// would end or begin in those does so at their start.  (With 1, 4, 8, 12 units,
+// 4 rows a block: 128 users of 2000 61, 57, 55, 54 us, 8 of 4000 28, 27, 22, 28.
+// With 1, 4, 6, 10, 256 rows: one prompt of 2048 136, 100, 100, 102 us.)
+template <int ROWS>
+struct Begin {
+  static constexpr int UNITS = ROWS == 256 ? 6 : 8;
+};
+template <int ROWS>
+__device__ __forceinline__ int units_of(const RowBlock& r) {
+  return max(r.tiles, 1) + Begin<ROWS>::UNITS;
+}
 template <int ROWS>
 __device__ __forceinline__ int64_t first_number(const AttnArgs& a, int b) {
   return (int64_t)max(a.s.starts[b], 0) * a.each / ROWS + b;
@@ -109,7 +121,7 @@ __device__ __forceinline__ bool numbered_block(const AttnArgs& a, int number, Ro
 }
 
 struct Walk {
-  int64_t at, end, base, total;      // this workgroup's stretch, where the current row block's tiles begin, all tiles
+  int64_t at, end, base, total;      // this workgroup's stretch, where the current row block's units begin, all units
   int number, b, groups;
   RowBlock R;
 };
@@ -143,7 +155,7 @@ __device__ __forceinline__ bool walk_begin(const AttnArgs& a, Walk& w) {
   if (a.whole) {
     if (!numbered_block<ROWS>(a, blockIdx.x / a.c.heads, &w.R, &w.b)) return false;
     walk_uniform(w);
-    const int n = max(w.R.tiles, 1);
+    const int n = units_of<ROWS>(w.R);
     w.base = 0;
     w.at = (int64_t)(blockIdx.x % a.c.heads) * n;
     w.end = w.at + n;
@@ -155,7 +167,7 @@ __device__ __forceinline__ bool walk_begin(const AttnArgs& a, Walk& w) {
   RowBlock r;
   int b;
   for (int n = n0; n < n1; n++)
-    if (numbered_block<ROWS>(a, n, &r, &b)) mine += (int64_t)max(r.tiles, 1) * a.c.heads;
+    if (numbered_block<ROWS>(a, n, &r, &b)) mine += (int64_t)units_of<ROWS>(r) * a.c.heads;
   int64_t to = mine;      // inclusive sum
   for (int d = 1; d < 64; d <<= 1) {
     const int64_t o = __shfl_up(to, d);
@@ -178,7 +190,7 @@ __device__ __forceinline__ bool walk_begin(const AttnArgs& a, Walk& w) {
     int64_t base = to - mine;
     for (int n = n0; n < n1; n++)
       if (numbered_block<ROWS>(a, n, &r, &b)) {
-        const int64_t size = (int64_t)max(r.tiles, 1) * a.c.heads;
+        const int64_t size = (int64_t)units_of<ROWS>(r) * a.c.heads;
         if (w.at < base + size) {
           found = n;
           found_base = base;
@@ -190,19 +202,10 @@ __device__ __forceinline__ bool walk_begin(const AttnArgs& a, Walk& w) {
   __syncthreads();
   w.base = uniform64(found_base);
   walk_to<ROWS>(a, w, __builtin_amdgcn_readfirstlane(found));
-  return true;
-}
-// Past `done` tiles; false at the stretch's end.
-template <int ROWS>
-__device__ __forceinline__ bool walk_on(const AttnArgs& a, Walk& w, int done) {
-  w.at += done;
-  if (w.at >= w.end) return false;
-  const int64_t size = (int64_t)max(w.R.tiles, 1) * a.c.heads;
-  if (w.at == w.base + size) {
-    w.base = w.at;
-    walk_to<ROWS>(a, w, w.number + 1);
-  }
-  return true;
+  const int n = units_of<ROWS>(w.R), off = (int)((w.at - w.base) % n);
+  if (off > Begin<ROWS>::UNITS) return true;
+  w.at -= off;
+  return w.end - w.at > Begin<ROWS>::UNITS;
 }
 // The row block's tiles of this turn: cache head, first and last tile, and where its part goes (null: it is whole).
 struct Turn {
@@ -212,11 +215,12 @@ struct Turn {
 template <int ROWS, int DIM>
 __device__ __forceinline__ Turn walk_turn(const AttnArgs& a, const Walk& w) {
   Turn u;
-  const int n = max(w.R.tiles, 1), off = (int)(w.at - w.base);
+  const int n = units_of<ROWS>(w.R), off = (int)(w.at - w.base), tiles = n - Begin<ROWS>::UNITS;
   u.h = off / n;
-  u.tile0 = off - u.h * n;
-  u.tile1 = (int)min((int64_t)n, u.tile0 + (w.end - w.at));
-  const bool whole = u.tile0 == 0 && u.tile1 == n;
+  const int from = off - u.h * n;
+  u.tile0 = from ? from - Begin<ROWS>::UNITS : 0;
+  u.tile1 = (int)min((int64_t)tiles, from + (w.end - w.at) - Begin<ROWS>::UNITS);
+  const bool whole = u.tile0 == 0 && u.tile1 == tiles;
   u.part = whole ? nullptr : a.part + ((int64_t)(2 * blockIdx.x + (u.tile0 == 0)) * ROWS) * (DIM + 4);
   if (!whole && u.tile0 == 0 && threadIdx.x == 0) {
     const int64_t last = w.base + (int64_t)u.h * n + n - 1;
@@ -224,6 +228,18 @@ __device__ __forceinline__ Turn walk_turn(const AttnArgs& a, const Walk& w) {
     a.shares[blockIdx.x] = {w.R.t0, w.R.rows, w.R.r0, u.h, count};
   }
   return u;
+}
+// To the next turn; false at the stretch's end.
+template <int ROWS>
+__device__ __forceinline__ bool walk_on(const AttnArgs& a, Walk& w, const Turn& u) {
+  const int n = units_of<ROWS>(w.R);
+  w.at = w.base + (int64_t)(u.h + 1) * n;
+  if (w.end - w.at <= Begin<ROWS>::UNITS) return false;
+  if (u.h + 1 == a.c.heads) {
+    w.base = w.at;
+    walk_to<ROWS>(a, w, w.number + 1);
+  }
+  return true;
 }
 
 template <int CTRL>
@@ -255,7 +271,7 @@ __device__ __forceinline__ float scale_of(unsigned word) {
 // Four signed base-256 digits of a whole number below 2^31 - 2^23, lowest first.
 __device__ __forceinline__ unsigned digits_of(int u) { return ((unsigned)u + 0x00808080u) ^ 0x00808080u; }
 
-// Attention of up to 4 RT rows over one part of a sequence, by integer matrix
+// Attention of up to four rows over one part of a sequence, by integer matrix
 // products.  The codes are whole numbers already; a query row enters as 31-bit
 // whole numbers (of its largest entry) in four base-256 digits, and so do the
 // softmax weights times the values' scales, 64 tokens at a time.  So
@@ -271,14 +287,14 @@ __device__ __forceinline__ unsigned digits_of(int u) { return ((unsigned)u + 0x0
 //
 // Four waves share a part; each takes every fourth tile of 64 tokens with its
 // own running maximum, and they are joined at the end.
-template <int DIM, int RT, bool FINE>
-__global__ __launch_bounds__(256, DIM * RT <= 128 ? 3 : 2) void k_attention_split(AttnArgs a) {
-  constexpr int NG = DIM / KV4_GROUP, HALF = DIM / 2, ROWS = 4 * RT;
+template <int DIM, bool FINE>
+__global__ __launch_bounds__(256, DIM <= 128 ? 3 : 2) void k_attention_split(AttnArgs a) {
+  constexpr int NG = DIM / KV4_GROUP, HALF = DIM / 2, ROWS = 4;
   constexpr int NU = DIM == 256 ? 2 : 1;     // 16-byte K loads of a lane and token
   constexpr int NC = DIM / 32;               // 16-byte V loads of a lane: 16 byte columns each
   constexpr int QROW = 80, PROW = 80;        // bytes of a digit row of 64 in LDS (padded against bank conflicts)
   constexpr int ACC = DIM + 4;               // floats of a row when waves join
-  constexpr int SHARED_Q = RT * NG * 16 * QROW, SHARED_P = 4 * NG * (16 * PROW + 64), SHARED_O = 4 * ROWS * ACC * 4;
+  constexpr int SHARED_Q = NG * 16 * QROW, SHARED_P = 4 * NG * (16 * PROW + 64), SHARED_O = 4 * ROWS * ACC * 4;
   constexpr int SHARED = SHARED_Q + SHARED_P > SHARED_O ? SHARED_Q + SHARED_P : SHARED_O;
   __shared__ __align__(16) uint8_t lds[SHARED];
   __shared__ float row_factor[ROWS];
@@ -300,7 +316,7 @@ __global__ __launch_bounds__(256, DIM * RT <= 128 ? 3 : 2) void k_attention_spli
         store_any(a.out, o * DIM + i % DIM, 0.f, a.dtype);
         if (a.lse && i % DIM == 0) a.lse[o] = -INFINITY;
       }
-      if (!walk_on<ROWS>(a, W, 1)) return;
+      if (!walk_on<ROWS>(a, W, turn)) return;
       continue;
     }
     const int c0 = R.lo + 64 * turn.tile0, c1 = (int)min((int64_t)R.hi, (int64_t)R.lo + 64 * (int64_t)turn.tile1);
@@ -377,8 +393,8 @@ __global__ __launch_bounds__(256, DIM * RT <= 128 ? 3 : 2) void k_attention_spli
     }
 
     // ---- the rows' digits, one wave per row ----
-    for (int r = wave; r < ROWS; r += 4) {
-      const int row = R.r0 + r;
+    {
+      const int r = wave, row = R.r0 + r;
       float x[NG], top = 0.f;
       bool bad = false;
 #pragma unroll
@@ -401,7 +417,7 @@ __global__ __launch_bounds__(256, DIM * RT <= 128 ? 3 : 2) void k_attention_spli
         const unsigned dg = digits_of(u);
         // channel 64 g + lane: its group's slot (the byte's place in a lane's K load)
         const int slot = DIM == 64 ? ((lane & 31) >> 3) * 16 + (lane >> 5) * 8 + (lane & 7) : lane;
-        uint8_t* to = lds + (((r >> 2) * NG + g) * 16 + (r & 3) * 4) * QROW + slot;
+        uint8_t* to = lds + (g * 16 + r * 4) * QROW + slot;
         int hi = 0, lo = 0;
 #pragma unroll
         for (int d = 0; d < 4; d++) {
@@ -422,35 +438,29 @@ __global__ __launch_bounds__(256, DIM * RT <= 128 ? 3 : 2) void k_attention_spli
       if (lane == 0) row_factor[r] = bad ? NAN : ldexpf(a.scale * 1.44269504088896340736f, e - 30);
     }
     __syncthreads();
-    v4i Q[RT][NG];
-    float factor[RT], m[RT], l[RT];
-    int qhi[RT][NG], qlo[RT][NG], last[RT], least[RT];
-    float O[RT][2 * NC], poison[RT][NG];
+    v4i Q[NG];
+    int qhi[NG], qlo[NG];
+    float O[2 * NC], poison[NG];
 #pragma unroll
-    for (int p = 0; p < RT; p++) {
-      const int r = p * 4 + seg, row = R.r0 + r;
-#pragma unroll
-      for (int g = 0; g < NG; g++) {
-        Q[p][g] = *(const v4i*)(lds + ((p * NG + g) * 16 + l16) * QROW + seg * 16);
-        qhi[p][g] = -row_sums[r][g][0];
-        qlo[p][g] = -row_sums[r][g][1];
-        poison[p][g] = 0.f;
-      }
-      factor[p] = row_factor[r];
-      m[p] = -INFINITY;
-      l[p] = 0.f;
-      const int pos = R.first + row / a.each;
-      last[p] = row < R.rows ? min(pos, c1 - 1) : -1;
-      least[p] = a.window > 0 ? pos - a.window + 1 : 0;
-#pragma unroll
-      for (int i = 0; i < 2 * NC; i++) O[p][i] = 0.f;
+    for (int g = 0; g < NG; g++) {
+      Q[g] = *(const v4i*)(lds + (g * 16 + l16) * QROW + seg * 16);
+      qhi[g] = -row_sums[seg][g][0];
+      qlo[g] = -row_sums[seg][g][1];
+      poison[g] = 0.f;
     }
+    const float factor = row_factor[seg];
+    float m = -INFINITY, l = 0.f;
+    const int row = R.r0 + seg, pos = R.first + row / a.each;
+    const int last = row < R.rows ? min(pos, c1 - 1) : -1;
+    const int least = a.window > 0 ? pos - a.window + 1 : 0;
+#pragma unroll
+    for (int i = 0; i < 2 * NC; i++) O[i] = 0.f;
     // One tile: K's registers are free once the scores are there and take the
     // next tile's K then; V's likewise at the end.
     auto compute = [&](int tile, int next_entry) {
       const int tok = c0 + tile * 64 + l16;
       const v4i zero = {0, 0, 0, 0};
-      float x[RT][4];
+      float x[4];
       // ---- scores ----
 #pragma unroll
       for (int t = 0; t < 4; t++) {
@@ -465,21 +475,18 @@ __global__ __launch_bounds__(256, DIM * RT <= 128 ? 3 : 2) void k_attention_spli
             kop[NU + u] = (v4i)((kr[t][u] >> 4) & 0x0F0F0F0Fu);
           }
         }
+        float sum = 0.f;
 #pragma unroll
-        for (int p = 0; p < RT; p++) {
-          float sum = 0.f;
-#pragma unroll
-          for (int g = 0; g < NG; g++) {
-            const unsigned word = k_word(t, g);
-            const v4i r = __builtin_amdgcn_mfma_i32_16x16x64_i8(Q[p][g], kop[g], zero, 0, 0, 0);
-            const int z = (int)(word & 15);
-            const int hi = __mul24(z, qhi[p][g]) + ((r[3] << 8) + r[2]);
-            const int lo = __mul24(z, qlo[p][g]) + ((r[1] << 8) + r[0]);
-            sum = fmaf(scale_of(word), fmaf((float)hi, 65536.f, (float)lo), sum);
-          }
-          x[p][t] = sum * factor[p];
+        for (int g = 0; g < NG; g++) {
+          const unsigned word = k_word(t, g);
+          const v4i r = __builtin_amdgcn_mfma_i32_16x16x64_i8(Q[g], kop[g], zero, 0, 0, 0);
+          const int z = (int)(word & 15);
+          const int hi = __mul24(z, qhi[g]) + ((r[3] << 8) + r[2]);
+          const int lo = __mul24(z, qlo[g]) + ((r[1] << 8) + r[0]);
+          sum = fmaf(scale_of(word), fmaf((float)hi, 65536.f, (float)lo), sum);
         }
-        if constexpr (RT * NG >= 4) __builtin_amdgcn_sched_barrier(0);      // one block's registers at a time
+        x[t] = sum * factor;
+        if constexpr (NG >= 4) __builtin_amdgcn_sched_barrier(0);      // one block's registers at a time
       }
       if constexpr (NG == 1) {
 #pragma unroll
@@ -498,90 +505,86 @@ __global__ __launch_bounds__(256, DIM * RT <= 128 ? 3 : 2) void k_attention_spli
 #pragma unroll
         for (int g = 0; g < NG; g++)
           zbuf[g * 64 + 16 * t + l16] = (uint8_t)(0u - (v_word(t, g) & 15));
+      // ---- softmax weights of this lane's row and tokens ----
+      bool seen[4];
+      float top = -INFINITY;
 #pragma unroll
-      for (int p = 0; p < RT; p++) {
-        // ---- softmax weights of this lane's row and tokens ----
-        bool seen[4];
-        float top = -INFINITY;
+      for (int t = 0; t < 4; t++) {
+        const int pos = tok + 16 * t;
+        seen[t] = (bool)(ok >> (16 * t) & 1) & (pos <= last) & (pos >= least);
+        x[t] = seen[t] ? x[t] : -INFINITY;
+        top = fmaxf(top, x[t]);
+      }
+      const float mn = fmaxf(m, row_max(top)), at = mn == -INFINITY ? 0.f : mn;
+      const float keep = __builtin_amdgcn_exp2f(m - at);
+      m = mn;
+      float w[4];
+      l *= keep;
+#pragma unroll
+      for (int t = 0; t < 4; t++) {
+        w[t] = __builtin_amdgcn_exp2f(x[t] - at);
+        l += w[t];
+      }
+      // ---- times the values' scales, as whole numbers of the tile's largest, four digits ----
+      float ws[NG][4];
+#pragma unroll
+      for (int g = 0; g < NG; g++)
 #pragma unroll
         for (int t = 0; t < 4; t++) {
-          const int pos = tok + 16 * t;
-          seen[t] = (bool)(ok >> (16 * t) & 1) & (pos <= last[p]) & (pos >= least[p]);
-          x[p][t] = seen[t] ? x[p][t] : -INFINITY;
-          top = fmaxf(top, x[p][t]);
+          ws[g][t] = seen[t] ? w[t] * scale_of(v_word(t, g)) : 0.f;
+          poison[g] = fmaf(ws[g][t], 0.f, poison[g]);
         }
-        const float mn = fmaxf(m[p], row_max(top)), at = mn == -INFINITY ? 0.f : mn;
-        const float keep = __builtin_amdgcn_exp2f(m[p] - at);
-        m[p] = mn;
-        float w[4];
-        l[p] *= keep;
 #pragma unroll
-        for (int t = 0; t < 4; t++) {
-          w[t] = __builtin_amdgcn_exp2f(x[p][t] - at);
-          l[p] += w[t];
-        }
-        // ---- times the values' scales, as whole numbers of the tile's largest, four digits ----
-        float ws[NG][4];
+      for (int c = 0; c < 2 * NC; c++) O[c] *= keep;
+      for (int round = 0; round < 8; round++) {
+        float back[NG], left = 0.f;
 #pragma unroll
-        for (int g = 0; g < NG; g++)
+        for (int g = 0; g < NG; g++) {
+          const float big = row_max(fmaxf(fmaxf(ws[g][0], ws[g][1]), fmaxf(ws[g][2], ws[g][3])));
+          // big < 2^(e - 126): whole numbers below 2^30
+          const unsigned e = max(__float_as_uint(big) >> 23, 30u);
+          const float up = __uint_as_float((283u - e) << 23);
+          back[g] = __uint_as_float((e - 29u) << 23);
 #pragma unroll
           for (int t = 0; t < 4; t++) {
-            ws[g][t] = seen[t] ? w[t] * scale_of(v_word(t, g)) : 0.f;
-            poison[p][g] = fmaf(ws[g][t], 0.f, poison[p][g]);
+            const int u = (int)(ws[g][t] * up);
+            ws[g][t] = fmaf(-(float)u, back[g], ws[g][t]);      // what the whole numbers leave, exactly
+            left = fmaxf(left, ws[g][t]);
+            const unsigned d0 = digits_of(u);
+            // 4 x 4 bytes among neighbouring lanes: lane i of four gets digit i of the four tokens
+            const unsigned d1 = __builtin_amdgcn_perm(dppu<0xB1>(d0), d0, lane & 1 ? 0x03070105u : 0x06020400u);
+            const unsigned d2 = __builtin_amdgcn_perm(dppu<0x4E>(d1), d1, lane & 2 ? 0x03020706u : 0x05040100u);
+            *(unsigned*)(pbuf + (g * 16 + seg * 4 + (lane & 3)) * PROW + 16 * t + (l16 & 12)) = d2;
           }
-#pragma unroll
-        for (int c = 0; c < 2 * NC; c++) O[p][c] *= keep;
-        for (int round = 0; round < 8; round++) {
-          float back[NG], left = 0.f;
-#pragma unroll
-          for (int g = 0; g < NG; g++) {
-            const float big = row_max(fmaxf(fmaxf(ws[g][0], ws[g][1]), fmaxf(ws[g][2], ws[g][3])));
-            // big < 2^(e - 126): whole numbers below 2^30
-            const unsigned e = max(__float_as_uint(big) >> 23, 30u);
-            const float up = __uint_as_float((283u - e) << 23);
-            back[g] = __uint_as_float((e - 29u) << 23);
-#pragma unroll
-            for (int t = 0; t < 4; t++) {
-              const int u = (int)(ws[g][t] * up);
-              ws[g][t] = fmaf(-(float)u, back[g], ws[g][t]);      // what the whole numbers leave, exactly
-              left = fmaxf(left, ws[g][t]);
-              const unsigned d0 = digits_of(u);
-              // 4 x 4 bytes among neighbouring lanes: lane i of four gets digit i of the four tokens
-              const unsigned d1 = __builtin_amdgcn_perm(dppu<0xB1>(d0), d0, lane & 1 ? 0x03070105u : 0x06020400u);
-              const unsigned d2 = __builtin_amdgcn_perm(dppu<0x4E>(d1), d1, lane & 2 ? 0x03020706u : 0x05040100u);
-              *(unsigned*)(pbuf + (g * 16 + seg * 4 + (lane & 3)) * PROW + 16 * t + (l16 & 12)) = d2;
-            }
-          }
-          // ---- weighted sums ----
-          v4i A[NG], start[NG];
-#pragma unroll
-          for (int g = 0; g < NG; g++) {
-            A[g] = *(const v4i*)(pbuf + (g * 16 + l16) * PROW + seg * 16);
-            const v4i zb = *(const v4i*)(zbuf + g * 64 + seg * 16);
-            start[g] = __builtin_amdgcn_mfma_i32_16x16x64_i8(A[g], zb, zero, 0, 0, 0);
-          }
-#pragma unroll
-          for (int c = 0; c < NC; c++) {
-            const v4i vlo = (v4i)(vr[c] & 0x0F0F0F0Fu), vhi = (v4i)((vr[c] >> 4) & 0x0F0F0F0Fu);
-            const int glo = c / 4, ghi = DIM == 64 ? 0 : NG / 2 + c / 4;
-            const v4i r0 = __builtin_amdgcn_mfma_i32_16x16x64_i8(A[glo], vlo, start[glo], 0, 0, 0);
-            const v4i r1 = __builtin_amdgcn_mfma_i32_16x16x64_i8(A[ghi], vhi, start[ghi], 0, 0, 0);
-            const float f0 = fmaf((float)((r0[3] << 8) + r0[2]), 65536.f, (float)((r0[1] << 8) + r0[0]));
-            const float f1 = fmaf((float)((r1[3] << 8) + r1[2]), 65536.f, (float)((r1[1] << 8) + r1[0]));
-            O[p][c] = fmaf(f0, back[glo], O[p][c]);
-            O[p][NC + c] = fmaf(f1, back[ghi], O[p][NC + c]);
-          }
-          // 16-bit results end here: what is left is below 2^-30 of the tile's largest weight.  fp32 results keep
-          // every weight's own 24 bits: again with what is left (twice in all where no weight is below 2^-37), until
-          // that is below the smallest normal number.  A round leaves less than 2^-29 of the largest weight, or
-          // less than 2^-126: weights are at most 4352, so six rounds at most.
-          // masks anew each time: kept, they cost 32 registers
-          if (FINE || RT > 1)
-#pragma unroll
-            for (int c = 0; c < NC; c++) asm volatile("" : "+v"(vr[c]));
-          if (!FINE || !__any(left >= 1.17549435e-38f)) break;
         }
-        if constexpr (RT > 1) __builtin_amdgcn_sched_barrier(0);      // one row tile's registers at a time
+        // ---- weighted sums ----
+        v4i A[NG], start[NG];
+#pragma unroll
+        for (int g = 0; g < NG; g++) {
+          A[g] = *(const v4i*)(pbuf + (g * 16 + l16) * PROW + seg * 16);
+          const v4i zb = *(const v4i*)(zbuf + g * 64 + seg * 16);
+          start[g] = __builtin_amdgcn_mfma_i32_16x16x64_i8(A[g], zb, zero, 0, 0, 0);
+        }
+#pragma unroll
+        for (int c = 0; c < NC; c++) {
+          const v4i vlo = (v4i)(vr[c] & 0x0F0F0F0Fu), vhi = (v4i)((vr[c] >> 4) & 0x0F0F0F0Fu);
+          const int glo = c / 4, ghi = DIM == 64 ? 0 : NG / 2 + c / 4;
+          const v4i r0 = __builtin_amdgcn_mfma_i32_16x16x64_i8(A[glo], vlo, start[glo], 0, 0, 0);
+          const v4i r1 = __builtin_amdgcn_mfma_i32_16x16x64_i8(A[ghi], vhi, start[ghi], 0, 0, 0);
+          const float f0 = fmaf((float)((r0[3] << 8) + r0[2]), 65536.f, (float)((r0[1] << 8) + r0[0]));
+          const float f1 = fmaf((float)((r1[3] << 8) + r1[2]), 65536.f, (float)((r1[1] << 8) + r1[0]));
+          O[c] = fmaf(f0, back[glo], O[c]);
+          O[NC + c] = fmaf(f1, back[ghi], O[NC + c]);
+        }
+        // 16-bit results end here: what is left is below 2^-30 of the tile's largest weight.  fp32 results keep
+        // every weight's own 24 bits: again with what is left (twice in all where no weight is below 2^-37), until
+        // that is below the smallest normal number.  A round leaves less than 2^-29 of the largest weight, or
+        // less than 2^-126: weights are at most 4352, so six rounds at most.
+        // masks anew each time: kept, they cost 32 registers
+        if (FINE)
+#pragma unroll
+          for (int c = 0; c < NC; c++) asm volatile("" : "+v"(vr[c]));
+        if (!FINE || !__any(left >= 1.17549435e-38f)) break;
       }
       __builtin_amdgcn_sched_barrier(0);      // into the registers that this tile's have left
       load_v(tile + 4, next);
@@ -600,21 +603,17 @@ __global__ __launch_bounds__(256, DIM * RT <= 128 ? 3 : 2) void k_attention_spli
     // ---- join the four waves: lane (row, channel) sums of each, then by the row's maximum ----
     __syncthreads();
     float* const acc = (float*)lds;
+    float* o = acc + (wave * ROWS + seg) * ACC;
+    const float sum = row_sum(l);
 #pragma unroll
-    for (int p = 0; p < RT; p++) {
-      const int r = p * 4 + seg;
-      float* o = acc + (wave * ROWS + r) * ACC;
-      const float sum = row_sum(l[p]);
-#pragma unroll
-      for (int c = 0; c < NC; c++) {
-        const int glo = c / 4, ghi = DIM == 64 ? 0 : NG / 2 + c / 4;
-        o[16 * c + l16] = O[p][c] + row_sum(poison[p][glo]);
-        o[HALF + 16 * c + l16] = O[p][NC + c] + row_sum(poison[p][ghi]);
-      }
-      if (l16 == 0) {
-        o[DIM] = m[p];
-        o[DIM + 1] = sum;
-      }
+    for (int c = 0; c < NC; c++) {
+      const int glo = c / 4, ghi = DIM == 64 ? 0 : NG / 2 + c / 4;
+      o[16 * c + l16] = O[c] + row_sum(poison[glo]);
+      o[HALF + 16 * c + l16] = O[NC + c] + row_sum(poison[ghi]);
+    }
+    if (l16 == 0) {
+      o[DIM] = m;
+      o[DIM + 1] = sum;
     }
     __syncthreads();
     for (int i = threadIdx.x; i < ROWS * DIM; i += 256) {
@@ -646,7 +645,7 @@ __global__ __launch_bounds__(256, DIM * RT <= 128 ? 3 : 2) void k_attention_spli
         }
       }
     }
-    if (!walk_on<ROWS>(a, W, ntiles)) return;
+    if (!walk_on<ROWS>(a, W, turn)) return;
     __syncthreads();
   }
 }
@@ -702,7 +701,7 @@ __global__ __launch_bounds__(512, 2) void k_attention_chunk(AttnArgs a) {
         for (int d = half; d < DIM; d += 2) ((T*)a.out)[to * DIM + d] = Elem<DT>::store(0.f);
         if (a.lse && !half) a.lse[to] = -INFINITY;
       }
-      if (!walk_on<ROWS>(a, W, 1)) return;
+      if (!walk_on<ROWS>(a, W, turn)) return;
       continue;
     }
     const int c0 = R.lo + 64 * turn.tile0, c1 = (int)min((int64_t)R.hi, (int64_t)R.lo + 64 * (int64_t)turn.tile1);
@@ -1086,7 +1085,7 @@ __global__ __launch_bounds__(512, 2) void k_attention_chunk(AttnArgs a) {
         part[DIM + 1] = l;
       }
     }
-    if (!walk_on<ROWS>(a, W, turn.tile1 - turn.tile0)) return;
+    if (!walk_on<ROWS>(a, W, turn)) return;
   }
 }
 
@@ -1222,14 +1221,20 @@ static void launch_join(const AttnArgs& a, int groups, hipStream_t s) {
   k_attention_join<DIM, ROWS><<<items < 1024 ? items : 1024, 256, 0, s>>>(a, groups);
 }
 
-// Row tiles of four that a workgroup takes (registers allow two at 256 channels).
-static int row_tiles(int rows, int dim) { return rows <= 4 ? 1 : rows <= 8 || dim == 256 ? 2 : 4; }
-
-constexpr int CHUNK_ROWS = 64;
-constexpr int WHOLE_TILES = 16;
+// k_attention_chunk takes a call whose sequences have about this many rows a
+// cache head and whose work (query heads x tokens x (tiles + 4)) is enough.  4
+// sequences of 8001, chunk against split in us: 64 rows 51 / 59, 40 rows 56 /
+// 52 (128 channels); 96 rows 53 / 60, 64 rows 46 / 42 (64); 128 rows 159 / 199,
+// 64 rows 136 / 105 (256).  One of 1500 with 512 rows (114 K) 39 / 54, one of
+// 128 with 512 rows (24 K) 21 / 17.
+static bool chunk_pays(int dim, int64_t rows, int64_t work) { return rows >= (dim == 128 ? 48 : 96) && work >= 65536; }
+// Up to this many tiles a workgroup takes a whole row block and cache head, and
+// nothing is joined; fewer where that leaves most of the chip idle (256 tokens
+// after 768: 50 us, shared by all 42; 512 tokens after none: 35, shared 41).
+constexpr int WHOLE_TILES = 16, WHOLE_TILES_FEW = 8, FEW = 128;
 
 struct Plan {
-  int rt, rows;              // row tiles of k_attention_split (0: k_attention_chunk), rows of a row block
+  int rows;                  // of a row block: 4 (k_attention_split) or 256 (k_attention_chunk)
   int whole, blocks, groups; // AttnArgs::whole, ::blocks; workgroups
 };
 // One workgroup per row block and cache head where lengths are short; else as
@@ -1239,19 +1244,17 @@ struct Plan {
 static bool attention_plan(int heads_q, int heads_kv, int dim, int dtype, int64_t tokens, int batch, bool starts,
                            int64_t max_new, int64_t max_len, Plan* p) {
   const int each = heads_q / heads_kv;
-  const int64_t rows = max_new * each;
-  p->rt = dtype != EXTERND_F32 && rows >= CHUNK_ROWS ? 0 : row_tiles((int)(rows > 64 ? 64 : rows), dim);
-  p->rows = p->rt ? 4 * p->rt : 256;
+  const int64_t tiles = max_len > 0 && max_len < 1 << 26 ? (max_len + 63) / 64 : 1 << 20;
+  p->rows = dtype != EXTERND_F32 && chunk_pays(dim, max_new * each, tokens * heads_q * (tiles + 4)) ? 256 : 4;
   const int64_t blocks = starts ? tokens * each / p->rows + batch : (int64_t)batch * ((each + p->rows - 1) / p->rows);
   if (blocks * heads_kv > INT32_MAX) return false;
   p->blocks = (int)blocks;
-  const int64_t tiles = max_len > 0 ? (max_len + 63) / 64 : 1 << 20;
-  p->whole = tiles <= WHOLE_TILES;
+  p->whole = tiles <= (p->rows == 256 && blocks * heads_kv < FEW ? WHOLE_TILES_FEW : WHOLE_TILES);
   if (p->whole) {
     p->groups = (int)(blocks * heads_kv);
     return true;
   }
-  int64_t most = !p->rt ? 256 : dim * p->rt <= 128 ? 768 : 512;
+  const int64_t most = p->rows == 256 ? 256 : dim <= 128 ? 768 : 512;
   const int64_t fit = (blocks * heads_kv * tiles + 3) / 4;
   p->groups = (int)(most < fit ? most : fit);
   return true;
@@ -1261,21 +1264,17 @@ static size_t plan_bytes(const Plan& p, int dim) {
   return ((size_t)p.groups * (2 * p.rows * (dim + 4) * sizeof(float) + sizeof(AttnShare)) + 255) & ~(size_t)255;
 }
 
-template <int DIM, int RT>
-static void launch_split(const AttnArgs& a, int groups, hipStream_t s) {
-  if (a.dtype == EXTERND_F32) k_attention_split<DIM, RT, true><<<groups, 256, 0, s>>>(a);
-  else k_attention_split<DIM, RT, false><<<groups, 256, 0, s>>>(a);
-  if (!a.whole) launch_join<DIM, 4 * RT>(a, groups, s);
-}
 template <int DIM>
-static void launch_split(const AttnArgs& a, const Plan& p, hipStream_t s) {
-  if (p.rt == 0) {
+static void launch_attention(const AttnArgs& a, const Plan& p, hipStream_t s) {
+  if (p.rows == 4) {
+    if (a.dtype == EXTERND_F32) k_attention_split<DIM, true><<<p.groups, 256, 0, s>>>(a);
+    else k_attention_split<DIM, false><<<p.groups, 256, 0, s>>>(a);
+    if (!a.whole) launch_join<DIM, 4>(a, p.groups, s);
+  } else {
     if (a.dtype == EXTERND_BF16) k_attention_chunk<DIM, EXTERND_BF16><<<p.groups, 512, 0, s>>>(a);
     else k_attention_chunk<DIM, EXTERND_F16><<<p.groups, 512, 0, s>>>(a);
     if (!a.whole) launch_join<DIM, 256>(a, p.groups, s);
-  } else if (p.rt == 1) launch_split<DIM, 1>(a, p.groups, s);
-  else if (p.rt == 2) launch_split<DIM, 2>(a, p.groups, s);
-  else if constexpr (DIM != 256) launch_split<DIM, 4>(a, p.groups, s);
+  }
 }
 
 // Heads, types and counts of an attention call.
@@ -1344,9 +1343,9 @@ int externd_kv4_attention(const void* cache, int64_t num_pages, int32_t heads_kv
   a.part = (float*)workspace;
   a.shares = p.whole ? nullptr : (AttnShare*)(a.part + (size_t)p.groups * 2 * p.rows * (head_dim + 4));
   const hipStream_t s = (hipStream_t)stream;
-  if (head_dim == 64) launch_split<64>(a, p, s);
-  else if (head_dim == 128) launch_split<128>(a, p, s);
-  else launch_split<256>(a, p, s);
+  if (head_dim == 64) launch_attention<64>(a, p, s);
+  else if (head_dim == 128) launch_attention<128>(a, p, s);
+  else launch_attention<256>(a, p, s);
   return hipGetLastError() == hipSuccess ? EXTERND_OK : EXTERND_EHIP;
 }
 
