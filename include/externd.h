@@ -531,7 +531,7 @@ int externd_kv4_attention(const void* cache, int64_t num_pages, int32_t heads_kv
  *  top        0 .. EXTERND_LOGPROBS_MAX_TOP, at most vocab; top_logprobs device
  *             fp32 and top_ids device int64, rows x top (NULL with top = 0).
  *  entropy, lse  device fp32[rows], each may be NULL.
- *  workspace  device, 256-byte aligned (may be NULL where no bytes are needed).
+ *  workspace  not used: externd_token_logprobs_workspace_bytes() is 0.
  * A row of nothing but -infinity: lse and log probabilities -infinity, entropy
  * 0.  A NaN or +infinity makes a row's lse, entropy and log probabilities NaN.
  * Sums are fp32 over at most 2^31 - 1 entries a row.                        */

@@ -112,23 +112,6 @@ struct Kv4Sequences {
   int batch;
 };
 
-// The sequence of new token t: the last b with starts[b] <= t.
-__device__ __forceinline__ int sequence_of(const Kv4Sequences& s, int64_t t) {
-  if (!s.starts) return (int)t;
-  int lo = 0, hi = s.batch - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (s.starts[mid] <= t) lo = mid; else hi = mid - 1;
-  }
-  return lo;
-}
-
-// Position of new token t of sequence b; below 0: none.
-__device__ __forceinline__ int64_t position_of(const Kv4Sequences& s, int b, int64_t t) {
-  const int64_t end = s.starts ? s.starts[b + 1] : b + 1;
-  return (int64_t)max(s.lens[b], 0) - (end - t);
-}
-
 // Page of position p of sequence b, or -1.
 __device__ __forceinline__ int64_t page_of(const Kv4Shape& c, const Kv4Sequences& s, int b, int64_t p) {
   if (p < 0) return -1;

@@ -248,18 +248,6 @@ __device__ __forceinline__ void take(const float (*x)[E], bool present, unsigned
   a.t += present ? (t[0] + t[1]) + (t[2] + t[3]) : 0.f;
 }
 
-struct RowPart {
-  float ref, s, t;
-  int pad;
-};
-
-struct LogprobSplit {
-  int parts;
-  int64_t each;        // a multiple of 64
-  RowPart* sums;       // rows x parts; `each`: 16-byte vectors of a wave
-  uint64_t* keys;      // rows x parts x top
-};
-
 // What a row's sums say (lane 0) and the largest logits (lanes below top).
 template <int DT>
 __device__ __forceinline__ void write_row(const LogprobArgs& a, int64_t r, float ref, float s, float t, uint64_t key) {
@@ -286,11 +274,11 @@ __device__ __forceinline__ void write_row(const LogprobArgs& a, int64_t r, float
 
 constexpr int MAX_WAVES = 16;
 
-// One workgroup per row, or per part of one: its waves take equal stretches, in
-// a single pass with four 16-byte loads of every lane in flight ahead of those
-// in work, and are joined in LDS.
+// One workgroup per row: its waves take equal stretches (`each` 16-byte vectors,
+// a multiple of 64), in a single pass with four 16-byte loads of every lane in
+// flight ahead of those in work, and are joined in LDS.
 template <int DT>
-__global__ __launch_bounds__(64 * MAX_WAVES) void k_logprobs(LogprobArgs a, LogprobSplit sp) {
+__global__ __launch_bounds__(64 * MAX_WAVES) void k_logprobs(LogprobArgs a, int64_t each) {
   typedef typename Elem<DT>::T T;
   constexpr int E = Vec<DT>::E, U = 4;
   extern __shared__ uint64_t waiting[];      // BEST_WORDS a wave, then the pool: 128 a wave
@@ -298,12 +286,10 @@ __global__ __launch_bounds__(64 * MAX_WAVES) void k_logprobs(LogprobArgs a, Logp
   __shared__ float bars[MAX_WAVES];
   __shared__ int pooled;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-  const int64_t r = blockIdx.x / sp.parts;
-  const int part = (int)(blockIdx.x - r * sp.parts);
-  const int64_t unit = (int64_t)part * waves + wave, units = (int64_t)sp.parts * waves;
+  const int64_t r = blockIdx.x;
   const T* x = (const T*)a.logits + r * a.stride;
   const int64_t head = row_head<DT>(x, a.vocab), nv = (a.vocab - head) / E, tail = head + nv * E;
-  const int64_t v0 = min(unit * sp.each, nv), v1 = unit == units - 1 ? nv : min(v0 + sp.each, nv);
+  const int64_t v0 = min(wave * each, nv), v1 = wave == waves - 1 ? nv : min(v0 + each, nv);
   const v4u* v = (const v4u*)(x + head);
   const float c = a.scale * 1.44269504088896340736f;
   Sums sum = {-3.402823466e38f, 0.f, 0.f};
@@ -328,7 +314,7 @@ __global__ __launch_bounds__(64 * MAX_WAVES) void k_logprobs(LogprobArgs a, Logp
     }
   };
   if (blocks > 0) load(A, i);
-  if (unit == 0 && head) {
+  if (wave == 0 && head) {
     float one[1][1] = {{-INFINITY}};
     if (lane < head) one[0][0] = Elem<DT>::load(x[lane]);
     take<1, 1>(one, lane < head, (unsigned)lane, c, sum, best, first);
@@ -348,7 +334,7 @@ __global__ __launch_bounds__(64 * MAX_WAVES) void k_logprobs(LogprobArgs a, Logp
     take<E, 1>(y, in, (unsigned)(head + (i + lane) * E), c, sum, best, first);
     first = false;
   }
-  if (unit == units - 1 && tail < a.vocab) {
+  if (wave == waves - 1 && tail < a.vocab) {
     const bool in = tail + lane < a.vocab;
     float one[1][1] = {{-INFINITY}};
     if (in) one[0][0] = Elem<DT>::load(x[tail + lane]);
@@ -387,40 +373,7 @@ __global__ __launch_bounds__(64 * MAX_WAVES) void k_logprobs(LogprobArgs a, Logp
       for (int k = 0; k < pooled; k += 64)
         best.key = merge_lists(best.key, sort_rising(k + lane < pooled ? waiting[waves * BEST_WORDS + k + lane] : 0));
   }
-  if (sp.parts == 1) {
-    write_row<DT>(a, r, sum.ref, sum.s, sum.t, best.key);
-    return;
-  }
-  if (lane == 0) sp.sums[blockIdx.x] = {sum.ref, sum.s, sum.t, 0};
-  if (lane < a.top) sp.keys[(int64_t)blockIdx.x * a.top + lane] = best.key;
-}
-
-// Joins a row's parts: one wave per row.
-template <int DT>
-__global__ __launch_bounds__(64) void k_logprobs_join(LogprobArgs a, LogprobSplit sp) {
-  const int64_t r = blockIdx.x;
-  const int lane = threadIdx.x;
-  const RowPart* p = sp.sums + r * sp.parts;
-  const float c = a.scale * 1.44269504088896340736f;
-  float ref = -3.402823466e38f;
-  for (int i = lane; i < sp.parts; i += 64) ref = fmaxf(ref, p[i].s > 0.f ? p[i].ref : ref);
-  ref = wave_max(ref);
-  float s = 0.f, t = 0.f;
-  for (int i = lane; i < sp.parts; i += 64) {
-    Sums one = {p[i].ref, p[i].s, p[i].t};
-    if (one.s != 0.f) {
-      one.move(ref, c);
-      s += one.s;
-      t += one.t;
-    }
-  }
-  uint64_t key = 0;
-  if (a.top)
-    for (int i = 0; i < sp.parts; i++) {      // each falling: turned round
-      const int j = 63 - lane;
-      key = merge_lists(key, j < a.top ? sp.keys[(r * sp.parts + i) * a.top + j] : 0);
-    }
-  write_row<DT>(a, r, ref, wave_sum(s), wave_sum(t), key);
+  write_row<DT>(a, r, sum.ref, sum.s, sum.t, best.key);
 }
 
 struct LogprobGradArgs {
@@ -484,28 +437,16 @@ __global__ __launch_bounds__(256) void k_logprobs_grad(LogprobGradArgs a) {
   }
 }
 
-// Waves of a workgroup and workgroups (parts) of a row: 4096 waves where there
-// is work for them, sixteen a CU, a wave not below 2048 entries; the row's
-// waves in one workgroup up to sixteen, which needs no second launch, and in
-// several only where sixteen would take over 16384 entries each.  A power of two
-// rounded down: 940 rows of 65536 with four waves 35, 42, 62 us (bf16; 5, 20, 64
-// largest), with eight 41, 53, 88.
-static LogprobSplit split_of(int64_t rows, int64_t vocab, int* waves) {
-  LogprobSplit sp = {};
+// Waves of a row: 4096 in all where there is work for them, sixteen a CU, a wave
+// not below 2048 entries.  A power of two rounded down: 940 rows of 65536 with
+// four waves 35, 42, 62 us (bf16; 5, 20, 64 largest), with eight 41, 53, 88.
+static int waves_of(int64_t rows, int64_t vocab) {
   int64_t want = (4096 + rows - 1) / rows;
   const int64_t most = (vocab + 2047) / 2048;
   want = want > most ? most : want;
   int w = 1;
   while (2 * w <= want && w < MAX_WAVES) w *= 2;
-  int64_t parts = 1;
-  if (w == MAX_WAVES && vocab > MAX_WAVES * 16384) parts = want / MAX_WAVES;
-  if (parts > 64) parts = 64;
-  sp.parts = (int)(parts < 1 ? 1 : parts);
-  *waves = w;
-  return sp;
-}
-static size_t split_bytes(int64_t rows, int parts, int top) {
-  return ((size_t)rows * parts * (sizeof(RowPart) + (size_t)top * 8) + 255) & ~(size_t)255;
+  return w;
 }
 
 static void launch_logprobs_grad(LogprobGradArgs a, int32_t dtype, int64_t r0, int64_t rows, int64_t stretches, hipStream_t s) {
@@ -517,10 +458,11 @@ static void launch_logprobs_grad(LogprobGradArgs a, int32_t dtype, int64_t r0, i
 }
 
 template <int DT>
-static void launch_logprobs(const LogprobArgs& a, const LogprobSplit& sp, int waves, hipStream_t s) {
+static void launch_logprobs(const LogprobArgs& a, hipStream_t s) {
+  const int waves = waves_of(a.rows, a.vocab);
+  const int64_t each = ((a.vocab / Vec<DT>::E + waves - 1) / waves + 63) & ~(int64_t)63;
   const size_t lds = a.top ? (size_t)waves * (BEST_WORDS + 128) * sizeof(uint64_t) : 0;
-  k_logprobs<DT><<<dim3((unsigned)(a.rows * sp.parts)), 64 * waves, lds, s>>>(a, sp);
-  if (sp.parts > 1) k_logprobs_join<DT><<<dim3((unsigned)a.rows), 64, 0, s>>>(a, sp);
+  k_logprobs<DT><<<dim3((unsigned)a.rows), 64 * waves, lds, s>>>(a, each);
 }
 
 static bool logprob_sizes_ok(int64_t rows, int64_t vocab, int32_t top) {
@@ -534,10 +476,8 @@ using namespace externd;
 extern "C" {
 
 size_t externd_token_logprobs_workspace_bytes(int64_t rows, int64_t vocab, int32_t top) {
-  if (!logprob_sizes_ok(rows, vocab, top) || !rows) return 0;
-  int waves;
-  const int parts = split_of(rows, vocab, &waves).parts;
-  return parts == 1 ? 0 : split_bytes(rows, parts, top);
+  (void)rows, (void)vocab, (void)top;      // a row is one workgroup's
+  return 0;
 }
 
 int externd_token_logprobs(const void* logits, int32_t dtype, int64_t rows, int64_t vocab, int64_t row_stride,
@@ -548,20 +488,13 @@ int externd_token_logprobs(const void* logits, int32_t dtype, int64_t rows, int6
       !std::isfinite(scale) || (top && (!top_logprobs || !top_ids)) || (rows && !logits) || (logprob && rows && !targets))
     return EXTERND_EINVAL;
   if (rows > INT32_MAX || vocab > INT32_MAX) return EXTERND_EUNSUPPORTED;
-  const size_t need = externd_token_logprobs_workspace_bytes(rows, vocab, top);
-  if (need && (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 255))) return EXTERND_EWORKSPACE;
+  (void)workspace, (void)workspace_bytes;
   if (!rows) return EXTERND_OK;
   const LogprobArgs a = {logits, rows, vocab, row_stride, targets, scale, top, logprob, entropy, lse, top_logprobs, top_ids};
-  int waves;
-  LogprobSplit sp = split_of(rows, vocab, &waves);
-  const int per = dtype == EXTERND_F32 ? 4 : 8;      // entries of a vector
-  sp.each = ((vocab / per + sp.parts * waves - 1) / (sp.parts * waves) + 63) & ~(int64_t)63;
-  sp.sums = (RowPart*)workspace;
-  sp.keys = (uint64_t*)(sp.sums + rows * sp.parts);
   const hipStream_t s = (hipStream_t)stream;
-  if (dtype == EXTERND_F32) launch_logprobs<EXTERND_F32>(a, sp, waves, s);
-  else if (dtype == EXTERND_BF16) launch_logprobs<EXTERND_BF16>(a, sp, waves, s);
-  else launch_logprobs<EXTERND_F16>(a, sp, waves, s);
+  if (dtype == EXTERND_F32) launch_logprobs<EXTERND_F32>(a, s);
+  else if (dtype == EXTERND_BF16) launch_logprobs<EXTERND_BF16>(a, s);
+  else launch_logprobs<EXTERND_F16>(a, s);
   return hipGetLastError() == hipSuccess ? EXTERND_OK : EXTERND_EHIP;
 }
 
