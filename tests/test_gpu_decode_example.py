@@ -1,0 +1,113 @@
+"""The decoding operators together, as examples/decode.py runs them: every stage of
+a prompt's and of two single-token steps against its definition in 64 bits on the
+stage's own inputs, so that the bounds are those of each stage (u = 2^-24):
+* projections: as in the tests of apply: (n + k + 4) u |B| |D| |C| |x|;
+* rotary: the turn of a pair has errors of a few u of |a| + |b| (4 u for two
+  products and a sum, 2 u for sin and cos, and their 2^-32 turns, 1.5e-9);
+* attention: a score is off by dx <= (D + 8) u scale sum |q k|; weights then by
+  a factor e^(2 dx) at most, and n + 16 roundings in sums: (4 dx + (n + 16) u) max |v|
+  (lse: 2 dx, the sum's roundings, 8 u of the largest score);
+* log probabilities: sums of V entries, (V + 16) u, and 8 u of the largest |z|.
+"""
+import importlib.util
+import os
+
+import numpy as np
+import pytest
+
+from oracle import decode_oracle as ref
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def example():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "decode.py")
+    spec = importlib.util.spec_from_file_location("decode_example", path)
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    return m
+
+
+def f64(t):
+    return t.double().cpu().numpy()
+
+
+def check_projection(binding, fac, X, Y):
+    k = fac.f.D.shape[0]
+    B = binding.unpack_trits(fac.f.B_packed.cpu().numpy(), k).astype(np.float64)
+    C = binding.unpack_trits(fac.f.C_packed.cpu().numpy(), fac.n).astype(np.float64)
+    D, X = f64(fac.f.D), f64(X)
+    want = (X @ C.T * D) @ B.T
+    tol = (fac.n + k + 4) * U * ((np.abs(X) @ np.abs(C).T * np.abs(D)) @ np.abs(B).T)
+    assert np.all(np.abs(f64(Y).reshape(want.shape) - want) <= tol)
+
+
+def test_stages(example):
+    binding = example.binding
+    model, gen = example.Model(), torch.Generator().manual_seed(5)
+    prompts = [torch.randint(0, model.vocab, (n,), generator=gen).tolist() for n in (70, 23, 1)]
+    session = example.Session(model, len(prompts))
+    freqs = model.freqs.cpu().numpy().view(np.uint64)
+    tokens, targets = prompts, [p[1:] + [-1] for p in prompts]
+    for _ in range(3):
+        out, s = session.step(tokens, targets)
+        torch.cuda.synchronize()
+        T = s["starts"][-1]
+        for fac, name in ((model.q, "q0"), (model.k, "k0"), (model.v, "v")):
+            check_projection(binding, fac, s["x"], s[name].reshape(T, -1))
+        check_projection(binding, model.o, s["att"].reshape(T, -1), s["o"])
+        check_projection(binding, model.head, s["y"], s["logits"])
+        for a, b in (("q0", "q"), ("k0", "k")):
+            want = ref.rotary(f64(s[a]), s["positions"], freqs, False, model.amplitude)
+            big = np.abs(f64(s[a])).max(axis=-1, keepdims=True)
+            assert np.all(np.abs(f64(s[b]) - want) <= 2 * big * model.amplitude * (6 * U + 2e-9))
+        # what the cache holds: within half a step of what was stored, for the new tokens
+        st = torch.tensor(s["starts"], dtype=torch.int32, device="cuda")
+        kh, vh = binding.kv4_read(session.cache, s["table"], s["lens"], model.dim, starts=st, tokens=T)
+        for got, x in ((f64(kh), f64(s["k"])), (f64(vh), f64(s["v"]))):
+            span = np.maximum(x.max(-1, keepdims=True), 0) - np.minimum(x.min(-1, keepdims=True), 0)
+            # the step is span / 15 rounded up to seven significant bits
+            assert np.all(np.abs(got - x) <= span / 15 * (1 + 2.0 ** -6) * (0.5 + 2.0 ** -20))
+        # attention over all that is held
+        lens = session.lens
+        whole = torch.tensor([0] + list(np.cumsum(lens)), dtype=torch.int32, device="cuda")
+        K, V = binding.kv4_read(session.cache, s["table"], s["lens"], model.dim, starts=whole, tokens=sum(lens))
+        K, V, q = f64(K), f64(V), f64(s["q"])
+        scale, each, at = model.dim ** -0.5, model.heads // model.heads_kv, np.concatenate([[0], np.cumsum(lens)])
+        for u in range(len(lens)):
+            for t in range(s["starts"][u], s["starts"][u + 1]):
+                n = s["positions"][t] + 1
+                for h in range(model.heads):
+                    k, v = K[at[u]:at[u] + n, h // each], V[at[u]:at[u] + n, h // each]
+                    x = scale * (k @ q[t, h])
+                    dx = (model.dim + 8) * U * scale * (np.abs(k) @ np.abs(q[t, h])).max()
+                    p = np.exp(x - x.max())
+                    want = p @ v / p.sum()
+                    assert np.all(np.abs(f64(s["att"][t, h]) - want) <= (4 * dx + (n + 16) * U) * np.abs(v).max())
+                    assert abs(float(s["lse"][t, h]) - (x.max() + np.log(p.sum()))) <= 2 * dx + (n + 16) * U + 8 * U * np.abs(x).max()
+        y = np.array([t for ts in targets for t in ts]) if targets is not None else np.full(T, -1)
+        lp, ent, lse, tl, ti, _ = ref.logprobs(f64(s["logits"]), y, 1.0, 5)
+        z = np.abs(f64(s["logits"])).max()
+        tol = (model.vocab + 16) * U + 8 * U * z
+        if targets is not None:
+            assert np.all(np.abs(f64(out.logprob) - lp) <= tol)
+        assert np.all(np.abs(f64(out.top_logprobs) - tl) <= tol) and np.array_equal(out.top_ids.cpu().numpy(), ti)
+        ends = [e - 1 for e in s["starts"][1:]]
+        tokens, targets = [[t] for t in out.top_ids[ends, 0].tolist()], None
+
+
+def test_pages_run_out(example):
+    session = example.Session(example.Model(vocab=100), 1, pages=2)
+    with pytest.raises(RuntimeError, match="no page left"):
+        session.step([[1] * 33])
+
+
+def test_main(example, capsys):
+    example.main()
+    assert "perplexity" in capsys.readouterr().out
