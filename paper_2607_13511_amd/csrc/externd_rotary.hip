@@ -38,6 +38,14 @@ __device__ __forceinline__ void sincos_turns(uint64_t phase, float* s, float* c)
   *c = (quarter + 1) & 2 ? -v : v;
 }
 
+// One form for all variants of the kernel, so that they agree bit for bit: a
+// fused multiply-add in fp32, not fused with the rounding to the storage type.
+__device__ __forceinline__ float turned(float a, float c, float b, float s) {
+  float r = fmaf(a, c, b * s);
+  asm("" : "+v"(r));
+  return r;
+}
+
 // A workgroup takes TW tokens and `span` heads of q and k side by side: sin and
 // cos of its tokens' pairs once, in LDS, then units of N entries (of both
 // partners, N each), the unit index running through a head first.  Bound by
@@ -60,43 +68,53 @@ __global__ __launch_bounds__(256) void k_rotary(RotaryArgs a, int tw, int span) 
   const int pairs = (a.interleaved ? a.rot : half) / N;      // units that turn
   constexpr int RN = VEC ? N : 1;      // entries of a unit that is only copied
   const int units = pairs + (a.dim - a.rot) / RN;
-  for (int e = threadIdx.x; e < nt * nh * units; e += 256) {
-    const int th = e / units, u = e - th * units, t = th / nh, h = h0 + th - t * nh;
-    const RotarySide& sd = h < a.side[0].heads ? a.side[0] : a.side[1];
-    const int hh = h < a.side[0].heads ? h : h - a.side[0].heads;
-    const T* in = (const T*)sd.in + (t0 + t) * sd.its + hh * sd.ihs;
-    T* out = (T*)sd.out + (t0 + t) * sd.ots + hh * sd.ohs;
-    const float2* cs = turn + t * half;
-    if (u >= pairs) {                     // entries behind the turned ones
-      const int d = a.rot + (u - pairs) * RN;
-      if (in == out) continue;
-      float x[RN];
-      load_n<DT, RN, VEC>(in + d, x);
-      store_n<DT, RN, VEC>(out + d, x);
-    } else if (a.interleaved) {
-      const int d = u * N;
-      float x[N], y[N];
-      load_n<DT, N, VEC>(in + d, x);
+  const int total = nt * nh * units;
+  const float by_units = 1.f / units, by_heads = 1.f / nh;
+  constexpr int U = VEC ? 2 : 1;      // units of a thread in flight (8191 tokens, half turned: 39, 37, 41 us with 1, 2, 4)
+  for (int e0 = threadIdx.x; e0 < total; e0 += 256 * U) {
+    T* out[U];
+    const float2* cs[U];
+    float x[U][N], y[U][N];
 #pragma unroll
-      for (int i = 0; i < N; i += 2) {
-        const float2 w = cs[d / 2 + i / 2];
-        y[i] = x[i] * w.x - x[i + 1] * w.y;
-        y[i + 1] = x[i + 1] * w.x + x[i] * w.y;
-      }
-      store_n<DT, N, VEC>(out + d, y);
-    } else {
-      const int d = u * N;
-      float x[N], y[N], p[N], q[N];
-      load_n<DT, N, VEC>(in + d, x);
-      load_n<DT, N, VEC>(in + half + d, y);
+    for (int i = 0; i < U; i++) {
+      // e / units and th / nh: exact below 2^20, and a workgroup's units are fewer
+      const int e = min(e0 + 256 * i, total - 1), th = (int)(((float)e + 0.5f) * by_units), u = e - th * units;
+      const int t = (int)(((float)th + 0.5f) * by_heads), h = h0 + th - t * nh;
+      const RotarySide& sd = h < a.side[0].heads ? a.side[0] : a.side[1];
+      const int hh = h < a.side[0].heads ? h : h - a.side[0].heads;
+      // entries behind the turned ones: cs null
+      const int d = u < pairs ? u * N : a.rot + (u - pairs) * RN;
+      const T* in = (const T*)sd.in + (t0 + t) * sd.its + hh * sd.ihs + d;
+      out[i] = (T*)sd.out + (t0 + t) * sd.ots + hh * sd.ohs + d;
+      cs[i] = u < pairs ? turn + t * half + (a.interleaved ? d / 2 : d) : nullptr;
+      if (VEC || u < pairs) load_n<DT, N, VEC>(in, x[i]);
+      else load_n<DT, RN, VEC>(in, x[i]);
+      if (!a.interleaved && (VEC || u < pairs)) load_n<DT, N, VEC>(u < pairs ? in + half : in, y[i]);
+    }
 #pragma unroll
-      for (int i = 0; i < N; i++) {
-        const float2 w = cs[d + i];
-        p[i] = x[i] * w.x - y[i] * w.y;
-        q[i] = y[i] * w.x + x[i] * w.y;
+    for (int i = 0; i < U; i++) {
+      if (e0 + 256 * i >= total) break;
+      if (!cs[i]) store_n<DT, RN, VEC>(out[i], x[i]);
+      else if (a.interleaved) {
+        float p[N];
+#pragma unroll
+        for (int j = 0; j < N; j += 2) {
+          const float2 w = cs[i][j / 2];
+          p[j] = turned(x[i][j], w.x, -x[i][j + 1], w.y);
+          p[j + 1] = turned(x[i][j + 1], w.x, x[i][j], w.y);
+        }
+        store_n<DT, N, VEC>(out[i], p);
+      } else {
+        float p[N], q[N];
+#pragma unroll
+        for (int j = 0; j < N; j++) {
+          const float2 w = cs[i][j];
+          p[j] = turned(x[i][j], w.x, -y[i][j], w.y);
+          q[j] = turned(y[i][j], w.x, x[i][j], w.y);
+        }
+        store_n<DT, N, VEC>(out[i], p);
+        store_n<DT, N, VEC>(out[i] + half, q);
       }
-      store_n<DT, N, VEC>(out + d, p);
-      store_n<DT, N, VEC>(out + half + d, q);
     }
   }
 }
