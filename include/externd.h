@@ -508,6 +508,13 @@ int externd_kv4_read(const void* cache, int64_t num_pages, int32_t heads_kv, int
  *  window >= 0; batch <= 65535, tokens heads_q < 2^31.
  *  workspace  device, >= externd_kv4_attention_workspace_bytes() bytes for the
  *             same sizes, 256-byte aligned (may be NULL where that is 0).
+ * The arithmetic: sums, maxima and lse are fp32.  Few rows a cache head: q as
+ * whole numbers of 31 bits below its row's largest entry, a weight times its
+ * value's scale as one of 30 bits below the largest of 64 tokens (with fp32
+ * results, what that leaves too), products and their sums exact.  Many rows
+ * (dtype bf16 or fp16): q as fp16 below 2^15 (entries below 2^-29 of the row's
+ * largest lose bits), scores exact products summed in fp32, weights rounded to
+ * fp16 for their product with the values.
  * A NaN or an infinity in q makes that row NaN; NaN values make those rows
  * NaN that see them.                                                       */
 size_t externd_kv4_attention_workspace_bytes(int32_t heads_q, int32_t heads_kv, int32_t head_dim, int32_t dtype,

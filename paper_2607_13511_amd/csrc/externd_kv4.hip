@@ -83,7 +83,11 @@ __device__ __forceinline__ unsigned kv4_quantize(float* x) {
 // One wave per block of 16 positions, cache head, and K or V.  Lane 4 t + c has
 // token t's byte columns c H / 4 ..: as many channels below D / 2 and, in the
 // high nibbles, above.  V's bytes are turned through LDS, so that a lane writes
-// 16 tokens' bytes of one column at once.
+// 16 tokens' bytes of one column at once.  Bound by memory: 6.8 K tokens of 8
+// heads of 128 in bf16, 28 MB read and 7 written, in 15.6 us (2.3 TB/s).
+// Entries are read one by one (VEC false) only where heads do not start at
+// multiples of 16 bytes; so, and with V's bytes scattered, this and reading
+// back took 82 us together, now 24.
 template <int DT, int DIM, bool VEC>
 __global__ __launch_bounds__(256) void k_kv4_append(uint8_t* cache, Kv4Shape c, Kv4Sequences q, Kv4Source k, Kv4Source v,
                                                     int64_t blocks) {
@@ -165,7 +169,7 @@ __global__ __launch_bounds__(256) void k_kv4_append(uint8_t* cache, Kv4Shape c, 
   }
 }
 
-// The same units, the other way.
+// The same units, the other way: 6.8 K tokens in 10.8 us (3.3 TB/s).
 template <int DT, int DIM>
 __global__ __launch_bounds__(256) void k_kv4_read(const uint8_t* cache, Kv4Shape c, Kv4Sequences q, void* k, void* v,
                                                   int64_t blocks) {

@@ -285,8 +285,18 @@ __device__ __forceinline__ unsigned digits_of(int u) { return ((unsigned)u + 0x0
 // 8 codes), where conversion to floating point would take 8 or more; this is
 // what the memory-bound case needs (14 TB/s of codes in instructions).
 //
+// Roundings: a query to 31 bits of its row's largest entry; a weight times a
+// scale to 30 bits of the tile's largest (to its own 24 and less with FINE, for
+// fp32 results); sums and the running maximum are fp32.
+//
 // Four waves share a part; each takes every fourth tile of 64 tokens with its
-// own running maximum, and they are joined at the end.
+// own running maximum, and they are joined at the end.  Four rows always: with
+// 8 or 16 rows a workgroup the codes are taken apart less often, but the
+// registers leave half the waves (20 rows over 4001 tokens 50 us, now 33; 8 rows of
+// 256 channels over 13848 50 us, now 36).  Bound by memory: 32 users' 363 MB in
+// 75 us (4.9 TB/s), 143 MB of one of 131071 tokens in 32 us (4.5), where a
+// start of about 8 us (lengths, table, first tiles, one after another) is what
+// is left above the 6.3 TB/s that plain loads reach.
 template <int DIM, bool FINE>
 __global__ __launch_bounds__(256, DIM <= 128 ? 3 : 2) void k_attention_split(AttnArgs a) {
   constexpr int NG = DIM / KV4_GROUP, HALF = DIM / 2, ROWS = 4;
@@ -661,9 +671,16 @@ __global__ __launch_bounds__(256, DIM <= 128 ? 3 : 2) void k_attention_split(Att
 // are: token order within 16 is free, so V is stored in the order that S^T has.
 //
 // A tile of TT tokens is converted once (4 operations for 2 codes: mask to
-// 1024 + code, subtract 1024 + z, times s) while the tile before is in work;
-// one barrier a tile.  The weights are taken against a running reference that
-// moves only when a row's maximum passes it by 2^8, so O is rarely rescaled.
+// 1024 + code, subtract 1024 + z, times s) while the tiles before are in work.
+// The weights are taken against a running reference that moves only when a
+// row's maximum passes it by 2^8, so O is rarely rescaled.
+//
+// Bound by the vector instructions between the products: a wave's step of 64
+// tokens at 128 channels has 1240 cycles of matrix instructions and about 2300 of
+// weights (32 exponentials of 16 cycles) and conversion, and its neighbour on the SIMD the
+// other way round, so the matrix cores work half the time: 3.5 K tokens of 32
+// heads over 12 K in 650 us, 795 TFLOP/s.  All waves in one phase: 700 us;
+// conversion among the products: 754.
 template <int DIM, int DT>
 __global__ __launch_bounds__(512, 2) void k_attention_chunk(AttnArgs a) {
   typedef typename Elem<DT>::T T;
@@ -1238,9 +1255,9 @@ struct Plan {
   int whole, blocks, groups; // AttnArgs::whole, ::blocks; workgroups
 };
 // One workgroup per row block and cache head where lengths are short; else as
-// many as are resident at once (three of four waves a CU where 168 registers
-// do, two elsewhere, one of eight for k_attention_chunk), but not below four
-// tiles each.
+// many as are resident at once (a CU holds three of four waves where 168
+// registers do, two elsewhere, one of eight for k_attention_chunk), but not
+// below four tiles each: a part costs its join about that much.
 static bool attention_plan(int heads_q, int heads_kv, int dim, int dtype, int64_t tokens, int batch, bool starts,
                            int64_t max_new, int64_t max_len, Plan* p) {
   const int each = heads_q / heads_kv;

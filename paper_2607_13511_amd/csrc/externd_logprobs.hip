@@ -276,7 +276,12 @@ constexpr int MAX_WAVES = 16;
 
 // One workgroup per row: its waves take equal stretches (`each` 16-byte vectors,
 // a multiple of 64), in a single pass with four 16-byte loads of every lane in
-// flight ahead of those in work, and are joined in LDS.
+// flight ahead of those in work, and are joined in LDS.  One exponential and
+// one fused multiply-add for y an entry; entries above the bar (the least of
+// the wave's largest so far) are rare, so only their lanes go through LDS.
+// Bound by memory: 2048 rows of 150001 in bf16, 615 MB, in 129 us (4.8 TB/s) with
+// the 20 largest.  8 rows of 65536 in fp32 with the 5 largest in 16 us, 9 without
+// them: sorting, which so few rows cannot hide.
 template <int DT>
 __global__ __launch_bounds__(64 * MAX_WAVES) void k_logprobs(LogprobArgs a, int64_t each) {
   typedef typename Elem<DT>::T T;
@@ -387,7 +392,9 @@ struct LogprobGradArgs {
 };
 
 // One workgroup per row and stretch of it: 16-byte loads and stores where a
-// row of both arrays starts at the same place within 16 bytes, else one by one.
+// row of both arrays starts at the same place within 16 bytes, else one by one
+// (218 us where the other takes 96).  Bound by memory: 2048 rows of 65537 in bf16,
+// 537 MB, in 96 us (5.6 TB/s).
 template <int DT>
 __global__ __launch_bounds__(256) void k_logprobs_grad(LogprobGradArgs a) {
   typedef typename Elem<DT>::T T;
