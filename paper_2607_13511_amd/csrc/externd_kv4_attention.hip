@@ -675,12 +675,14 @@ __global__ __launch_bounds__(256, DIM <= 128 ? 3 : 2) void k_attention_split(Att
 // The weights are taken against a running reference that moves only when a
 // row's maximum passes it by 2^8, so O is rarely rescaled.
 //
-// Bound by the vector instructions between the products: a wave's step of 64
-// tokens at 128 channels has 1240 cycles of matrix instructions and about 2300 of
-// weights (32 exponentials of 16 cycles) and conversion, and its neighbour on the SIMD the
-// other way round, so the matrix cores work half the time: 3.5 K tokens of 32
-// heads over 12 K in 650 us, 795 TFLOP/s.  All waves in one phase: 700 us;
-// conversion among the products: 754.
+// Bound by the vector instructions between the products, and by the clock that
+// falls to 1.8 GHz under both: a wave's step of 64 tokens at 128 channels has 32
+// products of 32 cycles and 328 vector instructions (32 exponentials of 16
+// cycles among them), so a SIMD's two waves have 2048 and 3400 cycles of the
+// 4560 that a step takes.  3.5 K tokens of 32 heads over 12 K in 613 us, 840
+// TFLOP/s.  All waves in one phase: 700 us; conversion among the products: 754;
+// rows padded to an odd number of units instead of permuted (48 instructions
+// fewer): 619.
 template <int DIM, int DT>
 __global__ __launch_bounds__(512, 2) void k_attention_chunk(AttnArgs a) {
   typedef typename Elem<DT>::T T;
@@ -1013,8 +1015,12 @@ __global__ __launch_bounds__(512, 2) void k_attention_chunk(AttnArgs a) {
       __builtin_amdgcn_sched_barrier(0);      // the sums here, not beside the products: their registers
     };
 
-    // Two groups of four waves, one of each on a SIMD, half a step apart: while one runs its products, the other
-    // turns scores into weights and converts a later tile (K two tiles ahead, V one, in three buffers each).
+    // Two groups of four waves, one of each on a SIMD.  Between two barriers the first turns its scores of tile n
+    // into weights, converts its share of later tiles (K's n + 2, V's n + 1) and then runs the products of tile n; the
+    // second first runs the products of tile n - 1 and then does the same for its scores of tile n.  So one group's
+    // products run beside the other's vector work, and what is written between two barriers (K n + 2, V n + 1) is read
+    // after the second one at the earliest, what is read (K n and n + 1, V n - 1 and n) is in the other two of three
+    // buffers each.  With a second barrier between the halves 631 us for 607, 316 for 242 at 64 channels.
     KRaw kr;
     VRaw vr;
     int e1 = entry(1), e2 = entry(2), e = entry(0);
@@ -1038,7 +1044,7 @@ __global__ __launch_bounds__(512, 2) void k_attention_chunk(AttnArgs a) {
     scores(kt[0]);
     for (int n = 0;; n++) {
       __builtin_amdgcn_s_setprio(0);
-      __syncthreads();
+      if (wave < 4) __syncthreads();
       weights(b0, n);
       convert_k(b2, kr);
       convert_v(b1, n + 1, vplace.there, vr);
@@ -1048,7 +1054,7 @@ __global__ __launch_bounds__(512, 2) void k_attention_chunk(AttnArgs a) {
       kplace = place_at(n + 3, e);
       load_k(kr, n + 3, kplace);
       e = entry(n + 4);
-      __syncthreads();
+      if (wave >= 4) __syncthreads();
       __builtin_amdgcn_s_setprio(1);
       values(vt[b0]);
       scores(kt[b1]);      // of no tile after the last one: not used then
