@@ -479,7 +479,8 @@ size_t externd_kv4_page_bytes(int32_t head_dim, int32_t page_tokens);  /* of one
 /* Stores the new tokens' k and v (device, tokens x heads_kv x head_dim).
  * Tokens whose position or page is none are not stored.  cache: device, 16-byte
  * aligned, num_pages x heads_kv x externd_kv4_page_bytes() bytes.  Two tokens
- * of one call must not share a place.  tokens, num_pages <= 2^31 - 1.     */
+ * of one call must not share a place.  num_pages, tokens heads_kv < 2^31,
+ * (tokens / 16 + 2 batch) heads_kv < 2^25.                                 */
 int externd_kv4_append(void* cache, int64_t num_pages, int32_t heads_kv, int32_t head_dim, int32_t page_tokens,
                        const void* k, const void* v, int32_t dtype, int64_t k_token_stride, int64_t k_head_stride,
                        int64_t v_token_stride, int64_t v_head_stride, int64_t tokens, int32_t batch,
@@ -541,7 +542,7 @@ int externd_kv4_attention(const void* cache, int64_t num_pages, int32_t heads_kv
  *  workspace  not used: externd_token_logprobs_workspace_bytes() is 0.
  * A row of nothing but -infinity: lse and log probabilities -infinity, entropy
  * 0.  A NaN or +infinity makes a row's lse, entropy and log probabilities NaN.
- * Sums are fp32 over at most 2^31 - 1 entries a row.                        */
+ * Sums are fp32 over at most 2^31 - 1 entries a row; rows < 2^26.           */
 #define EXTERND_LOGPROBS_MAX_TOP 64
 size_t externd_token_logprobs_workspace_bytes(int64_t rows, int64_t vocab, int32_t top);
 int externd_token_logprobs(const void* logits, int32_t dtype, int64_t rows, int64_t vocab, int64_t row_stride,

@@ -10,6 +10,9 @@
 
 namespace externd {
 
+// A launch holds fewer than 2^32 threads a dimension.
+constexpr int64_t MAX_THREADS = ((int64_t)1 << 32) - 1;
+
 inline bool dtype_ok(int32_t d) { return d == EXTERND_F32 || d == EXTERND_BF16 || d == EXTERND_F16; }
 inline int dtype_bytes(int32_t d) { return d == EXTERND_F32 ? 4 : 2; }
 

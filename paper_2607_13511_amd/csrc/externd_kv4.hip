@@ -283,6 +283,7 @@ int externd_kv4_append(void* cache, int64_t num_pages, int32_t heads_kv, int32_t
   const Kv4Sequences q = {starts, lens, table, table_pages, tokens, batch};
   const Kv4Source ks = {k, k_token_stride, k_head_stride}, vs = {v, v_token_stride, v_head_stride};
   const int64_t n = block_count(q);
+  if ((n * 2 * c.heads + 3) / 4 > MAX_THREADS / 256) return EXTERND_EUNSUPPORTED;
   const dim3 grid((unsigned)((n * 2 * c.heads + 3) / 4));
   const hipStream_t s = (hipStream_t)stream;
   const int es = dtype_bytes(dtype);
@@ -303,6 +304,7 @@ int externd_kv4_read(const void* cache, int64_t num_pages, int32_t heads_kv, int
   if (!k || !v || (((uintptr_t)k | (uintptr_t)v) & 15)) return EXTERND_EINVAL;
   const Kv4Sequences q = {starts, lens, table, table_pages, tokens, batch};
   const int64_t n = block_count(q);
+  if ((n * 2 * c.heads + 3) / 4 > MAX_THREADS / 256) return EXTERND_EUNSUPPORTED;
   const dim3 grid((unsigned)((n * 2 * c.heads + 3) / 4));
   const hipStream_t s = (hipStream_t)stream;
   if (dtype == EXTERND_F32) launch_read<EXTERND_F32>(c, n, grid, s, (const uint8_t*)cache, q, k, v);

@@ -1272,7 +1272,8 @@ static bool attention_plan(int heads_q, int heads_kv, int dim, int dtype, int64_
   const int64_t blocks = starts ? tokens * each / p->rows + batch : (int64_t)batch * ((each + p->rows - 1) / p->rows);
   if (blocks * heads_kv > INT32_MAX) return false;
   p->blocks = (int)blocks;
-  p->whole = tiles <= (p->rows == 256 && blocks * heads_kv < FEW ? WHOLE_TILES_FEW : WHOLE_TILES);
+  p->whole = tiles <= (p->rows == 256 && blocks * heads_kv < FEW ? WHOLE_TILES_FEW : WHOLE_TILES) &&
+             blocks * heads_kv <= MAX_THREADS / 512;
   if (p->whole) {
     p->groups = (int)(blocks * heads_kv);
     return true;

@@ -494,7 +494,7 @@ int externd_token_logprobs(const void* logits, int32_t dtype, int64_t rows, int6
   if (!dtype_ok(dtype) || !logprob_sizes_ok(rows, vocab, top) || row_stride < vocab || !(scale > 0) ||
       !std::isfinite(scale) || (top && (!top_logprobs || !top_ids)) || (rows && !logits) || (logprob && rows && !targets))
     return EXTERND_EINVAL;
-  if (rows > INT32_MAX || vocab > INT32_MAX) return EXTERND_EUNSUPPORTED;
+  if (rows > MAX_THREADS / 64 || vocab > INT32_MAX) return EXTERND_EUNSUPPORTED;      // many rows: one wave each
   (void)workspace, (void)workspace_bytes;
   if (!rows) return EXTERND_OK;
   const LogprobArgs a = {logits, rows, vocab, row_stride, targets, scale, top, logprob, entropy, lse, top_logprobs, top_ids};

@@ -136,11 +136,21 @@ static void launch_rotary(const RotaryArgs& a, bool vec, hipStream_t s) {
   tw = tw < 1 ? 1 : tw * half > 4096 ? (4096 / half > 1 ? 4096 / half : 1) : tw;
   int span = tw > 1 ? heads : (int)(per / units);
   span = span < 1 ? 1 : span > heads ? heads : span;
-  const dim3 grid((unsigned)((a.tokens + tw - 1) / tw), (unsigned)((heads + span - 1) / span));
   const size_t lds = (size_t)tw * half * sizeof(float2);
-  if (vec) k_rotary<DT, E, true><<<grid, 256, lds, s>>>(a, tw, span);
-  else if (n == 2) k_rotary<DT, 2, false><<<grid, 256, lds, s>>>(a, tw, span);
-  else k_rotary<DT, 1, false><<<grid, 256, lds, s>>>(a, tw, span);
+  const int64_t most = MAX_THREADS / 256 * tw;      // tokens of a launch
+  for (int64_t t0 = 0; t0 < a.tokens; t0 += most) {
+    RotaryArgs p = a;
+    p.tokens = a.tokens - t0 < most ? a.tokens - t0 : most;
+    p.positions += t0;
+    for (RotarySide& sd : p.side) {
+      sd.in = (const typename Elem<DT>::T*)sd.in + t0 * sd.its;
+      sd.out = (typename Elem<DT>::T*)sd.out + t0 * sd.ots;
+    }
+    const dim3 grid((unsigned)((p.tokens + tw - 1) / tw), (unsigned)((heads + span - 1) / span));
+    if (vec) k_rotary<DT, E, true><<<grid, 256, lds, s>>>(p, tw, span);
+    else if (n == 2) k_rotary<DT, 2, false><<<grid, 256, lds, s>>>(p, tw, span);
+    else k_rotary<DT, 1, false><<<grid, 256, lds, s>>>(p, tw, span);
+  }
 }
 
 }  // namespace externd
@@ -200,7 +210,7 @@ int externd_rotary(const void* q, void* q_out, int64_t q_token_stride, int64_t q
   a.interleaved = interleaved;
   a.amplitude = amplitude;
   a.sign = inverse ? -1.f : 1.f;
-  if (!k) a.side[1].heads = 0;
+  if (!k) a.side[1] = {};
   const int es = dtype_bytes(dtype), e = 16 / es;
   // 16-byte units: no unit may straddle the halves, the turned part or the head
   bool vec = !((interleaved ? rot_dim : rot_dim / 2) % e) && !((head_dim - rot_dim) % e);

@@ -198,3 +198,12 @@ def test_oracle_gradients_against_differences():
 
 def ref_words(half):
     return np.array([int(2.0 ** 64 / (2 * math.pi) * 1e4 ** (-i / half)) for i in range(half)], dtype=np.int64)
+
+
+def test_more_than_a_launch_holds_is_refused():
+    """A launch holds fewer than 2^32 threads: refused on the host, nothing is launched."""
+    L, d = binding.lib(), D256
+    assert L.externd_token_logprobs(d, 0, 1 << 26, 50, 50, d, 1.0, 4, d, d, d, d, d, None, 0, None) == binding.EUNSUPPORTED
+    for entry in (lambda n: L.externd_kv4_append(d, 1 << 20, 16, 128, 1024, d, d, 1, 2048, 128, 2048, 128, n, 1, d, d, d, 1 << 17, None),
+                  lambda n: L.externd_kv4_read(d, 1 << 20, 16, 128, 1024, d, d, 1, n, 1, d, d, d, 1 << 17, None)):
+        assert entry((1 << 27) - 1) == binding.EUNSUPPORTED
