@@ -527,6 +527,9 @@ def rotary_frequencies(rot_dim: int, base: float = 10000.0, scaling: str = "plai
 
 def _rotary(q, k, positions, freqs, interleaved, amplitude, inverse, out, stream):
     torch = _torch()
+    if stream is not None:      # as on that stream: its own memory for what is allocated here
+        with torch.cuda.stream(stream):
+            return _rotary(q, k, positions, freqs, interleaved, amplitude, inverse, out, None)
     if q.dim() != 3:
         raise ValueError(f"q: expected (tokens, heads, channels), got shape {tuple(q.shape)}")
     tokens, heads, dim = q.shape
@@ -647,6 +650,9 @@ def kv4_read(cache, table, lens, head_dim: int, starts=None, tokens=None, dtype=
     the new tokens that ``starts`` (and their number ``tokens``) names; with
     starts over whole sequences, for all tokens (externd_kv4_read)."""
     torch = _torch()
+    if stream is not None:      # as on that stream: its own memory for what is allocated here
+        with torch.cuda.stream(stream):
+            return kv4_read(cache, table, lens, head_dim, starts, tokens, dtype)
     if tokens is None:
         if starts is not None:
             raise ValueError("tokens: their number is needed with starts")
@@ -682,6 +688,9 @@ def kv4_attention(cache, q, table, lens, starts=None, max_new=None, max_len=None
     Returns (out, lse): tokens x query heads x channels in q's type, and fp32
     tokens x query heads."""
     torch = _torch()
+    if stream is not None:      # as on that stream: its own memory for what is allocated here
+        with torch.cuda.stream(stream):
+            return kv4_attention(cache, q, table, lens, starts, max_new, max_len, scale, window, out, None, workspace)
     if q.dim() != 3:
         raise ValueError(f"q: expected (tokens, heads, channels), got shape {tuple(q.shape)}")
     tokens, heads, dim = q.shape
@@ -742,6 +751,9 @@ def token_logprobs(logits, targets=None, top: int = 0, scale: float = 1.0, strea
     row's entropy, and its ``top`` most likely tokens, the lower index first
     among equals (externd_token_logprobs).  Without targets logprob is None."""
     torch = _torch()
+    if stream is not None:      # as on that stream: its own memory for what is allocated here
+        with torch.cuda.stream(stream):
+            return token_logprobs(logits, targets, top, scale, None, workspace)
     rows, vocab, stride, code = _req_logits(torch, logits, "logits")
     if not 0 <= top <= min(LOGPROBS_MAX_TOP, vocab):
         raise ExterndError(EINVAL, "externd_token_logprobs")
@@ -778,6 +790,9 @@ def token_logprobs_backward(logits, targets, lse, entropy, grad_logprob=None, gr
     entropy (externd_token_logprobs_backward); ``out`` may be the logits
     themselves.  Returns it (rows x vocabulary, the logits' type)."""
     torch = _torch()
+    if stream is not None:      # as on that stream: its own memory for what is allocated here
+        with torch.cuda.stream(stream):
+            return token_logprobs_backward(logits, targets, lse, entropy, grad_logprob, grad_entropy, scale, out)
     rows, vocab, stride, code = _req_logits(torch, logits, "logits")
     ptrs = [None] * 5
     for i, (t, dt, name) in enumerate(((targets, torch.int64, "targets"), (lse, torch.float32, "lse"),

@@ -111,3 +111,35 @@ def test_pages_run_out(example):
 def test_main(example, capsys):
     example.main()
     assert "perplexity" in capsys.readouterr().out
+
+
+def test_a_given_stream_has_its_own_memory(example):
+    """With ``stream`` given, results and workspace come from that stream's memory: what the current
+    stream has freed, with work on it pending, is not written.  The same bits as on the current one."""
+    b, g = example.binding, torch.Generator().manual_seed(3)
+    q, k = torch.randn((40, 8, 64), generator=g).cuda(), torch.randn((40, 2, 64), generator=g).cuda()
+    x = torch.randn((40, 5000), generator=g).cuda()
+    pos, freqs = torch.arange(40, device="cuda"), torch.from_numpy(b.rotary_frequencies(64)[0]).cuda()
+    cache, table = b.kv4_cache(300, 2, 64, 16), torch.arange(300, dtype=torch.int32, device="cuda")[None].contiguous()
+    lens, starts = torch.tensor([40], dtype=torch.int32, device="cuda"), torch.tensor([0, 40], dtype=torch.int32, device="cuda")
+    b.kv4_append(cache, k, k, table, lens, starts)
+    y = torch.arange(40, device="cuda")
+    lse, h = (lambda r: (r.lse, r.entropy))(b.token_logprobs(x, y))
+
+    def calls(**kw):
+        r = list(b.rotary(q, k, pos, freqs, **kw)) + list(b.rotary_backward(q, k, pos, freqs, **kw))
+        r += list(b.kv4_read(cache, table, lens, 64, starts=starts, tokens=40, **kw))
+        r += list(b.kv4_attention(cache, q, table, lens, starts=starts, **kw))
+        t = b.token_logprobs(x, y, top=7, **kw)
+        return r + [t.logprob, t.entropy, t.lse, t.top_logprobs, t.top_ids, b.token_logprobs_backward(x, y, lse, h, h, h, **kw)]
+    want = calls()
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    calls(stream=s)
+    torch.cuda.synchronize()
+    # memory that the current stream has freed must not come back for the other stream
+    free = {torch.empty_like(t).data_ptr() for t in want for _ in range(4)}
+    got = calls(stream=s)
+    s.synchronize()
+    assert all(torch.equal(a, c) for a, c in zip(got, want))
+    assert not free & {t.data_ptr() for t in got}
