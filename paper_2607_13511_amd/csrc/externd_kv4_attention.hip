@@ -679,8 +679,8 @@ __global__ __launch_bounds__(256, DIM <= 128 ? 3 : 2) void k_attention_split(Att
 // falls to 1.8 GHz under both: a wave's step of 64 tokens at 128 channels has 32
 // products of 32 cycles and 328 vector instructions (32 exponentials of 16
 // cycles among them), so a SIMD's two waves have 2048 and 3400 cycles of the
-// 4560 that a step takes.  3.5 K tokens of 32 heads over 12 K in 613 us, 840
-// TFLOP/s.  All waves in one phase: 700 us; conversion among the products: 754;
+// 4560 that a step takes.  3.5 K tokens of 32 heads over 12 K in 600 us, 860
+// TFLOP/s (577 to 613 as the clock allows).  All waves in one phase: 700 us; conversion among the products: 754;
 // rows padded to an odd number of units instead of permuted (48 instructions
 // fewer): 619.
 template <int DIM, int DT>
@@ -1278,6 +1278,7 @@ static bool attention_plan(int heads_q, int heads_kv, int dim, int dtype, int64_
     p->groups = (int)(blocks * heads_kv);
     return true;
   }
+  static_assert(MAX_GROUPS >= 768, "the join looks at as many shares");
   const int64_t most = p->rows == 256 ? 256 : dim <= 128 ? 768 : 512;
   const int64_t fit = (blocks * heads_kv * tiles + 3) / 4;
   p->groups = (int)(most < fit ? most : fit);

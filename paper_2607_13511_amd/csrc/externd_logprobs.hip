@@ -290,8 +290,8 @@ constexpr int MAX_WAVES = 16;
 // one fused multiply-add for y an entry; entries above the bar (the least of
 // the wave's largest so far) are rare, so only their lanes go through LDS.
 // Bound by memory: 2048 rows of 150001 in bf16, 615 MB, in 129 us (4.8 TB/s) with
-// the 20 largest.  8 rows of 65536 in fp32 with the 5 largest in 16 us, 9 without
-// them: sorting, which so few rows cannot hide.
+// the 20 largest, 113 without (5.4).  8 rows of 65536 in fp32 with the 5 largest in
+// 16 us, 10 without: sorting, which so few rows cannot hide.
 template <int DT>
 __global__ __launch_bounds__(64 * MAX_WAVES) void k_logprobs(LogprobArgs a, int64_t each) {
   typedef typename Elem<DT>::T T;
