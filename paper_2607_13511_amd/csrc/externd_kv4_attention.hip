@@ -666,14 +666,20 @@ __global__ __launch_bounds__(256, DIM <= 128 ? 3 : 2) void k_attention_split(Att
 // Every value s (code - z) is exactly an fp16 number and a query row enters as
 // fp16 with its largest entry near 2^15 (exact for bf16 entries within 2^-29
 // of it), so the scores are fp32 sums of exact products; only the softmax weights are
-// rounded (to 11 bits, for the second product; their sum takes them as they are).  S^T leaves a row's scores in two
+// rounded, to fp16 for the second product (their sum takes them as they are):
+// bf16 or fp16 results have 8 or 11 bits, and the values take the other
+// operand's 11 bits whole.  S^T leaves a row's scores in two
 // lanes, whose registers, rounded, are the second product's operand as they
 // are: token order within 16 is free, so V is stored in the order that S^T has.
 //
 // A tile of TT tokens is converted once (4 operations for 2 codes: mask to
 // 1024 + code, subtract 1024 + z, times s) while the tiles before are in work.
-// The weights are taken against a running reference that moves only when a
-// row's maximum passes it by 2^8, so O is rarely rescaled.
+// The weights are taken against a running reference, 2^-7 of the row's maximum
+// when it is set, that moves only when a weight passes 2^15, so O is rarely
+// rescaled and a weight below 2^8 times the maximum of then fits fp16 (65504).
+// So weights have 11 bits down to 2^-21 of that maximum and are 0 only below
+// 2^-32 of it: many weak keys beside a strong one whose value is small are the
+// result.  (Moving at 2^4 times, 2^-25 and 2^-36: 256 channels 1.5 % slower.)
 //
 // Bound by the vector instructions between the products, and by the clock that
 // falls to 1.8 GHz under both: a wave's step of 64 tokens at 128 channels has 32
@@ -692,6 +698,7 @@ __global__ __launch_bounds__(512, 2) void k_attention_chunk(AttnArgs a) {
   constexpr int KU = DIM / 8, VU = TT / 8;          // 16-byte units of a row of K (a token) and of V (a channel)
   constexpr int WB = 8 / PS;                        // waves of a 16-token block
   constexpr int AHEAD = 4;
+  constexpr float UP = 7.f, TOP = 15.f;             // powers of two of the weights (above)
   __shared__ __align__(16) _Float16 kt[3][TT * DIM], vt[3][DIM * TT];
   __shared__ __align__(8) uint8_t flags[3][8];      // of each wave's 8 values' tokens: 1 there, 3 some NaN among them
   __shared__ uint16_t nans[3][8][NG];               // which of the block's tokens
@@ -983,8 +990,8 @@ __global__ __launch_bounds__(512, 2) void k_attention_chunk(AttnArgs a) {
         for (int i = 0; i < 16; i++) top = fmaxf(top, S[s][i]);
       const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
       top = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * factor;
-      if (__any(top > ref + 8.f)) {
-        const float to = fmaxf(ref, top), keep = ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref - to);
+      if (__any(top > ref + TOP)) {
+        const float to = fmaxf(ref, top - UP), keep = ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref - to);
         ref = to;
         l *= keep;
 #pragma unroll
