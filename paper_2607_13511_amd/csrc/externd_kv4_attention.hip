@@ -47,6 +47,12 @@ __device__ __forceinline__ void store_any(void* p, int64_t i, float v, int dtype
   else ((__bf16*)p)[i] = (__bf16)v;
 }
 
+// The first position that a query at `pos` sees.  Positions below 0 see none
+// either way: counted as 0, so that no window leaves 32 bits.
+__device__ __forceinline__ int least_position(const AttnArgs& a, int pos) {
+  return a.window > 0 ? max(max(pos, 0) - a.window + 1, 0) : 0;
+}
+
 // The queries of one sequence and cache head are rows: row r is new token
 // r / each, query head r % each of the cache head.  A row block (ROWS rows)
 // sees the tokens lo .. hi - 1 among it, in tiles of 64.
@@ -71,7 +77,7 @@ __device__ __forceinline__ RowBlock row_block(const AttnArgs& a, int b, int rb) 
   r.r0 = rb * ROWS;
   const int r1 = min(r.rows, r.r0 + ROWS) - 1;
   r.hi = min(held, r.first + (r1 < 0 ? 0 : r1 / a.each) + 1);
-  r.lo = a.window > 0 ? max(0, r.first + r.r0 / a.each - a.window + 1) & ~63 : 0;
+  r.lo = least_position(a, r.first + r.r0 / a.each) & ~63;
   r.tiles = (max(0, r.hi - r.lo) + 63) >> 6;
   return r;
 }
@@ -462,7 +468,7 @@ __global__ __launch_bounds__(256, DIM <= 128 ? 3 : 2) void k_attention_split(Att
     float m = -INFINITY, l = 0.f;
     const int row = R.r0 + seg, pos = R.first + row / a.each;
     const int last = row < R.rows ? min(pos, c1 - 1) : -1;
-    const int least = a.window > 0 ? pos - a.window + 1 : 0;
+    const int least = least_position(a, pos);
 #pragma unroll
     for (int i = 0; i < 2 * NC; i++) O[i] = 0.f;
     // One tile: K's registers are free once the scores are there and take the
@@ -777,7 +783,7 @@ __global__ __launch_bounds__(512, 2) void k_attention_chunk(AttnArgs a) {
     }
     const int pos = R.first + row / a.each;
     const int last = row < R.rows ? min(pos, c1 - 1) : -1;
-    const int least = a.window > 0 ? pos - a.window + 1 : 0;
+    const int least = least_position(a, pos);
     // over the wave: where every row sees every token
     int all_from = row < R.rows ? least : INT_MIN, all_to = row < R.rows ? last : INT_MAX;
     for (int d = 16; d; d >>= 1) {

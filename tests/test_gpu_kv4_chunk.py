@@ -128,3 +128,22 @@ def test_weak_keys_beside_a_dominating_one(ext, dtype, nats):
     # as many tiles as for 10^6 tokens: the form with 256 rows a workgroup, and parts that are joined
     assert ext.kv4_attention_workspace_bytes(heads_q, 1, dim, q.dtype, new, 1, new, 10 ** 6) > 768 * (8 * (dim + 4) * 4 + 32)
     check(ext, c, q, dtype, max_len=10 ** 6)
+
+
+# ---------------------------------------------------------------------------
+# windows
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("lens,news", [([7, 30], [12, 1]), ([500, 90], [505, 40])])
+@pytest.mark.parametrize("window", [500, (1 << 31) - 1, (1 << 31) - 3])
+def test_windows_past_all_positions(ext, lens, news, window):
+    """A window wider than any distance masks nothing, also where a sequence holds fewer tokens than it has new ones
+    (positions below 0): the bits of the call without one."""
+    rng = np.random.default_rng(1)
+    ks, vs = ([rng.standard_normal((n, 2, 64)) for n in lens] for _ in range(2))
+    cache, table, dlens, starts = Cache(ks, vs, news, 32).gpu()
+    for dtype in (torch.float32, torch.bfloat16):
+        q = torch.randn((sum(news), 32, 64), device="cuda").to(dtype)
+        a, al = ext.kv4_attention(cache, q, table, dlens, starts=starts, max_new=max(news))
+        b, bl = ext.kv4_attention(cache, q, table, dlens, starts=starts, max_new=max(news), window=window)
+        assert torch.equal(a, b) and torch.equal(al, bl)
+        assert torch.isneginf(al[:5]).all() and torch.isfinite(al[5:]).all()
