@@ -710,6 +710,7 @@ def kv4_attention(cache, q, table, lens, starts=None, max_new=None, max_len=None
         max_len = table.shape[1] * page
     if scale is None:
         scale = dim ** -0.5
+    window = min(window, 0x7FFFFFFF)      # positions are below 2^31
     L = lib()
     nbytes = L.externd_kv4_attention_workspace_bytes(heads, kv, dim, code, tokens, batch, max_new, max_len)
     wp = None

@@ -134,7 +134,7 @@ def test_weak_keys_beside_a_dominating_one(ext, dtype, nats):
 # windows
 # ---------------------------------------------------------------------------
 @pytest.mark.parametrize("lens,news", [([7, 30], [12, 1]), ([500, 90], [505, 40])])
-@pytest.mark.parametrize("window", [500, (1 << 31) - 1, (1 << 31) - 3])
+@pytest.mark.parametrize("window", [500, (1 << 31) - 1, (1 << 31) - 3, 1 << 31, (1 << 32) + 5, 1 << 40])
 def test_windows_past_all_positions(ext, lens, news, window):
     """A window wider than any distance masks nothing, also where a sequence holds fewer tokens than it has new ones
     (positions below 0): the bits of the call without one."""
