@@ -77,8 +77,8 @@ __device__ __forceinline__ RowBlock row_block(const AttnArgs& a, int b, int rb) 
   r.r0 = rb * ROWS;
   const int r1 = min(r.rows, r.r0 + ROWS) - 1;
   r.hi = min(held, r.first + (r1 < 0 ? 0 : r1 / a.each) + 1);
-  r.lo = least_position(a, r.first + r.r0 / a.each) & ~63;
-  r.tiles = (max(0, r.hi - r.lo) + 63) >> 6;
+  r.lo = least_position(a, r.first + min(r.r0, max(r.rows - 1, 0)) / a.each) & ~63;
+  r.tiles = ((max(0, r.hi - r.lo) - 1) >> 6) + 1;      // lengths up to 2^31 - 1
   return r;
 }
 
@@ -345,12 +345,12 @@ __global__ __launch_bounds__(256, DIM <= 128 ? 3 : 2) void k_attention_split(Att
     uint64_t ok = 0;        // bit 16 t: block t of the tile has a page (as lanes say)
     // table entry of this lane's block (seg) of a tile; only read here, so that nothing waits for it yet
     auto entry = [&](int tile) -> int {
-      const unsigned tok = min((unsigned)c0 + (unsigned)(tile * 64 + seg * 16), (unsigned)(c1 - 1));
+      const unsigned tok = min((unsigned)c0 + (unsigned)tile * 64 + seg * 16, (unsigned)(c1 - 1));
       return a.s.table[(int64_t)b * a.s.table_pages + (tok >> a.c.page_log2)];
     };
     // its page's place in the cache; `has`: whether there is one (a page for no tokens reads page 0)
     auto place = [&](int tile, int page, bool* has) -> uint64_t {
-      *has = (unsigned)c0 + (unsigned)(tile * 64 + seg * 16) < (unsigned)c1 && page >= 0 && page < a.c.num_pages;
+      *has = (unsigned)c0 + (unsigned)tile * 64 + seg * 16 < (unsigned)c1 && page >= 0 && page < a.c.num_pages;
       return (uint64_t)((int64_t)(*has ? page : 0) * a.c.heads + h) * (uint64_t)a.c.head_bytes;
     };
     auto base_of = [&](uint64_t off, int t) -> const uint8_t* {
@@ -362,7 +362,7 @@ __global__ __launch_bounds__(256, DIM <= 128 ? 3 : 2) void k_attention_split(Att
 #pragma unroll
       for (int t = 0; t < 4; t++) {
         const uint8_t* base = base_of(off, t);
-        const unsigned o = (unsigned)((c0 + tile * 64 + 16 * t) & (P - 1)) + l16;
+        const unsigned o = (((unsigned)c0 + (unsigned)tile * 64 + 16 * t) & (P - 1)) + l16;
         const uint8_t* kp = base + o * HALF + seg * (DIM == 64 ? 8 : 16);
         if constexpr (DIM == 64) {
           const v2u x = *(const v2u*)kp;
@@ -377,17 +377,17 @@ __global__ __launch_bounds__(256, DIM <= 128 ? 3 : 2) void k_attention_split(Att
       }
     };
     auto load_v = [&](int tile, uint64_t off) {
-      const int tok = c0 + tile * 64;
+      const unsigned tok = (unsigned)c0 + (unsigned)tile * 64;
 #pragma unroll
       for (int t = 0; t < 4; t++) {
         if constexpr (NG > 1) {
-          const unsigned o = (unsigned)((tok + 16 * t) & (P - 1)) + l16;
+          const unsigned o = ((tok + 16 * t) & (P - 1)) + l16;
           const unsigned* wp = (const unsigned*)(base_of(off, t) + (unsigned)P * DIM + o * (4 * NG)) + NW;
 #pragma unroll
           for (int g = 0; g < NW; g++) vw[t][g] = wp[g];
         }
       }
-      const uint8_t* vp = a.cache + off + (unsigned)P * HALF + ((unsigned)((tok + 16 * seg) & (P - 1)) >> 4) * (HALF * 16) + l16 * 16;
+      const uint8_t* vp = a.cache + off + (unsigned)P * HALF + (((tok + 16 * seg) & (P - 1)) >> 4) * (HALF * 16) + l16 * 16;
 #pragma unroll
       for (int c = 0; c < NC; c++) vr[c] = *(const v4u*)(vp + c * 256);
     };
@@ -466,7 +466,7 @@ __global__ __launch_bounds__(256, DIM <= 128 ? 3 : 2) void k_attention_split(Att
     }
     const float factor = row_factor[seg];
     float m = -INFINITY, l = 0.f;
-    const int row = R.r0 + seg, pos = R.first + row / a.each;
+    const int row = R.r0 + seg, pos = R.first + min(row, R.rows - 1) / a.each;
     const int last = row < R.rows ? min(pos, c1 - 1) : -1;
     const int least = least_position(a, pos);
 #pragma unroll
@@ -781,8 +781,8 @@ __global__ __launch_bounds__(512, 2) void k_attention_chunk(AttnArgs a) {
       // above 0, so that a masked score of -infinity stays one
       factor = bad ? NAN : fmaxf(ldexpf(fabsf(a.scale) * 1.44269504088896340736f, e - 15), 1.17549435e-38f);
     }
-    const int pos = R.first + row / a.each;
-    const int last = row < R.rows ? min(pos, c1 - 1) : -1;
+    const int pos = R.first + min(row, R.rows - 1) / a.each;
+    const int last = row < R.rows ? max(min(pos, c1 - 1), -1) : -1;
     const int least = least_position(a, pos);
     // over the wave: where every row sees every token
     int all_from = row < R.rows ? least : INT_MIN, all_to = row < R.rows ? last : INT_MAX;
@@ -802,7 +802,7 @@ __global__ __launch_bounds__(512, 2) void k_attention_chunk(AttnArgs a) {
 #pragma unroll
     for (int g = 0; g < NG; g++) poison[g] = 0.f;
 
-    const int ntiles = (c1 - c0 + TT - 1) / TT;
+    const int ntiles = (c1 - c0 - 1) / TT + 1;
     struct KRaw {
       v2u codes;
       unsigned words[(NG + 1) / 2];
@@ -811,9 +811,11 @@ __global__ __launch_bounds__(512, 2) void k_attention_chunk(AttnArgs a) {
       unsigned codes[2], words[(NG + 1) / 2];      // words: of the token that lane % 8 stands for
     };
     const int vtok = 4 * vhalf + (lane & 3) + (lane & 4) * 2;
-    // table entry of this wave's block of a tile; only read here, so that nothing waits for it yet
+    // this wave's block of a tile; may be past the part's end, and 2^31
+    auto tile_at = [&](int tile) -> unsigned { return (unsigned)c0 + (unsigned)tile * TT + block * 16; };
+    // its table entry; only read here, so that nothing waits for it yet
     auto entry = [&](int tile) -> int {
-      const unsigned tok = min((unsigned)c0 + (unsigned)(tile * TT + block * 16), (unsigned)(c1 - 1));
+      const unsigned tok = min(tile_at(tile), (unsigned)(c1 - 1));
       return a.s.table[(int64_t)b * a.s.table_pages + (tok >> a.c.page_log2)];
     };
     // where the block is; no page (past the part's end as well): page 0, so that all loads are always issued and their
@@ -826,19 +828,19 @@ __global__ __launch_bounds__(512, 2) void k_attention_chunk(AttnArgs a) {
     const uint8_t* const head_base = a.cache + h * a.c.head_bytes;
     auto place_at = [&](int tile, int page) -> Place {
       page = __builtin_amdgcn_readfirstlane(page);
-      const bool there = (unsigned)c0 + (unsigned)(tile * TT + block * 16) < (unsigned)c1 && (unsigned)page < (unsigned)a.c.num_pages;
+      const bool there = tile_at(tile) < (unsigned)c1 && (unsigned)page < (unsigned)a.c.num_pages;
       return {head_base + (there ? page : 0) * page_bytes, there};
     };
     auto load_k = [&](KRaw& r, int tile, const Place& pl) {
       const uint8_t* base = pl.base;
-      const int t = ((c0 + tile * TT + block * 16) & (P - 1)) + (ktok & 15);
+      const int t = (int)(tile_at(tile) & (P - 1)) + (ktok & 15);
       r.codes = *(const v2u*)(base + t * HALF + kunit * 8);
 #pragma unroll
       for (int g = 0; g < (NG + 1) / 2; g++) r.words[g] = ((const unsigned*)(base + (unsigned)P * DIM + t * (4 * NG)))[g];
     };
     auto load_v = [&](VRaw& r, int tile, const Place& pl) {
       const uint8_t* base = pl.base;
-      const int o = (c0 + tile * TT + block * 16) & (P - 1);
+      const int o = (int)(tile_at(tile) & (P - 1));
       const unsigned* vp = (const unsigned*)(base + (unsigned)P * HALF + (o >> 4) * (HALF * 16) + (vin ? vcol : 0) * 16);
       r.codes[0] = vp[vhalf];
       r.codes[1] = vp[2 + vhalf];
@@ -877,7 +879,7 @@ __global__ __launch_bounds__(512, 2) void k_attention_chunk(AttnArgs a) {
     };
     auto convert_v = [&](int buf, int tile, bool there, const VRaw& raw) {
         // V: words of tokens that are not there count as 0, NaN ones too (kept as bits)
-        const bool in = there && c0 + tile * TT + block * 16 + vtok < c1;
+        const bool in = there && tile_at(tile) + vtok < (unsigned)c1;
         unsigned flag = there, bad[(NG + 1) / 2], scale[NG][4], minus[NG][4];
 #pragma unroll
         for (int g = 0; g < (NG + 1) / 2; g++) {

@@ -147,3 +147,41 @@ def test_windows_past_all_positions(ext, lens, news, window):
         b, bl = ext.kv4_attention(cache, q, table, dlens, starts=starts, max_new=max(news), window=window)
         assert torch.equal(a, b) and torch.equal(al, bl)
         assert torch.isneginf(al[:5]).all() and torch.isfinite(al[5:]).all()
+
+
+# ---------------------------------------------------------------------------
+# lengths up to 2^31 - 1
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_lengths_to_the_end_of_32_bits(ext, dim):
+    """The last tokens of a sequence of 2^31 - 1 whose other pages are none, beside the same tokens in a short sequence:
+    with a window the same tiles and bits, without one the same numbers (other parts are joined)."""
+    page, heads_q = 1024, 32
+    n, short = (1 << 31) - 1, 2047                        # alike modulo the page
+    rng = np.random.default_rng(dim)
+    c = Cache([rng.standard_normal((short, 1, dim))], [rng.standard_normal((short, 1, dim))], [1], page)
+    cache, table, lens, _ = c.gpu()
+    far = torch.full((1, 1 << 21), -1, dtype=torch.int32, device="cuda")
+    far[0, -2:] = table[0]
+    far_lens = torch.tensor([n], dtype=torch.int32, device="cuda")
+    for dtype, new in ((torch.float32, 1), (torch.bfloat16, 1), (torch.bfloat16, 40)):
+        q = torch.randn((new, heads_q, dim), device="cuda").to(dtype)
+        starts = torch.tensor([0, new], dtype=torch.int32, device="cuda")
+        kw = dict(starts=starts, max_new=new, max_len=10 ** 6)
+        for window in (1, 100, 0):
+            a, al = ext.kv4_attention(cache, q, far, far_lens, window=window, **kw)
+            b, bl = ext.kv4_attention(cache, q, table, lens, window=window, **kw)
+            torch.cuda.synchronize()
+            assert torch.isfinite(bl).all()
+            if window:
+                assert torch.equal(a, b) and torch.equal(al, bl)
+            else:      # sums of the same terms in another order: a few units of fp32, and one of the result's type
+                unit = 2.0 ** -20 if dtype is torch.float32 else 2.0 ** -7
+                assert torch.allclose(a.float(), b.float(), rtol=unit, atol=unit / 64) and torch.allclose(al, bl, rtol=1e-6, atol=1e-5)
+    # whole sequences, new tokens and all: kept and read at the end
+    k = torch.randn((3, 1, dim), device="cuda")
+    starts = torch.tensor([0, 3], dtype=torch.int32, device="cuda")
+    ext.kv4_append(cache, k, k, far, far_lens, starts=starts)
+    got, _ = ext.kv4_read(cache, table, lens, dim, starts=starts, tokens=3)
+    far_got, _ = ext.kv4_read(cache, far, far_lens, dim, starts=starts, tokens=3)
+    assert torch.equal(got, far_got) and (got != 0).any()
