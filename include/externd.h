@@ -506,7 +506,8 @@ int externd_kv4_read(const void* cache, int64_t num_pages, int32_t heads_kv, int
  *  max_len    the largest length, or more; 0: not known.  Both only choose
  *             the launch: results hold whatever they are.
  *  heads_q a multiple of heads_kv, heads_q / heads_kv <= 64; scale finite;
- *  window >= 0; batch <= 65535, tokens heads_q < 2^31.
+ *  window >= 0; batch <= 65535, tokens heads_q < 2^31 - 1024, and with R the
+ *  lesser of table_pages page_tokens and 2^31 - 1, (R / 64 + 16) heads_kv < 2^31.
  *  workspace  device, >= externd_kv4_attention_workspace_bytes() bytes for the
  *             same sizes, 256-byte aligned (may be NULL where that is 0).
  * The arithmetic: sums, maxima and lse are fp32.  Few rows a cache head: q as

@@ -1357,7 +1357,11 @@ int externd_kv4_attention(const void* cache, int64_t num_pages, int32_t heads_kv
   if (!cache || ((uintptr_t)cache & 15) || !lens || !table || table_pages < 1 || window < 0 || !std::isfinite(scale) ||
       (!starts && tokens != batch) || (tokens && (!q || !out)))
     return EXTERND_EINVAL;
-  if (tokens > INT32_MAX || tokens * heads_q > INT32_MAX || batch > 65535 || heads_q > 65535 || table_pages > INT32_MAX) return EXTERND_EUNSUPPORTED;
+  // rows of a sequence are counted in whole blocks of 256, and the units of a row block over all cache heads
+  if (tokens > INT32_MAX || tokens * heads_q > INT32_MAX - 1024 || batch > 65535 || heads_q > 65535 || table_pages > INT32_MAX)
+    return EXTERND_EUNSUPPORTED;
+  const int64_t room = table_pages * page_tokens < INT32_MAX ? table_pages * page_tokens : INT32_MAX;
+  if ((room / 64 + 16) * heads_kv > INT32_MAX) return EXTERND_EUNSUPPORTED;
   const size_t need =
       externd_kv4_attention_workspace_bytes(heads_q, heads_kv, head_dim, dtype, tokens, batch, max_new, max_len);
   if (need && (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 255))) return EXTERND_EWORKSPACE;
