@@ -518,8 +518,8 @@ int externd_kv4_read(const void* cache, int64_t num_pages, int32_t heads_kv, int
  * largest lose bits), scores exact products summed in fp32, weights rounded to
  * fp16 for their product with the values (11 bits of those above 2^-21 of the
  * row's largest, none of those below 2^-32).
- * A NaN or an infinity in q makes that row NaN; NaN values make those rows
- * NaN that see them.                                                       */
+ * A NaN or an infinity in q makes that row NaN where it sees a position; NaN
+ * values make those rows NaN that see them.                                                       */
 size_t externd_kv4_attention_workspace_bytes(int32_t heads_q, int32_t heads_kv, int32_t head_dim, int32_t dtype,
                                              int64_t tokens, int32_t batch, int32_t max_new, int64_t max_len);
 int externd_kv4_attention(const void* cache, int64_t num_pages, int32_t heads_kv, int32_t head_dim,

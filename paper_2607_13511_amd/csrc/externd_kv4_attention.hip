@@ -776,10 +776,10 @@ __global__ __launch_bounds__(512, 2) void k_attention_chunk(AttnArgs a) {
         float x[8];
         Vec<DT>::unpack(raw[k], x);
 #pragma unroll
-        for (int j = 0; j < 8; j++) Q[k][j] = (_Float16)(bad ? 0.f : ldexpf(sign * x[order[j]], 15 - e));
+        for (int j = 0; j < 8; j++) Q[k][j] = (_Float16)(bad ? NAN : ldexpf(sign * x[order[j]], 15 - e));
       }
-      // above 0, so that a masked score of -infinity stays one
-      factor = bad ? NAN : fmaxf(ldexpf(fabsf(a.scale) * 1.44269504088896340736f, e - 15), 1.17549435e-38f);
+      // above 0 and finite, so that a masked score of -infinity stays one (a row with a NaN among its entries sees NaN)
+      factor = bad ? 1.f : fmaxf(ldexpf(fabsf(a.scale) * 1.44269504088896340736f, e - 15), 1.17549435e-38f);
     }
     const int pos = R.first + min(row, R.rows - 1) / a.each;
     const int last = row < R.rows ? max(min(pos, c1 - 1), -1) : -1;

@@ -185,3 +185,31 @@ def test_lengths_to_the_end_of_32_bits(ext, dim):
     got, _ = ext.kv4_read(cache, table, lens, dim, starts=starts, tokens=3)
     far_got, _ = ext.kv4_read(cache, far, far_lens, dim, starts=starts, tokens=3)
     assert torch.equal(got, far_got) and (got != 0).any()
+
+
+# ---------------------------------------------------------------------------
+# queries that are not finite
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("max_len", [None, 10 ** 6])      # one launch, and parts that are joined
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+def test_nonfinite_queries_that_see_nothing(ext, dtype, max_len, bad):
+    """A query that sees no key gives 0 and -infinity whatever it holds; one that sees any gives NaN; no other row changes."""
+    lens, news, heads_q, dim = [500, 90], [505, 40], 16, 64
+    c = random_cache(lens, news, 1, dim, 16, 4)
+    c.table[1, 0] = -1                                    # the first 16 positions of the second sequence
+    c.lens[1] = 20                                        # its first 36 new tokens see nothing, 4 see a page
+    q = torch.randn((sum(news), heads_q, dim), device="cuda").to(TYPES.get(dtype, (torch.float32,))[0])
+    cache, table, dlens, starts = c.gpu()
+    kw = dict(starts=starts, max_new=max(news), max_len=max_len)
+    want, wl = ext.kv4_attention(cache, q, table, dlens, **kw)
+    sees = torch.tensor([t >= 5 for t in range(505)] + [t >= 36 for t in range(40)], device="cuda")
+    assert torch.isfinite(want).all() and torch.equal(torch.isfinite(wl), sees[:, None].expand(-1, heads_q))
+    hit = torch.zeros((sum(news), heads_q), dtype=torch.bool, device="cuda")
+    hit[::3, 1::5] = True
+    q2 = q.clone()
+    q2[..., 7] = torch.where(hit, torch.full_like(q[..., 7], bad), q[..., 7])
+    got, gl = ext.kv4_attention(cache, q2, table, dlens, **kw)
+    nan = hit & sees[:, None]
+    assert torch.isnan(got[nan]).all() and torch.isnan(gl[nan]).all()
+    assert torch.equal(got[~nan], want[~nan]) and torch.equal(gl[~nan], wl[~nan])
