@@ -705,6 +705,7 @@ __global__ __launch_bounds__(512, 2) void k_attention_chunk(AttnArgs a) {
   constexpr int WB = 8 / PS;                        // waves of a 16-token block
   constexpr int AHEAD = 4;
   constexpr float UP = 7.f, TOP = 15.f;             // powers of two of the weights (above)
+  constexpr float BAD = 5.87747175e-39f;            // 2^-127
   __shared__ __align__(16) _Float16 kt[3][TT * DIM], vt[3][DIM * TT];
   __shared__ __align__(8) uint8_t flags[3][8];      // of each wave's 8 values' tokens: 1 there, 3 some NaN among them
   __shared__ uint16_t nans[3][8][NG];               // which of the block's tokens
@@ -776,10 +777,10 @@ __global__ __launch_bounds__(512, 2) void k_attention_chunk(AttnArgs a) {
         float x[8];
         Vec<DT>::unpack(raw[k], x);
 #pragma unroll
-        for (int j = 0; j < 8; j++) Q[k][j] = (_Float16)(bad ? NAN : ldexpf(sign * x[order[j]], 15 - e));
+        for (int j = 0; j < 8; j++) Q[k][j] = (_Float16)(bad ? 0.f : ldexpf(sign * x[order[j]], 15 - e));
       }
-      // above 0 and finite, so that a masked score of -infinity stays one (a row with a NaN among its entries sees NaN)
-      factor = bad ? 1.f : fmaxf(ldexpf(fabsf(a.scale) * 1.44269504088896340736f, e - 15), 1.17549435e-38f);
+      // above 0, so that a masked score of -infinity stays one; below the least of other rows marks a row that is NaN
+      factor = bad ? BAD : fmaxf(ldexpf(fabsf(a.scale) * 1.44269504088896340736f, e - 15), 1.17549435e-38f);
     }
     const int pos = R.first + min(row, R.rows - 1) / a.each;
     const int last = row < R.rows ? max(min(pos, c1 - 1), -1) : -1;
@@ -1093,6 +1094,7 @@ __global__ __launch_bounds__(512, 2) void k_attention_chunk(AttnArgs a) {
 
     const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
     l = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+    if (factor == BAD && l > 0.f) l = NAN;      // some token is seen
 #pragma unroll
     for (int g = 0; g < NG; g++) poison[g] += __shfl_xor(poison[g], 32);
     if (row < R.rows) {
