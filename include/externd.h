@@ -500,7 +500,8 @@ int externd_kv4_read(const void* cache, int64_t num_pages, int32_t heads_kv, int
  * over the positions j <= p, and j > p - window where window > 0.  No such j
  * (an empty sequence, a position below 0, pages without tokens): out 0 and
  * lse -infinity.
- *  q          device, tokens x heads_q x head_dim; out device, dense, the same.
+ *  q          device, tokens x heads_q x head_dim; out device, dense, the same,
+ *             at any entry of its type.
  *  lse        device fp32, tokens x heads_q, or NULL.
  *  max_new    the largest number of new tokens of one sequence, or more.
  *  max_len    the largest length, or more; 0: not known.  Both only choose

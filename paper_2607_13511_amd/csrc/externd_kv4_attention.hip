@@ -11,6 +11,7 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef v2u v2u_any __attribute__((aligned(2)));      // 8 bytes at any entry of a 16-bit type (one store all the same)
 
 // A row block that a workgroup begins and others go on with.
 struct AttnShare {
@@ -1116,7 +1117,7 @@ __global__ __launch_bounds__(512, 2) void k_attention_chunk(AttnArgs a) {
             for (int j = 0; j < 2; j++)
               w[j] = (unsigned)__builtin_bit_cast(uint16_t, Elem<DT>::store(o[2 * j])) |
                      (unsigned)__builtin_bit_cast(uint16_t, Elem<DT>::store(o[2 * j + 1])) << 16;
-            *(v2u*)((T*)a.out + to * DIM + d) = w;
+            *(v2u_any*)((T*)a.out + to * DIM + d) = w;
           }
         }
       if (whole && a.lse && !half) a.lse[to] = none ? -INFINITY : (ref + log2f(l)) * 0.69314718055994530942f;

@@ -213,3 +213,25 @@ def test_nonfinite_queries_that_see_nothing(ext, dtype, max_len, bad):
     nan = hit & sees[:, None]
     assert torch.isnan(got[nan]).all() and torch.isnan(gl[nan]).all()
     assert torch.equal(got[~nan], want[~nan]) and torch.equal(gl[~nan], wl[~nan])
+
+
+# ---------------------------------------------------------------------------
+# alignment
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("max_len", [None, 10 ** 6])
+def test_results_at_any_place(ext, dtype, dim, max_len):
+    """``out`` as a dense view that starts at any entry: the bits of an aligned one, and nothing beside it."""
+    c = random_cache([300, 70], [300, 33], 1, dim, 32, 5)
+    heads_q, n = 32, 333 * 32 * dim
+    t = TYPES.get(dtype, (torch.float32,))[0]
+    q = torch.randn((333, heads_q, dim), device="cuda").to(t)
+    cache, table, lens, starts = c.gpu()
+    kw = dict(starts=starts, max_new=300, max_len=max_len)
+    want, wl = ext.kv4_attention(cache, q, table, lens, **kw)
+    for lead in (1, 2, 3):
+        flat = torch.zeros(n + 8, device="cuda", dtype=t)
+        got, gl = ext.kv4_attention(cache, q, table, lens, out=flat[lead:lead + n].view(333, heads_q, dim), **kw)
+        assert torch.equal(got, want) and torch.equal(gl, wl)
+        assert (flat[:lead] == 0).all() and (flat[lead + n:] == 0).all()
