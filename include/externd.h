@@ -519,10 +519,16 @@ int externd_kv4_read(const void* cache, int64_t num_pages, int32_t heads_kv, int
  * largest lose bits), scores exact products summed in fp32, weights rounded to
  * fp16 for their product with the values (11 bits of those above 2^-21 of the
  * row's largest, none of those below 2^-32).
- * A NaN or an infinity in q makes that row NaN where it sees a position; NaN
- * values make those rows NaN that see them.                                                       */
+ * A NaN or an infinity in q makes that row NaN where it sees a position, and so
+ * does a NaN key; a NaN value makes its 64 channels NaN in the rows that see it.
+ */
 size_t externd_kv4_attention_workspace_bytes(int32_t heads_q, int32_t heads_kv, int32_t head_dim, int32_t dtype,
                                              int64_t tokens, int32_t batch, int32_t max_new, int64_t max_len);
+/* Rows (new tokens x query heads of one cache head) that a workgroup of such a
+ * call takes together: 4, the arithmetic of few rows above, or 256, that of
+ * many rows; 0 on invalid arguments.                                        */
+int32_t externd_kv4_attention_block_rows(int32_t heads_q, int32_t heads_kv, int32_t head_dim, int32_t dtype,
+                                         int64_t tokens, int32_t batch, int32_t max_new, int64_t max_len);
 int externd_kv4_attention(const void* cache, int64_t num_pages, int32_t heads_kv, int32_t head_dim,
                           int32_t page_tokens, const void* q, int32_t dtype, int64_t q_token_stride,
                           int64_t q_head_stride, int32_t heads_q, void* out, float* lse, int64_t tokens,

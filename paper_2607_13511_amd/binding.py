@@ -78,6 +78,7 @@ _SIGNATURES = {
                                         _c_i32, _c_ptr, _c_ptr, _c_ptr, _c_i64, _c_ptr]),
     "externd_kv4_attention_workspace_bytes": (_c_size, [_c_i32, _c_i32, _c_i32, _c_i32, _c_i64, _c_i32, _c_i32,
                                                         _c_i64]),
+    "externd_kv4_attention_block_rows": (_c_i32, [_c_i32, _c_i32, _c_i32, _c_i32, _c_i64, _c_i32, _c_i32, _c_i64]),
     "externd_kv4_attention": (ctypes.c_int, [_c_ptr, _c_i64, _c_i32, _c_i32, _c_i32, _c_ptr, _c_i32, _c_i64, _c_i64,
                                              _c_i32, _c_ptr, _c_ptr, _c_i64, _c_i32, _c_i32, _c_i64, _c_ptr, _c_ptr,
                                              _c_ptr, _c_i64, ctypes.c_float, _c_i32, _c_ptr, _c_size, _c_ptr]),
@@ -676,6 +677,13 @@ def kv4_attention_workspace_bytes(heads_q: int, heads_kv: int, head_dim: int, dt
     return int(lib().externd_kv4_attention_workspace_bytes(heads_q, heads_kv, head_dim,
                                                            _dtype_code(_torch(), dtype, "dtype"), tokens, batch,
                                                            max_new, max_len))
+
+
+def kv4_attention_block_rows(heads_q: int, heads_kv: int, head_dim: int, dtype, tokens: int, batch: int, max_new: int = 1,
+                             max_len: int = 0) -> int:
+    """4 or 256: which of its two kernels ``kv4_attention`` takes (externd_kv4_attention_block_rows)."""
+    return int(lib().externd_kv4_attention_block_rows(heads_q, heads_kv, head_dim, _dtype_code(_torch(), dtype, "dtype"),
+                                                      tokens, batch, max_new, max_len))
 
 
 def kv4_attention(cache, q, table, lens, starts=None, max_new=None, max_len=None, scale=None, window: int = 0, out=None,

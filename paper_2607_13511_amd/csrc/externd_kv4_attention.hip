@@ -1348,6 +1348,15 @@ size_t externd_kv4_attention_workspace_bytes(int32_t heads_q, int32_t heads_kv, 
   return most;
 }
 
+int32_t externd_kv4_attention_block_rows(int32_t heads_q, int32_t heads_kv, int32_t head_dim, int32_t dtype,
+                                         int64_t tokens, int32_t batch, int32_t max_new, int64_t max_len) {
+  Plan p;
+  if (!attention_sizes_ok(heads_q, heads_kv, head_dim, dtype, tokens, batch, max_new, max_len) ||
+      !attention_plan(heads_q, heads_kv, head_dim, dtype, tokens, batch, true, max_new, max_len, &p))
+    return 0;
+  return p.rows;      // the same with and without starts
+}
+
 int externd_kv4_attention(const void* cache, int64_t num_pages, int32_t heads_kv, int32_t head_dim,
                           int32_t page_tokens, const void* q, int32_t dtype, int64_t q_token_stride,
                           int64_t q_head_stride, int32_t heads_q, void* out, float* lse, int64_t tokens,

@@ -25,3 +25,15 @@ def test_rows_in_whole_blocks():
     """Rows rounded up to blocks of 256, and one block more."""
     assert call(1, 1, (1 << 31) - 100, 1, 4) == binding.EUNSUPPORTED
     assert call(64, 1, (1 << 25) - 1, 1, 4) == binding.EUNSUPPORTED
+
+
+def test_block_rows():
+    """Which kernel a call takes: fp32 and few rows or little work 4, many rows of a 16-bit type 256."""
+    f = binding.lib().externd_kv4_attention_block_rows
+    assert f(32, 8, 128, 1, 4096, 2, 2048, 12001) == 256 and f(32, 8, 128, 2, 4096, 2, 2048, 0) == 256
+    assert f(32, 8, 128, 0, 4096, 2, 2048, 12001) == 4               # fp32
+    assert f(32, 8, 128, 1, 32, 32, 1, 16384) == 4                   # single tokens
+    assert f(8, 2, 128, 1, 64, 1, 64, 64) == 4                       # little work
+    for bad in [(33, 8, 128, 1, 1, 1, 1, 0), (32, 8, 96, 1, 1, 1, 1, 0), (32, 8, 128, 3, 1, 1, 1, 0), (32, 8, 128, 1, -1, 1, 1, 0),
+                (32, 8, 128, 1, 1, 0, 1, 0), (32, 8, 128, 1, 1, 1, 0, 0), (32, 8, 128, 1, 1, 1, 1, -1)]:
+        assert f(*bad) == 0
