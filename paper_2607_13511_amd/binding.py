@@ -723,7 +723,10 @@ def kv4_attention(cache, q, table, lens, starts=None, max_new=None, max_len=None
     nbytes = L.externd_kv4_attention_workspace_bytes(heads, kv, dim, code, tokens, batch, max_new, max_len)
     wp = None
     if workspace is not None:
-        wp, nbytes = workspace.data_ptr(), workspace.numel()
+        if not (workspace.is_cuda and workspace.is_contiguous()):
+            raise ValueError(f"workspace: expected a contiguous CUDA tensor, got {tuple(workspace.shape)} "
+                             f"{workspace.stride()} on {workspace.device}")
+        wp, nbytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
     elif nbytes:
         workspace = cache.new_empty((nbytes,))
         wp = workspace.data_ptr()

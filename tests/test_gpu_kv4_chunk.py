@@ -387,3 +387,24 @@ def test_wide_kernel_same_bits_every_time(ext):
         g.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, ext.kv4_attention(cache, q, table, lens, **kw)[0])
+
+
+def test_workspaces(ext):
+    """A given workspace is device memory without gaps and is counted in bytes; any other is refused before a launch."""
+    c = random_cache([900], [1], 1, 64, 64, 10)
+    cache, table, lens, starts = c.gpu()
+    q = queries(c, 8, "bf16")
+    kw = dict(starts=starts, max_new=1, max_len=10 ** 5)
+    need = ext.kv4_attention_workspace_bytes(8, 1, 64, q.dtype, 1, 1, 1, 10 ** 5)
+    assert need > 0 and need % 256 == 0
+    want, wl = ext.kv4_attention(cache, q, table, lens, **kw)
+    for ws in (torch.empty(need, dtype=torch.uint8, device="cuda"), torch.empty(need // 4, device="cuda"),
+               torch.empty((need // 512, 64), dtype=torch.float64, device="cuda")):
+        got, gl = ext.kv4_attention(cache, q, table, lens, workspace=ws, **kw)
+        assert torch.equal(got, want) and torch.equal(gl, wl)
+    for ws in (torch.empty(need, dtype=torch.uint8), torch.empty((need, 2), dtype=torch.uint8, device="cuda")[:, 0]):
+        with pytest.raises(ValueError):
+            ext.kv4_attention(cache, q, table, lens, workspace=ws, **kw)
+    for ws in (torch.empty(need - 256, dtype=torch.uint8, device="cuda"), torch.empty(need + 256, dtype=torch.uint8, device="cuda")[8:]):
+        with pytest.raises(ext.ExterndError):
+            ext.kv4_attention(cache, q, table, lens, workspace=ws, **kw)
