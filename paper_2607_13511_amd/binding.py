@@ -761,11 +761,12 @@ def token_logprobs(logits, targets=None, top: int = 0, scale: float = 1.0, strea
     """Log probabilities of the int64 ``targets`` (rows; below 0: none asked
     for) under the softmax of ``scale * logits`` (rows x vocabulary), each
     row's entropy, and its ``top`` most likely tokens, the lower index first
-    among equals (externd_token_logprobs).  Without targets logprob is None."""
+    among equals (externd_token_logprobs).  Without targets logprob is None.
+    ``workspace`` is not used: the operator needs none."""
     torch = _torch()
     if stream is not None:      # as on that stream: its own memory for what is allocated here
         with torch.cuda.stream(stream):
-            return token_logprobs(logits, targets, top, scale, None, workspace)
+            return token_logprobs(logits, targets, top, scale)
     rows, vocab, stride, code = _req_logits(torch, logits, "logits")
     if not 0 <= top <= min(LOGPROBS_MAX_TOP, vocab):
         raise ExterndError(EINVAL, "externd_token_logprobs")
@@ -780,17 +781,9 @@ def token_logprobs(logits, targets=None, top: int = 0, scale: float = 1.0, strea
     vals = logits.new_empty((rows, top), dtype=torch.float32)
     ids = logits.new_empty((rows, top), dtype=torch.int64)
     if rows:
-        L = lib()
-        nbytes = L.externd_token_logprobs_workspace_bytes(rows, vocab, top)
-        wp = None
-        if workspace is not None:
-            wp, nbytes = workspace.data_ptr(), workspace.numel()
-        elif nbytes:
-            workspace = logits.new_empty((nbytes,), dtype=torch.uint8)
-            wp = workspace.data_ptr()
-        st = L.externd_token_logprobs(logits.data_ptr(), code, rows, vocab, stride, tp, scale, top, lp,
-                                      entropy.data_ptr(), lse.data_ptr(), vals.data_ptr() if top else None,
-                                      ids.data_ptr() if top else None, wp, nbytes, _stream_ptr(torch, stream))
+        st = lib().externd_token_logprobs(logits.data_ptr(), code, rows, vocab, stride, tp, scale, top, lp,
+                                          entropy.data_ptr(), lse.data_ptr(), vals.data_ptr() if top else None,
+                                          ids.data_ptr() if top else None, None, 0, _stream_ptr(torch, stream))
         if st != OK:
             raise ExterndError(st, "externd_token_logprobs")
     return TokenLogprobs(logprob, entropy, lse, vals, ids)
