@@ -470,8 +470,9 @@ int externd_rotary(const void* q, void* q_out, int64_t q_token_stride, int64_t q
  * Device int32 starts[batch + 1] (rising from 0 to `tokens`) says where the
  * new tokens of each sequence are in the call's arrays; NULL: one token each
  * (tokens = batch).  The new tokens are the last ones: token i of a sequence's
- * n new ones is at position lens - n + i.  Lengths above table_pages P count
- * as that much, positions below 0 are in no sequence, and page numbers outside
+ * n new ones is at position lens - n + i, whatever the table holds.  Positions
+ * below 0 and from table_pages P on have no place: not stored, read as 0 and
+ * seen by no query, though a query may be there.  Page numbers outside
  * [0, num_pages) name pages without tokens.
  */
 size_t externd_kv4_page_bytes(int32_t head_dim, int32_t page_tokens);  /* of one head; 0 on invalid arguments */
@@ -564,7 +565,9 @@ int externd_token_logprobs(const void* logits, int32_t dtype, int64_t rows, int6
  * with the forward call's lse and entropy; g_logprob counts as 0 where a row
  * has no target.  Either gradient may be NULL (0); entropy may be NULL with
  * g_entropy.  grad: device, rows x vocab of dtype with its own row stride; it
- * may be `logits` itself with the same stride.  Where p_v = 0 the entry is 0. */
+ * may be `logits` itself with the same stride.  Where p_v = 0 its terms are 0,
+ * in a row of nothing but -infinity too (the target's entry is scale g_logprob).
+ * A target of vocab or more has no entry.                                   */
 int externd_token_logprobs_backward(const void* logits, int32_t dtype, int64_t rows, int64_t vocab,
                                     int64_t row_stride, const int64_t* targets, float scale, const float* lse,
                                     const float* entropy, const float* g_logprob, const float* g_entropy,

@@ -692,7 +692,8 @@ def kv4_attention(cache, q, table, lens, starts=None, max_new=None, max_len=None
     the cache, causal, within ``window`` positions where that is above 0
     (externd_kv4_attention).  ``max_new``, ``max_len``: the most new tokens
     and the greatest length of a sequence where the caller knows them (they
-    choose the launch only); ``scale``: 1 / sqrt(channels) unless given.
+    choose the launch only; without them all new tokens count as one
+    sequence's, which suits prompts and not drafts of many users); ``scale``: 1 / sqrt(channels) unless given.
     Returns (out, lse): tokens x query heads x channels in q's type, and fp32
     tokens x query heads."""
     torch = _torch()

@@ -408,3 +408,22 @@ def test_workspaces(ext):
     for ws in (torch.empty(need - 256, dtype=torch.uint8, device="cuda"), torch.empty(need + 256, dtype=torch.uint8, device="cuda")[8:]):
         with pytest.raises(ext.ExterndError):
             ext.kv4_attention(cache, q, table, lens, workspace=ws, **kw)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("window", [0, 30, 70])
+@pytest.mark.parametrize("each", [4, 32])
+def test_lengths_past_the_table(ext, dtype, window, each):
+    """Positions come from the length as it is; those past the table hold nothing, and a query there sees what the table
+    holds of its window."""
+    c = random_cache([256, 96], [200, 60], 1, 64, 32, 11)
+    c.lens = [256 + 50, 256 + 100]                         # tables hold 256: the second's pages from its fourth on are none
+    check(ext, c, queries(c, each, dtype), dtype, window=window)
+    cache, table, lens, starts = c.gpu()
+    before = cache.clone()
+    k = torch.randn((c.tokens, 1, 64), device="cuda")
+    ext.kv4_append(cache, k, k, table, lens, starts=starts)
+    got, _ = ext.kv4_read(cache, table, lens, 64, starts=starts, tokens=c.tokens)
+    assert (got[:150] != 0).any(-1).all() and (got[150:] == 0).all()
+    own = [int(p) for p in c.table[0]]
+    assert torch.equal(cache[[i for i in range(cache.shape[0]) if i not in own]], before[[i for i in range(cache.shape[0]) if i not in own]])
