@@ -58,12 +58,14 @@ class Session:
         self.table = torch.full((users, most_pages), -1, dtype=torch.int32)
 
     def _grow(self, news):
-        for u, n in enumerate(news):
-            have = -(-self.lens[u] // self.page_tokens)
-            self.lens[u] += n
-            need = -(-self.lens[u] // self.page_tokens)
-            if need > self.most_pages or need - have > len(self.free):
-                raise RuntimeError(f"user {u}: no page left for {self.lens[u]} tokens")
+        pages = [(-(-have // self.page_tokens), -(-(have + n) // self.page_tokens)) for have, n in zip(self.lens, news)]
+        wanted = 0
+        for u, (have, need) in enumerate(pages):      # nothing is taken unless all users have room
+            wanted += need - have
+            if need > self.most_pages or wanted > len(self.free):
+                raise RuntimeError(f"user {u}: no page left for {self.lens[u] + news[u]} tokens")
+        for u, (have, need) in enumerate(pages):
+            self.lens[u] += news[u]
             for i in range(have, need):
                 self.table[u, i] = self.free.pop()
 
