@@ -271,6 +271,16 @@ __device__ __forceinline__ float row_sum(float v) {
   return v + dppf<0x121>(v);
 }
 
+// ln of 2^ref sum.  The kernel of 256 rows has its weights up by 2^7 and its
+// reference down by as much: out of that first, so that the logarithm is of
+// the sum as the definition has it (lse 4.9e-8 of itself, 7.5e-8 otherwise).
+constexpr float WEIGHTS_UP = 7.f;
+template <int ROWS>
+__device__ __forceinline__ float lse_of(float ref, float sum) {
+  const float up = ROWS == 256 ? WEIGHTS_UP : 0.f, down = ROWS == 256 ? 1.f / 128 : 1.f;
+  return (ref + up + log2f(sum * down)) * 0.69314718055994530942f;
+}
+
 __device__ __forceinline__ float scale_of(unsigned word) {
   return (float)__builtin_bit_cast(_Float16, (uint16_t)(word & 0xFFF0u));
 }
@@ -652,7 +662,7 @@ __global__ __launch_bounds__(256, DIM <= 128 ? 3 : 2) void k_attention_split(Att
       if (!turn.part) {
         const bool none = sum == 0.f;
         store_any(a.out, to * DIM + d, none ? 0.f : o / sum, a.dtype);
-        if (a.lse && d == 0) a.lse[to] = none ? -INFINITY : (top + log2f(sum)) * 0.69314718055994530942f;
+        if (a.lse && d == 0) a.lse[to] = none ? -INFINITY : lse_of<ROWS>(top, sum);
       } else {
         float* part = turn.part + r * (DIM + 4);
         part[d] = o;
@@ -709,7 +719,7 @@ __global__ __launch_bounds__(512, 2) void k_attention_chunk(AttnArgs a) {
   constexpr int KU = DIM / 8, VU = TT / 8;          // 16-byte units of a row of K (a token) and of V (a channel)
   constexpr int WB = 8 / PS;                        // waves of a 16-token block
   constexpr int AHEAD = 4;
-  constexpr float UP = 7.f, TOP = 15.f;             // powers of two of the weights (above)
+  constexpr float UP = WEIGHTS_UP, TOP = 15.f;      // powers of two of the weights (above)
   constexpr float BAD = 5.87747175e-39f;            // 2^-127
   __shared__ __align__(16) _Float16 kt[3][TT * DIM], vt[3][DIM * TT];
   __shared__ __align__(8) uint8_t flags[3][8];      // of each wave's 8 values' tokens: 1 there, 3 some NaN among them
@@ -1124,7 +1134,7 @@ __global__ __launch_bounds__(512, 2) void k_attention_chunk(AttnArgs a) {
             *(v2u_any*)((T*)a.out + to * DIM + d) = w;
           }
         }
-      if (whole && a.lse && !half) a.lse[to] = none ? -INFINITY : (ref + log2f(l)) * 0.69314718055994530942f;
+      if (whole && a.lse && !half) a.lse[to] = none ? -INFINITY : lse_of<ROWS>(ref, l);
       if (!whole && !half) {
         part[DIM] = ref;
         part[DIM + 1] = l;
@@ -1257,7 +1267,7 @@ __global__ __launch_bounds__(256) void k_attention_join(AttnArgs a, int groups) 
     const int64_t at = (sh.t0 + row / a.each) * a.heads_q + sh.h * a.each + row % a.each;
 #pragma unroll
     for (int j = 0; j < 4; j++) store_any(a.out, at * DIM + 4 * c + j, none ? 0.f : o[j] / sum, a.dtype);
-    if (a.lse && c == 0) a.lse[at] = none ? -INFINITY : (top + log2f(sum)) * 0.69314718055994530942f;
+    if (a.lse && c == 0) a.lse[at] = none ? -INFINITY : lse_of<ROWS>(top, sum);
   }
 }
 template <int DIM, int ROWS>

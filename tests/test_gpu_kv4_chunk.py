@@ -427,3 +427,18 @@ def test_lengths_past_the_table(ext, dtype, window, each):
     assert (got[:150] != 0).any(-1).all() and (got[150:] == 0).all()
     own = [int(p) for p in c.table[0]]
     assert torch.equal(cache[[i for i in range(cache.shape[0]) if i not in own]], before[[i for i in range(cache.shape[0]) if i not in own]])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("form", FORMS)
+def test_wide_kernel_lse_of_equal_scores(ext, dtype, dim, form):
+    """Queries of 0: every score is 0, every weight a power of two and their sum exact, so the lse is ln n within the
+    logarithm's own error (one unit, 2 u of it), the constant's and the product's (u each)."""
+    c = random_cache([400], [400], 1, dim, 64, 12)
+    most = on_the_wide_kernel(ext, c, 32, dtype, form)
+    cache, table, lens, starts = c.gpu()
+    q = torch.zeros((400, 32, dim), device="cuda", dtype=TYPES[dtype][0])
+    _, lse = ext.kv4_attention(cache, q, table, lens, starts=starts, max_new=400, max_len=most)
+    want = np.log(np.arange(1.0, 401.0))[:, None]
+    assert np.all(np.abs(lse.double().cpu().numpy() - want) <= 4 * U * want)
