@@ -3,7 +3,8 @@ projections are ternary factors (random weights; ``python examples/decode.py``).
 
 A step, for the new tokens of all users side by side:
 
-    apply (q, k, v) -> rotary -> kv4_append -> kv4_attention -> apply (o) -> apply (head) -> token_logprobs
+    embedding -> apply (q, k, v) -> rotary -> kv4_append -> kv4_attention -> apply (o) -> apply (head) ->
+    token_logprobs
 
 The cache holds K and V in 4 bits, in pages that users take as they grow.
 """
@@ -80,7 +81,7 @@ class Session:
         lens = torch.tensor(self.lens, dtype=torch.int32, device="cuda")
         st = torch.tensor(starts, dtype=torch.int32, device="cuda")
         pos = torch.tensor(positions, dtype=torch.int64, device="cuda")
-        x = m.embedding[torch.tensor([t for ts in tokens for t in ts], device="cuda")]
+        x = binding.embedding(m.embedding, torch.tensor([t for ts in tokens for t in ts], device="cuda"))
         q0, k0 = m.q(x).view(T, m.heads, m.dim), m.k(x).view(T, m.heads_kv, m.dim)
         v = m.v(x).view(T, m.heads_kv, m.dim)
         q, k = binding.rotary(q0, k0, pos, m.freqs, amplitude=m.amplitude)

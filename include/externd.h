@@ -573,6 +573,99 @@ int externd_token_logprobs_backward(const void* logits, int32_t dtype, int64_t r
                                     const float* entropy, const float* g_logprob, const float* g_entropy,
                                     void* grad, int64_t grad_row_stride, void* stream);
 
+/*
+ * Operators at a model's dense ends, which its factorization leaves as they
+ * are: the embedding, the head with the log probabilities behind it, and the
+ * norm of all gradients.  The conventions of the decoding operators hold; the
+ * innermost dimension of every array is dense, and outputs overlap no input
+ * but where a call says so.
+ */
+
+/* Embedding: out[t] = scale table[ids[t]], rounded once; an id outside
+ * [0, vocab) gives a row of zeros.
+ *  table  device, vocab x width of dtype, table_stride >= width.
+ *  ids    device int64[tokens]; out device, tokens x width, out_stride >= width.
+ * vocab, width, tokens < 2^31; scale finite; tokens 0 is a valid call.       */
+int externd_embedding(const void* table, int32_t dtype, int64_t vocab, int64_t width, int64_t table_stride,
+                      const int64_t* ids, int64_t tokens, float scale, void* out, int64_t out_stride, void* stream);
+
+/* Gradient of the above for the table:
+ *   grad_table[v] = scale sum over the tokens t with ids[t] = v of grad[t],
+ * summed in fp32 in the tokens' order and rounded once; ids outside [0, vocab)
+ * add nothing, whatever grad holds there.  accumulate = 1: the sum is added
+ * to what grad_table holds (the head's gradient, where the head is the
+ * embedding), and rows without tokens are left as they are; 0: they become 0.
+ *  workspace  device, >= externd_embedding_backward_workspace_bytes(), 256-byte
+ *             aligned (may be NULL with tokens = 0).
+ * tokens <= 2^26, vocab < 2^31, width <= 2^20.                               */
+size_t externd_embedding_backward_workspace_bytes(int64_t tokens, int64_t vocab, int64_t width);  /* 0 on invalid arguments */
+int externd_embedding_backward(const void* grad, int32_t dtype, int64_t tokens, int64_t width, int64_t grad_stride,
+                               const int64_t* ids, int64_t vocab, float scale, int32_t accumulate, void* grad_table,
+                               int64_t grad_table_stride, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Log probabilities behind a dense head: externd_token_logprobs of the logits
+ * x weight^T, which are never held.  With z = scale x weight^T, for each row
+ *   lse = ln sum_v exp z_v,  logprob = z_target - lse,  entropy = lse - sum_v p_v z_v.
+ *  x          device, rows x width of dtype, x_stride >= width; weight device,
+ *             vocab x width of dtype, weight_stride >= width.
+ *  targets    device int64[rows], or NULL with logprob NULL.  Below 0: no token
+ *             is asked for, logprob 0.  vocab or more: logprob NaN.
+ *  scale      finite, > 0.
+ *  logprob, entropy, lse  device fp32[rows], each may be NULL.
+ *  workspace  device, >= externd_linear_logprobs_workspace_bytes(), 256-byte aligned.
+ * Logits are exact products summed in fp32 (fp32 operands enter as three bf16
+ * parts each, whose products below 2^-24 of the largest are left out).  A logit
+ * of -infinity counts as probability 0; a NaN or +infinity makes its row's
+ * results NaN, and so do, in fp32, an infinity in x or weight.
+ * rows <= 2^22, vocab < 2^31 - 1024, width <= 2^20; strides < 2^22.          */
+size_t externd_linear_logprobs_workspace_bytes(int32_t dtype, int64_t rows, int64_t vocab, int64_t width);  /* 0 on invalid arguments */
+int externd_linear_logprobs(const void* x, int64_t x_stride, const void* weight, int64_t weight_stride, int32_t dtype,
+                            int64_t rows, int64_t vocab, int64_t width, const int64_t* targets, float scale,
+                            float* logprob, float* entropy, float* lse, void* workspace, size_t workspace_bytes,
+                            void* stream);
+
+/* Gradients of the above for x and weight: with the forward call's lse and
+ * entropy and
+ *   G_v = scale [ g_logprob ([v = target] - p_v) - g_entropy p_v (ln p_v + entropy) ],
+ *   grad_x = G weight,  grad_weight = G^T x.
+ * The logits are computed again, in pieces of the vocabulary.  g_logprob
+ * counts as 0 where a row has no target (below 0, or vocab or more); either
+ * gradient may be NULL (0), entropy may be NULL with g_entropy, and either
+ * output may be NULL where it is not asked for.  A row whose two gradients are 0
+ * takes no part, whatever x, lse and entropy hold there: its grad_x is 0.
+ * rows = 0 gives a grad_weight of zeros.
+ *  grad_x     device, rows x width of dtype; grad_weight device, vocab x width.
+ *  workspace  device, >= externd_linear_logprobs_backward_workspace_bytes() with
+ *             need_x, need_weight = whether the outputs are given; 256-byte aligned.
+ * Sums are fp32; G enters its products in dtype (rounded to bf16, or to fp16
+ * below 2^15 with a power of two for each row; fp32 as three bf16 parts).    */
+size_t externd_linear_logprobs_backward_workspace_bytes(int32_t dtype, int64_t rows, int64_t vocab, int64_t width,
+                                                        int32_t need_x, int32_t need_weight);  /* 0 on invalid arguments */
+int externd_linear_logprobs_backward(const void* x, int64_t x_stride, const void* weight, int64_t weight_stride,
+                                     int32_t dtype, int64_t rows, int64_t vocab, int64_t width, const int64_t* targets,
+                                     float scale, const float* lse, const float* entropy, const float* g_logprob,
+                                     const float* g_entropy, void* grad_x, int64_t grad_x_stride, void* grad_weight,
+                                     int64_t grad_weight_stride, void* workspace, size_t workspace_bytes, void* stream);
+
+/* The norm over many tensors, and clipping by it:
+ *   norm = sqrt(sum over all entries of g^2),  out = g min(1, max_norm / norm).
+ *  tensors    host array of `count` device pointers, each to sizes[i] dense
+ *             entries of dtypes[i] (host arrays, not read after the call returns).
+ *  out        host array of device pointers of the same sizes and types, each
+ *             tensors[i] itself or apart from all tensors; NULL: in place.
+ *  max_norm   >= 0; INFINITY: only the norm, and `out` is not written.
+ *  norm       device fp32[1], out.
+ *  workspace  device, >= externd_clip_gradients_workspace_bytes(count), 256-byte aligned.
+ * The sum and the factor are fp64, so that no square overflows; a product is
+ * rounded once after the factor's rounding to fp32.  A norm of 0 leaves all as
+ * it is; an infinite one gives 0 (and NaN for infinite entries); NaN gives NaN.
+ * count <= 2^20; sizes may be 0.  The same entry must not be in two tensors
+ * that are written.                                                         */
+size_t externd_clip_gradients_workspace_bytes(int64_t count);  /* 0 on invalid arguments */
+int externd_clip_gradients(int64_t count, const void* const* tensors, void* const* out, const int64_t* sizes,
+                           const int32_t* dtypes, double max_norm, float* norm, void* workspace,
+                           size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -87,6 +87,21 @@ _SIGNATURES = {
                                               _c_ptr, _c_ptr, _c_ptr, _c_ptr, _c_ptr, _c_ptr, _c_size, _c_ptr]),
     "externd_token_logprobs_backward": (ctypes.c_int, [_c_ptr, _c_i32, _c_i64, _c_i64, _c_i64, _c_ptr, ctypes.c_float,
                                                        _c_ptr, _c_ptr, _c_ptr, _c_ptr, _c_ptr, _c_i64, _c_ptr]),
+    "externd_embedding": (ctypes.c_int, [_c_ptr, _c_i32, _c_i64, _c_i64, _c_i64, _c_ptr, _c_i64, ctypes.c_float, _c_ptr,
+                                         _c_i64, _c_ptr]),
+    "externd_embedding_backward_workspace_bytes": (_c_size, [_c_i64, _c_i64, _c_i64]),
+    "externd_embedding_backward": (ctypes.c_int, [_c_ptr, _c_i32, _c_i64, _c_i64, _c_i64, _c_ptr, _c_i64, ctypes.c_float,
+                                                  _c_i32, _c_ptr, _c_i64, _c_ptr, _c_size, _c_ptr]),
+    "externd_linear_logprobs_workspace_bytes": (_c_size, [_c_i32, _c_i64, _c_i64, _c_i64]),
+    "externd_linear_logprobs": (ctypes.c_int, [_c_ptr, _c_i64, _c_ptr, _c_i64, _c_i32, _c_i64, _c_i64, _c_i64, _c_ptr,
+                                               ctypes.c_float, _c_ptr, _c_ptr, _c_ptr, _c_ptr, _c_size, _c_ptr]),
+    "externd_linear_logprobs_backward_workspace_bytes": (_c_size, [_c_i32, _c_i64, _c_i64, _c_i64, _c_i32, _c_i32]),
+    "externd_linear_logprobs_backward": (ctypes.c_int, [_c_ptr, _c_i64, _c_ptr, _c_i64, _c_i32, _c_i64, _c_i64, _c_i64,
+                                                        _c_ptr, ctypes.c_float, _c_ptr, _c_ptr, _c_ptr, _c_ptr, _c_ptr,
+                                                        _c_i64, _c_ptr, _c_i64, _c_ptr, _c_size, _c_ptr]),
+    "externd_clip_gradients_workspace_bytes": (_c_size, [_c_i64]),
+    "externd_clip_gradients": (ctypes.c_int, [_c_i64, _c_ptr, _c_ptr, _c_ptr, _c_ptr, _c_dbl, _c_ptr, _c_ptr, _c_size,
+                                              _c_ptr]),
 }
 EXPORTED = tuple(_SIGNATURES)
 
@@ -745,8 +760,8 @@ class TokenLogprobs:
     logprob: "object"          # torch.float32 (rows,): of the targets; 0 where none is asked for
     entropy: "object"          # torch.float32 (rows,)
     lse: "object"              # torch.float32 (rows,)
-    top_logprobs: "object"     # torch.float32 (rows, top), the largest first
-    top_ids: "object"          # torch.int64 (rows, top)
+    top_logprobs: "object"     # torch.float32 (rows, top), the largest first; None from linear_logprobs
+    top_ids: "object"          # torch.int64 (rows, top); None from linear_logprobs
 
 
 def _req_logits(torch, t, name):
@@ -820,6 +835,299 @@ def token_logprobs_backward(logits, targets, lse, entropy, grad_logprob=None, gr
         if st != OK:
             raise ExterndError(st, "externd_token_logprobs_backward")
     return out
+
+
+# ---------------------------------------------------------------------------
+# operators at a model's dense ends: the embedding, the head with the log
+# probabilities behind it, and the norm of all gradients
+# ---------------------------------------------------------------------------
+def _given_workspace(workspace):
+    """(pointer, bytes) of a workspace that the caller brings."""
+    if not (workspace.is_cuda and workspace.is_contiguous()):
+        raise ValueError(f"workspace: expected a contiguous CUDA tensor, got {tuple(workspace.shape)} "
+                         f"{workspace.stride()} on {workspace.device}")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def _req_rows(torch, t, dtype, rows, width, name):
+    """A CUDA matrix of dtype with dense rows; returns its row stride.  None for rows or width: any."""
+    if not (t.is_cuda and t.dtype is dtype and t.dim() == 2 and (rows is None or t.shape[0] == rows)
+            and (width is None or t.shape[1] == width) and (t.stride(1) == 1 or t.shape[1] == 1)):
+        raise ValueError(f"{name}: expected a {dtype} CUDA tensor ({'rows' if rows is None else rows}, "
+                         f"{'width' if width is None else width}) with dense rows, got {t.dtype} {tuple(t.shape)} "
+                         f"{t.stride()} on {t.device}")
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _overlaps(a, b) -> bool:
+    """Whether two matrices with dense rows have bytes in common."""
+    if not a.numel() or not b.numel():
+        return False
+    size, (a0, b0) = a.element_size(), (a.data_ptr(), b.data_ptr())
+    sa, sb = (t.stride(0) * size if t.shape[0] > 1 else t.shape[1] * size for t in (a, b))
+    wa, wb = a.shape[1] * size, b.shape[1] * size
+    if a0 >= b0 + (b.shape[0] - 1) * sb + wb or b0 >= a0 + (a.shape[0] - 1) * sa + wa:
+        return False
+    return not (sa == sb and (b0 - a0) % sa >= wa and (b0 - a0) % sa + wb <= sa)      # columns side by side in one buffer
+
+
+def _elsewhere(torch, t, stream):
+    """Where the call has to be made again: on the given stream (with its own
+    memory for what is allocated) or on the device of t; None: here."""
+    if stream is not None:
+        if stream.device != t.device:
+            raise ValueError(f"stream: on {stream.device}, the tensors on {t.device}")
+        return torch.cuda.stream(stream)
+    if t.is_cuda and t.device.index != torch.cuda.current_device():
+        return torch.cuda.device(t.device)
+    return None
+
+
+def _same_device(t, *others):
+    for o in others:
+        if o is not None and o.device != t.device:
+            raise ValueError(f"all tensors must be on one device, got {t.device} and {o.device}")
+
+
+def embedding(table, ids, scale: float = 1.0, out=None, stream=None):
+    """``scale * table[ids]`` (externd_embedding): table (vocabulary x width),
+    ids int64 of any shape, in a row; one outside the vocabulary (padding) gives
+    zeros.  Returns ids.shape + (width,) in the table's type, or ``out`` (tokens
+    x width, dense rows)."""
+    torch = _torch()
+    there = _elsewhere(torch, table, stream)
+    if there is not None:
+        with there:
+            return embedding(table, ids, scale, out)
+    code = _dtype_code(torch, table.dtype, "table")
+    stride = _req_rows(torch, table, table.dtype, None, None, "table")
+    vocab, width = table.shape
+    _req(ids, torch, torch.int64, ids.shape, "ids")
+    _same_device(table, ids, out)
+    tokens = ids.numel()
+    if out is None:
+        got = table.new_empty((*ids.shape, width))
+        ostride = width
+    else:
+        got = out
+        ostride = _req_rows(torch, out, table.dtype, tokens, width, "out")
+        if _overlaps(out, table):
+            raise ValueError("out: must not overlap the table")
+    st = lib().externd_embedding(table.data_ptr(), code, vocab, width, stride, ids.data_ptr(), tokens, scale, got.data_ptr(),
+                                 ostride, _stream_ptr(torch, stream))
+    if st != OK:
+        raise ExterndError(st, "externd_embedding")
+    return got
+
+
+def embedding_backward(grad, ids, vocab: int, scale: float = 1.0, out=None, accumulate: bool = False, stream=None,
+                       workspace=None):
+    """Gradient of ``embedding`` for the table (externd_embedding_backward):
+    grad (ids.shape + (width,), dense rows) summed over each id's places, times
+    scale.  ``out`` (vocab x width): where it goes; with ``accumulate`` it is
+    added to what ``out`` holds, as where head and embedding are one matrix.
+    Bit-identical from run to run.  Returns (vocab x width)."""
+    torch = _torch()
+    there = _elsewhere(torch, grad, stream)
+    if there is not None:
+        with there:
+            return embedding_backward(grad, ids, vocab, scale, out, accumulate, None, workspace)
+    code = _dtype_code(torch, grad.dtype, "grad")
+    _req(ids, torch, torch.int64, ids.shape, "ids")
+    if grad.dim() < 1 or grad.shape[:-1] != ids.shape:
+        raise ValueError(f"grad: expected shape {tuple(ids.shape)} + (width,), got {tuple(grad.shape)}")
+    width, tokens = grad.shape[-1], ids.numel()
+    if grad.dim() != 2:
+        if not grad.is_contiguous():
+            raise ValueError(f"grad: more or fewer than two dimensions must be contiguous, got strides {grad.stride()}")
+        grad = grad.view(tokens, width)
+    gstride = _req_rows(torch, grad, grad.dtype, tokens, width, "grad")
+    if out is None:
+        if accumulate:
+            raise ValueError("out: needed to accumulate into")
+        out = grad.new_empty((vocab, width))
+    ostride = _req_rows(torch, out, grad.dtype, vocab, width, "out")
+    _same_device(grad, ids, out, workspace)
+    if _overlaps(out, grad):
+        raise ValueError("out: must not overlap grad")
+    L = lib()
+    nbytes = L.externd_embedding_backward_workspace_bytes(tokens, vocab, width)
+    wp = None
+    if workspace is not None:
+        wp, nbytes = _given_workspace(workspace)
+    elif nbytes:
+        workspace = grad.new_empty((nbytes,), dtype=torch.uint8)
+        wp = workspace.data_ptr()
+    st = L.externd_embedding_backward(grad.data_ptr(), code, tokens, width, gstride, ids.data_ptr(), vocab, scale,
+                                      int(accumulate), out.data_ptr(), ostride, wp, nbytes, _stream_ptr(torch, stream))
+    if st != OK:
+        raise ExterndError(st, "externd_embedding_backward")
+    return out
+
+
+def linear_logprobs(x, weight, targets=None, scale: float = 1.0, stream=None, workspace=None) -> TokenLogprobs:
+    """``token_logprobs`` of the logits ``x weight^T`` (x: rows x width, weight:
+    vocabulary x width, of one type), which are never held
+    (externd_linear_logprobs): log probabilities of the int64 ``targets``, entropies
+    and lse.  The largest logits are not kept: the top fields are None, and
+    without targets logprob is."""
+    torch = _torch()
+    there = _elsewhere(torch, x, stream)
+    if there is not None:
+        with there:
+            return linear_logprobs(x, weight, targets, scale, None, workspace)
+    code = _dtype_code(torch, x.dtype, "x")
+    xs = _req_rows(torch, x, x.dtype, None, None, "x")
+    rows, width = x.shape
+    ws = _req_rows(torch, weight, x.dtype, None, width, "weight")
+    vocab = weight.shape[0]
+    _same_device(x, weight, targets, workspace)
+    entropy, lse, logprob = x.new_empty((3, rows), dtype=torch.float32).unbind(0)
+    tp = lp = None
+    if targets is not None:
+        _req(targets, torch, torch.int64, (rows,), "targets")
+        tp, lp = targets.data_ptr(), logprob.data_ptr()
+    else:
+        logprob = None
+    L = lib()
+    wp, nbytes = None, 0
+    if workspace is not None:
+        wp, nbytes = _given_workspace(workspace)
+    elif rows:
+        nbytes = L.externd_linear_logprobs_workspace_bytes(code, rows, vocab, width)
+        workspace = x.new_empty((nbytes,), dtype=torch.uint8)
+        wp = workspace.data_ptr()
+    st = L.externd_linear_logprobs(x.data_ptr(), xs, weight.data_ptr(), ws, code, rows, vocab, width, tp, scale, lp,
+                                   entropy.data_ptr(), lse.data_ptr(), wp, nbytes, _stream_ptr(torch, stream))
+    if st != OK:
+        raise ExterndError(st, "externd_linear_logprobs")
+    return TokenLogprobs(logprob, entropy, lse, None, None)
+
+
+def linear_logprobs_backward(x, weight, targets, lse, entropy, grad_logprob=None, grad_entropy=None, scale: float = 1.0,
+                             need_x: bool = True, need_weight: bool = True, out=None, stream=None, workspace=None):
+    """Gradients for x and weight from those of ``linear_logprobs``'s logprob
+    and entropy (externd_linear_logprobs_backward), with its lse and entropy.
+    ``need_x``, ``need_weight``: which are asked for; ``out``: (grad_x,
+    grad_weight), where they go.  Rows whose two gradients are 0 (padding) take no
+    part, whatever x holds there.  Returns (grad_x, grad_weight), None for what
+    is not asked for."""
+    torch = _torch()
+    there = _elsewhere(torch, x, stream)
+    if there is not None:
+        with there:
+            return linear_logprobs_backward(x, weight, targets, lse, entropy, grad_logprob, grad_entropy, scale, need_x,
+                                            need_weight, out, None, workspace)
+    code = _dtype_code(torch, x.dtype, "x")
+    xs = _req_rows(torch, x, x.dtype, None, None, "x")
+    rows, width = x.shape
+    ws = _req_rows(torch, weight, x.dtype, None, width, "weight")
+    vocab = weight.shape[0]
+    ptrs = [None] * 5
+    for i, (t, dt, name) in enumerate(((targets, torch.int64, "targets"), (lse, torch.float32, "lse"),
+                                       (entropy, torch.float32, "entropy"),
+                                       (grad_logprob, torch.float32, "grad_logprob"),
+                                       (grad_entropy, torch.float32, "grad_entropy"))):
+        if t is not None:
+            _req(t, torch, dt, (rows,), name)
+            ptrs[i] = t.data_ptr()
+    gx, gw = out if out is not None else (None, None)
+    gx = (x.new_empty((rows, width)) if gx is None else gx) if need_x else None
+    gw = (x.new_empty((vocab, width)) if gw is None else gw) if need_weight else None
+    gxs = _req_rows(torch, gx, x.dtype, rows, width, "grad_x") if need_x else width
+    gws = _req_rows(torch, gw, x.dtype, vocab, width, "grad_weight") if need_weight else width
+    _same_device(x, weight, targets, lse, entropy, grad_logprob, grad_entropy, gx, gw, workspace)
+    outs = [t for t in (gx, gw) if t is not None]
+    if any(_overlaps(o, t) for o in outs for t in (x, weight)) or (len(outs) == 2 and _overlaps(*outs)):
+        raise ValueError("out: must overlap neither x nor weight nor each other")
+    if not outs:
+        return None, None
+    L = lib()
+    if workspace is not None:
+        wp, nbytes = _given_workspace(workspace)
+    else:
+        nbytes = L.externd_linear_logprobs_backward_workspace_bytes(code, rows, vocab, width, int(need_x), int(need_weight))
+        workspace = x.new_empty((nbytes,), dtype=torch.uint8)
+        wp = workspace.data_ptr()
+    st = L.externd_linear_logprobs_backward(x.data_ptr(), xs, weight.data_ptr(), ws, code, rows, vocab, width, ptrs[0], scale,
+                                            ptrs[1], ptrs[2], ptrs[3], ptrs[4], gx.data_ptr() if need_x else None, gxs,
+                                            gw.data_ptr() if need_weight else None, gws, wp, nbytes,
+                                            _stream_ptr(torch, stream))
+    if st != OK:
+        raise ExterndError(st, "externd_linear_logprobs_backward")
+    return gx, gw
+
+
+def _dense(t) -> bool:
+    """Whether t's entries fill its memory without gaps, in any order of the dimensions."""
+    if t.is_contiguous():
+        return True
+    want = 1
+    for n, s in sorted(((n, s) for n, s in zip(t.shape, t.stride()) if n > 1), key=lambda d: d[1]):
+        if s != want:
+            return False
+        want *= n
+    return True
+
+
+def clip_gradients(tensors, max_norm: float = float("inf"), out=None, stream=None, workspace=None):
+    """The norm over all entries of ``tensors`` (CUDA, dense, float32, bfloat16
+    or float16, mixed), and each of them times min(1, max_norm / norm), in place
+    or into ``out`` (as many tensors of the same shapes, strides and types)
+    (externd_clip_gradients).  With max_norm infinite only the norm.  Returns
+    the norm, a float32 CUDA scalar; nothing is copied to the host."""
+    torch = _torch()
+    tensors = list(tensors)
+    if tensors or stream is not None:
+        there = _elsewhere(torch, tensors[0] if tensors else stream, stream)
+        if there is not None:
+            with there:
+                return clip_gradients(tensors, max_norm, out, None, workspace)
+    outs = tensors if out is None else list(out)
+    if len(outs) != len(tensors):
+        raise ValueError(f"out: expected {len(tensors)} tensors, got {len(outs)}")
+    if not max_norm >= 0:
+        raise ExterndError(EINVAL, "externd_clip_gradients")
+    device = tensors[0].device if tensors else torch.device("cuda", torch.cuda.current_device())
+    spans = []
+    for i, (t, o) in enumerate(zip(tensors, outs)):
+        _dtype_code(torch, t.dtype, f"tensors[{i}]")
+        if not (t.is_cuda and t.device == device and _dense(t)):
+            raise ValueError(f"tensors[{i}]: expected a dense CUDA tensor on {device}, got {tuple(t.shape)} {t.stride()} "
+                             f"on {t.device}")
+        if o is not t and not (o.dtype is t.dtype and o.shape == t.shape and o.device == t.device and _dense(o)
+                               and o.stride() == t.stride()):
+            raise ValueError(f"out[{i}]: expected {t.dtype} {tuple(t.shape)} {t.stride()} on {t.device}, got {o.dtype} "
+                             f"{tuple(o.shape)} {o.stride()} on {o.device}")
+        if max_norm != float("inf") and t.numel():
+            spans.append((o.data_ptr(), o.data_ptr() + o.numel() * o.element_size(), i, i))
+            if o.data_ptr() != t.data_ptr():
+                spans.append((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size(), -1, i))
+    # what is written lies in no other tensor (a tensor that is only read may be given twice)
+    spans.sort()
+    end, wrote = 0, True
+    for a, b, w, i in spans:
+        if a < end and (w >= 0 or wrote):
+            raise ValueError(f"tensors[{i}]: what is written overlaps another tensor")
+        if b > end:
+            end, wrote = b, w >= 0
+    n = len(tensors)
+    norm = torch.empty((), dtype=torch.float32, device=device)
+    L = lib()
+    if workspace is not None:
+        wp, nbytes = _given_workspace(workspace)
+    else:
+        nbytes = L.externd_clip_gradients_workspace_bytes(n)
+        workspace = torch.empty((nbytes,), dtype=torch.uint8, device=device)
+        wp = workspace.data_ptr()
+    ins = (_c_ptr * n)(*[t.data_ptr() for t in tensors])
+    ops = (_c_ptr * n)(*[t.data_ptr() for t in outs])
+    sizes = (_c_i64 * n)(*[t.numel() for t in tensors])
+    codes = (_c_i32 * n)(*[_dtype_codes[t.dtype] for t in tensors])
+    st = L.externd_clip_gradients(n, ins, ops, sizes, codes, max_norm, norm.data_ptr(), wp, nbytes, _stream_ptr(torch, stream))
+    if st != OK:
+        raise ExterndError(st, "externd_clip_gradients")
+    return norm
 
 
 # ---------------------------------------------------------------------------

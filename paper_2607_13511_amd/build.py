@@ -16,7 +16,8 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB_NAME = "libexternd.so"
 LIB_PATH = os.path.join(PKG_DIR, LIB_NAME)
 SOURCES = ["externd_kernels.hip", "externd_api.hip", "externd_apply.hip", "externd_seq.hip", "externd_rotary.hip",
-           "externd_kv4.hip", "externd_kv4_attention.hip", "externd_logprobs.hip"]
+           "externd_kv4.hip", "externd_kv4_attention.hip", "externd_logprobs.hip", "externd_embedding.hip", "externd_linear.hip",
+           "externd_clip.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"

@@ -69,6 +69,13 @@ template <int DT> struct Vec {
   }
 };
 
+// 16 bytes at any entry: the instructions take every address.
+typedef v4u v4u_any __attribute__((aligned(2)));
+template <typename T>
+__device__ __forceinline__ v4u load_any(const T* p) { return *(const v4u_any*)p; }
+template <typename T>
+__device__ __forceinline__ void store_any(T* p, v4u v) { *(v4u_any*)p = v; }
+
 // N entries at p, in 16-byte loads or stores where VEC (p is 16-byte aligned then).
 template <int DT, int N, bool VEC>
 __device__ __forceinline__ void load_n(const typename Elem<DT>::T* p, float* x) {
