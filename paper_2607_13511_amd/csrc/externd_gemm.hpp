@@ -1,0 +1,338 @@
+// Matrix products on the matrix cores for the operators behind a dense head:
+// C(m, n) = sum over k of A(m, k) B(n, k) by tiles of a workgroup.
+//
+// Either operand lies in memory as rows of k ("by rows") or as rows of m or n,
+// one for each k ("by columns"); both reach the same fragments, eight
+// consecutive k of one m in a lane, the latter through LDS reads that transpose
+// 4 x 16 entries.  A tile's LDS holds vectors of 16 bytes in an order that keeps
+// the reads of a fragment apart in the banks; as loads write LDS in lane order,
+// each lane picks its vector of global memory accordingly.
+#pragma once
+
+#include "externd_decode.hpp"
+
+namespace externd {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) char lds_char;
+
+constexpr int GEMM_THREADS = 512;
+
+// An operand of a product: `count` of m (or n) and K of k, with rows `stride` entries apart.
+struct Operand {
+  const void* p;
+  int64_t stride;
+};
+
+// What a product of type DT takes: fp32 operands become three bf16 parts of 8
+// bits each, x = x1 + x2 + x3 exactly (cut, not rounded), of which the six
+// products not below 2^-24 are summed.
+template <int DT> struct Kind {
+  static constexpr int PLANES = DT == EXTERND_F32 ? 3 : 1;
+  static constexpr int BK = DT == EXTERND_F32 ? 32 : 64;      // k of a step
+};
+
+template <int DT>
+__device__ __forceinline__ f32x16 mfma(v4u a, v4u b, f32x16 c) {
+  if constexpr (DT == EXTERND_F16) return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  else return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+// The LDS tile of one operand: X of m (or n) by BK of k.
+template <bool COL, int X, int BK>
+struct Tile {
+  static constexpr int VECTORS = X * BK / 8;                  // of 16 bytes, in each plane
+  static constexpr int BYTES = VECTORS * 16;
+  static constexpr int LOADS = VECTORS / GEMM_THREADS;        // of a thread
+  static_assert(VECTORS % GEMM_THREADS == 0 || VECTORS < GEMM_THREADS, "whole loads");
+  static constexpr int CH = COL ? X / 8 : BK / 8;             // vectors of a row in memory
+  // Where in the operand the vector at place `i` of the tile is: its row in memory and its vector there.
+  static __device__ __forceinline__ void place(int i, int* row, int* vec) {
+    *row = i / CH;
+    const int v = i % CH;
+    if constexpr (COL) *vec = ((v >> 1) ^ spread(*row)) << 1 | (v & 1);
+    else *vec = v ^ ((*row / (8 / CH)) & (CH - 1));
+  }
+  // By columns: pairs of vectors (16 columns) of four rows of k go to different banks.
+  static __device__ __forceinline__ int spread(int k) { return (2 * (k & 3)) & (X / 16 - 1); }
+  // The byte at which a lane reads its fragment of 32 columns from x0 on, without what depends on x0 and on the step of 16 k.
+  static __device__ __forceinline__ v4u fragment(const lds_char* t, int x0, int ks) {
+    const int lane = threadIdx.x & 63;
+    if constexpr (COL) {
+      const int k = ks * 16 + (lane >> 5) * 8 + ((lane & 15) >> 2), q = (x0 >> 4) + ((lane >> 4) & 1);
+      const lds_char* at = t + k * (X * 2) + ((q ^ spread(k)) << 5) + (lane & 3) * 8;
+      typedef __attribute__((address_space(3))) s16x4* four;
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((four)at);
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((four)(at + 4 * (X * 2)));
+      const v2u a = __builtin_bit_cast(v2u, lo), b = __builtin_bit_cast(v2u, hi);
+      return v4u{a[0], a[1], b[0], b[1]};
+    } else {
+      const int row = x0 + (lane & 31), v = (ks * 2 + (lane >> 5)) ^ ((row / (8 / CH)) & (CH - 1));
+      return *(const __attribute__((address_space(3))) v4u*)(t + (row * CH + v) * 16);
+    }
+  }
+};
+
+// Loads of 16-bit operands whose rows begin at multiples of 16 bytes and are whole
+// vectors, straight into LDS.  (Part of a vector would come as zeros where the operand
+// ends.  K is rounded up to whole vectors by rows: zeros in memory.)  The buffer's base moves on with the
+// steps, and what lies past its end, or is no vector of the tile, becomes zeros.
+template <bool COL, int X, int BK>
+struct Direct {
+  typedef Tile<COL, X, BK> T;
+  static constexpr int LOADS = T::LOADS ? T::LOADS : 1;      // of a wave, whether or not all of it has one
+  static constexpr unsigned NONE = 0xFFFFFFFFu;
+  const char* base;
+  int64_t left, k_left;      // bytes from the base to the operand's end; k's from the next step on
+  unsigned offset[LOADS];
+  int step;
+
+  // count of m (or n) from x0 on, K of k from k0 on.
+  __device__ __forceinline__ void init(const Operand& o, int64_t x0, int64_t count, int64_t k0, int64_t K) {
+    const int64_t row = o.stride * 2, cols = min(count, (int64_t)X);
+    if (!COL) K = (K + 7) & ~(int64_t)7;
+    const int64_t rows = COL ? K : cols, width = (COL ? cols : K) * 2;
+    base = (const char*)o.p + (COL ? k0 * row + x0 * 2 : x0 * row + k0 * 2);
+    left = rows > 0 ? (rows - 1) * row + width : 0;
+    k_left = K;
+    step = (int)(COL ? BK * row : BK * 2);
+#pragma unroll
+    for (int i = 0; i < LOADS; i++) {
+      int r, v;
+      T::place(i * GEMM_THREADS + (int)threadIdx.x, &r, &v);
+      const bool in = i * GEMM_THREADS + (int)threadIdx.x < T::VECTORS && (COL ? v * 16 < width : r < rows);
+      offset[i] = in ? (unsigned)(r * row + v * 16) : NONE;
+    }
+  }
+  // The vectors of the next step, to the tile at `lds`.
+  __device__ __forceinline__ void issue(lds_char* lds) {
+    if (T::LOADS == 0 && (int)(threadIdx.x & ~63u) >= T::VECTORS) return;
+    const unsigned to = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)lds + (threadIdx.x >> 6) * 1024);
+    const i32x4 resource = {__builtin_amdgcn_readfirstlane((int)(uintptr_t)base), __builtin_amdgcn_readfirstlane((int)((uintptr_t)base >> 32)),
+                            __builtin_amdgcn_readfirstlane((int)(unsigned)min(max(left, (int64_t)0), (int64_t)0xFFFFFFF0)), 0x00020000};
+    if (COL || k_left >= BK) {
+#pragma unroll
+      for (int i = 0; i < LOADS; i++) load(to + i * (GEMM_THREADS * 16), offset[i], resource);
+    } else {                 // by rows, the last step: the next row's entries are none of this one's
+#pragma unroll
+      for (int i = 0; i < LOADS; i++) {
+        int r, v;
+        T::place(i * GEMM_THREADS + (int)threadIdx.x, &r, &v);
+        load(to + i * (GEMM_THREADS * 16), v * 8 < k_left ? offset[i] : NONE, resource);
+      }
+    }
+    base += step;
+    left -= step;
+    k_left -= BK;
+  }
+  // LDS is written behind the compiler's back: whoever reads it waits for it (wait_loads).
+  static __device__ __forceinline__ void load(unsigned to, unsigned from, i32x4 resource) {
+    asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(from), "s"(resource) : "memory");
+  }
+};
+
+// At most N of this wave's loads are under way, and its LDS reads are done.
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void barrier() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// Loads of any operand through registers: rows that begin anywhere, entries past
+// an end left out one by one, and fp32 operands, cut into their parts.
+template <int DT, bool COL, int X, int BK>
+struct Staged {
+  typedef typename Elem<DT>::T E;
+  typedef Tile<COL, X, BK> T;
+  static constexpr int LOADS = T::LOADS ? T::LOADS : 1, WORDS = DT == EXTERND_F32 ? 2 : 1;
+  const E* at[LOADS];
+  v4u held[LOADS][WORDS];
+  int64_t stride, k_left;
+  int cols;
+
+  __device__ __forceinline__ void init(const Operand& o, int64_t x0, int64_t count, int64_t k0, int64_t K) {
+    stride = o.stride;
+    cols = (int)min(count, (int64_t)X);
+    k_left = K;
+    const E* base = (const E*)o.p + (COL ? k0 * stride + x0 : x0 * stride + k0);
+#pragma unroll
+    for (int i = 0; i < LOADS; i++) {
+      int r, v;
+      T::place(i * GEMM_THREADS + (int)threadIdx.x, &r, &v);
+      at[i] = base + r * stride + v * 8;
+    }
+  }
+  // The next step's vectors, into registers.
+  __device__ __forceinline__ void fetch() {
+#pragma unroll
+    for (int i = 0; i < LOADS; i++) {
+      int r, v;
+      T::place(i * GEMM_THREADS + (int)threadIdx.x, &r, &v);
+      const bool in = i * GEMM_THREADS + (int)threadIdx.x < T::VECTORS && (COL ? r < k_left : r < cols);
+      const int n = !in ? 0 : (int)min((COL ? (int64_t)cols : k_left) - v * 8, (int64_t)8);
+      if (n >= 8) {
+#pragma unroll
+        for (int w = 0; w < WORDS; w++) held[i][w] = load_any(at[i] + w * Vec<DT>::E);
+      } else {
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; e++) x[e] = e < n ? Elem<DT>::load(at[i][e]) : 0.f;
+#pragma unroll
+        for (int w = 0; w < WORDS; w++) held[i][w] = Vec<DT>::pack(x + w * Vec<DT>::E);
+      }
+      at[i] += COL ? BK * stride : BK;
+    }
+    k_left -= BK;
+  }
+  // To the tile at `lds`; planes lie `plane` bytes apart.
+  __device__ __forceinline__ void put(lds_char* lds, int plane) const {
+    typedef __attribute__((address_space(3))) v4u* vec;
+#pragma unroll
+    for (int i = 0; i < LOADS; i++) {
+      if (i * GEMM_THREADS + (int)threadIdx.x >= T::VECTORS) return;
+      lds_char* const to = lds + (i * GEMM_THREADS + (int)threadIdx.x) * 16;
+      if constexpr (DT != EXTERND_F32) *(vec)to = held[i][0];
+      else {
+        unsigned part[3][8];
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+          const unsigned x = held[i][e / 4][e % 4];
+          const bool whole = (x & 0x7F800000u) == 0x7F800000u;      // infinite or NaN: one part holds it
+          unsigned y = x & 0xFFFF0000u;
+          if (whole && (x & 0x007FFFFFu)) y |= 0x00400000u;         // a NaN stays one
+          const float r = whole ? 0.f : __uint_as_float(x) - __uint_as_float(y);
+          const unsigned z = __float_as_uint(r) & 0xFFFF0000u;
+          part[0][e] = y;
+          part[1][e] = z;
+          part[2][e] = __float_as_uint(r - __uint_as_float(z));
+        }
+#pragma unroll
+        for (int p = 0; p < 3; p++) {
+          v4u o;
+#pragma unroll
+          for (int w = 0; w < 4; w++) o[w] = part[p][2 * w] >> 16 | (part[p][2 * w + 1] & 0xFFFF0000u);
+          *(vec)(to + p * plane) = o;
+        }
+      }
+    }
+  }
+};
+
+// How a workgroup of eight waves divides a tile of BM x BN: WM of them along m.
+template <int DT_, bool DIRECT_, bool ACOL_, bool BCOL_, int BM_, int BN_, int WM_, int STAGES_>
+struct Product {
+  static constexpr int DT = DT_, BM = BM_, BN = BN_, WM = WM_, WN = 8 / WM_, STAGES = STAGES_;
+  static constexpr bool DIRECT = DIRECT_, ACOL = ACOL_, BCOL = BCOL_;
+  static constexpr int BK = Kind<DT>::BK, PLANES = Kind<DT>::PLANES;
+  static constexpr int TM = BM / WM / 32, TN = BN / WN / 32;
+  typedef Tile<ACOL, BM, BK> TA;
+  typedef Tile<BCOL, BN, BK> TB;
+  static constexpr int STAGE = (TA::BYTES + TB::BYTES) * PLANES, LDS = STAGE * STAGES;
+  static_assert(LDS <= 160 * 1024 && TM >= 1 && TN >= 1 && !(DIRECT && DT == EXTERND_F32), "fits");
+
+  // Entry `r` (0 .. 15) of acc[i][j] is C(m0 + row(i, r), n0 + col(j)).
+  static __device__ __forceinline__ int row(int i, int r) {
+    return ((threadIdx.x >> 6) / WN * TM + i) * 32 + 8 * (r >> 2) + 4 * ((threadIdx.x & 63) >> 5) + (r & 3);
+  }
+  static __device__ __forceinline__ int col(int j) { return ((threadIdx.x >> 6) % WN * TN + j) * 32 + (threadIdx.x & 31); }
+
+  // One step's products, from the tiles at `s`.
+  static __device__ __forceinline__ void step(const lds_char* s, f32x16 (*acc)[TN]) {
+    const lds_char *a = s, *b = s + TA::BYTES * PLANES;
+    const int wave = threadIdx.x >> 6, ma = wave / WN * TM * 32, nb = wave % WN * TN * 32;
+#pragma unroll
+    for (int ks = 0; ks < BK / 16; ks++) {
+      v4u fa[PLANES][TM], fb[PLANES][TN];
+#pragma unroll
+      for (int p = 0; p < PLANES; p++) {
+#pragma unroll
+        for (int j = 0; j < TN; j++) fb[p][j] = TB::fragment(b + p * TB::BYTES, nb + j * 32, ks);
+#pragma unroll
+        for (int i = 0; i < TM; i++) fa[p][i] = TA::fragment(a + p * TA::BYTES, ma + i * 32, ks);
+      }
+#pragma unroll
+      for (int i = 0; i < TM; i++)
+#pragma unroll
+        for (int j = 0; j < TN; j++) {
+          if constexpr (PLANES == 3) {      // small products first
+            acc[i][j] = mfma<DT>(fa[1][i], fb[1][j], acc[i][j]);
+            acc[i][j] = mfma<DT>(fa[0][i], fb[2][j], acc[i][j]);
+            acc[i][j] = mfma<DT>(fa[2][i], fb[0][j], acc[i][j]);
+            acc[i][j] = mfma<DT>(fa[0][i], fb[1][j], acc[i][j]);
+            acc[i][j] = mfma<DT>(fa[1][i], fb[0][j], acc[i][j]);
+          }
+          acc[i][j] = mfma<DT>(fa[0][i], fb[0][j], acc[i][j]);
+        }
+    }
+  }
+
+  // acc = the products over K k's from k0 of A and k0 + b_k of B on; all threads of the workgroup, which has `lds` to itself.
+  static __device__ __forceinline__ void run(const Operand& A, int64_t m0, int64_t m_count, const Operand& B, int64_t n0, int64_t n_count,
+                                             int64_t k0, int64_t K, lds_char* lds, f32x16 (*acc)[TN], int64_t b_k = 0) {
+#pragma unroll
+    for (int i = 0; i < TM; i++)
+#pragma unroll
+      for (int j = 0; j < TN; j++)
+#pragma unroll
+        for (int r = 0; r < 16; r++) acc[i][j][r] = 0.f;
+    const int64_t steps = (K + BK - 1) / BK;
+    if constexpr (DIRECT) {
+      Direct<ACOL, BM, BK> la;
+      Direct<BCOL, BN, BK> lb;
+      la.init(A, m0, m_count, k0, K);
+      lb.init(B, n0, n_count, k0 + b_k, K);
+      static_assert(TA::LOADS > 0, "every wave loads of A");
+      constexpr int EACH = Direct<ACOL, BM, BK>::LOADS + Direct<BCOL, BN, BK>::LOADS;
+      const bool fewer = TB::LOADS == 0 && (int)(threadIdx.x & ~63u) >= TB::VECTORS;      // this wave loads of A only
+      auto issue = [&](int stage) {
+        la.issue(lds + stage * STAGE);
+        lb.issue(lds + stage * STAGE + TA::BYTES);
+      };
+      for (int s = 0; s < STAGES - 1; s++) issue(s);      // past the last step: zeros, which nothing reads
+      int stage = 0, next = STAGES - 1;
+      for (int64_t t = 0; t < steps; t++) {
+        if (fewer) wait_loads<TA::LOADS*(STAGES - 2)>();
+        else wait_loads<EACH*(STAGES - 2)>();
+        barrier();
+        issue(next);
+        step(lds + stage * STAGE, acc);
+        stage = stage + 1 == STAGES ? 0 : stage + 1;
+        next = next + 1 == STAGES ? 0 : next + 1;
+      }
+      wait_loads<0>();
+      barrier();
+    } else {
+      static_assert(DIRECT || STAGES == 2, "two buffers");
+      Staged<DT, ACOL, BM, BK> la;
+      Staged<DT, BCOL, BN, BK> lb;
+      la.init(A, m0, m_count, k0, K);
+      lb.init(B, n0, n_count, k0 + b_k, K);
+      la.fetch();
+      lb.fetch();
+      for (int64_t t = 0; t < steps; t++) {
+        lds_char* const s = lds + (t & 1) * STAGE;
+        la.put(s, TA::BYTES);
+        lb.put(s + TA::BYTES * PLANES, TB::BYTES);
+        wait_loads<63>();
+        barrier();
+        if (t + 1 < steps) {
+          la.fetch();
+          lb.fetch();
+        }
+        step(s, acc);
+      }
+      wait_loads<0>();
+      barrier();
+    }
+  }
+};
+
+}  // namespace externd

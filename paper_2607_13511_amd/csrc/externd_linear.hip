@@ -2,129 +2,209 @@
 // its matrix, without holding the logits.
 #include <cmath>
 
-#include "externd_decode.hpp"
+#include "externd_gemm.hpp"
 
 namespace externd {
 
-constexpr int TILE = 64, DEPTH = 16;
-constexpr int64_t FORWARD_ROWS = 8192;      // of a pass, so that the parts stay small
-
-// C(i, j) = sum over k of A(i, k) B(j, k) of a 64 x 64 tile; 256 threads, 4 x 4 entries each.
-template <typename LA, typename LB>
-__device__ __forceinline__ void tile_product(LA A, LB B, int64_t k0, int64_t k1, float (*sum)[4]) {
-  __shared__ float a[DEPTH][TILE + 4], b[DEPTH][TILE + 4];
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  for (int64_t k = k0; k < k1; k += DEPTH) {
-    for (int e = threadIdx.x; e < TILE * DEPTH; e += 256) {
-      const int i = e / DEPTH, q = e % DEPTH;
-      a[q][i] = k + q < k1 ? A(i, k + q) : 0.f;
-      b[q][i] = k + q < k1 ? B(i, k + q) : 0.f;
-    }
-    __syncthreads();
-    for (int q = 0; q < DEPTH; q++)
-      for (int i = 0; i < 4; i++)
-        for (int j = 0; j < 4; j++) sum[i][j] = fmaf(a[q][ty * 4 + i], b[q][tx * 4 + j], sum[i][j]);
-    __syncthreads();
-  }
-}
+constexpr int64_t FORWARD_ROWS = 8192;                // of a pass, so that the parts stay small
+constexpr int64_t PIECE_ENTRIES = (int64_t)1 << 26;   // of G in a piece of the vocabulary, where rows allow it
+constexpr int CUS = 256;
 
 struct Part {
   float top, sum, mean, none;      // largest z, sum of e = exp(z - top), sum of e (z - top)
 };
 
+// What a row's gradient is made of, times `up`, a power of two that brings fp16's G below 2^15.
+struct RowInfo {
+  float g, ge, lse, h, up;
+  int32_t y;                       // -1: no target
+  int32_t present, none;
+};
+
 struct LinearArgs {
-  const void *x, *weight;
-  int64_t x_stride, weight_stride, rows, vocab, width;
+  Operand x, weight;
+  int64_t rows, vocab, width;
   const int64_t* targets;
   float scale;
+  int row_tiles, vocab_tiles;
+  int64_t step;                    // vocabulary of a tile
   // forward
   float *logprob, *entropy, *lse;
-  Part* parts;          // rows x tiles
-  int64_t tiles;
-  float* at_target;     // z of the target
+  Part* parts;                     // rows x vocab_tiles
+  float* at_target;                // z of the target
   // backward
   const float *lse_in, *entropy_in, *g_logprob, *g_entropy;
+  RowInfo* info;
+  float* up_all;                   // the least `up` of the rows that take part
   void *grad_x, *grad_weight;
   int64_t grad_x_stride, grad_weight_stride, v0, v1;      // this piece of the vocabulary
-  float *G, *dx;        // rows x piece; rows x width
-  int64_t piece;
+  void *G, *packed;                // rows x piece; rows x packed_width: x, zero where a row takes no part
+  int64_t piece, packed_width;
+  float* dx;                       // splits x rows x dx_width
+  int64_t dx_width, split;         // k of a split
+  int splits;
 };
+
+// Tiles in an order in which those that run together share operands: an XCD
+// (workgroups go round robin over the eight) takes a stretch of them, eight
+// row tiles of one vocabulary tile after another.
+__device__ __forceinline__ void place_tile(int rows, int others, int* row, int* other) {
+  const int total = rows * others, xcd = blockIdx.x & 7, per = total >> 3, more = total & 7;
+  const int at = xcd * per + min(xcd, more) + (int)(blockIdx.x >> 3);
+  const int panel = at / (8 * others), in = at - panel * 8 * others, w = min(8, rows - panel * 8);
+  *row = panel * 8 + in % w;
+  *other = in / w;
+}
 
 __device__ __forceinline__ float propagating_max(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 
-// What a row's gradient is made of; false: the row takes no part.
-__device__ __forceinline__ bool row_gradients(const LinearArgs& a, int64_t r, float* g, float* ge, int64_t* y) {
-  *y = a.targets ? a.targets[r] : -1;
-  *g = a.g_logprob && *y >= 0 && *y < a.vocab ? a.g_logprob[r] : 0.f;
-  *ge = a.g_entropy ? a.g_entropy[r] : 0.f;
-  return *g != 0.f || *ge != 0.f;
-}
+constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
 
-// Rows of x against 64 rows of weight.  BACK: G of the tile, else the tile's part of each row's softmax.
-template <int DT, bool BACK>
-__global__ __launch_bounds__(256) void k_logits(LinearArgs a) {
-  typedef typename Elem<DT>::T T;
-  __shared__ float z[TILE][TILE + 1];
-  const int64_t r0 = (int64_t)blockIdx.y * TILE, c0 = a.v0 + (int64_t)blockIdx.x * TILE;
-  const T *x = (const T*)a.x, *w = (const T*)a.weight;
-  float sum[4][4] = {};
-  tile_product([&](int i, int64_t k) { return r0 + i < a.rows ? Elem<DT>::load(x[(r0 + i) * a.x_stride + k]) : 0.f; },
-               [&](int i, int64_t k) { return c0 + i < a.v1 ? Elem<DT>::load(w[(c0 + i) * a.weight_stride + k]) : 0.f; }, 0, a.width, sum);
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  for (int i = 0; i < 4; i++)
-    for (int j = 0; j < 4; j++) z[ty * 4 + i][tx * 4 + j] = c0 + tx * 4 + j < a.v1 ? sum[i][j] * a.scale : -INFINITY;
-  __syncthreads();
-  if (threadIdx.x >= TILE || r0 + threadIdx.x >= a.rows) return;
-  const float* row = z[threadIdx.x];
-  const int64_t r = r0 + threadIdx.x;
+// Logits of a tile: rows of weight along m, rows of x along n, so that a lane
+// holds one row's logits and its softmax needs no other lane but at the end.
+// BACK: G of the tile; else its part of each row's softmax.
+template <typename P, bool BACK>
+__global__ __launch_bounds__(GEMM_THREADS, 2) void k_logits(LinearArgs a) {
+  constexpr int DT = P::DT, TM = P::TM, TN = P::TN;
+  __shared__ __align__(16) char lds[P::LDS];
+  int rt, vt;
+  place_tile(a.row_tiles, a.vocab_tiles, &rt, &vt);
+  const int64_t m0 = a.v0 + vt * a.step, n0 = (int64_t)rt * P::BN, ms = min(a.step, a.v1 - m0);
+  f32x16 acc[TM][TN];
+  P::run(a.weight, m0, ms, a.x, n0, a.rows - n0, 0, a.width, (lds_char*)lds, acc);
   if constexpr (BACK) {
-    float g, ge;
-    int64_t y;
-    const bool present = row_gradients(a, r, &g, &ge, &y);
-    for (int c = 0; c < TILE && c0 + c < a.v1; c++) {
-      float o = 0.f;
-      if (present) {
-        const float lp = row[c] - a.lse_in[r], p = expf(lp);
-        o = p == 0.f ? 0.f : -p * (ge == 0.f ? g : fmaf(ge, lp + a.entropy_in[r], g));
-        if (c0 + c == y) o += g;
-      }
-      a.G[r * a.piece + c0 - a.v0 + c] = o;
+    typedef typename Elem<DT>::T T;
+#pragma unroll
+    for (int j = 0; j < TN; j++) {
+      const int64_t n = n0 + P::col(j);
+      if (n >= a.rows) continue;
+      const RowInfo w = a.info[n];
+      T* const to = (T*)a.G + n * a.piece + (m0 - a.v0);
+      const int y = (int)(w.y >= m0 && w.y < m0 + ms ? w.y - m0 : -1);
+#pragma unroll
+      for (int i = 0; i < TM; i++)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+          const int v = P::row(i, r);
+          if (v >= ((ms + 7) & ~(int64_t)7)) continue;      // the last vector of 16 bytes is whole, with zeros
+          float o[4];
+#pragma unroll
+          for (int e = 0; e < 4; e++) {
+            const float lp = fmaf(acc[i][j][r + e], a.scale, -w.lse), p = __builtin_amdgcn_exp2f(lp * LOG2E);
+            o[e] = p == 0.f ? 0.f : -p * (w.ge == 0.f ? w.g : fmaf(w.ge, lp + w.h, w.g));
+            if (v + e == y) o[e] += w.g;
+            if (!w.present || v + e >= ms) o[e] = 0.f;
+          }
+          if constexpr (DT == EXTERND_F32) *(float4*)(to + v) = float4{o[0], o[1], o[2], o[3]};
+          else {
+            v2u b;
+#pragma unroll
+            for (int e = 0; e < 2; e++)
+              b[e] = (unsigned)__builtin_bit_cast(uint16_t, Elem<DT>::store(o[2 * e])) |
+                     (unsigned)__builtin_bit_cast(uint16_t, Elem<DT>::store(o[2 * e + 1])) << 16;
+            *(v2u*)(to + v) = b;
+          }
+        }
     }
   } else {
-    float top = -INFINITY;
-    for (int c = 0; c < TILE; c++) top = fmaxf(top, row[c]);
-    Part p = {top, 0.f, 0.f, 0.f};
-    const float ref = fmaxf(top, -3.402823466e38f);
-    for (int c = 0; c < TILE; c++) {
-      const float d = propagating_max(row[c] - ref, -150.f), e = expf(d);
-      p.sum += row[c] == -INFINITY ? 0.f : e;
-      p.mean += row[c] == -INFINITY ? 0.f : e * d;
+    Part* const shared = (Part*)lds;      // WM x BN
+    const int wave = threadIdx.x >> 6;
+    const float c = a.scale * LOG2E;
+#pragma unroll
+    for (int j = 0; j < TN; j++) {
+      const int64_t n = n0 + P::col(j), y = a.targets && n < a.rows ? a.targets[n] - m0 : -1;
+      if (ms < P::BM) {
+#pragma unroll
+        for (int i = 0; i < TM; i++)
+#pragma unroll
+          for (int r = 0; r < 16; r++)
+            if (P::row(i, r) >= ms) acc[i][j][r] = -INFINITY;
+      }
+      if (__any(y >= P::row(0, 0) && y < P::row(0, 0) + TM * 32)) {      // a target among this wave's
+#pragma unroll
+        for (int i = 0; i < TM; i++)
+#pragma unroll
+          for (int r = 0; r < 16; r++)
+            if (P::row(i, r) == y) a.at_target[n] = acc[i][j][r] * a.scale;
+      }
+      float top = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < TM; i++)
+#pragma unroll
+        for (int r = 0; r < 16; r++) top = fmaxf(top, acc[i][j][r]);
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const float ref = fmaxf(top, -3.402823466e38f);
+      float s[4] = {}, t[4] = {};
+#pragma unroll
+      for (int i = 0; i < TM; i++)
+#pragma unroll
+        for (int r = 0; r < 16; r++) {
+          // 2^-200 is 0; the maximum passes a NaN on
+          const float d = propagating_max((acc[i][j][r] - ref) * c, -200.f), e = __builtin_amdgcn_exp2f(d);
+          s[r & 3] += e;
+          t[r & 3] = fmaf(e, d, t[r & 3]);
+        }
+      float sum = (s[0] + s[1]) + (s[2] + s[3]), mean = ((t[0] + t[1]) + (t[2] + t[3]));
+      sum += __shfl_xor(sum, 32);
+      mean += __shfl_xor(mean, 32);
+      top *= a.scale;
+      if (!(threadIdx.x & 32)) shared[wave / P::WN * P::BN + P::col(j)] = Part{top, sum, mean * LN2, 0.f};
     }
-    a.parts[r * a.tiles + blockIdx.x] = p;
-    if (a.targets && a.targets[r] >= c0 && a.targets[r] < min(c0 + TILE, a.v1)) a.at_target[r] = row[a.targets[r] - c0];
+    __syncthreads();
+    const int n = threadIdx.x;
+    if (n < P::BN && n0 + n < a.rows) {
+      float top = -INFINITY, sum = 0.f, mean = 0.f;
+      for (int w = 0; w < P::WM; w++) top = fmaxf(top, shared[w * P::BN + n].top);
+      const float ref = fmaxf(top, -3.402823466e38f);
+      for (int w = 0; w < P::WM; w++) {
+        const Part p = shared[w * P::BN + n];
+        const float d = fmaxf(p.top, -3.402823466e38f) - ref, f = __builtin_amdgcn_exp2f(d * LOG2E);
+        if (p.sum == 0.f) continue;
+        sum += p.sum * f;
+        mean += f == 0.f ? 0.f : fmaf(p.sum, d, p.mean) * f;
+      }
+      a.parts[(n0 + n) * a.vocab_tiles + vt] = Part{top, sum, mean, 0.f};
+    }
   }
 }
 
-// A wave joins a row's parts.
-__global__ __launch_bounds__(64) void k_logits_join(LinearArgs a) {
+// A workgroup joins a row's parts.
+__global__ __launch_bounds__(256) void k_logits_join(LinearArgs a) {
+  __shared__ float lds[3][4];
   const int64_t r = blockIdx.x;
-  const Part* p = a.parts + r * a.tiles;
-  float top = -3.402823466e38f, sum = 0.f, mean = 0.f;
-  for (int64_t i = threadIdx.x; i < a.tiles; i += 64) top = fmaxf(top, p[i].top);
-  for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-  for (int64_t i = threadIdx.x; i < a.tiles; i += 64) {
-    if (p[i].sum == 0.f) continue;
-    const float d = fmaxf(p[i].top, -3.402823466e38f) - top, f = expf(d);
-    sum += p[i].sum * f;
-    mean += f == 0.f ? 0.f : fmaf(p[i].sum, d, p[i].mean) * f;
+  const Part* p = a.parts + r * a.vocab_tiles;
+  float top = -3.402823466e38f, sum = 0.f, mean = 0.f;      // of this thread's parts, against the largest so far
+  for (int i = threadIdx.x; i < a.vocab_tiles; i += 256) {
+    const Part q = p[i];
+    if (q.sum == 0.f) continue;
+    const float to = fmaxf(top, q.top), f = __builtin_amdgcn_exp2f((top - to) * LOG2E), d = fmaxf(q.top, -3.402823466e38f) - to,
+                e = __builtin_amdgcn_exp2f(d * LOG2E);
+    mean = (f == 0.f ? 0.f : fmaf(sum, top - to, mean) * f) + (e == 0.f ? 0.f : fmaf(q.sum, d, q.mean) * e);
+    sum = sum * f + q.sum * e;
+    top = to;
   }
-  for (int d = 32; d; d >>= 1) {
-    sum += __shfl_xor(sum, d);
-    mean += __shfl_xor(mean, d);
+  float all = top;
+  for (int d = 32; d; d >>= 1) all = fmaxf(all, __shfl_xor(all, d));
+  if ((threadIdx.x & 63) == 0) lds[0][threadIdx.x >> 6] = all;
+  __syncthreads();
+  all = fmaxf(fmaxf(lds[0][0], lds[0][1]), fmaxf(lds[0][2], lds[0][3]));
+  const float d = top - all, f = __builtin_amdgcn_exp2f(d * LOG2E);
+  mean = sum == 0.f || f == 0.f ? 0.f : fmaf(sum, d, mean) * f;
+  sum = sum == 0.f ? 0.f : sum * f;
+  for (int x = 32; x; x >>= 1) {
+    sum += __shfl_xor(sum, x);
+    mean += __shfl_xor(mean, x);
   }
+  if ((threadIdx.x & 63) == 0) {
+    lds[1][threadIdx.x >> 6] = sum;
+    lds[2][threadIdx.x >> 6] = mean;
+  }
+  __syncthreads();
   if (threadIdx.x) return;
+  sum = (lds[1][0] + lds[1][1]) + (lds[1][2] + lds[1][3]);
+  mean = (lds[2][0] + lds[2][1]) + (lds[2][2] + lds[2][3]);
   const bool none = sum == 0.f;
-  const float l = logf(sum), lse = none ? -INFINITY : top + l;
+  const float l = LN2 * log2f(sum), lse = none ? -INFINITY : all + l;
   if (a.lse) a.lse[r] = lse;
   if (a.entropy) a.entropy[r] = none ? 0.f : l - mean / sum;
   if (a.logprob) {
@@ -133,49 +213,176 @@ __global__ __launch_bounds__(64) void k_logits_join(LinearArgs a) {
   }
 }
 
-// grad_x (+)= G weight over this piece, in fp32.
-template <int DT>
-__global__ __launch_bounds__(256) void k_grad_x(LinearArgs a) {
-  typedef typename Elem<DT>::T T;
-  const int64_t r0 = (int64_t)blockIdx.y * TILE, c0 = (int64_t)blockIdx.x * TILE;
-  const T* w = (const T*)a.weight;
-  float sum[4][4] = {};
-  tile_product([&](int i, int64_t k) { return r0 + i < a.rows ? a.G[(r0 + i) * a.piece + k] : 0.f; },
-               [&](int i, int64_t k) { return c0 + i < a.width ? Elem<DT>::load(w[(a.v0 + k) * a.weight_stride + c0 + i]) : 0.f; }, 0,
-               a.v1 - a.v0, sum);
-  for (int i = 0; i < 4; i++)
-    for (int j = 0; j < 4; j++) {
-      const int64_t r = r0 + (threadIdx.x >> 4) * 4 + i, c = c0 + (threadIdx.x & 15) * 4 + j;
-      if (r >= a.rows || c >= a.width) continue;
-      float* d = a.dx + r * a.width + c;
-      const float all = (a.v0 ? *d : 0.f) + sum[i][j];
-      *d = all;
-      if (a.v1 == a.vocab) {
-        float g, ge;
-        int64_t y;
-        ((T*)a.grad_x)[r * a.grad_x_stride + c] = Elem<DT>::store(row_gradients(a, r, &g, &ge, &y) ? all * a.scale : 0.f);
-      }
+// What each row's gradient is made of.  For fp16 one workgroup goes over all
+// rows, as the least `up` scales what the rows' sum is made of.
+__global__ __launch_bounds__(1024) void k_rows(LinearArgs a, int fp16) {
+  __shared__ float least[16];
+  float up_all = 0x1p120f;
+  for (int64_t r = (int64_t)blockIdx.x * 1024 + threadIdx.x; r < a.rows; r += (int64_t)gridDim.x * 1024) {
+    const int64_t y = a.targets ? a.targets[r] : -1;
+    const bool asked = y >= 0 && y < a.vocab;
+    RowInfo w = {};
+    w.y = asked ? (int32_t)y : -1;
+    w.g = a.g_logprob && asked ? a.g_logprob[r] : 0.f;
+    w.ge = a.g_entropy ? a.g_entropy[r] : 0.f;
+    w.present = w.g != 0.f || w.ge != 0.f;
+    w.lse = a.lse_in[r];
+    w.h = a.g_entropy ? a.entropy_in[r] : 0.f;
+    w.up = 1.f;
+    if (fp16 && w.present) {
+      // |G| <= |g| + |ge| (p |ln p| + p H) < |g| + |ge| (1 + H)
+      const float most = fabsf(w.g) + (w.ge == 0.f ? 0.f : fabsf(w.ge) * (1.f + fabsf(w.h)));
+      const int k = most <= 3.402823466e38f ? 14 - ilogbf(most) : 0;
+      w.up = ldexpf(1.f, k > 120 ? 120 : k < -120 ? -120 : k);
+      w.g *= w.up;
+      w.ge *= w.up;
+      up_all = fminf(up_all, w.up);
     }
+    a.info[r] = w;
+  }
+  if (!fp16) {
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.up_all = 1.f;
+    return;
+  }
+  for (int d = 32; d; d >>= 1) up_all = fminf(up_all, __shfl_xor(up_all, d));
+  if ((threadIdx.x & 63) == 0) least[threadIdx.x >> 6] = up_all;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int i = 1; i < 16; i++) up_all = fminf(up_all, least[i]);
+    *a.up_all = up_all;
+  }
 }
 
+// x for its product with G: rows that take no part are zeros whatever they hold,
+// fp16 rows are down by what their G is up beyond the least (a power of two:
+// exact but for entries that it takes below 2^-14).
 template <int DT>
-__global__ __launch_bounds__(256) void k_grad_weight(LinearArgs a) {
+__global__ __launch_bounds__(256) void k_pack(LinearArgs a) {
   typedef typename Elem<DT>::T T;
-  const int64_t r0 = (int64_t)blockIdx.y * TILE, c0 = (int64_t)blockIdx.x * TILE;
-  const T* x = (const T*)a.x;
-  float sum[4][4] = {};
-  tile_product([&](int i, int64_t k) { return a.v0 + r0 + i < a.v1 ? a.G[k * a.piece + r0 + i] : 0.f; },
-               [&](int i, int64_t k) {
-                 float g, ge;
-                 int64_t y;
-                 return c0 + i < a.width && row_gradients(a, k, &g, &ge, &y) ? Elem<DT>::load(x[k * a.x_stride + c0 + i]) : 0.f;
-               },
-               0, a.rows, sum);
-  for (int i = 0; i < 4; i++)
-    for (int j = 0; j < 4; j++) {
-      const int64_t r = r0 + (threadIdx.x >> 4) * 4 + i, c = c0 + (threadIdx.x & 15) * 4 + j;
-      if (a.v0 + r < a.v1 && c < a.width) ((T*)a.grad_weight)[(a.v0 + r) * a.grad_weight_stride + c] = Elem<DT>::store(sum[i][j] * a.scale);
+  constexpr int E = Vec<DT>::E;
+  const int64_t units = a.packed_width / E, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= units * a.rows) return;
+  const int64_t r = i / units, c = (i - r * units) * E;
+  const RowInfo w = a.info[r];
+  const T* from = (const T*)a.x.p + r * a.x.stride + c;
+  float x[E] = {};
+  if (w.present) {
+    if (c + E <= a.width) Vec<DT>::unpack(load_any(from), x);
+    else
+      for (int e = 0; e < E; e++) x[e] = c + e < a.width ? Elem<DT>::load(from[e]) : 0.f;
+    const float f = DT == EXTERND_F16 ? *a.up_all / w.up : 1.f;
+#pragma unroll
+    for (int e = 0; e < E; e++) x[e] *= f;
+  }
+  *(v4u*)((T*)a.packed + r * a.packed_width + c) = Vec<DT>::pack(x);
+}
+
+// G weight of this piece (columns of weight along m, rows of G along n), added to
+// the split's sums so far.
+template <typename P>
+__global__ __launch_bounds__(GEMM_THREADS, 2) void k_grad_x(LinearArgs a) {
+  __shared__ __align__(16) char lds[P::LDS];
+  const int cols = (int)((a.width + P::BM - 1) / P::BM);
+  int rt, other;
+  place_tile(a.row_tiles, cols * a.splits, &rt, &other);
+  const int s = other / cols;
+  const int64_t m0 = (int64_t)(other - s * cols) * P::BM, n0 = (int64_t)rt * P::BN, k0 = s * a.split, K = min(a.split, a.v1 - a.v0 - k0);
+  f32x16 acc[P::TM][P::TN];
+  const Operand G = {a.G, a.piece};
+  P::run(a.weight, m0, a.width - m0, G, n0, a.rows - n0, a.v0 + k0, K > 0 ? K : 0, (lds_char*)lds, acc, -a.v0);
+#pragma unroll
+  for (int j = 0; j < P::TN; j++) {
+    const int64_t n = n0 + P::col(j);
+    if (n >= a.rows) continue;
+    float* const to = a.dx + (s * a.rows + n) * a.dx_width + m0;
+#pragma unroll
+    for (int i = 0; i < P::TM; i++)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4) {
+        const int c = P::row(i, r);
+        if (m0 + c >= a.dx_width) continue;
+        float4 x = {acc[i][j][r], acc[i][j][r + 1], acc[i][j][r + 2], acc[i][j][r + 3]};
+        if (a.v0) {
+          const float4 b = *(const float4*)(to + c);
+          x = float4{x.x + b.x, x.y + b.y, x.z + b.z, x.w + b.w};
+        }
+        *(float4*)(to + c) = x;
+      }
+  }
+}
+
+// The splits' sums joined in order, scaled and rounded.
+template <int DT>
+__global__ __launch_bounds__(256) void k_grad_x_join(LinearArgs a) {
+  typedef typename Elem<DT>::T T;
+  const int64_t units = a.dx_width / 4, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= units * a.rows) return;
+  const int64_t r = i / units, c = (i - r * units) * 4;
+  const RowInfo w = a.info[r];
+  float x[4] = {};
+  if (w.present) {
+    for (int s = 0; s < a.splits; s++) {
+      const float4 b = *(const float4*)(a.dx + (s * a.rows + r) * a.dx_width + c);
+      x[0] += b.x, x[1] += b.y, x[2] += b.z, x[3] += b.w;
     }
+  }
+  const float f = a.scale, down = 1.f / w.up;
+  T* const to = (T*)a.grad_x + r * a.grad_x_stride + c;
+#pragma unroll
+  for (int e = 0; e < 4; e++)
+    if (c + e < a.width) to[e] = Elem<DT>::store(x[e] * f * down);
+}
+
+// G^T x of this piece: columns of x along m, of G (the vocabulary) along n.
+template <typename P>
+__global__ __launch_bounds__(GEMM_THREADS, 2) void k_grad_weight(LinearArgs a) {
+  typedef typename Elem<P::DT>::T T;
+  __shared__ __align__(16) char lds[P::LDS];
+  int ct, vt;
+  place_tile((int)((a.width + P::BM - 1) / P::BM), a.vocab_tiles, &ct, &vt);
+  const int64_t m0 = (int64_t)ct * P::BM, n0 = (int64_t)vt * P::BN, ns = a.v1 - a.v0;
+  f32x16 acc[P::TM][P::TN];
+  const Operand x = {a.packed, a.packed_width}, G = {a.G, a.piece};
+  P::run(x, m0, a.packed_width - m0, G, n0, (ns - n0 + 7) & ~(int64_t)7, 0, a.rows, (lds_char*)lds, acc);      // whole vectors: G's rows have room
+  const float f = a.scale, down = 1.f / *a.up_all;
+#pragma unroll
+  for (int j = 0; j < P::TN; j++) {
+    const int64_t n = n0 + P::col(j);
+    if (n >= ns) continue;
+    T* const to = (T*)a.grad_weight + (a.v0 + n) * a.grad_weight_stride + m0;
+#pragma unroll
+    for (int i = 0; i < P::TM; i++)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4) {
+        const int c = P::row(i, r);
+        float o[4];
+#pragma unroll
+        for (int e = 0; e < 4; e++) o[e] = acc[i][j][r + e] * f * down;
+        if (m0 + c + 4 <= a.width) {
+          if constexpr (P::DT == EXTERND_F32) {
+            store_any(to + c, Vec<EXTERND_F32>::pack(o));
+          } else {
+            typedef v2u any __attribute__((aligned(2)));
+            v2u b;
+#pragma unroll
+            for (int e = 0; e < 2; e++)
+              b[e] = (unsigned)__builtin_bit_cast(uint16_t, Elem<P::DT>::store(o[2 * e])) |
+                     (unsigned)__builtin_bit_cast(uint16_t, Elem<P::DT>::store(o[2 * e + 1])) << 16;
+            *(any*)(to + c) = b;
+          }
+        } else
+          for (int e = 0; e < 4; e++)
+            if (m0 + c + e < a.width) to[c + e] = Elem<P::DT>::store(o[e]);
+      }
+  }
+}
+
+// grad_weight without rows.
+template <int DT>
+__global__ __launch_bounds__(256) void k_zero_rows(LinearArgs a) {
+  typedef typename Elem<DT>::T T;
+  for (int64_t r = blockIdx.x; r < a.vocab; r += gridDim.x)
+    for (int64_t c = threadIdx.x; c < a.width; c += 256) ((T*)a.grad_weight)[r * a.grad_weight_stride + c] = T(0);
 }
 
 // ---------------------------------------------------------------------------
@@ -188,48 +395,136 @@ static bool linear_sizes(int64_t rows, int64_t vocab, int64_t width) {
   return rows <= (1 << 22) && vocab < INT32_MAX - 1023 && width <= (1 << 20);
 }
 
+// Rows of a tile.
+static int tile_rows(int32_t dtype, int64_t rows) {
+  if (rows <= 32) return 32;
+  return dtype == EXTERND_F32 || rows <= 128 ? 128 : 256;
+}
+
+// Vocabulary of a forward tile.  One row tile reads weight once, so the card's
+// CUs take equally many tiles of equal length: 65537 rows are 512 tiles of 136
+// and not 256 of 256 and one of 1.
+static int64_t forward_step(int64_t row_tiles, int64_t vocab) {
+  if (row_tiles > 1 || vocab <= 256 * CUS / 8) return 256;
+  const int64_t tiles = ceil_div(ceil_div(vocab, 256), CUS) * CUS;
+  return ceil_div(ceil_div(vocab, tiles), 8) * 8;
+}
+
 struct LinearWork {
-  size_t parts, at_target, G, dx, bytes;
-  int64_t tiles, piece;
+  size_t parts, at_target, info, up_all, packed, G, dx, bytes;
+  int64_t tiles, step, piece, packed_width, dx_width, split;
+  int splits;
 };
 
-static LinearWork forward_work(int64_t rows, int64_t vocab) {
+static LinearWork forward_work(int32_t dtype, int64_t rows, int64_t vocab) {
   LinearWork w = {};
   const int64_t r = rows < FORWARD_ROWS ? rows : FORWARD_ROWS;
-  w.tiles = ceil_div(vocab, TILE);
+  w.step = forward_step(ceil_div(r, tile_rows(dtype, r)), vocab);
+  w.tiles = ceil_div(vocab, w.step);
   w.parts = 0;
   w.at_target = round256((size_t)(r * w.tiles) * sizeof(Part));
   w.bytes = w.at_target + round256((size_t)r * 4);
   return w;
 }
 
-static LinearWork backward_work(int64_t rows, int64_t vocab, int64_t width, bool need_x) {
+static LinearWork backward_work(int32_t dtype, int64_t rows, int64_t vocab, int64_t width, bool need_x, bool need_weight) {
   LinearWork w = {};
-  w.piece = ((int64_t)1 << 25) / (rows ? rows : 1);
-  w.piece = ceil_div(w.piece < 1024 ? 1024 : w.piece, TILE) * TILE;
-  if (w.piece > ceil_div(vocab, TILE) * TILE) w.piece = ceil_div(vocab, TILE) * TILE;
-  w.G = 0;
-  w.dx = round256((size_t)(rows * w.piece) * 4);
-  w.bytes = w.dx + (need_x ? round256((size_t)(rows * width) * 4) : 0);
+  const int64_t most = PIECE_ENTRIES / rows, pieces = ceil_div(vocab, most < 2048 ? 2048 : most);
+  w.piece = ceil_div(ceil_div(vocab, pieces), 256) * 256;
+  const int vec = 16 / dtype_bytes(dtype);
+  w.packed_width = ceil_div(width, vec) * vec;
+  w.dx_width = ceil_div(width, 4) * 4;
+  const int64_t tiles = ceil_div(width, 256) * ceil_div(rows, tile_rows(dtype, rows));
+  int64_t splits = CUS / tiles;
+  const int64_t max_splits = ceil_div(w.piece, 512);
+  splits = splits < 1 ? 1 : splits > max_splits ? max_splits : splits;
+  w.split = ceil_div(ceil_div(w.piece, splits), 64) * 64;
+  w.splits = (int)ceil_div(w.piece, w.split);
+  size_t at = 0;
+  w.info = at, at += round256((size_t)rows * sizeof(RowInfo));
+  w.up_all = at, at += 256;
+  w.packed = at, at += need_weight ? round256((size_t)(rows * w.packed_width) * dtype_bytes(dtype)) : 0;
+  w.G = at, at += round256((size_t)(rows * w.piece) * dtype_bytes(dtype));
+  w.dx = at, at += need_x ? round256((size_t)(w.splits * rows * w.dx_width) * 4) : 0;
+  w.bytes = at;
   return w;
 }
 
-template <int DT>
-static void launch_forward(LinearArgs a, hipStream_t s) {
-  k_logits<DT, false><<<dim3((unsigned)a.tiles, (unsigned)ceil_div(a.rows, TILE)), 256, 0, s>>>(a);
-  k_logits_join<<<(unsigned)a.rows, 64, 0, s>>>(a);
+// Whether rows of 16-bit entries are whole vectors of 16 bytes at multiples of 16.
+static bool direct_rows(const Operand& o, int64_t width) { return !((uintptr_t)o.p & 15) && o.stride % 8 == 0 && width % 8 == 0; }
+
+template <typename P, bool BACK>
+static void launch_logits(LinearArgs a, hipStream_t s) {
+  a.row_tiles = (int)ceil_div(a.rows, P::BN);
+  a.vocab_tiles = (int)ceil_div(a.v1 - a.v0, a.step);
+  k_logits<P, BACK><<<(unsigned)(a.row_tiles * a.vocab_tiles), GEMM_THREADS, 0, s>>>(a);
+}
+template <typename P>
+static void launch_grad_x(LinearArgs a, hipStream_t s) {
+  a.row_tiles = (int)ceil_div(a.rows, P::BN);
+  k_grad_x<P><<<(unsigned)(a.row_tiles * ceil_div(a.width, P::BM) * a.splits), GEMM_THREADS, 0, s>>>(a);
+}
+template <typename P>
+static void launch_grad_weight(LinearArgs a, hipStream_t s) {
+  a.vocab_tiles = (int)ceil_div(a.v1 - a.v0, P::BN);
+  k_grad_weight<P><<<(unsigned)(ceil_div(a.width, P::BM) * a.vocab_tiles), GEMM_THREADS, 0, s>>>(a);
+}
+
+template <int DT, bool DIRECT, bool BACK>
+static void choose_logits(const LinearArgs& a, hipStream_t s) {
+  const int n = tile_rows(DT, a.rows);
+  if constexpr (DT == EXTERND_F32) {
+    if (n == 32) launch_logits<Product<DT, false, false, false, 256, 32, 8, 2>, BACK>(a, s);
+    else launch_logits<Product<DT, false, false, false, 256, 128, 4, 2>, BACK>(a, s);
+  } else {
+    if (n == 32) launch_logits<Product<DT, DIRECT, false, false, 256, 32, 8, DIRECT ? 4 : 2>, BACK>(a, s);
+    else if (n == 128) launch_logits<Product<DT, DIRECT, false, false, 256, 128, 4, DIRECT ? 3 : 2>, BACK>(a, s);
+    else launch_logits<Product<DT, DIRECT, false, false, 256, 256, 2, 2>, BACK>(a, s);
+  }
+}
+template <int DT, bool DIRECT>
+static void choose_grad_x(const LinearArgs& a, hipStream_t s) {
+  const int n = tile_rows(DT, a.rows);
+  if constexpr (DT == EXTERND_F32) {
+    if (n == 32) launch_grad_x<Product<DT, false, true, false, 256, 32, 8, 2>>(a, s);
+    else launch_grad_x<Product<DT, false, true, false, 256, 128, 4, 2>>(a, s);
+  } else {
+    if (n == 32) launch_grad_x<Product<DT, DIRECT, true, false, 256, 32, 8, DIRECT ? 4 : 2>>(a, s);
+    else if (n == 128) launch_grad_x<Product<DT, DIRECT, true, false, 256, 128, 4, DIRECT ? 3 : 2>>(a, s);
+    else launch_grad_x<Product<DT, DIRECT, true, false, 256, 256, 2, 2>>(a, s);
+  }
 }
 
 template <int DT>
-static void launch_backward(LinearArgs a, hipStream_t s) {
-  const unsigned rows = (unsigned)ceil_div(a.rows, TILE), cols = (unsigned)ceil_div(a.width, TILE);
+static void launch_forward(LinearArgs a, bool direct, hipStream_t s) {
+  if (DT != EXTERND_F32 && direct) choose_logits<DT, DT != EXTERND_F32, false>(a, s);
+  else choose_logits<DT, false, false>(a, s);
+  a.vocab_tiles = (int)ceil_div(a.vocab, a.step);
+  k_logits_join<<<(unsigned)a.rows, 256, 0, s>>>(a);
+}
+
+template <int DT>
+static void launch_backward(LinearArgs a, bool direct, hipStream_t s) {
+  if (!a.rows) {
+    k_zero_rows<DT><<<(unsigned)(a.vocab < 4096 ? a.vocab : 4096), 256, 0, s>>>(a);
+    return;
+  }
+  k_rows<<<DT == EXTERND_F16 ? 1 : (unsigned)ceil_div(a.rows, 1024), 1024, 0, s>>>(a, DT == EXTERND_F16);
+  if (a.grad_weight) k_pack<DT><<<(unsigned)ceil_div(a.rows * (a.packed_width / Vec<DT>::E), 256), 256, 0, s>>>(a);
   for (a.v0 = 0; a.v0 < a.vocab; a.v0 = a.v1) {
     a.v1 = a.v0 + a.piece < a.vocab ? a.v0 + a.piece : a.vocab;
-    const unsigned tiles = (unsigned)ceil_div(a.v1 - a.v0, TILE);
-    if (rows) k_logits<DT, true><<<dim3(tiles, rows), 256, 0, s>>>(a);
-    if (rows && a.grad_x) k_grad_x<DT><<<dim3(cols, rows), 256, 0, s>>>(a);
-    if (a.grad_weight) k_grad_weight<DT><<<dim3(cols, tiles), 256, 0, s>>>(a);
+    if (DT != EXTERND_F32 && direct) choose_logits<DT, DT != EXTERND_F32, true>(a, s);
+    else choose_logits<DT, false, true>(a, s);
+    if (a.grad_x) {
+      if (DT != EXTERND_F32 && direct) choose_grad_x<DT, DT != EXTERND_F32>(a, s);
+      else choose_grad_x<DT, false>(a, s);
+    }
+    if (a.grad_weight) {
+      if constexpr (DT == EXTERND_F32) launch_grad_weight<Product<DT, false, true, true, 256, 128, 4, 2>>(a, s);
+      else launch_grad_weight<Product<DT, true, true, true, 256, 256, 2, 2>>(a, s);
+    }
   }
+  if (a.grad_x) k_grad_x_join<DT><<<(unsigned)ceil_div(a.rows * (a.dx_width / 4), 256), 256, 0, s>>>(a);
 }
 
 }  // namespace externd
@@ -240,7 +535,7 @@ extern "C" {
 
 size_t externd_linear_logprobs_workspace_bytes(int32_t dtype, int64_t rows, int64_t vocab, int64_t width) {
   if (!dtype_ok(dtype) || rows < 0 || vocab < 1 || width < 1 || !linear_sizes(rows, vocab, width)) return 0;
-  return forward_work(rows ? rows : 1, vocab).bytes;
+  return forward_work(dtype, rows ? rows : 1, vocab).bytes;
 }
 
 int externd_linear_logprobs(const void* x, int64_t x_stride, const void* weight, int64_t weight_stride, int32_t dtype,
@@ -253,15 +548,13 @@ int externd_linear_logprobs(const void* x, int64_t x_stride, const void* weight,
   if (!linear_sizes(rows, vocab, width) || x_stride >= (1 << 22) || weight_stride >= (1 << 22)) return EXTERND_EUNSUPPORTED;
   if (!rows) return EXTERND_OK;
   if ((uintptr_t)workspace & 255) return EXTERND_EINVAL;
-  const LinearWork w = forward_work(rows, vocab);
+  const LinearWork w = forward_work(dtype, rows, vocab);
   if (!workspace || workspace_bytes < w.bytes) return EXTERND_EWORKSPACE;
   const hipStream_t s = (hipStream_t)stream;
   for (int64_t r = 0; r < rows; r += FORWARD_ROWS) {
     LinearArgs a = {};
-    a.x = (const char*)x + r * x_stride * dtype_bytes(dtype);
-    a.weight = weight;
-    a.x_stride = x_stride;
-    a.weight_stride = weight_stride;
+    a.x = {(const char*)x + r * x_stride * dtype_bytes(dtype), x_stride};
+    a.weight = {weight, weight_stride};
     a.rows = rows - r < FORWARD_ROWS ? rows - r : FORWARD_ROWS;
     a.vocab = a.v1 = vocab;
     a.width = width;
@@ -272,19 +565,19 @@ int externd_linear_logprobs(const void* x, int64_t x_stride, const void* weight,
     a.lse = lse ? lse + r : nullptr;
     a.parts = (Part*)((char*)workspace + w.parts);
     a.at_target = (float*)((char*)workspace + w.at_target);
-    a.tiles = w.tiles;
-    if (dtype == EXTERND_F32) launch_forward<EXTERND_F32>(a, s);
-    else if (dtype == EXTERND_BF16) launch_forward<EXTERND_BF16>(a, s);
-    else launch_forward<EXTERND_F16>(a, s);
+    a.step = w.step;
+    const bool direct = direct_rows(a.x, width) && direct_rows(a.weight, width);
+    if (dtype == EXTERND_F32) launch_forward<EXTERND_F32>(a, false, s);
+    else if (dtype == EXTERND_BF16) launch_forward<EXTERND_BF16>(a, direct, s);
+    else launch_forward<EXTERND_F16>(a, direct, s);
   }
   return hipGetLastError() == hipSuccess ? EXTERND_OK : EXTERND_EHIP;
 }
 
 size_t externd_linear_logprobs_backward_workspace_bytes(int32_t dtype, int64_t rows, int64_t vocab, int64_t width,
                                                         int32_t need_x, int32_t need_weight) {
-  (void)need_weight;
   if (!dtype_ok(dtype) || rows < 0 || vocab < 1 || width < 1 || !linear_sizes(rows, vocab, width)) return 0;
-  return backward_work(rows ? rows : 1, vocab, width, need_x).bytes;
+  return backward_work(dtype, rows ? rows : 1, vocab, width, need_x, need_weight).bytes;
 }
 
 int externd_linear_logprobs_backward(const void* x, int64_t x_stride, const void* weight, int64_t weight_stride,
@@ -299,18 +592,17 @@ int externd_linear_logprobs_backward(const void* x, int64_t x_stride, const void
   if (!linear_sizes(rows, vocab, width) || x_stride >= (1 << 22) || weight_stride >= (1 << 22)) return EXTERND_EUNSUPPORTED;
   if (!grad_weight && (!grad_x || !rows)) return EXTERND_OK;
   if ((uintptr_t)workspace & 255) return EXTERND_EINVAL;
-  const LinearWork w = backward_work(rows ? rows : 1, vocab, width, grad_x);
+  const LinearWork w = backward_work(dtype, rows ? rows : 1, vocab, width, grad_x, grad_weight);
   if (!workspace || workspace_bytes < w.bytes) return EXTERND_EWORKSPACE;
   LinearArgs a = {};
-  a.x = x;
-  a.weight = weight;
-  a.x_stride = x_stride;
-  a.weight_stride = weight_stride;
+  a.x = {x, x_stride};
+  a.weight = {weight, weight_stride};
   a.rows = rows;
   a.vocab = vocab;
   a.width = width;
   a.targets = targets;
   a.scale = scale;
+  a.step = 256;
   a.lse_in = lse;
   a.entropy_in = entropy;
   a.g_logprob = g_logprob;
@@ -319,13 +611,22 @@ int externd_linear_logprobs_backward(const void* x, int64_t x_stride, const void
   a.grad_weight = grad_weight;
   a.grad_x_stride = grad_x_stride;
   a.grad_weight_stride = grad_weight_stride;
-  a.G = (float*)((char*)workspace + w.G);
-  a.dx = (float*)((char*)workspace + w.dx);
+  char* const at = (char*)workspace;
+  a.info = (RowInfo*)(at + w.info);
+  a.up_all = (float*)(at + w.up_all);
+  a.packed = at + w.packed;
+  a.G = at + w.G;
+  a.dx = (float*)(at + w.dx);
   a.piece = w.piece;
+  a.packed_width = w.packed_width;
+  a.dx_width = w.dx_width;
+  a.split = w.split;
+  a.splits = w.splits;
+  const bool direct = direct_rows(a.x, width) && direct_rows(a.weight, width);
   const hipStream_t s = (hipStream_t)stream;
-  if (dtype == EXTERND_F32) launch_backward<EXTERND_F32>(a, s);
-  else if (dtype == EXTERND_BF16) launch_backward<EXTERND_BF16>(a, s);
-  else launch_backward<EXTERND_F16>(a, s);
+  if (dtype == EXTERND_F32) launch_backward<EXTERND_F32>(a, false, s);
+  else if (dtype == EXTERND_BF16) launch_backward<EXTERND_BF16>(a, direct, s);
+  else launch_backward<EXTERND_F16>(a, direct, s);
   return hipGetLastError() == hipSuccess ? EXTERND_OK : EXTERND_EHIP;
 }
 
