@@ -1089,28 +1089,45 @@ def clip_gradients(tensors, max_norm: float = float("inf"), out=None, stream=Non
     if not max_norm >= 0:
         raise ExterndError(EINVAL, "externd_clip_gradients")
     device = tensors[0].device if tensors else torch.device("cuda", torch.cuda.current_device())
-    spans = []
-    for i, (t, o) in enumerate(zip(tensors, outs)):
-        _dtype_code(torch, t.dtype, f"tensors[{i}]")
-        if not (t.is_cuda and t.device == device and _dense(t)):
-            raise ValueError(f"tensors[{i}]: expected a dense CUDA tensor on {device}, got {tuple(t.shape)} {t.stride()} "
-                             f"on {t.device}")
-        if o is not t and not (o.dtype is t.dtype and o.shape == t.shape and o.device == t.device and _dense(o)
-                               and o.stride() == t.stride()):
-            raise ValueError(f"out[{i}]: expected {t.dtype} {tuple(t.shape)} {t.stride()} on {t.device}, got {o.dtype} "
-                             f"{tuple(o.shape)} {o.stride()} on {o.device}")
-        if max_norm != float("inf") and t.numel():
-            spans.append((o.data_ptr(), o.data_ptr() + o.numel() * o.element_size(), i, i))
-            if o.data_ptr() != t.data_ptr():
-                spans.append((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size(), -1, i))
-    # what is written lies in no other tensor (a tensor that is only read may be given twice)
-    spans.sort()
-    end, wrote = 0, True
-    for a, b, w, i in spans:
-        if a < end and (w >= 0 or wrote):
-            raise ValueError(f"tensors[{i}]: what is written overlaps another tensor")
-        if b > end:
-            end, wrote = b, w >= 0
+    index = device.index
+    if _dtype_codes is None:
+        _dtype_code(torch, torch.float32, "")
+    # hundreds of tensors are ordinary: one look at each
+    ins, sizes, codes = [], [], []
+    for i, t in enumerate(tensors):
+        code = _dtype_codes.get(t.dtype)
+        if code is None or t.get_device() != index or not (t.is_contiguous() or _dense(t)):
+            raise ValueError(f"tensors[{i}]: expected a dense CUDA tensor of float32, bfloat16 or float16 on {device}, got "
+                             f"{t.dtype} {tuple(t.shape)} {t.stride()} on {t.device}")
+        ins.append(t.data_ptr())
+        sizes.append(t.numel())
+        codes.append(code)
+    if out is None:
+        ops = ins
+    else:
+        ops = []
+        for i, (t, o) in enumerate(zip(tensors, outs)):
+            if not (o.dtype is t.dtype and o.shape == t.shape and o.get_device() == index
+                    and (o.is_contiguous() and t.is_contiguous() or o.stride() == t.stride())):
+                raise ValueError(f"out[{i}]: expected {t.dtype} {tuple(t.shape)} {t.stride()} on {t.device}, got {o.dtype} "
+                                 f"{tuple(o.shape)} {o.stride()} on {o.device}")
+            ops.append(o.data_ptr())
+    if max_norm != float("inf") and tensors:
+        # what is written lies in no other tensor (one that is only read may be given twice)
+        a, n = np.array([ops, ins], dtype=np.int64), np.array([sizes, sizes], dtype=np.int64)
+        b = a + n * np.where(np.array(codes) == 0, 4, 2)
+        wrote = np.zeros(a.shape, dtype=bool)
+        wrote[0] = True
+        keep = n > 0
+        keep[1] &= a[0] != a[1]
+        a, b, wrote = a[keep], b[keep], wrote[keep]
+        order = np.lexsort((b, a))
+        a, b, wrote = a[order], b[order], wrote[order]
+        # ends so far, of all and of what is written
+        end = np.maximum.accumulate(b)[:-1]
+        end_wrote = np.maximum.accumulate(np.where(wrote, b, 0))[:-1]
+        if np.any((a[1:] < end) & wrote[1:]) or np.any(a[1:] < end_wrote):
+            raise ValueError("tensors: what is written overlaps another tensor")
     n = len(tensors)
     norm = torch.empty((), dtype=torch.float32, device=device)
     L = lib()
@@ -1120,11 +1137,9 @@ def clip_gradients(tensors, max_norm: float = float("inf"), out=None, stream=Non
         nbytes = L.externd_clip_gradients_workspace_bytes(n)
         workspace = torch.empty((nbytes,), dtype=torch.uint8, device=device)
         wp = workspace.data_ptr()
-    ins = (_c_ptr * n)(*[t.data_ptr() for t in tensors])
-    ops = (_c_ptr * n)(*[t.data_ptr() for t in outs])
-    sizes = (_c_i64 * n)(*[t.numel() for t in tensors])
-    codes = (_c_i32 * n)(*[_dtype_codes[t.dtype] for t in tensors])
-    st = L.externd_clip_gradients(n, ins, ops, sizes, codes, max_norm, norm.data_ptr(), wp, nbytes, _stream_ptr(torch, stream))
+    ptrs, counts, types = np.array([ins, ops], dtype=np.int64), np.array(sizes, dtype=np.int64), np.array(codes, dtype=np.int32)
+    st = L.externd_clip_gradients(n, ptrs.ctypes.data, ptrs.ctypes.data + 8 * n, counts.ctypes.data, types.ctypes.data, max_norm,
+                                  norm.data_ptr(), wp, nbytes, _stream_ptr(torch, stream))
     if st != OK:
         raise ExterndError(st, "externd_clip_gradients")
     return norm

@@ -136,10 +136,11 @@ __global__ __launch_bounds__(256) void k_scale(ClipList l, const double* partial
   // what that takes below fp32's normal numbers ends as 0
   const float before = ratio < 0x1p-100 && ratio > 0.0 ? exp2f((float)(ilogb(ratio) / 2)) : 1.f;
   const float factor = whole ? 1.f : (float)(ratio / before);      // NaN: it stays
+  // from the stretch's end, which k_squares read last and which may still be in the cache
   const uint32_t c0 = blockIdx.x * l.each, c1 = min(c0 + l.each, l.chunks);
-  int t = c0 < c1 ? tensor_of(l, c0) : 0;
-  for (uint32_t c = c0; c < c1; c++) {
-    while (t + 1 < l.count && l.first[t + 1] <= c) t++;
+  int t = c0 < c1 ? tensor_of(l, c1 - 1) : 0;
+  for (uint32_t c = c1; c-- > c0;) {
+    while (l.first[t] > c) t--;
     if (whole && l.in[t] == l.out[t]) continue;
     const int64_t at = (int64_t)(c - l.first[t]) * CLIP_CHUNK;
     const int n = (int)min(CLIP_CHUNK, l.size[t] - at);
