@@ -9,6 +9,8 @@
 // each lane picks its vector of global memory accordingly.
 #pragma once
 
+#include <type_traits>
+
 #include "externd_decode.hpp"
 
 namespace externd {
@@ -55,7 +57,7 @@ struct Tile {
     *row = i / CH;
     const int v = i % CH;
     if constexpr (COL) *vec = ((v >> 1) ^ spread(*row)) << 1 | (v & 1);
-    else *vec = v ^ ((*row / (8 / CH)) & (CH - 1));
+    else *vec = v ^ ((*row / (16 / CH)) & (CH - 1));
   }
   // By columns: pairs of vectors (16 columns) of four rows of k go to different banks.
   static __device__ __forceinline__ int spread(int k) { return (2 * (k & 3)) & (X / 16 - 1); }
@@ -71,7 +73,7 @@ struct Tile {
       const v2u a = __builtin_bit_cast(v2u, lo), b = __builtin_bit_cast(v2u, hi);
       return v4u{a[0], a[1], b[0], b[1]};
     } else {
-      const int row = x0 + (lane & 31), v = (ks * 2 + (lane >> 5)) ^ ((row / (8 / CH)) & (CH - 1));
+      const int row = x0 + (lane & 31), v = (ks * 2 + (lane >> 5)) ^ ((row / (16 / CH)) & (CH - 1));
       return *(const __attribute__((address_space(3))) v4u*)(t + (row * CH + v) * 16);
     }
   }
@@ -296,16 +298,46 @@ struct Product {
         la.issue(lds + stage * STAGE);
         lb.issue(lds + stage * STAGE + TA::BYTES);
       };
-      for (int s = 0; s < STAGES - 1; s++) issue(s);      // past the last step: zeros, which nothing reads
-      int stage = 0, next = STAGES - 1;
-      for (int64_t t = 0; t < steps; t++) {
-        if (fewer) wait_loads<TA::LOADS*(STAGES - 2)>();
-        else wait_loads<EACH*(STAGES - 2)>();
+      auto wait = [&](auto stages) {
+        constexpr int N = decltype(stages)::value;
+        if (fewer) wait_loads<TA::LOADS * N>();
+        else wait_loads<EACH * N>();
         barrier();
-        issue(next);
-        step(lds + stage * STAGE, acc);
-        stage = stage + 1 == STAGES ? 0 : stage + 1;
-        next = next + 1 == STAGES ? 0 : next + 1;
+      };
+      // A step's fragments are read one sixteenth of K ahead of their products,
+      // those of the next step as well: the barrier and the loads of a step
+      // stand in front of products whose operands are in registers.
+      constexpr int NK = BK / 16;
+      static_assert(NK % 2 == 0, "two sets of fragments in turn");
+      v4u fa[2][TM], fb[2][TN];
+      const int wave = threadIdx.x >> 6, ma = wave / WN * TM * 32, nb = wave % WN * TN * 32;
+      auto read = [&](int set, const lds_char* s, int ks) {
+#pragma unroll
+        for (int j = 0; j < TN; j++) fb[set][j] = TB::fragment(s + TA::BYTES, nb + j * 32, ks);
+#pragma unroll
+        for (int i = 0; i < TM; i++) fa[set][i] = TA::fragment(s, ma + i * 32, ks);
+      };
+      for (int s = 0; s < STAGES; s++) issue(s);      // past the last step: zeros, which nothing reads
+      wait(std::integral_constant<int, STAGES - 1>());
+      read(0, lds, 0);
+      int stage = 0;
+      for (int64_t t = 0; t < steps; t++) {
+        const int next = stage + 1 == STAGES ? 0 : stage + 1;
+#pragma unroll
+        for (int ks = 0; ks < NK; ks++) {
+          if (ks < NK - 1) read((ks + 1) & 1, lds + stage * STAGE, ks + 1);
+          else if (t + 1 < steps) {
+            wait(std::integral_constant<int, STAGES - 2>());
+            issue(stage);
+            read(0, lds + next * STAGE, 0);
+          }
+#pragma unroll
+          for (int i = 0; i < TM; i++)
+#pragma unroll
+            for (int j = 0; j < TN; j++) acc[i][j] = mfma<DT>(fa[ks & 1][i], fb[ks & 1][j], acc[i][j]);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        stage = next;
       }
       wait_loads<0>();
       barrier();
