@@ -309,36 +309,46 @@ struct Product {
       // stand in front of products whose operands are in registers.
       constexpr int NK = BK / 16;
       static_assert(NK % 2 == 0, "two sets of fragments in turn");
-      v4u fa[2][TM], fb[2][TN];
       const int wave = threadIdx.x >> 6, ma = wave / WN * TM * 32, nb = wave % WN * TN * 32;
-      auto read = [&](int set, const lds_char* s, int ks) {
-#pragma unroll
-        for (int j = 0; j < TN; j++) fb[set][j] = TB::fragment(s + TA::BYTES, nb + j * 32, ks);
-#pragma unroll
-        for (int i = 0; i < TM; i++) fa[set][i] = TA::fragment(s, ma + i * 32, ks);
-      };
+      // of this wave's 32 x 32 products, how many lie in the operands
+      const int tm = (int)max((int64_t)0, min((m_count - ma + 31) / 32, (int64_t)TM)), tn = (int)max((int64_t)0, min((n_count - nb + 31) / 32, (int64_t)TN));
       for (int s = 0; s < STAGES; s++) issue(s);      // past the last step: zeros, which nothing reads
       wait(std::integral_constant<int, STAGES - 1>());
-      read(0, lds, 0);
-      int stage = 0;
-      for (int64_t t = 0; t < steps; t++) {
-        const int next = stage + 1 == STAGES ? 0 : stage + 1;
+      auto loop = [&](auto partial) {
+        v4u fa[2][TM], fb[2][TN];
+        auto read = [&](int set, const lds_char* s, int ks) {
 #pragma unroll
-        for (int ks = 0; ks < NK; ks++) {
-          if (ks < NK - 1) read((ks + 1) & 1, lds + stage * STAGE, ks + 1);
-          else if (t + 1 < steps) {
-            wait(std::integral_constant<int, STAGES - 2>());
-            issue(stage);
-            read(0, lds + next * STAGE, 0);
-          }
+          for (int j = 0; j < TN; j++)
+            if (!partial || j < tn) fb[set][j] = TB::fragment(s + TA::BYTES, nb + j * 32, ks);
 #pragma unroll
           for (int i = 0; i < TM; i++)
+            if (!partial || i < tm) fa[set][i] = TA::fragment(s, ma + i * 32, ks);
+        };
+        read(0, lds, 0);
+        int stage = 0;
+        for (int64_t t = 0; t < steps; t++) {
+          const int next = stage + 1 == STAGES ? 0 : stage + 1;
 #pragma unroll
-            for (int j = 0; j < TN; j++) acc[i][j] = mfma<DT>(fa[ks & 1][i], fb[ks & 1][j], acc[i][j]);
-          __builtin_amdgcn_sched_barrier(0);
+          for (int ks = 0; ks < NK; ks++) {
+            if (ks < NK - 1) read((ks + 1) & 1, lds + stage * STAGE, ks + 1);
+            else if (t + 1 < steps) {
+              wait(std::integral_constant<int, STAGES - 2>());
+              issue(stage);
+              read(0, lds + next * STAGE, 0);
+            }
+#pragma unroll
+            for (int i = 0; i < TM; i++)
+#pragma unroll
+              for (int j = 0; j < TN; j++)
+                if (!partial || (i < tm && j < tn)) acc[i][j] = mfma<DT>(fa[ks & 1][i], fb[ks & 1][j], acc[i][j]);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+          stage = next;
         }
-        stage = next;
-      }
+      };
+      // a tile at the operands' ends costs what it holds: 65537 columns are 256 tiles and a small one
+      if (TM * TN > 1 && (tm < TM || tn < TN)) loop(std::true_type());
+      else loop(std::false_type());
       wait_loads<0>();
       barrier();
     } else {

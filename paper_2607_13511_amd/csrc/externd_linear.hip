@@ -14,9 +14,10 @@ struct Part {
   float top, sum, mean, none;      // largest z, sum of e = exp(z - top), sum of e (z - top)
 };
 
-// What a row's gradient is made of, times `up`, a power of two that brings fp16's G below 2^15.
+// What a row's gradient is made of: with l = log2 p, G = p (a l + b) and, at the
+// target, g more.  All times `up`, a power of two that brings fp16's G below 2^15.
 struct RowInfo {
-  float g, ge, lse, h, up;
+  float a, b, g, lse2, up;         // lse2 = lse log2 e; infinite where all p are 0
   int32_t y;                       // -1: no target
   int32_t present, none;
 };
@@ -38,8 +39,8 @@ struct LinearArgs {
   float* up_all;                   // the least `up` of the rows that take part
   void *grad_x, *grad_weight;
   int64_t grad_x_stride, grad_weight_stride, v0, v1;      // this piece of the vocabulary
-  void *G, *packed;                // rows x piece; rows x packed_width: x, zero where a row takes no part
-  int64_t piece, packed_width;
+  void *G, *packed;                // rows x G_width; rows x packed_width: x, zero where a row takes no part
+  int64_t piece, G_width, packed_width;
   float* dx;                       // splits x rows x dx_width
   int64_t dx_width, split;         // k of a split
   int splits;
@@ -60,6 +61,43 @@ __device__ __forceinline__ float propagating_max(float a, float b) { return __bu
 
 constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
 
+// A tile on its way to memory: rows of n with BM entries of m, gathered in LDS so
+// that whole lines are written (a lane holds four entries of each of its rows; at
+// 8 bytes a store lines are written in parts, which with rows at some distances
+// cost a fifth of k_logits).  Vectors of 16 bytes are exchanged within a row so
+// that neither side meets in the banks.
+template <typename P>
+struct Gathered {
+  typedef typename Elem<P::DT>::T T;
+  static constexpr int E = Vec<P::DT>::E, VECTORS = P::BM / E;
+  static_assert(P::BN * P::BM * (int)sizeof(T) <= P::LDS && VECTORS >= 32, "fits");
+  static __device__ __forceinline__ char* at(char* lds, int n, int m) {
+    return lds + (n * VECTORS + ((m / E) ^ (n & 31))) * 16 + m % E * (int)sizeof(T);
+  }
+  // Entries m .. m + 3 of row n.
+  static __device__ __forceinline__ void put(char* lds, int n, int m, const float* o) {
+    if constexpr (P::DT == EXTERND_F32) *(v4u*)at(lds, n, m) = Vec<P::DT>::pack(o);
+    else {
+      v2u b;
+#pragma unroll
+      for (int e = 0; e < 2; e++)
+        b[e] = (unsigned)__builtin_bit_cast(uint16_t, Elem<P::DT>::store(o[2 * e])) |
+               (unsigned)__builtin_bit_cast(uint16_t, Elem<P::DT>::store(o[2 * e + 1])) << 16;
+      *(v2u*)at(lds, n, m) = b;
+    }
+  }
+  // Calls store(n, m, vector) for the vectors of rows below n_count that begin below m_count; all threads.
+  template <typename F>
+  static __device__ __forceinline__ void write(char* lds, int64_t n_count, int64_t m_count, F store) {
+    __syncthreads();
+#pragma unroll 4
+    for (int i = threadIdx.x; i < P::BN * VECTORS; i += GEMM_THREADS) {
+      const int n = i / VECTORS, m = i % VECTORS * E;
+      if (n < n_count && m < m_count) store(n, m, *(const v4u*)at(lds, n, m));
+    }
+  }
+};
+
 // Logits of a tile: rows of weight along m, rows of x along n, so that a lane
 // holds one row's logits and its softmax needs no other lane but at the end.
 // BACK: G of the tile; else its part of each row's softmax.
@@ -74,38 +112,53 @@ __global__ __launch_bounds__(GEMM_THREADS, 2) void k_logits(LinearArgs a) {
   P::run(a.weight, m0, ms, a.x, n0, a.rows - n0, 0, a.width, (lds_char*)lds, acc);
   if constexpr (BACK) {
     typedef typename Elem<DT>::T T;
+    const float c = a.scale * LOG2E;
 #pragma unroll
     for (int j = 0; j < TN; j++) {
       const int64_t n = n0 + P::col(j);
-      if (n >= a.rows) continue;
-      const RowInfo w = a.info[n];
-      T* const to = (T*)a.G + n * a.piece + (m0 - a.v0);
-      const int y = (int)(w.y >= m0 && w.y < m0 + ms ? w.y - m0 : -1);
+      RowInfo w = {};
+      w.y = -1;
+      if (n < a.rows) w = a.info[n];
+      if (ms < P::BM) {      // zeros behind the end: G's last vector is whole
+#pragma unroll
+        for (int i = 0; i < TM; i++)
+#pragma unroll
+          for (int r = 0; r < 16; r++)
+            if (P::row(i, r) >= ms) acc[i][j][r] = -INFINITY;
+      }
+      if (__any(!w.present)) {
+#pragma unroll
+        for (int i = 0; i < TM; i++)
+#pragma unroll
+          for (int r = 0; r < 16; r++)
+            if (!w.present) acc[i][j][r] = -INFINITY;
+      }
+#pragma unroll
+      for (int i = 0; i < TM; i++)
+#pragma unroll
+        for (int r = 0; r < 16; r++) {
+          // p below 2^-200 is 0; the maximum passes a NaN on
+          const float l = propagating_max(fmaf(acc[i][j][r], c, -w.lse2), -200.f);
+          acc[i][j][r] = __builtin_amdgcn_exp2f(l) * fmaf(w.a, l, w.b);
+        }
+      const int64_t y = w.y < 0 ? -1 : w.y - m0;
+      if (__any(y >= P::row(0, 0) && y < P::row(0, 0) + TM * 32)) {      // a target among this wave's
+#pragma unroll
+        for (int i = 0; i < TM; i++)
+#pragma unroll
+          for (int r = 0; r < 16; r++)
+            if (P::row(i, r) == y && y < ms) acc[i][j][r] += w.g;
+      }
 #pragma unroll
       for (int i = 0; i < TM; i++)
 #pragma unroll
         for (int r = 0; r < 16; r += 4) {
-          const int v = P::row(i, r);
-          if (v >= ((ms + 7) & ~(int64_t)7)) continue;      // the last vector of 16 bytes is whole, with zeros
-          float o[4];
-#pragma unroll
-          for (int e = 0; e < 4; e++) {
-            const float lp = fmaf(acc[i][j][r + e], a.scale, -w.lse), p = __builtin_amdgcn_exp2f(lp * LOG2E);
-            o[e] = p == 0.f ? 0.f : -p * (w.ge == 0.f ? w.g : fmaf(w.ge, lp + w.h, w.g));
-            if (v + e == y) o[e] += w.g;
-            if (!w.present || v + e >= ms) o[e] = 0.f;
-          }
-          if constexpr (DT == EXTERND_F32) *(float4*)(to + v) = float4{o[0], o[1], o[2], o[3]};
-          else {
-            v2u b;
-#pragma unroll
-            for (int e = 0; e < 2; e++)
-              b[e] = (unsigned)__builtin_bit_cast(uint16_t, Elem<DT>::store(o[2 * e])) |
-                     (unsigned)__builtin_bit_cast(uint16_t, Elem<DT>::store(o[2 * e + 1])) << 16;
-            *(v2u*)(to + v) = b;
-          }
+          const float o[4] = {acc[i][j][r], acc[i][j][r + 1], acc[i][j][r + 2], acc[i][j][r + 3]};
+          Gathered<P>::put(lds, P::col(j), P::row(i, r), o);
         }
     }
+    T* const to = (T*)a.G + n0 * a.G_width + (m0 - a.v0);
+    Gathered<P>::write(lds, a.rows - n0, ms, [&](int n, int m, v4u x) { *(v4u*)(to + n * a.G_width + m) = x; });
   } else {
     Part* const shared = (Part*)lds;      // WM x BN
     const int wave = threadIdx.x >> 6;
@@ -223,21 +276,22 @@ __global__ __launch_bounds__(1024) void k_rows(LinearArgs a, int fp16) {
     const bool asked = y >= 0 && y < a.vocab;
     RowInfo w = {};
     w.y = asked ? (int32_t)y : -1;
-    w.g = a.g_logprob && asked ? a.g_logprob[r] : 0.f;
-    w.ge = a.g_entropy ? a.g_entropy[r] : 0.f;
-    w.present = w.g != 0.f || w.ge != 0.f;
-    w.lse = a.lse_in[r];
-    w.h = a.g_entropy ? a.entropy_in[r] : 0.f;
+    const float g = a.g_logprob && asked ? a.g_logprob[r] : 0.f, ge = a.g_entropy ? a.g_entropy[r] : 0.f;
+    const float h = ge == 0.f ? 0.f : a.entropy_in[r], lse = a.lse_in[r];
+    w.present = g != 0.f || ge != 0.f;
+    w.lse2 = !w.present || lse == -INFINITY ? INFINITY : lse * LOG2E;
     w.up = 1.f;
     if (fp16 && w.present) {
       // |G| <= |g| + |ge| (p |ln p| + p H) < |g| + |ge| (1 + H)
-      const float most = fabsf(w.g) + (w.ge == 0.f ? 0.f : fabsf(w.ge) * (1.f + fabsf(w.h)));
+      const float most = fabsf(g) + (ge == 0.f ? 0.f : fabsf(ge) * (1.f + fabsf(h)));
       const int k = most <= 3.402823466e38f ? 14 - ilogbf(most) : 0;
       w.up = ldexpf(1.f, k > 120 ? 120 : k < -120 ? -120 : k);
-      w.g *= w.up;
-      w.ge *= w.up;
       up_all = fminf(up_all, w.up);
     }
+    // -p (g + ge (ln p + H))
+    w.g = g * w.up;
+    w.a = -ge * w.up * LN2;
+    w.b = -fmaf(ge, h, g) * w.up;
     a.info[r] = w;
   }
   if (!fp16) {
@@ -288,7 +342,7 @@ __global__ __launch_bounds__(GEMM_THREADS, 2) void k_grad_x(LinearArgs a) {
   const int s = other / cols;
   const int64_t m0 = (int64_t)(other - s * cols) * P::BM, n0 = (int64_t)rt * P::BN, k0 = s * a.split, K = min(a.split, a.v1 - a.v0 - k0);
   f32x16 acc[P::TM][P::TN];
-  const Operand G = {a.G, a.piece};
+  const Operand G = {a.G, a.G_width};
   P::run(a.weight, m0, a.width - m0, G, n0, a.rows - n0, a.v0 + k0, K > 0 ? K : 0, (lds_char*)lds, acc, -a.v0);
 #pragma unroll
   for (int j = 0; j < P::TN; j++) {
@@ -342,39 +396,33 @@ __global__ __launch_bounds__(GEMM_THREADS, 2) void k_grad_weight(LinearArgs a) {
   place_tile((int)((a.width + P::BM - 1) / P::BM), a.vocab_tiles, &ct, &vt);
   const int64_t m0 = (int64_t)ct * P::BM, n0 = (int64_t)vt * P::BN, ns = a.v1 - a.v0;
   f32x16 acc[P::TM][P::TN];
-  const Operand x = {a.packed, a.packed_width}, G = {a.G, a.piece};
+  const Operand x = {a.packed, a.packed_width}, G = {a.G, a.G_width};
   P::run(x, m0, a.packed_width - m0, G, n0, (ns - n0 + 7) & ~(int64_t)7, 0, a.rows, (lds_char*)lds, acc);      // whole vectors: G's rows have room
   const float f = a.scale, down = 1.f / *a.up_all;
 #pragma unroll
-  for (int j = 0; j < P::TN; j++) {
-    const int64_t n = n0 + P::col(j);
-    if (n >= ns) continue;
-    T* const to = (T*)a.grad_weight + (a.v0 + n) * a.grad_weight_stride + m0;
+  for (int j = 0; j < P::TN; j++)
 #pragma unroll
     for (int i = 0; i < P::TM; i++)
 #pragma unroll
       for (int r = 0; r < 16; r += 4) {
-        const int c = P::row(i, r);
         float o[4];
 #pragma unroll
         for (int e = 0; e < 4; e++) o[e] = acc[i][j][r + e] * f * down;
-        if (m0 + c + 4 <= a.width) {
-          if constexpr (P::DT == EXTERND_F32) {
-            store_any(to + c, Vec<EXTERND_F32>::pack(o));
-          } else {
-            typedef v2u any __attribute__((aligned(2)));
-            v2u b;
-#pragma unroll
-            for (int e = 0; e < 2; e++)
-              b[e] = (unsigned)__builtin_bit_cast(uint16_t, Elem<P::DT>::store(o[2 * e])) |
-                     (unsigned)__builtin_bit_cast(uint16_t, Elem<P::DT>::store(o[2 * e + 1])) << 16;
-            *(any*)(to + c) = b;
-          }
-        } else
-          for (int e = 0; e < 4; e++)
-            if (m0 + c + e < a.width) to[c + e] = Elem<P::DT>::store(o[e]);
+        Gathered<P>::put(lds, P::col(j), P::row(i, r), o);
       }
-  }
+  T* const to = (T*)a.grad_weight + (a.v0 + n0) * a.grad_weight_stride + m0;
+  const int64_t width = a.width - m0;
+  Gathered<P>::write(lds, ns - n0, width, [&](int n, int m, v4u x) {
+    T* const at = to + n * a.grad_weight_stride + m;
+    if (m + Vec<P::DT>::E <= width) store_any(at, x);
+    else {
+      float y[Vec<P::DT>::E];
+      Vec<P::DT>::unpack(x, y);
+#pragma unroll
+      for (int e = 0; e < Vec<P::DT>::E; e++)
+        if (m + e < width) at[e] = Elem<P::DT>::store(y[e]);      // exact: of its type
+    }
+  });
 }
 
 // grad_weight without rows.
@@ -412,7 +460,7 @@ static int64_t forward_step(int64_t row_tiles, int64_t vocab) {
 
 struct LinearWork {
   size_t parts, at_target, info, up_all, packed, G, dx, bytes;
-  int64_t tiles, step, piece, packed_width, dx_width, split;
+  int64_t tiles, step, piece, G_width, packed_width, dx_width, split;
   int splits;
 };
 
@@ -427,24 +475,47 @@ static LinearWork forward_work(int32_t dtype, int64_t rows, int64_t vocab) {
   return w;
 }
 
+// Vocabulary of a piece, of which the last takes up to 255 more: G of a piece
+// stays below PIECE_ENTRIES where rows allow it, and among such pieces the one is
+// taken whose tiles leave the fewest rounds of the CUs partly empty (a round of
+// logits costs width, one of grad_weight rows).  2048 rows, 65537 x 2560: two of 32768,
+// 4 and 5 whole rounds, where three equal ones are 3 and 4 each: TODO
+static int64_t choose_piece(int64_t rows, int64_t vocab, int64_t width, int64_t row_tiles, int64_t weight_tiles) {
+  const int64_t tiles = vocab / 256, most = PIECE_ENTRIES / rows / 256, least = ceil_div(tiles, most < 8 ? 8 : most);
+  if (tiles <= 1) return 256;
+  int64_t best = 0, best_cost = 0;
+  for (int64_t pieces = least; pieces <= least + 4 && pieces <= tiles; pieces++) {
+    const int64_t each = ceil_div(tiles, pieces), last = tiles - (ceil_div(tiles, each) - 1) * each;
+    // a small tile (of the last 255) takes most of a round's time too, as it waits as often
+    auto cost = [&](int64_t n) { return ceil_div(n * row_tiles, CUS) * width + ceil_div(n * weight_tiles, CUS) * rows; };
+    const int64_t all = (ceil_div(tiles, each) - 1) * cost(each) + cost(last + (vocab % 256 ? 1 : 0));
+    if (!best || all < best_cost) {
+      best = each;
+      best_cost = all;
+    }
+  }
+  return best * 256;
+}
+
 static LinearWork backward_work(int32_t dtype, int64_t rows, int64_t vocab, int64_t width, bool need_x, bool need_weight) {
   LinearWork w = {};
-  const int64_t most = PIECE_ENTRIES / rows, pieces = ceil_div(vocab, most < 2048 ? 2048 : most);
-  w.piece = ceil_div(ceil_div(vocab, pieces), 256) * 256;
+  const int64_t row_tiles = ceil_div(rows, tile_rows(dtype, rows)), cols = ceil_div(width, 256);
+  w.piece = choose_piece(rows, vocab, width, row_tiles, need_weight ? cols * (dtype == EXTERND_F32 ? 2 : 1) : 0);
+  // rows an odd number of 512 bytes apart: at a power of two they share the caches' sets (4095 rows 16384 entries apart: 738 us for 607)
+  w.G_width = (ceil_div(vocab < w.piece + 256 ? vocab : w.piece + 256, 256) | 1) * 256;
   const int vec = 16 / dtype_bytes(dtype);
   w.packed_width = ceil_div(width, vec) * vec;
   w.dx_width = ceil_div(width, 4) * 4;
-  const int64_t tiles = ceil_div(width, 256) * ceil_div(rows, tile_rows(dtype, rows));
-  int64_t splits = CUS / tiles;
-  const int64_t max_splits = ceil_div(w.piece, 512);
+  int64_t splits = CUS / (cols * row_tiles);
+  const int64_t max_splits = ceil_div(w.G_width, 512);
   splits = splits < 1 ? 1 : splits > max_splits ? max_splits : splits;
-  w.split = ceil_div(ceil_div(w.piece, splits), 64) * 64;
-  w.splits = (int)ceil_div(w.piece, w.split);
+  w.split = ceil_div(ceil_div(w.G_width, splits), 64) * 64;
+  w.splits = (int)ceil_div(w.G_width, w.split);
   size_t at = 0;
   w.info = at, at += round256((size_t)rows * sizeof(RowInfo));
   w.up_all = at, at += 256;
   w.packed = at, at += need_weight ? round256((size_t)(rows * w.packed_width) * dtype_bytes(dtype)) : 0;
-  w.G = at, at += round256((size_t)(rows * w.piece) * dtype_bytes(dtype));
+  w.G = at, at += round256((size_t)(rows * w.G_width) * dtype_bytes(dtype));
   w.dx = at, at += need_x ? round256((size_t)(w.splits * rows * w.dx_width) * 4) : 0;
   w.bytes = at;
   return w;
@@ -512,7 +583,7 @@ static void launch_backward(LinearArgs a, bool direct, hipStream_t s) {
   k_rows<<<DT == EXTERND_F16 ? 1 : (unsigned)ceil_div(a.rows, 1024), 1024, 0, s>>>(a, DT == EXTERND_F16);
   if (a.grad_weight) k_pack<DT><<<(unsigned)ceil_div(a.rows * (a.packed_width / Vec<DT>::E), 256), 256, 0, s>>>(a);
   for (a.v0 = 0; a.v0 < a.vocab; a.v0 = a.v1) {
-    a.v1 = a.v0 + a.piece < a.vocab ? a.v0 + a.piece : a.vocab;
+    a.v1 = a.v0 + a.piece + 256 > a.vocab ? a.vocab : a.v0 + a.piece;
     if (DT != EXTERND_F32 && direct) choose_logits<DT, DT != EXTERND_F32, true>(a, s);
     else choose_logits<DT, false, true>(a, s);
     if (a.grad_x) {
@@ -618,6 +689,7 @@ int externd_linear_logprobs_backward(const void* x, int64_t x_stride, const void
   a.G = at + w.G;
   a.dx = (float*)(at + w.dx);
   a.piece = w.piece;
+  a.G_width = w.G_width;
   a.packed_width = w.packed_width;
   a.dx_width = w.dx_width;
   a.split = w.split;
