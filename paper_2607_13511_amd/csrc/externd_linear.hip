@@ -27,18 +27,20 @@ struct LinearArgs {
   int64_t rows, vocab, width;
   const int64_t* targets;
   float scale;
-  int row_tiles, vocab_tiles;
+  int row_tiles, vocab_tiles;      // of this launch
   int64_t step;                    // vocabulary of a tile
+  int64_t v0, v1;                  // vocabulary of this launch
   // forward
   float *logprob, *entropy, *lse;
-  Part* parts;                     // rows x vocab_tiles
+  Part* parts;                     // rows x all_parts
+  int first_part, all_parts;
   float* at_target;                // z of the target
   // backward
   const float *lse_in, *entropy_in, *g_logprob, *g_entropy;
   RowInfo* info;
   float* up_all;                   // the least `up` of the rows that take part
   void *grad_x, *grad_weight;
-  int64_t grad_x_stride, grad_weight_stride, v0, v1;      // this piece of the vocabulary
+  int64_t grad_x_stride, grad_weight_stride, p0, p1;      // this piece of the vocabulary, G's columns
   void *G, *packed;                // rows x G_width; rows x packed_width: x, zero where a row takes no part
   int64_t piece, G_width, packed_width;
   float* dx;                       // splits x rows x dx_width
@@ -157,7 +159,7 @@ __global__ __launch_bounds__(GEMM_THREADS, 2) void k_logits(LinearArgs a) {
           Gathered<P>::put(lds, P::col(j), P::row(i, r), o);
         }
     }
-    T* const to = (T*)a.G + n0 * a.G_width + (m0 - a.v0);
+    T* const to = (T*)a.G + n0 * a.G_width + (m0 - a.p0);
     Gathered<P>::write(lds, a.rows - n0, ms, [&](int n, int m, v4u x) { *(v4u*)(to + n * a.G_width + m) = x; });
   } else {
     Part* const shared = (Part*)lds;      // WM x BN
@@ -216,7 +218,7 @@ __global__ __launch_bounds__(GEMM_THREADS, 2) void k_logits(LinearArgs a) {
         sum += p.sum * f;
         mean += f == 0.f ? 0.f : fmaf(p.sum, d, p.mean) * f;
       }
-      a.parts[(n0 + n) * a.vocab_tiles + vt] = Part{top, sum, mean, 0.f};
+      a.parts[(n0 + n) * a.all_parts + a.first_part + vt] = Part{top, sum, mean, 0.f};
     }
   }
 }
@@ -225,9 +227,9 @@ __global__ __launch_bounds__(GEMM_THREADS, 2) void k_logits(LinearArgs a) {
 __global__ __launch_bounds__(256) void k_logits_join(LinearArgs a) {
   __shared__ float lds[3][4];
   const int64_t r = blockIdx.x;
-  const Part* p = a.parts + r * a.vocab_tiles;
+  const Part* p = a.parts + r * a.all_parts;
   float top = -3.402823466e38f, sum = 0.f, mean = 0.f;      // of this thread's parts, against the largest so far
-  for (int i = threadIdx.x; i < a.vocab_tiles; i += 256) {
+  for (int i = threadIdx.x; i < a.all_parts; i += 256) {
     const Part q = p[i];
     if (q.sum == 0.f) continue;
     const float to = fmaxf(top, q.top), f = __builtin_amdgcn_exp2f((top - to) * LOG2E), d = fmaxf(q.top, -3.402823466e38f) - to,
@@ -340,10 +342,10 @@ __global__ __launch_bounds__(GEMM_THREADS, 2) void k_grad_x(LinearArgs a) {
   int rt, other;
   place_tile(a.row_tiles, cols * a.splits, &rt, &other);
   const int s = other / cols;
-  const int64_t m0 = (int64_t)(other - s * cols) * P::BM, n0 = (int64_t)rt * P::BN, k0 = s * a.split, K = min(a.split, a.v1 - a.v0 - k0);
+  const int64_t m0 = (int64_t)(other - s * cols) * P::BM, n0 = (int64_t)rt * P::BN, k0 = s * a.split, K = min(a.split, a.p1 - a.p0 - k0);
   f32x16 acc[P::TM][P::TN];
   const Operand G = {a.G, a.G_width};
-  P::run(a.weight, m0, a.width - m0, G, n0, a.rows - n0, a.v0 + k0, K > 0 ? K : 0, (lds_char*)lds, acc, -a.v0);
+  P::run(a.weight, m0, a.width - m0, G, n0, a.rows - n0, a.p0 + k0, K > 0 ? K : 0, (lds_char*)lds, acc, -a.p0);
 #pragma unroll
   for (int j = 0; j < P::TN; j++) {
     const int64_t n = n0 + P::col(j);
@@ -356,7 +358,7 @@ __global__ __launch_bounds__(GEMM_THREADS, 2) void k_grad_x(LinearArgs a) {
         const int c = P::row(i, r);
         if (m0 + c >= a.dx_width) continue;
         float4 x = {acc[i][j][r], acc[i][j][r + 1], acc[i][j][r + 2], acc[i][j][r + 3]};
-        if (a.v0) {
+        if (a.p0) {
           const float4 b = *(const float4*)(to + c);
           x = float4{x.x + b.x, x.y + b.y, x.z + b.z, x.w + b.w};
         }
@@ -396,7 +398,7 @@ __global__ __launch_bounds__(GEMM_THREADS, 2) void k_grad_weight(LinearArgs a) {
   place_tile((int)((a.width + P::BM - 1) / P::BM), a.vocab_tiles, &ct, &vt);
   const int64_t m0 = (int64_t)ct * P::BM, n0 = (int64_t)vt * P::BN, ns = a.v1 - a.v0;
   f32x16 acc[P::TM][P::TN];
-  const Operand x = {a.packed, a.packed_width}, G = {a.G, a.G_width};
+  const Operand x = {a.packed, a.packed_width}, G = {(T*)a.G + (a.v0 - a.p0), a.G_width};
   P::run(x, m0, a.packed_width - m0, G, n0, (ns - n0 + 7) & ~(int64_t)7, 0, a.rows, (lds_char*)lds, acc);      // whole vectors: G's rows have room
   const float f = a.scale, down = 1.f / *a.up_all;
 #pragma unroll
@@ -486,9 +488,8 @@ static int64_t choose_piece(int64_t rows, int64_t vocab, int64_t width, int64_t 
   int64_t best = 0, best_cost = 0;
   for (int64_t pieces = least; pieces <= least + 4 && pieces <= tiles; pieces++) {
     const int64_t each = ceil_div(tiles, pieces), last = tiles - (ceil_div(tiles, each) - 1) * each;
-    // a small tile (of the last 255) takes most of a round's time too, as it waits as often
     auto cost = [&](int64_t n) { return ceil_div(n * row_tiles, CUS) * width + ceil_div(n * weight_tiles, CUS) * rows; };
-    const int64_t all = (ceil_div(tiles, each) - 1) * cost(each) + cost(last + (vocab % 256 ? 1 : 0));
+    const int64_t all = (ceil_div(tiles, each) - 1) * cost(each) + cost(last);
     if (!best || all < best_cost) {
       best = each;
       best_cost = all;
@@ -530,6 +531,22 @@ static void launch_logits(LinearArgs a, hipStream_t s) {
   a.vocab_tiles = (int)ceil_div(a.v1 - a.v0, a.step);
   k_logits<P, BACK><<<(unsigned)(a.row_tiles * a.vocab_tiles), GEMM_THREADS, 0, s>>>(a);
 }
+
+// Calls `large` for a launch's vocabulary, or for its tiles of 256 and then
+// `small` for the last few columns, where those alone would begin one more round of
+// the CUs: a small tile waits for memory as often as a large one, and takes 70 us of a
+// round's 85 (2048 rows, 65537 columns); in tiles of 32 rows it takes TODO.
+template <typename L, typename S>
+static void with_tail(LinearArgs a, int64_t other_tiles, L large, S small) {
+  const int64_t tiles = (a.v1 - a.v0) / 256, rest = (a.v1 - a.v0) % 256;
+  if (a.step != 256 || !tiles || !rest || ceil_div((tiles + 1) * other_tiles, CUS) == ceil_div(tiles * other_tiles, CUS)) return large(a);
+  LinearArgs b = a;
+  a.v1 = b.v0 = a.v0 + tiles * 256;
+  b.first_part += (int)tiles;
+  large(a);
+  small(b);
+}
+
 template <typename P>
 static void launch_grad_x(LinearArgs a, hipStream_t s) {
   a.row_tiles = (int)ceil_div(a.rows, P::BN);
@@ -548,9 +565,12 @@ static void choose_logits(const LinearArgs& a, hipStream_t s) {
     if (n == 32) launch_logits<Product<DT, false, false, false, 256, 32, 8, 2>, BACK>(a, s);
     else launch_logits<Product<DT, false, false, false, 256, 128, 4, 2>, BACK>(a, s);
   } else {
-    if (n == 32) launch_logits<Product<DT, DIRECT, false, false, 256, 32, 8, DIRECT ? 4 : 2>, BACK>(a, s);
+    typedef Product<DT, DIRECT, false, false, 256, 32, 8, DIRECT ? 4 : 2> Small;
+    if (n == 32) launch_logits<Small, BACK>(a, s);
     else if (n == 128) launch_logits<Product<DT, DIRECT, false, false, 256, 128, 4, DIRECT ? 3 : 2>, BACK>(a, s);
-    else launch_logits<Product<DT, DIRECT, false, false, 256, 256, 2, 2>, BACK>(a, s);
+    else
+      with_tail(a, ceil_div(a.rows, 256), [&](const LinearArgs& b) { launch_logits<Product<DT, DIRECT, false, false, 256, 256, 2, 2>, BACK>(b, s); },
+                [&](const LinearArgs& b) { launch_logits<Small, BACK>(b, s); });
   }
 }
 template <int DT, bool DIRECT>
@@ -570,7 +590,6 @@ template <int DT>
 static void launch_forward(LinearArgs a, bool direct, hipStream_t s) {
   if (DT != EXTERND_F32 && direct) choose_logits<DT, DT != EXTERND_F32, false>(a, s);
   else choose_logits<DT, false, false>(a, s);
-  a.vocab_tiles = (int)ceil_div(a.vocab, a.step);
   k_logits_join<<<(unsigned)a.rows, 256, 0, s>>>(a);
 }
 
@@ -582,8 +601,10 @@ static void launch_backward(LinearArgs a, bool direct, hipStream_t s) {
   }
   k_rows<<<DT == EXTERND_F16 ? 1 : (unsigned)ceil_div(a.rows, 1024), 1024, 0, s>>>(a, DT == EXTERND_F16);
   if (a.grad_weight) k_pack<DT><<<(unsigned)ceil_div(a.rows * (a.packed_width / Vec<DT>::E), 256), 256, 0, s>>>(a);
-  for (a.v0 = 0; a.v0 < a.vocab; a.v0 = a.v1) {
-    a.v1 = a.v0 + a.piece + 256 > a.vocab ? a.vocab : a.v0 + a.piece;
+  for (a.p0 = 0; a.p0 < a.vocab; a.p0 = a.p1) {
+    a.p1 = a.p0 + a.piece + 256 > a.vocab ? a.vocab : a.p0 + a.piece;
+    a.v0 = a.p0;
+    a.v1 = a.p1;
     if (DT != EXTERND_F32 && direct) choose_logits<DT, DT != EXTERND_F32, true>(a, s);
     else choose_logits<DT, false, true>(a, s);
     if (a.grad_x) {
@@ -592,7 +613,9 @@ static void launch_backward(LinearArgs a, bool direct, hipStream_t s) {
     }
     if (a.grad_weight) {
       if constexpr (DT == EXTERND_F32) launch_grad_weight<Product<DT, false, true, true, 256, 128, 4, 2>>(a, s);
-      else launch_grad_weight<Product<DT, true, true, true, 256, 256, 2, 2>>(a, s);
+      else
+        with_tail(a, ceil_div(a.width, 256), [&](const LinearArgs& b) { launch_grad_weight<Product<DT, true, true, true, 256, 256, 2, 2>>(b, s); },
+                  [&](const LinearArgs& b) { launch_grad_weight<Product<DT, true, true, true, 256, 32, 8, 4>>(b, s); });
     }
   }
   if (a.grad_x) k_grad_x_join<DT><<<(unsigned)ceil_div(a.rows * (a.dx_width / 4), 256), 256, 0, s>>>(a);
@@ -628,6 +651,7 @@ int externd_linear_logprobs(const void* x, int64_t x_stride, const void* weight,
     a.weight = {weight, weight_stride};
     a.rows = rows - r < FORWARD_ROWS ? rows - r : FORWARD_ROWS;
     a.vocab = a.v1 = vocab;
+    a.all_parts = (int)w.tiles;
     a.width = width;
     a.targets = logprob ? targets + r : nullptr;
     a.scale = scale;
