@@ -44,14 +44,14 @@ __device__ __forceinline__ f32x16 mfma(v4u a, v4u b, f32x16 c) {
   else return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
-// The LDS tile of one operand: X of m (or n) by BK of k.
-template <bool COL, int X, int BK>
+// The LDS tile of one operand: X of m (or n) by BK of k, EV entries in 16 bytes.
+template <bool COL, int X, int BK, int EV = 8>
 struct Tile {
-  static constexpr int VECTORS = X * BK / 8;                  // of 16 bytes, in each plane
+  static constexpr int VECTORS = X * BK / EV;                 // of 16 bytes, in each plane
   static constexpr int BYTES = VECTORS * 16;
   static constexpr int LOADS = VECTORS / GEMM_THREADS;        // of a thread
   static_assert(VECTORS % GEMM_THREADS == 0 || VECTORS < GEMM_THREADS, "whole loads");
-  static constexpr int CH = COL ? X / 8 : BK / 8;             // vectors of a row in memory
+  static constexpr int CH = COL ? X / EV : BK / EV;            // vectors of a row in memory
   // Where in the operand the vector at place `i` of the tile is: its row in memory and its vector there.
   static __device__ __forceinline__ void place(int i, int* row, int* vec) {
     *row = i / CH;
@@ -77,15 +77,53 @@ struct Tile {
       return *(const __attribute__((address_space(3))) v4u*)(t + (row * CH + v) * 16);
     }
   }
+  // The same of a tile of fp32 entries by rows: the fragment's eight in two vectors.
+  static __device__ __forceinline__ void fragment_f32(const lds_char* t, int x0, int ks, v4u* x) {
+    const int lane = threadIdx.x & 63, row = x0 + (lane & 31), swap = (row / (16 / CH)) & (CH - 1);
+#pragma unroll
+    for (int i = 0; i < 2; i++)
+      x[i] = *(const __attribute__((address_space(3))) v4u*)(t + (row * CH + ((ks * 4 + (lane >> 5) * 2 + i) ^ swap)) * 16);
+  }
 };
 
-// Loads of 16-bit operands whose rows begin at multiples of 16 bytes and are whole
+// Eight fp32 entries as three vectors of bf16: x = x1 + x2 + x3 exactly, 8 bits each,
+// cut and not rounded.  An infinity or a NaN becomes NaN in one of them.
+__device__ __forceinline__ void cut(const v4u* x, v4u* part) {
+#pragma unroll
+  for (int w = 0; w < 4; w++) {
+    unsigned p[3][2];
+#pragma unroll
+    for (int h = 0; h < 2; h++) {
+      const unsigned v = x[w >> 1][(w & 1) * 2 + h], y = v & 0xFFFF0000u;
+      const float r = __uint_as_float(v) - __uint_as_float(y);
+      const unsigned z = __float_as_uint(r) & 0xFFFF0000u;
+      p[0][h] = y;
+      p[1][h] = z;
+      p[2][h] = __float_as_uint(r - __uint_as_float(z));
+    }
+#pragma unroll
+    for (int i = 0; i < 3; i++) part[i][w] = __builtin_amdgcn_perm(p[i][1], p[i][0], 0x07060302u);      // the upper halves
+  }
+}
+
+// The six products of two operands' parts that are not below 2^-24, small ones first.
+__device__ __forceinline__ f32x16 mfma_cut(const v4u* a, const v4u* b, f32x16 c) {
+  c = mfma<EXTERND_BF16>(a[1], b[1], c);
+  c = mfma<EXTERND_BF16>(a[0], b[2], c);
+  c = mfma<EXTERND_BF16>(a[2], b[0], c);
+  c = mfma<EXTERND_BF16>(a[0], b[1], c);
+  c = mfma<EXTERND_BF16>(a[1], b[0], c);
+  return mfma<EXTERND_BF16>(a[0], b[0], c);
+}
+
+// Loads of operands whose rows begin at multiples of 16 bytes and are whole
 // vectors, straight into LDS.  (Part of a vector would come as zeros where the operand
 // ends.  K is rounded up to whole vectors by rows: zeros in memory.)  The buffer's base moves on with the
 // steps, and what lies past its end, or is no vector of the tile, becomes zeros.
-template <bool COL, int X, int BK>
+template <bool COL, int X, int BK, int EV = 8>
 struct Direct {
-  typedef Tile<COL, X, BK> T;
+  typedef Tile<COL, X, BK, EV> T;
+  static constexpr int B = 16 / EV;                           // bytes of an entry
   static constexpr int LOADS = T::LOADS ? T::LOADS : 1;      // of a wave, whether or not all of it has one
   static constexpr unsigned NONE = 0xFFFFFFFFu;
   const char* base;
@@ -95,13 +133,13 @@ struct Direct {
 
   // count of m (or n) from x0 on, K of k from k0 on.
   __device__ __forceinline__ void init(const Operand& o, int64_t x0, int64_t count, int64_t k0, int64_t K) {
-    const int64_t row = o.stride * 2, cols = min(count, (int64_t)X);
-    if (!COL) K = (K + 7) & ~(int64_t)7;
-    const int64_t rows = COL ? K : cols, width = (COL ? cols : K) * 2;
-    base = (const char*)o.p + (COL ? k0 * row + x0 * 2 : x0 * row + k0 * 2);
+    const int64_t row = o.stride * B, cols = min(count, (int64_t)X);
+    if (!COL) K = (K + EV - 1) & ~(int64_t)(EV - 1);
+    const int64_t rows = COL ? K : cols, width = (COL ? cols : K) * B;
+    base = (const char*)o.p + (COL ? k0 * row + x0 * B : x0 * row + k0 * B);
     left = rows > 0 ? (rows - 1) * row + width : 0;
     k_left = K;
-    step = (int)(COL ? BK * row : BK * 2);
+    step = (int)(COL ? BK * row : BK * B);
 #pragma unroll
     for (int i = 0; i < LOADS; i++) {
       int r, v;
@@ -124,7 +162,7 @@ struct Direct {
       for (int i = 0; i < LOADS; i++) {
         int r, v;
         T::place(i * GEMM_THREADS + (int)threadIdx.x, &r, &v);
-        load(to + i * (GEMM_THREADS * 16), v * 8 < k_left ? offset[i] : NONE, resource);
+        load(to + i * (GEMM_THREADS * 16), v * EV < k_left ? offset[i] : NONE, resource);
       }
     }
     base += step;
@@ -203,26 +241,10 @@ struct Staged {
       lds_char* const to = lds + (i * GEMM_THREADS + (int)threadIdx.x) * 16;
       if constexpr (DT != EXTERND_F32) *(vec)to = held[i][0];
       else {
-        unsigned part[3][8];
+        v4u part[3];
+        cut(held[i], part);
 #pragma unroll
-        for (int e = 0; e < 8; e++) {
-          const unsigned x = held[i][e / 4][e % 4];
-          const bool whole = (x & 0x7F800000u) == 0x7F800000u;      // infinite or NaN: one part holds it
-          unsigned y = x & 0xFFFF0000u;
-          if (whole && (x & 0x007FFFFFu)) y |= 0x00400000u;         // a NaN stays one
-          const float r = whole ? 0.f : __uint_as_float(x) - __uint_as_float(y);
-          const unsigned z = __float_as_uint(r) & 0xFFFF0000u;
-          part[0][e] = y;
-          part[1][e] = z;
-          part[2][e] = __float_as_uint(r - __uint_as_float(z));
-        }
-#pragma unroll
-        for (int p = 0; p < 3; p++) {
-          v4u o;
-#pragma unroll
-          for (int w = 0; w < 4; w++) o[w] = part[p][2 * w] >> 16 | (part[p][2 * w + 1] & 0xFFFF0000u);
-          *(vec)(to + p * plane) = o;
-        }
+        for (int p = 0; p < 3; p++) *(vec)(to + p * plane) = part[p];
       }
     }
   }
@@ -233,12 +255,15 @@ template <int DT_, bool DIRECT_, bool ACOL_, bool BCOL_, int BM_, int BN_, int W
 struct Product {
   static constexpr int DT = DT_, BM = BM_, BN = BN_, WM = WM_, WN = 8 / WM_, STAGES = STAGES_;
   static constexpr bool DIRECT = DIRECT_, ACOL = ACOL_, BCOL = BCOL_;
-  static constexpr int BK = Kind<DT>::BK, PLANES = Kind<DT>::PLANES;
+  // fp32 by rows: A's entries in LDS, cut as they are read; B comes as its three
+  // parts, cut ahead, each BN rows of bf16 behind the other.
+  static constexpr bool RAW = DIRECT && DT == EXTERND_F32;
+  static constexpr int BK = Kind<DT>::BK, PLANES = RAW ? 1 : Kind<DT>::PLANES, EV = RAW ? 4 : 8, BROWS = RAW ? 3 * BN : BN;
   static constexpr int TM = BM / WM / 32, TN = BN / WN / 32;
-  typedef Tile<ACOL, BM, BK> TA;
-  typedef Tile<BCOL, BN, BK> TB;
+  typedef Tile<ACOL, BM, BK, EV> TA;
+  typedef Tile<BCOL, BROWS, BK, 8> TB;
   static constexpr int STAGE = (TA::BYTES + TB::BYTES) * PLANES, LDS = STAGE * STAGES;
-  static_assert(LDS <= 160 * 1024 && TM >= 1 && TN >= 1 && !(DIRECT && DT == EXTERND_F32), "fits");
+  static_assert(LDS <= 160 * 1024 && TM >= 1 && TN >= 1 && !(RAW && (ACOL || BCOL || TM > 1 || TN > 1)), "fits");
 
   // Entry `r` (0 .. 15) of acc[i][j] is C(m0 + row(i, r), n0 + col(j)).
   static __device__ __forceinline__ int row(int i, int r) {
@@ -264,14 +289,10 @@ struct Product {
       for (int i = 0; i < TM; i++)
 #pragma unroll
         for (int j = 0; j < TN; j++) {
-          if constexpr (PLANES == 3) {      // small products first
-            acc[i][j] = mfma<DT>(fa[1][i], fb[1][j], acc[i][j]);
-            acc[i][j] = mfma<DT>(fa[0][i], fb[2][j], acc[i][j]);
-            acc[i][j] = mfma<DT>(fa[2][i], fb[0][j], acc[i][j]);
-            acc[i][j] = mfma<DT>(fa[0][i], fb[1][j], acc[i][j]);
-            acc[i][j] = mfma<DT>(fa[1][i], fb[0][j], acc[i][j]);
-          }
-          acc[i][j] = mfma<DT>(fa[0][i], fb[0][j], acc[i][j]);
+          if constexpr (PLANES == 3) {
+            const v4u x[3] = {fa[0][i], fa[1][i], fa[2][i]}, y[3] = {fb[0][j], fb[1][j], fb[2][j]};
+            acc[i][j] = mfma_cut(x, y, acc[i][j]);
+          } else acc[i][j] = mfma<DT>(fa[0][i], fb[0][j], acc[i][j]);
         }
     }
   }
@@ -287,12 +308,12 @@ struct Product {
         for (int r = 0; r < 16; r++) acc[i][j][r] = 0.f;
     const int64_t steps = (K + BK - 1) / BK;
     if constexpr (DIRECT) {
-      Direct<ACOL, BM, BK> la;
-      Direct<BCOL, BN, BK> lb;
+      Direct<ACOL, BM, BK, EV> la;
+      Direct<BCOL, BROWS, BK, 8> lb;
       la.init(A, m0, m_count, k0, K);
       lb.init(B, n0, n_count, k0 + b_k, K);
       static_assert(TA::LOADS > 0, "every wave loads of A");
-      constexpr int EACH = Direct<ACOL, BM, BK>::LOADS + Direct<BCOL, BN, BK>::LOADS;
+      constexpr int EACH = Direct<ACOL, BM, BK, EV>::LOADS + Direct<BCOL, BROWS, BK, 8>::LOADS;
       const bool fewer = TB::LOADS == 0 && (int)(threadIdx.x & ~63u) >= TB::VECTORS;      // this wave loads of A only
       auto issue = [&](int stage) {
         la.issue(lds + stage * STAGE);
@@ -315,14 +336,27 @@ struct Product {
       for (int s = 0; s < STAGES; s++) issue(s);      // past the last step: zeros, which nothing reads
       wait(std::integral_constant<int, STAGES - 1>());
       auto loop = [&](auto partial) {
-        v4u fa[2][TM], fb[2][TN];
+        v4u fa[2][TM][RAW ? 2 : 1], fb[2][TN][RAW ? 3 : 1];
         auto read = [&](int set, const lds_char* s, int ks) {
 #pragma unroll
           for (int j = 0; j < TN; j++)
-            if (!partial || j < tn) fb[set][j] = TB::fragment(s + TA::BYTES, nb + j * 32, ks);
+            if (!partial || j < tn) {
+#pragma unroll
+              for (int p = 0; p < (RAW ? 3 : 1); p++) fb[set][j][p] = TB::fragment(s + TA::BYTES, p * BN + nb + j * 32, ks);
+            }
 #pragma unroll
           for (int i = 0; i < TM; i++)
-            if (!partial || i < tm) fa[set][i] = TA::fragment(s, ma + i * 32, ks);
+            if (!partial || i < tm) {
+              if constexpr (RAW) TA::fragment_f32(s, ma + i * 32, ks, fa[set][i]);
+              else fa[set][i][0] = TA::fragment(s, ma + i * 32, ks);
+            }
+        };
+        auto multiply = [&](int set, int i, int j) {
+          if constexpr (RAW) {
+            v4u x[3];
+            cut(fa[set][i], x);
+            acc[i][j] = mfma_cut(x, fb[set][j], acc[i][j]);
+          } else acc[i][j] = mfma<DT>(fa[set][i][0], fb[set][j][0], acc[i][j]);
         };
         read(0, lds, 0);
         int stage = 0;
@@ -340,14 +374,14 @@ struct Product {
             for (int i = 0; i < TM; i++)
 #pragma unroll
               for (int j = 0; j < TN; j++)
-                if (!partial || (i < tm && j < tn)) acc[i][j] = mfma<DT>(fa[ks & 1][i], fb[ks & 1][j], acc[i][j]);
+                if (!partial || (i < tm && j < tn)) multiply(ks & 1, i, j);
             __builtin_amdgcn_sched_barrier(0);
           }
           stage = next;
         }
       };
       // a tile at the operands' ends costs what it holds: 65537 columns are 256 tiles and a small one
-      if (TM * TN > 1 && (tm < TM || tn < TN)) loop(std::true_type());
+      if (tm < TM || tn < TN) loop(std::true_type());
       else loop(std::false_type());
       wait_loads<0>();
       barrier();

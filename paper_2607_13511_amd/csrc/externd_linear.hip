@@ -34,6 +34,9 @@ struct LinearArgs {
   float *logprob, *entropy, *lse;
   Part* parts;                     // rows x all_parts
   int first_part, all_parts;
+  // of 32 rows of fp32 or fewer: x cut into its parts, 3 x 32 x cut_width
+  void* cut;
+  int64_t cut_width;
   float* at_target;                // z of the target
   // backward
   const float *lse_in, *entropy_in, *g_logprob, *g_entropy;
@@ -111,7 +114,8 @@ __global__ __launch_bounds__(GEMM_THREADS, 2) void k_logits(LinearArgs a) {
   place_tile(a.row_tiles, a.vocab_tiles, &rt, &vt);
   const int64_t m0 = a.v0 + vt * a.step, n0 = (int64_t)rt * P::BN, ms = min(a.step, a.v1 - m0);
   f32x16 acc[TM][TN];
-  P::run(a.weight, m0, ms, a.x, n0, a.rows - n0, 0, a.width, (lds_char*)lds, acc);
+  if constexpr (P::RAW) P::run(a.weight, m0, ms, Operand{a.cut, a.cut_width}, 0, P::BROWS, 0, a.width, (lds_char*)lds, acc);
+  else P::run(a.weight, m0, ms, a.x, n0, a.rows - n0, 0, a.width, (lds_char*)lds, acc);
   if constexpr (BACK) {
     typedef typename Elem<DT>::T T;
     const float c = a.scale * LOG2E;
@@ -333,6 +337,20 @@ __global__ __launch_bounds__(256) void k_pack(LinearArgs a) {
   *(v4u*)((T*)a.packed + r * a.packed_width + c) = Vec<DT>::pack(x);
 }
 
+// At most 32 rows of x cut into their parts, with zeros behind rows and columns.
+__global__ __launch_bounds__(256) void k_cut(LinearArgs a) {
+  const int64_t units = a.cut_width / 8, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= 32 * units) return;
+  const int64_t r = i / units, c = (i - r * units) * 8;
+  const float* x = (const float*)a.x.p + r * a.x.stride + c;
+  v4u held[2], part[3];
+#pragma unroll
+  for (int e = 0; e < 8; e++) held[e / 4][e % 4] = r < a.rows && c + e < a.width ? __float_as_uint(x[e]) : 0u;
+  cut(held, part);
+#pragma unroll
+  for (int p = 0; p < 3; p++) *(v4u*)((uint16_t*)a.cut + (p * 32 + r) * a.cut_width + c) = part[p];
+}
+
 // G weight of this piece (columns of weight along m, rows of G along n), added to
 // the split's sums so far.
 template <typename P>
@@ -461,18 +479,24 @@ static int64_t forward_step(int64_t row_tiles, int64_t vocab) {
 }
 
 struct LinearWork {
-  size_t parts, at_target, info, up_all, packed, G, dx, bytes;
-  int64_t tiles, step, piece, G_width, packed_width, dx_width, split;
+  size_t cut, parts, at_target, info, up_all, packed, G, dx, bytes;
+  int64_t tiles, step, piece, G_width, packed_width, dx_width, cut_width, split;
   int splits;
 };
 
-static LinearWork forward_work(int32_t dtype, int64_t rows, int64_t vocab) {
+// Room for the parts of x; its width is whole vectors of 8.
+static size_t cut_bytes(int32_t dtype, int64_t rows, int64_t width, LinearWork* w) {
+  w->cut_width = ceil_div(width, 8) * 8;
+  return dtype == EXTERND_F32 && rows <= 32 ? round256((size_t)(3 * 32 * w->cut_width) * 2) : 0;
+}
+
+static LinearWork forward_work(int32_t dtype, int64_t rows, int64_t vocab, int64_t width) {
   LinearWork w = {};
   const int64_t r = rows < FORWARD_ROWS ? rows : FORWARD_ROWS;
   w.step = forward_step(ceil_div(r, tile_rows(dtype, r)), vocab);
   w.tiles = ceil_div(vocab, w.step);
-  w.parts = 0;
-  w.at_target = round256((size_t)(r * w.tiles) * sizeof(Part));
+  w.parts = cut_bytes(dtype, r, width, &w);
+  w.at_target = w.parts + round256((size_t)(r * w.tiles) * sizeof(Part));
   w.bytes = w.at_target + round256((size_t)r * 4);
   return w;
 }
@@ -512,7 +536,7 @@ static LinearWork backward_work(int32_t dtype, int64_t rows, int64_t vocab, int6
   splits = splits < 1 ? 1 : splits > max_splits ? max_splits : splits;
   w.split = ceil_div(ceil_div(w.G_width, splits), 64) * 64;
   w.splits = (int)ceil_div(w.G_width, w.split);
-  size_t at = 0;
+  size_t at = cut_bytes(dtype, rows, width, &w);
   w.info = at, at += round256((size_t)rows * sizeof(RowInfo));
   w.up_all = at, at += 256;
   w.packed = at, at += need_weight ? round256((size_t)(rows * w.packed_width) * dtype_bytes(dtype)) : 0;
@@ -522,8 +546,11 @@ static LinearWork backward_work(int32_t dtype, int64_t rows, int64_t vocab, int6
   return w;
 }
 
-// Whether rows of 16-bit entries are whole vectors of 16 bytes at multiples of 16.
-static bool direct_rows(const Operand& o, int64_t width) { return !((uintptr_t)o.p & 15) && o.stride % 8 == 0 && width % 8 == 0; }
+// Whether rows are whole vectors of 16 bytes at multiples of 16.
+static bool direct_rows(const Operand& o, int64_t width, int32_t dtype) {
+  const int vec = 16 / dtype_bytes(dtype);
+  return !((uintptr_t)o.p & 15) && o.stride % vec == 0 && width % vec == 0;
+}
 
 template <typename P, bool BACK>
 static void launch_logits(LinearArgs a, hipStream_t s) {
@@ -562,7 +589,7 @@ template <int DT, bool DIRECT, bool BACK>
 static void choose_logits(const LinearArgs& a, hipStream_t s) {
   const int n = tile_rows(DT, a.rows);
   if constexpr (DT == EXTERND_F32) {
-    if (n == 32) launch_logits<Product<DT, false, false, false, 256, 32, 8, 2>, BACK>(a, s);
+    if (n == 32) launch_logits<Product<DT, DIRECT, false, false, 256, 32, 8, DIRECT ? 4 : 2>, BACK>(a, s);
     else launch_logits<Product<DT, false, false, false, 256, 128, 4, 2>, BACK>(a, s);
   } else {
     typedef Product<DT, DIRECT, false, false, 256, 32, 8, DIRECT ? 4 : 2> Small;
@@ -587,9 +614,16 @@ static void choose_grad_x(const LinearArgs& a, hipStream_t s) {
 }
 
 template <int DT>
+static void launch_cut(const LinearArgs& a, hipStream_t s) {
+  if (DT == EXTERND_F32 && tile_rows(DT, a.rows) == 32) k_cut<<<(unsigned)ceil_div(32 * (a.cut_width / 8), 256), 256, 0, s>>>(a);
+}
+
+template <int DT>
 static void launch_forward(LinearArgs a, bool direct, hipStream_t s) {
-  if (DT != EXTERND_F32 && direct) choose_logits<DT, DT != EXTERND_F32, false>(a, s);
-  else choose_logits<DT, false, false>(a, s);
+  if (direct) {
+    launch_cut<DT>(a, s);
+    choose_logits<DT, true, false>(a, s);
+  } else choose_logits<DT, false, false>(a, s);
   k_logits_join<<<(unsigned)a.rows, 256, 0, s>>>(a);
 }
 
@@ -600,12 +634,13 @@ static void launch_backward(LinearArgs a, bool direct, hipStream_t s) {
     return;
   }
   k_rows<<<DT == EXTERND_F16 ? 1 : (unsigned)ceil_div(a.rows, 1024), 1024, 0, s>>>(a, DT == EXTERND_F16);
+  if (direct) launch_cut<DT>(a, s);
   if (a.grad_weight) k_pack<DT><<<(unsigned)ceil_div(a.rows * (a.packed_width / Vec<DT>::E), 256), 256, 0, s>>>(a);
   for (a.p0 = 0; a.p0 < a.vocab; a.p0 = a.p1) {
     a.p1 = a.p0 + a.piece + 256 > a.vocab ? a.vocab : a.p0 + a.piece;
     a.v0 = a.p0;
     a.v1 = a.p1;
-    if (DT != EXTERND_F32 && direct) choose_logits<DT, DT != EXTERND_F32, true>(a, s);
+    if (direct) choose_logits<DT, true, true>(a, s);
     else choose_logits<DT, false, true>(a, s);
     if (a.grad_x) {
       if (DT != EXTERND_F32 && direct) choose_grad_x<DT, DT != EXTERND_F32>(a, s);
@@ -629,7 +664,7 @@ extern "C" {
 
 size_t externd_linear_logprobs_workspace_bytes(int32_t dtype, int64_t rows, int64_t vocab, int64_t width) {
   if (!dtype_ok(dtype) || rows < 0 || vocab < 1 || width < 1 || !linear_sizes(rows, vocab, width)) return 0;
-  return forward_work(dtype, rows ? rows : 1, vocab).bytes;
+  return forward_work(dtype, rows ? rows : 1, vocab, width).bytes;
 }
 
 int externd_linear_logprobs(const void* x, int64_t x_stride, const void* weight, int64_t weight_stride, int32_t dtype,
@@ -642,7 +677,7 @@ int externd_linear_logprobs(const void* x, int64_t x_stride, const void* weight,
   if (!linear_sizes(rows, vocab, width) || x_stride >= (1 << 22) || weight_stride >= (1 << 22)) return EXTERND_EUNSUPPORTED;
   if (!rows) return EXTERND_OK;
   if ((uintptr_t)workspace & 255) return EXTERND_EINVAL;
-  const LinearWork w = forward_work(dtype, rows, vocab);
+  const LinearWork w = forward_work(dtype, rows, vocab, width);
   if (!workspace || workspace_bytes < w.bytes) return EXTERND_EWORKSPACE;
   const hipStream_t s = (hipStream_t)stream;
   for (int64_t r = 0; r < rows; r += FORWARD_ROWS) {
@@ -658,11 +693,13 @@ int externd_linear_logprobs(const void* x, int64_t x_stride, const void* weight,
     a.logprob = logprob ? logprob + r : nullptr;
     a.entropy = entropy ? entropy + r : nullptr;
     a.lse = lse ? lse + r : nullptr;
+    a.cut = workspace;
+    a.cut_width = w.cut_width;
     a.parts = (Part*)((char*)workspace + w.parts);
     a.at_target = (float*)((char*)workspace + w.at_target);
     a.step = w.step;
-    const bool direct = direct_rows(a.x, width) && direct_rows(a.weight, width);
-    if (dtype == EXTERND_F32) launch_forward<EXTERND_F32>(a, false, s);
+    const bool direct = direct_rows(a.x, width, dtype) && direct_rows(a.weight, width, dtype);
+    if (dtype == EXTERND_F32) launch_forward<EXTERND_F32>(a, direct, s);
     else if (dtype == EXTERND_BF16) launch_forward<EXTERND_BF16>(a, direct, s);
     else launch_forward<EXTERND_F16>(a, direct, s);
   }
@@ -707,6 +744,8 @@ int externd_linear_logprobs_backward(const void* x, int64_t x_stride, const void
   a.grad_x_stride = grad_x_stride;
   a.grad_weight_stride = grad_weight_stride;
   char* const at = (char*)workspace;
+  a.cut = at;
+  a.cut_width = w.cut_width;
   a.info = (RowInfo*)(at + w.info);
   a.up_all = (float*)(at + w.up_all);
   a.packed = at + w.packed;
@@ -718,9 +757,9 @@ int externd_linear_logprobs_backward(const void* x, int64_t x_stride, const void
   a.dx_width = w.dx_width;
   a.split = w.split;
   a.splits = w.splits;
-  const bool direct = direct_rows(a.x, width) && direct_rows(a.weight, width);
+  const bool direct = direct_rows(a.x, width, dtype) && direct_rows(a.weight, width, dtype);
   const hipStream_t s = (hipStream_t)stream;
-  if (dtype == EXTERND_F32) launch_backward<EXTERND_F32>(a, false, s);
+  if (dtype == EXTERND_F32) launch_backward<EXTERND_F32>(a, direct, s);
   else if (dtype == EXTERND_BF16) launch_backward<EXTERND_BF16>(a, direct, s);
   else launch_backward<EXTERND_F16>(a, direct, s);
   return hipGetLastError() == hipSuccess ? EXTERND_OK : EXTERND_EHIP;
