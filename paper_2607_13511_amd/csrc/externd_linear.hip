@@ -184,7 +184,7 @@ __global__ __launch_bounds__(GEMM_THREADS, 2) void k_logits(LinearArgs a) {
         for (int i = 0; i < TM; i++)
 #pragma unroll
           for (int r = 0; r < 16; r++)
-            if (P::row(i, r) == y) a.at_target[n] = acc[i][j][r] * a.scale;
+            if (P::row(i, r) == y && y < ms) a.at_target[n] = acc[i][j][r] * a.scale;      // what lies behind is another tile's
       }
       float top = -INFINITY;
 #pragma unroll

@@ -99,6 +99,25 @@ def test_forward_whole_numbers(ext, dtype, rows, width, vocab):
     check(ext, *make(rows, width, vocab, dtype, rows, True), whole=True)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,width,vocab", [(1, 16, 70001), (3, 40, 9000), (8, 65, 20011), (32, 24, 65537), (31, 7, 8193)])
+def test_few_rows_of_a_large_vocabulary(ext, dtype, rows, width, vocab):
+    """Tiles of less than 256 columns; every target's own logit, one by one the columns around the tiles' ends."""
+    x, w, _ = make(rows, width, vocab, dtype, rows, True)
+    for first in (0, 130, 255, vocab - rows):
+        check(ext, x, w, torch.arange(first, first + rows, device="cuda"), whole=True)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("width", [264, 261])
+def test_last_columns_by_themselves(ext, dtype, width):
+    """128 tiles for each of two row tiles, and one column more."""
+    x, w, y = make(300, width, 32769, dtype, 20, True)
+    y[7], y[8] = 32768, 32767
+    check(ext, x, w, y, whole=True)
+    check_backward(ext, x, w, y, *gradients(300, y, 21, "ge"), dtype, whole=True)
+
+
 def gradients(rows, y, seed, kind):
     rng = np.random.default_rng(seed)
     g = (rng.standard_normal(rows) / rows).astype(np.float32) if "g" in kind else None
