@@ -57,8 +57,10 @@ struct Tile {
     *row = i / CH;
     const int v = i % CH;
     if constexpr (COL) *vec = ((v >> 1) ^ spread(*row)) << 1 | (v & 1);
-    else *vec = v ^ ((*row / (16 / CH)) & (CH - 1));
+    else *vec = v ^ swap(*row);
   }
+  // By rows: the sixteen rows that are read together go to different banks (256 bytes of them).
+  static __device__ __forceinline__ int swap(int row) { return CH >= 16 ? row & 15 : (row / (16 / (CH < 16 ? CH : 16))) & (CH - 1); }
   // By columns: pairs of vectors (16 columns) of four rows of k go to different banks.
   static __device__ __forceinline__ int spread(int k) { return (2 * (k & 3)) & (X / 16 - 1); }
   // The byte at which a lane reads its fragment of 32 columns from x0 on, without what depends on x0 and on the step of 16 k.
@@ -73,16 +75,16 @@ struct Tile {
       const v2u a = __builtin_bit_cast(v2u, lo), b = __builtin_bit_cast(v2u, hi);
       return v4u{a[0], a[1], b[0], b[1]};
     } else {
-      const int row = x0 + (lane & 31), v = (ks * 2 + (lane >> 5)) ^ ((row / (16 / CH)) & (CH - 1));
+      const int row = x0 + (lane & 31), v = (ks * 2 + (lane >> 5)) ^ swap(row);
       return *(const __attribute__((address_space(3))) v4u*)(t + (row * CH + v) * 16);
     }
   }
   // The same of a tile of fp32 entries by rows: the fragment's eight in two vectors.
   static __device__ __forceinline__ void fragment_f32(const lds_char* t, int x0, int ks, v4u* x) {
-    const int lane = threadIdx.x & 63, row = x0 + (lane & 31), swap = (row / (16 / CH)) & (CH - 1);
+    const int lane = threadIdx.x & 63, row = x0 + (lane & 31);
 #pragma unroll
     for (int i = 0; i < 2; i++)
-      x[i] = *(const __attribute__((address_space(3))) v4u*)(t + (row * CH + ((ks * 4 + (lane >> 5) * 2 + i) ^ swap)) * 16);
+      x[i] = *(const __attribute__((address_space(3))) v4u*)(t + (row * CH + ((ks * 4 + (lane >> 5) * 2 + i) ^ swap(row))) * 16);
   }
 };
 
@@ -186,97 +188,177 @@ __device__ __forceinline__ void barrier() {
   asm volatile("" ::: "memory");
 }
 
-// Loads of any operand through registers: rows that begin anywhere, entries past
-// an end left out one by one, and fp32 operands, cut into their parts.
-template <int DT, bool COL, int X, int BK>
+// Moves the eight entries of a vector down by s, 0 .. 7, with zeros behind.
+template <int DT, int WORDS>
+__device__ __forceinline__ void shift_down(v4u* x, int s) {
+  unsigned w[4 * WORDS + 4] = {};
+#pragma unroll
+  for (int i = 0; i < 4 * WORDS; i++) w[i] = x[i / 4][i % 4];
+  const int words = DT == EXTERND_F32 ? s : s >> 1;
+#pragma unroll
+  for (int d = 4; d; d >>= 1)
+#pragma unroll
+    for (int i = 0; i < 4 * WORDS; i++) w[i] = words & d ? (i + d < 4 * WORDS ? w[i + d] : 0u) : w[i];
+  if (DT != EXTERND_F32 && (s & 1)) {
+#pragma unroll
+    for (int i = 0; i < 4; i++) w[i] = w[i] >> 16 | w[i + 1] << 16;
+  }
+#pragma unroll
+  for (int i = 0; i < 4 * WORDS; i++) x[i / 4][i % 4] = w[i];
+}
+
+// Loads of any operand through registers: rows that begin anywhere and end within
+// a vector, and fp32 operands, cut into their parts.  DEPTH steps are under way at
+// a time, and no load stands behind a branch that waits: a vector that is only
+// partly there is read so that it ends where its row does, and moved into place
+// on its way to LDS.
+template <int DT, bool COL, int X, int BK, int DEPTH>
 struct Staged {
   typedef typename Elem<DT>::T E;
   typedef Tile<COL, X, BK> T;
   static constexpr int LOADS = T::LOADS ? T::LOADS : 1, WORDS = DT == EXTERND_F32 ? 2 : 1;
-  const E* at[LOADS];
-  v4u held[LOADS][WORDS];
+  const E *at[LOADS], *safe, *begin;      // safe: eight entries that are there; begin: of the step, for put_tiny
+  v4u held[DEPTH][LOADS][WORDS];
   int64_t stride, k_left;
-  int cols;
+  int cols, over, tail;         // of m (or n); by columns, entries that the last vector lacks; k of the last step, if fewer than BK
+  bool tiny;                    // rows of fewer than eight entries: put_tiny
+
+  __device__ __forceinline__ bool none(int i) const { return i * GEMM_THREADS + (int)threadIdx.x >= T::VECTORS; }
+  __device__ __forceinline__ bool short_column(int v) const { return v * 8 < cols && cols < v * 8 + 8; }
 
   __device__ __forceinline__ void init(const Operand& o, int64_t x0, int64_t count, int64_t k0, int64_t K) {
     stride = o.stride;
     cols = (int)min(count, (int64_t)X);
+    over = COL && cols & 7 ? 8 - (cols & 7) : 0;
+    tail = (int)(K % BK);
     k_left = K;
+    tiny = (COL ? x0 + cols : k0 + K) < 8;
     const E* base = (const E*)o.p + (COL ? k0 * stride + x0 : x0 * stride + k0);
+    begin = base;
+    safe = (const E*)o.p + (COL ? k0 * stride + x0 + cols - 8 : x0 * stride);
 #pragma unroll
     for (int i = 0; i < LOADS; i++) {
       int r, v;
       T::place(i * GEMM_THREADS + (int)threadIdx.x, &r, &v);
-      at[i] = base + r * stride + v * 8;
+      // past the last m (or n) any entries do, as what becomes of them is not used: the first ones
+      if (COL ? v * 8 >= cols : r >= cols) COL ? v = 0 : r = 0;
+      at[i] = base + r * stride + v * 8 - (!tiny && COL && short_column(v) ? over : 0);
     }
   }
-  // The next step's vectors, into registers.
-  __device__ __forceinline__ void fetch() {
+  // The next step's vectors, into set `set`.  It always loads, so that waits can count the loads behind their own.
+  __device__ __forceinline__ void fetch(int set) {
+    const int n = (int)max((int64_t)0, min(k_left, (int64_t)BK));
+    k_left -= BK;
 #pragma unroll
     for (int i = 0; i < LOADS; i++) {
-      int r, v;
-      T::place(i * GEMM_THREADS + (int)threadIdx.x, &r, &v);
-      const bool in = i * GEMM_THREADS + (int)threadIdx.x < T::VECTORS && (COL ? r < k_left : r < cols);
-      const int n = !in ? 0 : (int)min((COL ? (int64_t)cols : k_left) - v * 8, (int64_t)8);
-      if (n >= 8) {
-#pragma unroll
-        for (int w = 0; w < WORDS; w++) held[i][w] = load_any(at[i] + w * Vec<DT>::E);
-      } else {
-        float x[8];
-#pragma unroll
-        for (int e = 0; e < 8; e++) x[e] = e < n ? Elem<DT>::load(at[i][e]) : 0.f;
-#pragma unroll
-        for (int w = 0; w < WORDS; w++) held[i][w] = Vec<DT>::pack(x + w * Vec<DT>::E);
+      const E* from = at[i];
+      if (n < BK) {      // the last step, or none: in the place of what is not there, entries that are
+        int r, v;
+        T::place(i * GEMM_THREADS + (int)threadIdx.x, &r, &v);
+        if (n == 0) from = safe;
+        else if (COL) from -= r < n ? 0 : r * stride;
+        else from -= n - v * 8 >= 8 ? 0 : v * 8 + 8 - n;
       }
+#pragma unroll
+      for (int w = 0; w < WORDS; w++) held[set][i][w] = load_any(from + w * Vec<DT>::E);
       at[i] += COL ? BK * stride : BK;
     }
-    k_left -= BK;
   }
-  // To the tile at `lds`; planes lie `plane` bytes apart.
-  __device__ __forceinline__ void put(lds_char* lds, int plane) const {
+  static __device__ __forceinline__ void write(lds_char* to, int plane, const v4u* x) {
     typedef __attribute__((address_space(3))) v4u* vec;
+    if constexpr (DT != EXTERND_F32) *(vec)to = x[0];
+    else {
+      v4u part[3];
+      cut(x, part);
+#pragma unroll
+      for (int p = 0; p < 3; p++) *(vec)(to + p * plane) = part[p];
+    }
+  }
+  // Set `set`, to the tile at `lds`; planes lie `plane` bytes apart.  LAST: a step of `tail` k.
+  template <bool LAST>
+  __device__ __forceinline__ void put(int set, lds_char* lds, int plane) {
 #pragma unroll
     for (int i = 0; i < LOADS; i++) {
-      if (i * GEMM_THREADS + (int)threadIdx.x >= T::VECTORS) return;
-      lds_char* const to = lds + (i * GEMM_THREADS + (int)threadIdx.x) * 16;
-      if constexpr (DT != EXTERND_F32) *(vec)to = held[i][0];
-      else {
-        v4u part[3];
-        cut(held[i], part);
+      if (none(i)) return;
+      int r, v;
+      T::place(i * GEMM_THREADS + (int)threadIdx.x, &r, &v);
+      v4u x[WORDS];
 #pragma unroll
-        for (int p = 0; p < 3; p++) *(vec)(to + p * plane) = part[p];
+      for (int w = 0; w < WORDS; w++) x[w] = held[set][i][w];
+      if (COL && over) {
+        if (short_column(v)) shift_down<DT, WORDS>(x, over);
       }
+      if constexpr (LAST) {
+        if (!COL && tail - v * 8 > 0 && tail - v * 8 < 8) shift_down<DT, WORDS>(x, 8 - (tail & 7));
+        if (COL ? r >= tail : v * 8 >= tail) {
+#pragma unroll
+          for (int w = 0; w < WORDS; w++) x[w] = v4u{0, 0, 0, 0};
+        }
+      }
+      write(lds + (i * GEMM_THREADS + (int)threadIdx.x) * 16, plane, x);
     }
+  }
+  // A step of an operand with short rows, entry by entry.
+  __device__ __forceinline__ void put_tiny(lds_char* lds, int plane) {
+    const int n = (int)max((int64_t)0, min(k_left, (int64_t)BK));
+#pragma unroll 1
+    for (int i = threadIdx.x; i < T::VECTORS; i += GEMM_THREADS) {
+      int r, v;
+      T::place(i, &r, &v);
+      const bool first = COL ? v * 8 >= cols : r >= cols;      // in the place of a column or row that is not there
+      const E* from = begin + (int64_t)(!COL && first ? 0 : r) * stride + (COL && first ? 0 : v * 8);
+      const int there = COL ? r >= n ? 0 : first ? min(cols, 8) : min(cols - v * 8, 8) : min(n - v * 8, 8);
+      float y[8];
+#pragma unroll
+      for (int e = 0; e < 8; e++) y[e] = e < there ? Elem<DT>::load(from[e]) : 0.f;
+      v4u x[WORDS];
+#pragma unroll
+      for (int w = 0; w < WORDS; w++) x[w] = Vec<DT>::pack(y + w * Vec<DT>::E);
+      write(lds + i * 16, plane, x);
+    }
+    k_left -= BK;
+    begin += COL ? BK * stride : BK;
   }
 };
 
-// How a workgroup of eight waves divides a tile of BM x BN: WM of them along m.
-template <int DT_, bool DIRECT_, bool ACOL_, bool BCOL_, int BM_, int BN_, int WM_, int STAGES_>
+// How a workgroup of eight waves divides a tile of BM x BN: WM x WN of them over
+// the tile, and KW over the k of a step (for small tiles, which need many k in
+// flight to keep a CU busy): those are summed at the end, and the first WM x WN
+// waves hold the result.
+template <int DT_, bool DIRECT_, bool ACOL_, bool BCOL_, int BM_, int BN_, int WM_, int STAGES_, int KW_ = 1>
 struct Product {
-  static constexpr int DT = DT_, BM = BM_, BN = BN_, WM = WM_, WN = 8 / WM_, STAGES = STAGES_;
+  static constexpr int DT = DT_, BM = BM_, BN = BN_, WM = WM_, KW = KW_, WN = 8 / WM_ / KW_, STAGES = STAGES_;
   static constexpr bool DIRECT = DIRECT_, ACOL = ACOL_, BCOL = BCOL_;
   // fp32 by rows: A's entries in LDS, cut as they are read; B comes as its three
   // parts, cut ahead, each BN rows of bf16 behind the other.
   static constexpr bool RAW = DIRECT && DT == EXTERND_F32;
-  static constexpr int BK = Kind<DT>::BK, PLANES = RAW ? 1 : Kind<DT>::PLANES, EV = RAW ? 4 : 8, BROWS = RAW ? 3 * BN : BN;
+  static constexpr int BK = Kind<DT>::BK * (KW > 1 ? 4 : 1), PLANES = RAW ? 1 : Kind<DT>::PLANES, EV = RAW ? 4 : 8, BROWS = RAW ? 3 * BN : BN;
+  static constexpr int NK = BK / 16 / KW;                     // of a wave, 16 k each
   static constexpr int TM = BM / WM / 32, TN = BN / WN / 32;
   typedef Tile<ACOL, BM, BK, EV> TA;
   typedef Tile<BCOL, BROWS, BK, 8> TB;
-  static constexpr int STAGE = (TA::BYTES + TB::BYTES) * PLANES, LDS = STAGE * STAGES;
+  // steps in registers ahead, where loads go through them: small tiles wait for memory
+  static constexpr int DEPTH = BN > 32 ? 1 : DT == EXTERND_F32 || KW > 1 ? 2 : 4;
+  static constexpr int STAGE = (TA::BYTES + TB::BYTES) * PLANES, LOOP_LDS = STAGE * STAGES, JOIN_LDS = KW > 1 ? KW * BM * BN * 4 : 0;
+  static constexpr int LDS = LOOP_LDS > JOIN_LDS ? LOOP_LDS : JOIN_LDS;
   static_assert(LDS <= 160 * 1024 && TM >= 1 && TN >= 1 && !(RAW && (ACOL || BCOL || TM > 1 || TN > 1)), "fits");
 
+  static __device__ __forceinline__ int wave() { return (threadIdx.x >> 6) % (WM * WN); }
+  static __device__ __forceinline__ int k_wave() { return (threadIdx.x >> 6) / (WM * WN); }
+  static __device__ __forceinline__ bool holds() { return KW == 1 || k_wave() == 0; }
   // Entry `r` (0 .. 15) of acc[i][j] is C(m0 + row(i, r), n0 + col(j)).
   static __device__ __forceinline__ int row(int i, int r) {
-    return ((threadIdx.x >> 6) / WN * TM + i) * 32 + 8 * (r >> 2) + 4 * ((threadIdx.x & 63) >> 5) + (r & 3);
+    return (wave() / WN * TM + i) * 32 + 8 * (r >> 2) + 4 * ((threadIdx.x & 63) >> 5) + (r & 3);
   }
-  static __device__ __forceinline__ int col(int j) { return ((threadIdx.x >> 6) % WN * TN + j) * 32 + (threadIdx.x & 31); }
+  static __device__ __forceinline__ int col(int j) { return (wave() % WN * TN + j) * 32 + (threadIdx.x & 31); }
 
   // One step's products, from the tiles at `s`.
   static __device__ __forceinline__ void step(const lds_char* s, f32x16 (*acc)[TN]) {
     const lds_char *a = s, *b = s + TA::BYTES * PLANES;
-    const int wave = threadIdx.x >> 6, ma = wave / WN * TM * 32, nb = wave % WN * TN * 32;
+    const int ma = wave() / WN * TM * 32, nb = wave() % WN * TN * 32;
 #pragma unroll
-    for (int ks = 0; ks < BK / 16; ks++) {
+    for (int k = 0; k < NK; k++) {
+      const int ks = k_wave() * NK + k;
       v4u fa[PLANES][TM], fb[PLANES][TN];
 #pragma unroll
       for (int p = 0; p < PLANES; p++) {
@@ -325,12 +407,11 @@ struct Product {
         else wait_loads<EACH * N>();
         barrier();
       };
-      // A step's fragments are read one sixteenth of K ahead of their products,
-      // those of the next step as well: the barrier and the loads of a step
-      // stand in front of products whose operands are in registers.
-      constexpr int NK = BK / 16;
+      // Fragments are read 16 k ahead of their products, those of the next step
+      // as well: the barrier and the loads of a step stand in front of products
+      // whose operands are in registers.
       static_assert(NK % 2 == 0, "two sets of fragments in turn");
-      const int wave = threadIdx.x >> 6, ma = wave / WN * TM * 32, nb = wave % WN * TN * 32;
+      const int ma = wave() / WN * TM * 32, nb = wave() % WN * TN * 32, k0s = k_wave() * NK;
       // of this wave's 32 x 32 products, how many lie in the operands
       const int tm = (int)max((int64_t)0, min((m_count - ma + 31) / 32, (int64_t)TM)), tn = (int)max((int64_t)0, min((n_count - nb + 31) / 32, (int64_t)TN));
       for (int s = 0; s < STAGES; s++) issue(s);      // past the last step: zeros, which nothing reads
@@ -342,13 +423,13 @@ struct Product {
           for (int j = 0; j < TN; j++)
             if (!partial || j < tn) {
 #pragma unroll
-              for (int p = 0; p < (RAW ? 3 : 1); p++) fb[set][j][p] = TB::fragment(s + TA::BYTES, p * BN + nb + j * 32, ks);
+              for (int p = 0; p < (RAW ? 3 : 1); p++) fb[set][j][p] = TB::fragment(s + TA::BYTES, p * BN + nb + j * 32, k0s + ks);
             }
 #pragma unroll
           for (int i = 0; i < TM; i++)
             if (!partial || i < tm) {
-              if constexpr (RAW) TA::fragment_f32(s, ma + i * 32, ks, fa[set][i]);
-              else fa[set][i][0] = TA::fragment(s, ma + i * 32, ks);
+              if constexpr (RAW) TA::fragment_f32(s, ma + i * 32, k0s + ks, fa[set][i]);
+              else fa[set][i][0] = TA::fragment(s, ma + i * 32, k0s + ks);
             }
         };
         auto multiply = [&](int set, int i, int j) {
@@ -387,25 +468,80 @@ struct Product {
       barrier();
     } else {
       static_assert(DIRECT || STAGES == 2, "two buffers");
-      Staged<DT, ACOL, BM, BK> la;
-      Staged<DT, BCOL, BN, BK> lb;
+      Staged<DT, ACOL, BM, BK, DEPTH> la;
+      Staged<DT, BCOL, BN, BK, DEPTH> lb;
       la.init(A, m0, m_count, k0, K);
       lb.init(B, n0, n_count, k0 + b_k, K);
-      la.fetch();
-      lb.fetch();
-      for (int64_t t = 0; t < steps; t++) {
-        lds_char* const s = lds + (t & 1) * STAGE;
-        la.put(s, TA::BYTES);
-        lb.put(s + TA::BYTES * PLANES, TB::BYTES);
+      auto stage = [&](int u, auto last, bool more) {
+        lds_char* const s = lds + (u & 1) * STAGE;
+        la.template put<decltype(last)::value>(u % DEPTH, s, TA::BYTES);
+        lb.template put<decltype(last)::value>(u % DEPTH, s + TA::BYTES * PLANES, TB::BYTES);
         wait_loads<63>();
         barrier();
-        if (t + 1 < steps) {
-          la.fetch();
-          lb.fetch();
+        if (more) {
+          la.fetch(u % DEPTH);
+          lb.fetch(u % DEPTH);
+          __builtin_amdgcn_sched_barrier(0);      // the loads go out before the products, not among them
         }
         step(s, acc);
+      };
+      if (la.tiny || lb.tiny) {
+        for (int64_t t = 0; t < steps; t++) {
+          la.put_tiny(lds, TA::BYTES);
+          lb.put_tiny(lds + TA::BYTES * PLANES, TB::BYTES);
+          wait_loads<63>();
+          barrier();
+          step(lds, acc);
+          wait_loads<63>();
+          barrier();
+        }
+      } else {
+#pragma unroll
+        for (int d = 0; d < DEPTH; d++) {
+          la.fetch(d);
+          lb.fetch(d);
+        }
+        constexpr int UNROLL = DEPTH > 1 ? DEPTH : 2;
+        const int64_t whole = K / BK;
+        int64_t t = 0;
+        for (; t + UNROLL <= whole; t += UNROLL) {
+#pragma unroll
+          for (int u = 0; u < UNROLL; u++) stage(u, std::false_type(), true);
+        }
+#pragma unroll
+        for (int u = 0; u < UNROLL; u++) {
+          if (t + u < whole) stage(u, std::false_type(), DEPTH == 1);
+          else if (t + u == whole && whole < steps) stage(u, std::true_type(), false);
+        }
       }
       wait_loads<0>();
+      barrier();
+    }
+    if constexpr (KW > 1) {
+      // the waves' sums over their k, [wave][entry][lane]: each wave adds up its share, the first reads it all
+      typedef __attribute__((address_space(3))) float* floats;
+      constexpr int EACH = TM * TN * 16;
+      static_assert(WM * WN == 1 && EACH % KW == 0, "one wave holds the tile");
+      floats all = (floats)lds + (threadIdx.x & 63);
+#pragma unroll
+      for (int e = 0; e < EACH; e++) all[(k_wave() * EACH + e) * 64] = acc[e / 16 / TN][e / 16 % TN][e % 16];
+      wait_loads<63>();
+      barrier();
+#pragma unroll
+      for (int i = 0; i < EACH / KW; i++) {
+        const int e = k_wave() * (EACH / KW) + i;
+        float x = 0.f;
+#pragma unroll
+        for (int w = 0; w < KW; w++) x += all[(w * EACH + e) * 64];
+        all[e * 64] = x;
+      }
+      wait_loads<63>();
+      barrier();
+      if (holds()) {
+#pragma unroll
+        for (int e = 0; e < EACH; e++) acc[e / 16 / TN][e / 16 % TN][e % 16] = all[e * 64];
+      }
+      wait_loads<63>();
       barrier();
     }
   }

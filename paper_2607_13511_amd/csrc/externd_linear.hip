@@ -75,9 +75,9 @@ template <typename P>
 struct Gathered {
   typedef typename Elem<P::DT>::T T;
   static constexpr int E = Vec<P::DT>::E, VECTORS = P::BM / E;
-  static_assert(P::BN * P::BM * (int)sizeof(T) <= P::LDS && VECTORS >= 32, "fits");
+  static_assert(P::BN * P::BM * (int)sizeof(T) <= P::LDS, "fits");
   static __device__ __forceinline__ char* at(char* lds, int n, int m) {
-    return lds + (n * VECTORS + ((m / E) ^ (n & 31))) * 16 + m % E * (int)sizeof(T);
+    return lds + (n * VECTORS + ((m / E) ^ (n & 31 & (VECTORS - 1)))) * 16 + m % E * (int)sizeof(T);
   }
   // Entries m .. m + 3 of row n.
   static __device__ __forceinline__ void put(char* lds, int n, int m, const float* o) {
@@ -119,6 +119,7 @@ __global__ __launch_bounds__(GEMM_THREADS, 2) void k_logits(LinearArgs a) {
   if constexpr (BACK) {
     typedef typename Elem<DT>::T T;
     const float c = a.scale * LOG2E;
+    if (P::holds())
 #pragma unroll
     for (int j = 0; j < TN; j++) {
       const int64_t n = n0 + P::col(j);
@@ -167,8 +168,8 @@ __global__ __launch_bounds__(GEMM_THREADS, 2) void k_logits(LinearArgs a) {
     Gathered<P>::write(lds, a.rows - n0, ms, [&](int n, int m, v4u x) { *(v4u*)(to + n * a.G_width + m) = x; });
   } else {
     Part* const shared = (Part*)lds;      // WM x BN
-    const int wave = threadIdx.x >> 6;
     const float c = a.scale * LOG2E;
+    if (P::holds())
 #pragma unroll
     for (int j = 0; j < TN; j++) {
       const int64_t n = n0 + P::col(j), y = a.targets && n < a.rows ? a.targets[n] - m0 : -1;
@@ -207,7 +208,7 @@ __global__ __launch_bounds__(GEMM_THREADS, 2) void k_logits(LinearArgs a) {
       sum += __shfl_xor(sum, 32);
       mean += __shfl_xor(mean, 32);
       top *= a.scale;
-      if (!(threadIdx.x & 32)) shared[wave / P::WN * P::BN + P::col(j)] = Part{top, sum, mean * LN2, 0.f};
+      if (!(threadIdx.x & 32)) shared[P::wave() / P::WN * P::BN + P::col(j)] = Part{top, sum, mean * LN2, 0.f};
     }
     __syncthreads();
     const int n = threadIdx.x;
@@ -385,21 +386,40 @@ __global__ __launch_bounds__(GEMM_THREADS, 2) void k_grad_x(LinearArgs a) {
   }
 }
 
-// The splits' sums joined in order, scaled and rounded.
-template <int DT>
+// The splits' sums joined in order, scaled and rounded.  A thread has four
+// columns; GROUPS of them share many splits (few rows, whose loads would otherwise
+// wait for each other) and are joined in LDS.
+template <int DT, int GROUPS>
 __global__ __launch_bounds__(256) void k_grad_x_join(LinearArgs a) {
   typedef typename Elem<DT>::T T;
-  const int64_t units = a.dx_width / 4, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= units * a.rows) return;
-  const int64_t r = i / units, c = (i - r * units) * 4;
+  constexpr int UNITS = 256 / GROUPS;
+  __shared__ float4 part[GROUPS][UNITS];
+  const int64_t units = a.dx_width / 4, i = (int64_t)blockIdx.x * UNITS + threadIdx.x % UNITS;
+  const int group = threadIdx.x / UNITS;
+  const bool in = i < units * a.rows;
+  const int64_t r = in ? i / units : 0, c = in ? (i - r * units) * 4 : 0;
   const RowInfo w = a.info[r];
   float x[4] = {};
-  if (w.present) {
-    for (int s = 0; s < a.splits; s++) {
-      const float4 b = *(const float4*)(a.dx + (s * a.rows + r) * a.dx_width + c);
+  if (in && w.present) {
+    const int each = (a.splits + GROUPS - 1) / GROUPS, s1 = min((group + 1) * each, a.splits);
+    const float* p = a.dx + r * a.dx_width + c;
+#pragma unroll 8
+    for (int s = group * each; s < s1; s++) {
+      const float4 b = *(const float4*)(p + s * a.rows * a.dx_width);
       x[0] += b.x, x[1] += b.y, x[2] += b.z, x[3] += b.w;
     }
   }
+  if constexpr (GROUPS > 1) {
+    part[group][threadIdx.x % UNITS] = float4{x[0], x[1], x[2], x[3]};
+    __syncthreads();
+    if (group) return;
+#pragma unroll
+    for (int g = 1; g < GROUPS; g++) {
+      const float4 b = part[g][threadIdx.x];
+      x[0] += b.x, x[1] += b.y, x[2] += b.z, x[3] += b.w;
+    }
+  }
+  if (!in) return;
   const float f = a.scale, down = 1.f / w.up;
   T* const to = (T*)a.grad_x + r * a.grad_x_stride + c;
 #pragma unroll
@@ -463,17 +483,26 @@ static bool linear_sizes(int64_t rows, int64_t vocab, int64_t width) {
   return rows <= (1 << 22) && vocab < INT32_MAX - 1023 && width <= (1 << 20);
 }
 
-// Rows of a tile.
+// Rows of a tile; operands that go through registers take 128 at most (256 would not leave enough of them).
 static int tile_rows(int32_t dtype, int64_t rows) {
   if (rows <= 32) return 32;
   return dtype == EXTERND_F32 || rows <= 128 ? 128 : 256;
 }
 
-// Vocabulary of a forward tile.  One row tile reads weight once, so the card's
+// Few large tiles leave CUs without work: small ones then, 64 columns by 32
+// rows, whose eight waves share the k of a step.  A large tile takes as long as
+// about four small ones (121 rows of 2556, width 4026: TODO).
+static bool small_tiles(int32_t dtype, int64_t rows, int64_t vocab) {
+  const int64_t small = ceil_div(vocab, 64) * ceil_div(rows, 32);
+  return ceil_div(vocab, 256) * ceil_div(rows, tile_rows(dtype, rows)) < CUS && small <= CUS * (rows <= 32 ? 1 : 4);
+}
+
+// Vocabulary of a tile of logits.  One row tile reads weight once, so the card's
 // CUs take equally many tiles of equal length: 65537 rows are 512 tiles of 136
 // and not 256 of 256 and one of 1.
-static int64_t forward_step(int64_t row_tiles, int64_t vocab) {
-  if (row_tiles > 1 || vocab <= 256 * CUS / 8) return 256;
+static int64_t forward_step(int32_t dtype, int64_t rows, int64_t vocab) {
+  if (small_tiles(dtype, rows, vocab)) return 64;
+  if (rows > tile_rows(dtype, rows) || vocab <= 256 * CUS / 8) return 256;
   const int64_t tiles = ceil_div(ceil_div(vocab, 256), CUS) * CUS;
   return ceil_div(ceil_div(vocab, tiles), 8) * 8;
 }
@@ -493,7 +522,7 @@ static size_t cut_bytes(int32_t dtype, int64_t rows, int64_t width, LinearWork* 
 static LinearWork forward_work(int32_t dtype, int64_t rows, int64_t vocab, int64_t width) {
   LinearWork w = {};
   const int64_t r = rows < FORWARD_ROWS ? rows : FORWARD_ROWS;
-  w.step = forward_step(ceil_div(r, tile_rows(dtype, r)), vocab);
+  w.step = forward_step(dtype, r, vocab);
   w.tiles = ceil_div(vocab, w.step);
   w.parts = cut_bytes(dtype, r, width, &w);
   w.at_target = w.parts + round256((size_t)(r * w.tiles) * sizeof(Part));
@@ -588,15 +617,16 @@ static void launch_grad_weight(LinearArgs a, hipStream_t s) {
 template <int DT, bool DIRECT, bool BACK>
 static void choose_logits(const LinearArgs& a, hipStream_t s) {
   const int n = tile_rows(DT, a.rows);
+  if (a.step == 64) return launch_logits<Product<DT, DIRECT && DT != EXTERND_F32, false, false, 64, 32, 1, DIRECT && DT != EXTERND_F32 ? 3 : 2, 8>, BACK>(a, s);
   if constexpr (DT == EXTERND_F32) {
     if (n == 32) launch_logits<Product<DT, DIRECT, false, false, 256, 32, 8, DIRECT ? 4 : 2>, BACK>(a, s);
     else launch_logits<Product<DT, false, false, false, 256, 128, 4, 2>, BACK>(a, s);
   } else {
     typedef Product<DT, DIRECT, false, false, 256, 32, 8, DIRECT ? 4 : 2> Small;
     if (n == 32) launch_logits<Small, BACK>(a, s);
-    else if (n == 128) launch_logits<Product<DT, DIRECT, false, false, 256, 128, 4, DIRECT ? 3 : 2>, BACK>(a, s);
-    else
-      with_tail(a, ceil_div(a.rows, 256), [&](const LinearArgs& b) { launch_logits<Product<DT, DIRECT, false, false, 256, 256, 2, 2>, BACK>(b, s); },
+    else if (n == 128 || !DIRECT) launch_logits<Product<DT, DIRECT, false, false, 256, 128, 4, DIRECT ? 3 : 2>, BACK>(a, s);
+    else if constexpr (DIRECT)
+      with_tail(a, ceil_div(a.rows, 256), [&](const LinearArgs& b) { launch_logits<Product<DT, true, false, false, 256, 256, 2, 2>, BACK>(b, s); },
                 [&](const LinearArgs& b) { launch_logits<Small, BACK>(b, s); });
   }
 }
@@ -608,14 +638,14 @@ static void choose_grad_x(const LinearArgs& a, hipStream_t s) {
     else launch_grad_x<Product<DT, false, true, false, 256, 128, 4, 2>>(a, s);
   } else {
     if (n == 32) launch_grad_x<Product<DT, DIRECT, true, false, 256, 32, 8, DIRECT ? 4 : 2>>(a, s);
-    else if (n == 128) launch_grad_x<Product<DT, DIRECT, true, false, 256, 128, 4, DIRECT ? 3 : 2>>(a, s);
-    else launch_grad_x<Product<DT, DIRECT, true, false, 256, 256, 2, 2>>(a, s);
+    else if (n == 128 || !DIRECT) launch_grad_x<Product<DT, DIRECT, true, false, 256, 128, 4, DIRECT ? 3 : 2>>(a, s);
+    else if constexpr (DIRECT) launch_grad_x<Product<DT, true, true, false, 256, 256, 2, 2>>(a, s);
   }
 }
 
 template <int DT>
 static void launch_cut(const LinearArgs& a, hipStream_t s) {
-  if (DT == EXTERND_F32 && tile_rows(DT, a.rows) == 32) k_cut<<<(unsigned)ceil_div(32 * (a.cut_width / 8), 256), 256, 0, s>>>(a);
+  if (DT == EXTERND_F32 && a.step != 64 && tile_rows(DT, a.rows) == 32) k_cut<<<(unsigned)ceil_div(32 * (a.cut_width / 8), 256), 256, 0, s>>>(a);
 }
 
 template <int DT>
@@ -653,7 +683,11 @@ static void launch_backward(LinearArgs a, bool direct, hipStream_t s) {
                   [&](const LinearArgs& b) { launch_grad_weight<Product<DT, true, true, true, 256, 32, 8, 4>>(b, s); });
     }
   }
-  if (a.grad_x) k_grad_x_join<DT><<<(unsigned)ceil_div(a.rows * (a.dx_width / 4), 256), 256, 0, s>>>(a);
+  if (a.grad_x) {
+    const int64_t units = a.rows * (a.dx_width / 4);
+    if (a.splits >= 8) k_grad_x_join<DT, 8><<<(unsigned)ceil_div(units, 32), 256, 0, s>>>(a);
+    else k_grad_x_join<DT, 1><<<(unsigned)ceil_div(units, 256), 256, 0, s>>>(a);
+  }
 }
 
 }  // namespace externd
@@ -734,7 +768,7 @@ int externd_linear_logprobs_backward(const void* x, int64_t x_stride, const void
   a.width = width;
   a.targets = targets;
   a.scale = scale;
-  a.step = 256;
+  a.step = small_tiles(dtype, rows, vocab) ? 64 : 256;
   a.lse_in = lse;
   a.entropy_in = entropy;
   a.g_logprob = g_logprob;

@@ -159,6 +159,19 @@ def check_backward(ext, x, w, y, g, ge, dtype, scale=1.0, whole=False, given=Non
     return gx, gw
 
 
+LARGE = [(100, 72, 16500), (100, 73, 16500), (128, 8, 16500), (300, 136, 6700), (300, 71, 6700), (512, 64, 4200)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,width,vocab", LARGE)
+def test_large_tiles(ext, dtype, rows, width, vocab):
+    """More than 1024 tiles of 64 columns and 32 rows: these calls take the large ones, aligned or not."""
+    assert -(-vocab // 64) * -(-rows // 32) > 1024
+    x, w, y = make(rows, width, vocab, dtype, rows, True)
+    check(ext, x, w, y, scale=0.7)
+    check_backward(ext, x, w, y, *gradients(rows, y, 1, "ge"), dtype, scale=0.7)
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("rows,width,vocab", SIZES)
 def test_backward(ext, dtype, rows, width, vocab):
