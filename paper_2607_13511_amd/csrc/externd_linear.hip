@@ -497,12 +497,16 @@ static bool small_tiles(int32_t dtype, int64_t rows, int64_t vocab) {
   return ceil_div(vocab, 256) * ceil_div(rows, tile_rows(dtype, rows)) < CUS && small <= CUS * (rows <= 32 ? 1 : 4);
 }
 
-// Vocabulary of a tile of logits.  One row tile reads weight once, so the card's
-// CUs take equally many tiles of equal length: 65537 rows are 512 tiles of 136
-// and not 256 of 256 and one of 1.
-static int64_t forward_step(int32_t dtype, int64_t rows, int64_t vocab) {
+// Vocabulary of a tile of logits: 64 for small tiles; 128 where tiles of 256 are
+// so few that half as large ones still take one round (452 fp32 rows of 7232, 116
+// tiles or 228: TODO); else 256.  One row tile of the forward call reads weight once,
+// so there the card's CUs take equally many tiles of equal length: 65537 columns
+// are 512 tiles of 136 and not 256 of 256 and one of 1.
+static int64_t tile_step(int32_t dtype, int64_t rows, int64_t vocab, bool back) {
   if (small_tiles(dtype, rows, vocab)) return 64;
-  if (rows > tile_rows(dtype, rows) || vocab <= 256 * CUS / 8) return 256;
+  const int64_t n = tile_rows(dtype, rows);
+  if (n >= 128 && 2 * ceil_div(vocab, 256) * ceil_div(rows, n) <= CUS && (dtype == EXTERND_F32 || n == 256)) return 128;
+  if (back || rows > n || vocab <= 256 * CUS / 8) return 256;
   const int64_t tiles = ceil_div(ceil_div(vocab, 256), CUS) * CUS;
   return ceil_div(ceil_div(vocab, tiles), 8) * 8;
 }
@@ -522,7 +526,7 @@ static size_t cut_bytes(int32_t dtype, int64_t rows, int64_t width, LinearWork* 
 static LinearWork forward_work(int32_t dtype, int64_t rows, int64_t vocab, int64_t width) {
   LinearWork w = {};
   const int64_t r = rows < FORWARD_ROWS ? rows : FORWARD_ROWS;
-  w.step = forward_step(dtype, r, vocab);
+  w.step = tile_step(dtype, r, vocab, false);
   w.tiles = ceil_div(vocab, w.step);
   w.parts = cut_bytes(dtype, r, width, &w);
   w.at_target = w.parts + round256((size_t)(r * w.tiles) * sizeof(Part));
@@ -620,11 +624,13 @@ static void choose_logits(const LinearArgs& a, hipStream_t s) {
   if (a.step == 64) return launch_logits<Product<DT, DIRECT && DT != EXTERND_F32, false, false, 64, 32, 1, DIRECT && DT != EXTERND_F32 ? 3 : 2, 8>, BACK>(a, s);
   if constexpr (DT == EXTERND_F32) {
     if (n == 32) launch_logits<Product<DT, DIRECT, false, false, 256, 32, 8, DIRECT ? 4 : 2>, BACK>(a, s);
+    else if (a.step == 128) launch_logits<Product<DT, false, false, false, 128, 128, 2, 2>, BACK>(a, s);
     else launch_logits<Product<DT, false, false, false, 256, 128, 4, 2>, BACK>(a, s);
   } else {
     typedef Product<DT, DIRECT, false, false, 256, 32, 8, DIRECT ? 4 : 2> Small;
     if (n == 32) launch_logits<Small, BACK>(a, s);
     else if (n == 128 || !DIRECT) launch_logits<Product<DT, DIRECT, false, false, 256, 128, 4, DIRECT ? 3 : 2>, BACK>(a, s);
+    else if (a.step == 128) launch_logits<Product<DT, true, false, false, 128, 256, 2, 3>, BACK>(a, s);
     else if constexpr (DIRECT)
       with_tail(a, ceil_div(a.rows, 256), [&](const LinearArgs& b) { launch_logits<Product<DT, true, false, false, 256, 256, 2, 2>, BACK>(b, s); },
                 [&](const LinearArgs& b) { launch_logits<Small, BACK>(b, s); });
@@ -768,7 +774,7 @@ int externd_linear_logprobs_backward(const void* x, int64_t x_stride, const void
   a.width = width;
   a.targets = targets;
   a.scale = scale;
-  a.step = small_tiles(dtype, rows, vocab) ? 64 : 256;
+  a.step = tile_step(dtype, rows, vocab, true);
   a.lse_in = lse;
   a.entropy_in = entropy;
   a.g_logprob = g_logprob;
