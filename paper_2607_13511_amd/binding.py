@@ -1073,7 +1073,7 @@ def _dense(t) -> bool:
 def clip_gradients(tensors, max_norm: float = float("inf"), out=None, stream=None, workspace=None):
     """The norm over all entries of ``tensors`` (CUDA, dense, float32, bfloat16
     or float16, mixed), and each of them times min(1, max_norm / norm), in place
-    or into ``out`` (as many tensors of the same shapes, strides and types)
+    or into ``out`` (as many tensors of the same sizes and types, and of the same strides where they are not contiguous)
     (externd_clip_gradients).  With max_norm infinite only the norm.  Returns
     the norm, a float32 CUDA scalar; nothing is copied to the host."""
     torch = _torch()
@@ -1092,41 +1092,42 @@ def clip_gradients(tensors, max_norm: float = float("inf"), out=None, stream=Non
     index = device.index
     if _dtype_codes is None:
         _dtype_code(torch, torch.float32, "")
-    # hundreds of tensors are ordinary: one look at each
-    ins, sizes, codes = [], [], []
-    for i, t in enumerate(tensors):
-        code = _dtype_codes.get(t.dtype)
-        if code is None or t.get_device() != index or not (t.is_contiguous() or _dense(t)):
-            raise ValueError(f"tensors[{i}]: expected a dense CUDA tensor of float32, bfloat16 or float16 on {device}, got "
-                             f"{t.dtype} {tuple(t.shape)} {t.stride()} on {t.device}")
-        ins.append(t.data_ptr())
-        sizes.append(t.numel())
-        codes.append(code)
-    if out is None:
-        ops = ins
-    else:
-        ops = []
-        for i, (t, o) in enumerate(zip(tensors, outs)):
-            if not (o.dtype is t.dtype and o.shape == t.shape and o.get_device() == index
-                    and (o.is_contiguous() and t.is_contiguous() or o.stride() == t.stride())):
-                raise ValueError(f"out[{i}]: expected {t.dtype} {tuple(t.shape)} {t.stride()} on {t.device}, got {o.dtype} "
-                                 f"{tuple(o.shape)} {o.stride()} on {o.device}")
-            ops.append(o.data_ptr())
+    # hundreds of tensors are ordinary, so each property is taken of all at once
+    dtypes = [t.dtype for t in tensors]
+    codes = [_dtype_codes.get(d) for d in dtypes]
+    gaps = False in [t.is_contiguous() for t in tensors]
+    if None in codes or any([t.get_device() != index for t in tensors]) or (gaps and not all([_dense(t) for t in tensors])):
+        i = next(i for i, t in enumerate(tensors) if t.dtype not in _dtype_codes or t.get_device() != index or not _dense(t))
+        t = tensors[i]
+        raise ValueError(f"tensors[{i}]: expected a dense CUDA tensor of float32, bfloat16 or float16 on {device}, got "
+                         f"{t.dtype} {tuple(t.shape)} {t.stride()} on {t.device}")
+    ops = ins = [t.data_ptr() for t in tensors]
+    sizes = [t.numel() for t in tensors]
+    if out is not None:
+        if (gaps or False in [o.is_contiguous() for o in outs] or [o.dtype for o in outs] != dtypes
+                or [o.numel() for o in outs] != sizes or any([o.get_device() != index for o in outs])):
+            for i, (t, o) in enumerate(zip(tensors, outs)):
+                if not (o.dtype is t.dtype and o.get_device() == index and o.shape == t.shape
+                        and (o.is_contiguous() and t.is_contiguous() or o.stride() == t.stride())):
+                    raise ValueError(f"out[{i}]: expected {t.dtype} {tuple(t.shape)} {t.stride()} on {t.device}, got {o.dtype} "
+                                     f"{tuple(o.shape)} {o.stride()} on {o.device}")
+        ops = [o.data_ptr() for o in outs]
     if max_norm != float("inf") and tensors:
         # what is written lies in no other tensor (one that is only read may be given twice)
-        a, n = np.array([ops, ins], dtype=np.int64), np.array([sizes, sizes], dtype=np.int64)
-        b = a + n * np.where(np.array(codes) == 0, 4, 2)
-        wrote = np.zeros(a.shape, dtype=bool)
-        wrote[0] = True
-        keep = n > 0
-        keep[1] &= a[0] != a[1]
-        a, b, wrote = a[keep], b[keep], wrote[keep]
-        order = np.lexsort((b, a))
-        a, b, wrote = a[order], b[order], wrote[order]
+        n = np.array(sizes, dtype=np.int64)
+        bytes_ = n * np.where(np.array(codes) == 0, 4, 2)
+        a, keep = np.array(ops, dtype=np.int64), n > 0
+        a, size, wrote = a[keep], bytes_[keep], np.ones(int(keep.sum()), dtype=bool)
+        if out is not None:
+            c = np.array(ins, dtype=np.int64)
+            keep &= c != np.array(ops, dtype=np.int64)
+            a, size = np.concatenate([a, c[keep]]), np.concatenate([size, bytes_[keep]])
+            wrote = np.concatenate([wrote, np.zeros(int(keep.sum()), dtype=bool)])
+        order = np.argsort(a, kind="stable")
+        a, b, wrote = a[order], (a + size)[order], wrote[order]
         # ends so far, of all and of what is written
-        end = np.maximum.accumulate(b)[:-1]
-        end_wrote = np.maximum.accumulate(np.where(wrote, b, 0))[:-1]
-        if np.any((a[1:] < end) & wrote[1:]) or np.any(a[1:] < end_wrote):
+        end, end_wrote = np.maximum.accumulate(b), np.maximum.accumulate(np.where(wrote, b, 0))
+        if np.any((a[1:] < end[:-1]) & wrote[1:]) or np.any(a[1:] < end_wrote[:-1]):
             raise ValueError("tensors: what is written overlaps another tensor")
     n = len(tensors)
     norm = torch.empty((), dtype=torch.float32, device=device)

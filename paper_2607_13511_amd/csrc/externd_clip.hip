@@ -6,7 +6,7 @@
 namespace externd {
 
 constexpr int CLIP_TENSORS = 120;       // of a launch: their descriptions are its arguments, so nothing is copied ahead of it
-constexpr int64_t CLIP_CHUNK = 8192;    // entries of a chunk; a chunk is one tensor's
+constexpr int64_t CLIP_CHUNK = 16384;    // entries of a chunk; a chunk is one tensor's
 constexpr int CLIP_BLOCKS = 2048;       // workgroups of a launch, each with equally many chunks, and as many partial sums
 
 struct ClipList {
@@ -52,16 +52,21 @@ __device__ __forceinline__ int lead_of(const void* p, int n) {
 template <int DT>
 __device__ __forceinline__ void add_squares(const void* p, int n, double* sum) {
   typedef typename Elem<DT>::T T;
-  constexpr int E = Vec<DT>::E;
+  constexpr int E = Vec<DT>::E, U = 8;
   const T* x = (const T*)p;
   const int lead = lead_of<DT>(p, n), nv = (n - lead) / E, tail = n - lead - nv * E;
   const v4u* v = (const v4u*)(x + lead);
-#pragma unroll 4
-  for (int i = threadIdx.x; i < nv; i += 256) {
-    float f[E];
-    Vec<DT>::unpack(v[i], f);
+  for (int i = threadIdx.x; i < nv; i += 256 * U) {
+    v4u x[U];
 #pragma unroll
-    for (int e = 0; e < E; e++) sum[e & 3] = fma((double)f[e], (double)f[e], sum[e & 3]);
+    for (int u = 0; u < U; u++) x[u] = i + u * 256 < nv ? v[i + u * 256] : v4u{0, 0, 0, 0};
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+      float f[E];
+      Vec<DT>::unpack(x[u], f);
+#pragma unroll
+      for (int e = 0; e < E; e++) sum[e & 3] = fma((double)f[e], (double)f[e], sum[e & 3]);
+    }
   }
   const int i = threadIdx.x;
   if (i < lead + tail) {
@@ -110,10 +115,10 @@ __device__ __forceinline__ void scale_entries(const void* p, void* q, int n, flo
 #pragma unroll 4
   for (int i = threadIdx.x; i < nv; i += 256) {
     float f[E];
-    Vec<DT>::unpack(((const v4u*)(x + lead))[i], f);
+    Vec<DT>::unpack(__builtin_nontemporal_load((const v4u*)(x + lead) + i), f);
 #pragma unroll
     for (int e = 0; e < E; e++) f[e] = f[e] * before * factor;
-    ((v4u*)(y + lead))[i] = Vec<DT>::pack(f);
+    __builtin_nontemporal_store(Vec<DT>::pack(f), (v4u*)(y + lead) + i);
   }
   const int i = threadIdx.x;
   if (i < lead + tail) {
