@@ -617,7 +617,8 @@ int externd_embedding_backward(const void* grad, int32_t dtype, int64_t tokens, 
  * parts each, whose products below 2^-24 of the largest are left out).  A logit
  * of -infinity counts as probability 0; a NaN or +infinity makes its row's
  * results NaN, and so do, in fp32, an infinity in x or weight.
- * rows <= 2^22, vocab < 2^31 - 1024, width <= 2^20; strides < 2^22.          */
+ * rows <= 2^22, vocab <= 2^25, width <= 2^20, rows width <= 2^33, vocab width <= 2^37;
+ * strides < 2^22.                                                           */
 size_t externd_linear_logprobs_workspace_bytes(int32_t dtype, int64_t rows, int64_t vocab, int64_t width);  /* 0 on invalid arguments */
 int externd_linear_logprobs(const void* x, int64_t x_stride, const void* weight, int64_t weight_stride, int32_t dtype,
                             int64_t rows, int64_t vocab, int64_t width, const int64_t* targets, float scale,

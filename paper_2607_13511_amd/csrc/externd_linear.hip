@@ -479,8 +479,9 @@ __global__ __launch_bounds__(256) void k_zero_rows(LinearArgs a) {
 static size_t round256(size_t n) { return (n + 255) & ~(size_t)255; }
 static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+// Tiles of a launch, of 512 threads each, and vectors of x are counted in 32 bits.
 static bool linear_sizes(int64_t rows, int64_t vocab, int64_t width) {
-  return rows <= (1 << 22) && vocab < INT32_MAX - 1023 && width <= (1 << 20);
+  return rows <= (1 << 22) && vocab <= (1 << 25) && width <= (1 << 20) && rows * width <= (int64_t)1 << 33 && vocab * width <= (int64_t)1 << 37;
 }
 
 // Rows of a tile; operands that go through registers take 128 at most (256 would not leave enough of them).
@@ -565,7 +566,7 @@ static LinearWork backward_work(int32_t dtype, int64_t rows, int64_t vocab, int6
   w.packed_width = ceil_div(width, vec) * vec;
   w.dx_width = ceil_div(width, 4) * 4;
   int64_t splits = CUS / (cols * row_tiles);
-  const int64_t max_splits = ceil_div(w.G_width, 512);
+  const int64_t max_splits = ceil_div(w.G_width, 128);
   splits = splits < 1 ? 1 : splits > max_splits ? max_splits : splits;
   w.split = ceil_div(ceil_div(w.G_width, splits), 64) * 64;
   w.splits = (int)ceil_div(w.G_width, w.split);
@@ -656,7 +657,7 @@ static void launch_cut(const LinearArgs& a, hipStream_t s) {
 
 template <int DT>
 static void launch_forward(LinearArgs a, bool direct, hipStream_t s) {
-  if (direct) {
+  if (direct && (DT != EXTERND_F32 || a.cut || tile_rows(DT, a.rows) > 32)) {
     launch_cut<DT>(a, s);
     choose_logits<DT, true, false>(a, s);
   } else choose_logits<DT, false, false>(a, s);
@@ -733,7 +734,7 @@ int externd_linear_logprobs(const void* x, int64_t x_stride, const void* weight,
     a.logprob = logprob ? logprob + r : nullptr;
     a.entropy = entropy ? entropy + r : nullptr;
     a.lse = lse ? lse + r : nullptr;
-    a.cut = workspace;
+    a.cut = w.parts ? workspace : nullptr;      // there only if all rows are few, not if those of the last pass are
     a.cut_width = w.cut_width;
     a.parts = (Part*)((char*)workspace + w.parts);
     a.at_target = (float*)((char*)workspace + w.at_target);

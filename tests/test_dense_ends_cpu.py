@@ -59,7 +59,8 @@ def test_linear_refuses_before_device_work():
     for bad in sizes + (dict(lse=None), dict(y=None), dict(h=None), dict(gxs=7), dict(gws=7)):
         assert _linear_backward(**bad) == EINVAL, bad
     for f in (_linear, _linear_backward):
-        for bad in (dict(rows=(1 << 22) + 1), dict(vocab=(1 << 31) - 1024), dict(width=(1 << 20) + 1, xs=1 << 21, ws=1 << 21, **({} if f is _linear else dict(gxs=1 << 21, gws=1 << 21))),
+        for bad in (dict(rows=(1 << 22) + 1), dict(vocab=(1 << 25) + 1), dict(vocab=(1 << 31) - 1024), dict(rows=1 << 22, width=2049, xs=2049, ws=2049, **({} if f is _linear else dict(gxs=2049, gws=2049))),
+                    dict(vocab=1 << 25, width=4097, xs=4097, ws=4097, **({} if f is _linear else dict(gxs=4097, gws=4097))), dict(width=(1 << 20) + 1, xs=1 << 21, ws=1 << 21, **({} if f is _linear else dict(gxs=1 << 21, gws=1 << 21))),
                     dict(xs=1 << 22), dict(ws=1 << 22)):
             assert f(**bad) == EUNSUPPORTED, bad
         assert f(work=None) == EWORKSPACE

@@ -207,6 +207,18 @@ def test_many_rows_and_pieces(ext, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+def test_a_last_pass_of_few_rows(ext, dtype):
+    """8192 rows and three more, whose tiles outnumber the CUs."""
+    x, w, y = make(8195, 64, 70001, dtype, 22, True)
+    y[8192:] = torch.tensor([70000, 5, 300], device="cuda")
+    got = ext.linear_logprobs(x, w, y)
+    last = Bounds(x[8192:], w, 1.0, True)
+    for g, want, tol in ((got.lse, last.lse, last.dl), (got.entropy, last.entropy, last.dh),
+                         (got.logprob, last.z[np.arange(3), [70000, 5, 300]] - last.lse, last.dp)):
+        assert np.all(np.abs(f64(g[8192:]) - want) <= tol)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("offset,gap", [(1, 0), (0, 1), (3, 5), (2, 6), (8, 8), (5, 11)])
 def test_strides(ext, dtype, offset, gap):
     """Rows that begin anywhere, with gaps that hold NaN; outputs between other columns."""
