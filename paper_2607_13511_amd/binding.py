@@ -1070,6 +1070,34 @@ def _dense(t) -> bool:
     return True
 
 
+def _written_twice(ins, ops, nbytes) -> bool:
+    """Whether an output's memory has bytes in common with another output, or with
+    an input that is not its own (inputs may share theirs: they are only read)."""
+    if len(ins) <= 32:
+        spans = [(o, o + n, True) for o, n in zip(ops, nbytes) if n]
+        if ops is not ins:
+            spans += [(i, i + n, False) for i, o, n in zip(ins, ops, nbytes) if n and i != o]
+        spans.sort()
+        end = end_wrote = 0
+        for a, b, wrote in spans:
+            if a < end_wrote or (wrote and a < end):
+                return True
+            end = max(end, b)
+            end_wrote = max(end_wrote, b) if wrote else end_wrote
+        return False
+    a, size = np.array(ops, dtype=np.int64), np.array(nbytes, dtype=np.int64)      # the same without a loop
+    keep, wrote = size > 0, np.ones(len(ops), dtype=bool)
+    if ops is not ins:
+        i = np.array(ins, dtype=np.int64)
+        keep = np.concatenate([keep, keep & (i != a)])
+        a, size, wrote = np.concatenate([a, i]), np.concatenate([size, size]), np.concatenate([wrote, ~wrote])
+    a, size, wrote = a[keep], size[keep], wrote[keep]
+    order = np.argsort(a, kind="stable")
+    a, b, wrote = a[order], (a + size)[order], wrote[order]
+    end, end_wrote = np.maximum.accumulate(b), np.maximum.accumulate(np.where(wrote, b, 0))
+    return bool(np.any((a[1:] < end[:-1]) & wrote[1:]) or np.any(a[1:] < end_wrote[:-1]))
+
+
 def clip_gradients(tensors, max_norm: float = float("inf"), out=None, stream=None, workspace=None):
     """The norm over all entries of ``tensors`` (CUDA, dense, float32, bfloat16
     or float16, mixed), and each of them times min(1, max_norm / norm), in place
@@ -1113,21 +1141,7 @@ def clip_gradients(tensors, max_norm: float = float("inf"), out=None, stream=Non
                                      f"{tuple(o.shape)} {o.stride()} on {o.device}")
         ops = [o.data_ptr() for o in outs]
     if max_norm != float("inf") and tensors:
-        # what is written lies in no other tensor (one that is only read may be given twice)
-        n = np.array(sizes, dtype=np.int64)
-        bytes_ = n * np.where(np.array(codes) == 0, 4, 2)
-        a, keep = np.array(ops, dtype=np.int64), n > 0
-        a, size, wrote = a[keep], bytes_[keep], np.ones(int(keep.sum()), dtype=bool)
-        if out is not None:
-            c = np.array(ins, dtype=np.int64)
-            keep &= c != np.array(ops, dtype=np.int64)
-            a, size = np.concatenate([a, c[keep]]), np.concatenate([size, bytes_[keep]])
-            wrote = np.concatenate([wrote, np.zeros(int(keep.sum()), dtype=bool)])
-        order = np.argsort(a, kind="stable")
-        a, b, wrote = a[order], (a + size)[order], wrote[order]
-        # ends so far, of all and of what is written
-        end, end_wrote = np.maximum.accumulate(b), np.maximum.accumulate(np.where(wrote, b, 0))
-        if np.any((a[1:] < end[:-1]) & wrote[1:]) or np.any(a[1:] < end_wrote[:-1]):
+        if _written_twice(ins, ops, [n * (4 if c == 0 else 2) for n, c in zip(sizes, codes)]):
             raise ValueError("tensors: what is written overlaps another tensor")
     n = len(tensors)
     norm = torch.empty((), dtype=torch.float32, device=device)

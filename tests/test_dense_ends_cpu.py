@@ -139,6 +139,21 @@ def test_oracle_clip():
     assert ref.clip([[3.0, 4.0]], 9.0)[1][0].tolist() == [3.0, 4.0] and ref.clip([[0.0]], 0.0)[1][0].tolist() == [0.0]
 
 
+@pytest.mark.parametrize("many", [0, 100])
+def test_what_is_written_twice(many):
+    """Few spans and many, which are looked at differently; the others lie far behind."""
+    def f(*spans):
+        """(input, output, bytes) of each tensor."""
+        spans = list(spans) + [(10000 + 10 * i,) * 2 + (10,) for i in range(many)]
+        ins, ops, n = (list(c) for c in zip(*spans))
+        return binding._written_twice(ins, ins if ins == ops else ops, n)
+    assert not f((0, 0, 10), (10, 10, 10)) and not f((20, 20, 4), (0, 0, 20)) and not f((0, 0, 10), (0, 0, 0))
+    assert f((0, 0, 10), (9, 9, 10)) and f((0, 0, 10), (0, 0, 10)) and f((0, 0, 100), (50, 50, 1))
+    assert not f((0, 100, 10), (0, 200, 10))            # an input given twice, two outputs
+    assert f((0, 100, 10), (0, 105, 10)) and f((0, 100, 10), (100, 200, 10)) and f((0, 5, 10))
+    assert f((0, 500, 300), (900, 290, 10)) and not f((0, 500, 300), (900, 300, 10)) and f((0, 500, 300), (600, 300, 10))
+
+
 @pytest.mark.parametrize("name", ["embedding", "embedding_backward", "linear_logprobs", "linear_logprobs_backward", "clip_gradients"])
 def test_needs_a_gpu(name):
     """There is no fallback on the CPU."""
