@@ -388,6 +388,7 @@ struct Product {
       for (int j = 0; j < TN; j++)
 #pragma unroll
         for (int r = 0; r < 16; r++) acc[i][j][r] = 0.f;
+    if (K <= 0) return;      // before any load: row k0 need not exist
     const int64_t steps = (K + BK - 1) / BK;
     if constexpr (DIRECT) {
       Direct<ACOL, BM, BK, EV> la;

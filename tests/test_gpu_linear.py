@@ -207,6 +207,14 @@ def test_many_rows_and_pieces(ext, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,width,vocab", [(70, 256, 1000), (40, 900, 1300), (452, 1002, 1030), (7, 300, 257), (3, 40, 129)])
+def test_splits_behind_the_end(ext, dtype, rows, width, vocab):
+    """The last of the splits of grad_x's sum have nothing to add (and weight ends where its memory does)."""
+    x, w, y = make(rows, width, vocab, dtype, 23, True)
+    check_backward(ext, x, w, y, *gradients(rows, y, 24, "ge"), dtype, whole=True)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 def test_a_last_pass_of_few_rows(ext, dtype):
     """8192 rows and three more, whose tiles outnumber the CUs."""
     x, w, y = make(8195, 64, 70001, dtype, 22, True)
