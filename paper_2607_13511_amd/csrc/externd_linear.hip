@@ -14,10 +14,10 @@ struct Part {
   float top, sum, mean, none;      // largest z, sum of e = exp(z - top), sum of e (z - top)
 };
 
-// What a row's gradient is made of: with l = log2 p, G = p (a l + b) and, at the
-// target, g more.  All times `up`, a power of two that brings fp16's G below 2^15.
+// What a row's gradient is made of: with l = log2 p (ln p for fp32), G = p (a l + b)
+// and, at the target, g more.  All times `up`, a power of two that brings fp16's G below 2^15.
 struct RowInfo {
-  float a, b, g, lse2, up;         // lse2 = lse log2 e; infinite where all p are 0
+  float a, b, g, lse, up;          // lse in the units of l; infinite where all p are 0
   int32_t y;                       // -1: no target
   int32_t present, none;
 };
@@ -103,6 +103,14 @@ struct Gathered {
   }
 };
 
+// e^x for x >= -200 with what the product x log2 e loses: p is within 2 u of itself and
+// not within u |x|, which bounded fp32's gradients (517 rows of 8191: TODO).
+__device__ __forceinline__ float exp_whole(float x) {
+  const float y = x * LOG2E, rest = fmaf(x, 1.92596299112661746887e-8f, fmaf(x, LOG2E, -y));
+  const float p = __builtin_amdgcn_exp2f(y);
+  return fmaf(p * rest, LN2, p);
+}
+
 // Logits of a tile: rows of weight along m, rows of x along n, so that a lane
 // holds one row's logits and its softmax needs no other lane but at the end.
 // BACK: G of the tile; else its part of each row's softmax.
@@ -145,8 +153,8 @@ __global__ __launch_bounds__(GEMM_THREADS, 2) void k_logits(LinearArgs a) {
 #pragma unroll
         for (int r = 0; r < 16; r++) {
           // p below 2^-200 is 0; the maximum passes a NaN on
-          const float l = propagating_max(fmaf(acc[i][j][r], c, -w.lse2), -200.f);
-          acc[i][j][r] = __builtin_amdgcn_exp2f(l) * fmaf(w.a, l, w.b);
+          const float l = propagating_max(fmaf(acc[i][j][r], DT == EXTERND_F32 ? a.scale : c, -w.lse), -200.f);
+          acc[i][j][r] = (DT == EXTERND_F32 ? exp_whole(l) : __builtin_amdgcn_exp2f(l)) * fmaf(w.a, l, w.b);
         }
       const int64_t y = w.y < 0 ? -1 : w.y - m0;
       if (__any(y >= P::row(0, 0) && y < P::row(0, 0) + TM * 32)) {      // a target among this wave's
@@ -275,7 +283,7 @@ __global__ __launch_bounds__(256) void k_logits_join(LinearArgs a) {
 
 // What each row's gradient is made of.  For fp16 one workgroup goes over all
 // rows, as the least `up` scales what the rows' sum is made of.
-__global__ __launch_bounds__(1024) void k_rows(LinearArgs a, int fp16) {
+__global__ __launch_bounds__(1024) void k_rows(LinearArgs a, int fp16, int fp32) {
   __shared__ float least[16];
   float up_all = 0x1p120f;
   for (int64_t r = (int64_t)blockIdx.x * 1024 + threadIdx.x; r < a.rows; r += (int64_t)gridDim.x * 1024) {
@@ -286,7 +294,7 @@ __global__ __launch_bounds__(1024) void k_rows(LinearArgs a, int fp16) {
     const float g = a.g_logprob && asked ? a.g_logprob[r] : 0.f, ge = a.g_entropy ? a.g_entropy[r] : 0.f;
     const float h = ge == 0.f ? 0.f : a.entropy_in[r], lse = a.lse_in[r];
     w.present = g != 0.f || ge != 0.f;
-    w.lse2 = !w.present || lse == -INFINITY ? INFINITY : lse * LOG2E;
+    w.lse = !w.present || lse == -INFINITY ? INFINITY : fp32 ? lse : lse * LOG2E;
     w.up = 1.f;
     if (fp16 && w.present) {
       // |G| <= |g| + |ge| (p |ln p| + p H) < |g| + |ge| (1 + H)
@@ -297,7 +305,7 @@ __global__ __launch_bounds__(1024) void k_rows(LinearArgs a, int fp16) {
     }
     // -p (g + ge (ln p + H))
     w.g = g * w.up;
-    w.a = -ge * w.up * LN2;
+    w.a = -ge * w.up * (fp32 ? 1.f : LN2);
     w.b = -fmaf(ge, h, g) * w.up;
     a.info[r] = w;
   }
@@ -670,7 +678,7 @@ static void launch_backward(LinearArgs a, bool direct, hipStream_t s) {
     k_zero_rows<DT><<<(unsigned)(a.vocab < 4096 ? a.vocab : 4096), 256, 0, s>>>(a);
     return;
   }
-  k_rows<<<DT == EXTERND_F16 ? 1 : (unsigned)ceil_div(a.rows, 1024), 1024, 0, s>>>(a, DT == EXTERND_F16);
+  k_rows<<<DT == EXTERND_F16 ? 1 : (unsigned)ceil_div(a.rows, 1024), 1024, 0, s>>>(a, DT == EXTERND_F16, DT == EXTERND_F32);
   if (direct) launch_cut<DT>(a, s);
   if (a.grad_weight) k_pack<DT><<<(unsigned)ceil_div(a.rows * (a.packed_width / Vec<DT>::E), 256), 256, 0, s>>>(a);
   for (a.p0 = 0; a.p0 < a.vocab; a.p0 = a.p1) {
