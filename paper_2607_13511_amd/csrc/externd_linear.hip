@@ -41,6 +41,11 @@ struct LinearArgs {
   // backward
   const float *lse_in, *entropy_in, *g_logprob, *g_entropy;
   RowInfo* info;
+  // The target's entry is a row's one large one, and its rounding in a 16-bit G would
+  // be in all of the row's grad_x, and of the target's grad_weight, alike: what it has
+  // lost is added to both.
+  int32_t* target;                 // of a row that takes part, or -1
+  float* rest;
   float* up_all;                   // the least `up` of the rows that take part
   void *grad_x, *grad_weight;
   int64_t grad_x_stride, grad_weight_stride, p0, p1;      // this piece of the vocabulary, G's columns
@@ -114,6 +119,12 @@ __device__ __forceinline__ float exp_whole(float x) {
 // Logits of a tile: rows of weight along m, rows of x along n, so that a lane
 // holds one row's logits and its softmax needs no other lane but at the end.
 // BACK: G of the tile; else its part of each row's softmax.
+__device__ __forceinline__ float finite(float x) { return __builtin_isfinite(x) ? x : 0.f; }
+
+// What x loses when it is stored.
+template <int DT>
+__device__ __forceinline__ float lost(float x) { return finite(x - Elem<DT>::load(Elem<DT>::store(x))); }
+
 template <typename P, bool BACK>
 __global__ __launch_bounds__(GEMM_THREADS, 2) void k_logits(LinearArgs a) {
   constexpr int DT = P::DT, TM = P::TM, TN = P::TN;
@@ -162,7 +173,10 @@ __global__ __launch_bounds__(GEMM_THREADS, 2) void k_logits(LinearArgs a) {
         for (int i = 0; i < TM; i++)
 #pragma unroll
           for (int r = 0; r < 16; r++)
-            if (P::row(i, r) == y && y < ms) acc[i][j][r] += w.g;
+            if (P::row(i, r) == y && y < ms) {
+              acc[i][j][r] += w.g;
+              if constexpr (DT != EXTERND_F32) a.rest[n] = lost<DT>(acc[i][j][r]);
+            }
       }
 #pragma unroll
       for (int i = 0; i < TM; i++)
@@ -308,6 +322,8 @@ __global__ __launch_bounds__(1024) void k_rows(LinearArgs a, int fp16, int fp32)
     w.a = -ge * w.up * (fp32 ? 1.f : LN2);
     w.b = -fmaf(ge, h, g) * w.up;
     a.info[r] = w;
+    a.target[r] = w.present ? w.y : -1;
+    a.rest[r] = 0.f;
   }
   if (!fp16) {
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.up_all = 1.f;
@@ -428,11 +444,74 @@ __global__ __launch_bounds__(256) void k_grad_x_join(LinearArgs a) {
     }
   }
   if (!in) return;
+  if (DT != EXTERND_F32 && a.target[r] >= 0) {
+    const float rest = a.rest[r];
+    const T* y = (const T*)a.weight.p + a.target[r] * a.weight.stride + c;
+#pragma unroll
+    for (int e = 0; e < 4; e++)
+      if (c + e < a.width) x[e] += finite(rest * Elem<DT>::load(y[e]));
+  }
   const float f = a.scale, down = 1.f / w.up;
   T* const to = (T*)a.grad_x + r * a.grad_x_stride + c;
 #pragma unroll
   for (int e = 0; e < 4; e++)
     if (c + e < a.width) to[e] = Elem<DT>::store(x[e] * f * down);
+}
+
+// Adds what the targets' entries of G have lost, for the rows whose target is one of
+// this tile's columns: steps of up to 64 such rows, of their rows of x and of a tile
+// with one entry for each.  All threads, none of which reads `lds` before.
+template <typename P>
+__device__ __forceinline__ void add_rests(const LinearArgs& a, f32x16 (*acc)[P::TN], int64_t m0, int64_t n0, char* lds) {
+  typedef typename Elem<P::DT>::T T;
+  constexpr int WAVES = GEMM_THREADS / 64, U = 4, ROWS = U * GEMM_THREADS;
+  static_assert(P::BK == 64 && P::STAGES >= 2 && P::STAGE >= 4 * (ROWS + U * WAVES), "the list is in the second stage");
+  int* const list = (int*)(lds + P::STAGE);
+  int* const counts = list + ROWS;
+  char* const b = lds + P::TA::BYTES;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t first = a.v0 + n0;
+  const int last = (int)min((int64_t)P::BN, a.v1 - first);
+  for (int64_t r0 = 0; r0 < a.rows; r0 += ROWS) {
+    uint64_t mine[U];
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+      const int64_t r = r0 + u * GEMM_THREADS + threadIdx.x;
+      const int64_t c = (r < a.rows ? a.target[r] : -1) - first;
+      mine[u] = __ballot(c >= 0 && c < last);
+      if (lane == 0) counts[u * WAVES + wave] = __popcll(mine[u]);
+    }
+    __syncthreads();
+    int have = 0;
+#pragma unroll
+    for (int u = 0; u < U; u++)
+      for (int w = 0; w < WAVES; w++) {
+        if (w == wave && (mine[u] >> lane & 1)) list[have + __popcll(mine[u] & ((1ull << lane) - 1))] = (int)(r0 + u * GEMM_THREADS + threadIdx.x);
+        have += counts[u * WAVES + w];
+      }
+    __syncthreads();
+    for (int from = 0; from < have; from += 64) {
+      const int n = min(64, have - from);
+#pragma unroll 1
+      for (int i = threadIdx.x; i < P::TA::VECTORS; i += GEMM_THREADS) {
+        int k, v;
+        P::TA::place(i, &k, &v);
+        v4u x = {0, 0, 0, 0};
+        if (k < n && m0 + v * 8 < a.packed_width) x = *(const v4u*)((const T*)a.packed + list[from + k] * a.packed_width + m0 + v * 8);
+        *(v4u*)(lds + i * 16) = x;
+      }
+#pragma unroll 1
+      for (int i = threadIdx.x; i < P::TB::VECTORS; i += GEMM_THREADS) *(v4u*)(b + i * 16) = v4u{0, 0, 0, 0};
+      __syncthreads();
+      if ((int)threadIdx.x < n) {
+        const int k = threadIdx.x, r = list[from + k], c = (int)(a.target[r] - first);
+        *(T*)(b + (k * P::TB::CH + ((c >> 4 ^ P::TB::spread(k)) << 1 | (c >> 3 & 1))) * 16 + (c & 7) * 2) = Elem<P::DT>::store(a.rest[r]);
+      }
+      __syncthreads();
+      P::step((const lds_char*)lds, acc);
+      __syncthreads();
+    }
+  }
 }
 
 // G^T x of this piece: columns of x along m, of G (the vocabulary) along n.
@@ -446,6 +525,7 @@ __global__ __launch_bounds__(GEMM_THREADS, 2) void k_grad_weight(LinearArgs a) {
   f32x16 acc[P::TM][P::TN];
   const Operand x = {a.packed, a.packed_width}, G = {(T*)a.G + (a.v0 - a.p0), a.G_width};
   P::run(x, m0, a.packed_width - m0, G, n0, (ns - n0 + 7) & ~(int64_t)7, 0, a.rows, (lds_char*)lds, acc);      // whole vectors: G's rows have room
+  if constexpr (P::DT != EXTERND_F32) add_rests<P>(a, acc, m0, n0, lds);
   const float f = a.scale, down = 1.f / *a.up_all;
 #pragma unroll
   for (int j = 0; j < P::TN; j++)
@@ -521,7 +601,7 @@ static int64_t tile_step(int32_t dtype, int64_t rows, int64_t vocab, bool back) 
 }
 
 struct LinearWork {
-  size_t cut, parts, at_target, info, up_all, packed, G, dx, bytes;
+  size_t cut, parts, at_target, info, target, rest, up_all, packed, G, dx, bytes;
   int64_t tiles, step, piece, G_width, packed_width, dx_width, cut_width, split;
   int splits;
 };
@@ -580,6 +660,8 @@ static LinearWork backward_work(int32_t dtype, int64_t rows, int64_t vocab, int6
   w.splits = (int)ceil_div(w.G_width, w.split);
   size_t at = cut_bytes(dtype, rows, width, &w);
   w.info = at, at += round256((size_t)rows * sizeof(RowInfo));
+  w.target = at, at += round256((size_t)rows * 4);
+  w.rest = at, at += round256((size_t)rows * 4);
   w.up_all = at, at += 256;
   w.packed = at, at += need_weight ? round256((size_t)(rows * w.packed_width) * dtype_bytes(dtype)) : 0;
   w.G = at, at += round256((size_t)(rows * w.G_width) * dtype_bytes(dtype));
@@ -796,6 +878,8 @@ int externd_linear_logprobs_backward(const void* x, int64_t x_stride, const void
   a.cut = at;
   a.cut_width = w.cut_width;
   a.info = (RowInfo*)(at + w.info);
+  a.target = (int32_t*)(at + w.target);
+  a.rest = (float*)(at + w.rest);
   a.up_all = (float*)(at + w.up_all);
   a.packed = at + w.packed;
   a.G = at + w.G;

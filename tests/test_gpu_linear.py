@@ -226,6 +226,43 @@ def test_a_last_pass_of_few_rows(ext, dtype):
         assert np.all(np.abs(f64(g[8192:]) - want) <= tol)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("rows,width,vocab", [(3, 24, 1000), (40, 72, 8192), (200, 300, 8200), (2500, 1031, 8200)])
+@pytest.mark.parametrize("one", [False, True])
+def test_the_targets_entry_is_not_rounded(ext, dtype, rows, width, vocab, one):
+    """Of G's entries g (1 at the target - p) with p = 1 / vocab, all logits being 0.
+    A 16-bit G rounds the target's to e of itself, and its rest, which is added,
+    to e of that: e e of the target's share is left, and e of the others' (p's
+    rounding; none in grad_x, whose weights cancel in pairs), of the scale and
+    its kind 8 u, of m terms (m + 64) u; and the result is rounded once."""
+    t, e = TYPES[dtype]
+    rng = np.random.default_rng(rows)
+    y = np.full(rows, vocab - 3) if one else rng.integers(0, vocab, rows)
+    y[::7] = vocab - 1
+    g, scale = rng.uniform(1, 2, rows).astype(np.float32), 1.37
+    lse, H = torch.full((rows,), math.log(vocab), device="cuda"), torch.full((rows,), math.log(vocab), device="cuda")
+    where = torch.from_numpy(y).cuda(), lse, H, torch.from_numpy(g).cuda()
+    g = g.astype(np.float64)
+
+    half = torch.from_numpy(rng.uniform(1, 2, (vocab // 2, width))).to(t).cuda()
+    w = torch.stack((half, -half), 1).reshape(vocab, width)
+    x = torch.zeros((rows, width), dtype=t, device="cuda")
+    gx, _ = ext.linear_logprobs_backward(x, w, *where, scale=scale, need_weight=False)
+    share = scale * g[:, None] * f64(w)[y]
+    terms = scale * g[:, None] / vocab * np.abs(f64(w)).sum(0)
+    off = np.abs(f64(gx) - share)
+    assert (off <= e * np.abs(share) + (e * e + 8 * U + 64 * U) * np.abs(share) * 1.01 + (vocab + 72) * U * terms).all()
+
+    x = torch.from_numpy(rng.uniform(1, 2, (rows, width))).to(t).cuda()
+    _, gw = ext.linear_logprobs_backward(x, torch.zeros_like(w), *where, scale=scale, need_x=False)
+    first = np.zeros((vocab, width))
+    np.add.at(first, y, scale * g[:, None] * f64(x))
+    second = scale / vocab * (g[:, None] * f64(x)).sum(0)
+    want, parts = first - second, first + second
+    bound = e * np.abs(want) + (e * second + e * e * parts) * 1.01 + (rows + 72 + 8 * math.log(vocab)) * U * parts
+    assert (np.abs(f64(gw) - want) <= bound).all()
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("offset,gap", [(1, 0), (0, 1), (3, 5), (2, 6), (8, 8), (5, 11)])
 def test_strides(ext, dtype, offset, gap):
