@@ -591,7 +591,7 @@ int externd_embedding(const void* table, int32_t dtype, int64_t vocab, int64_t w
 
 /* Gradient of the above for the table:
  *   grad_table[v] = scale sum over the tokens t with ids[t] = v of grad[t],
- * summed in fp32 in the tokens' order and rounded once; ids outside [0, vocab)
+ * summed in fp32 in an order that only ids and tokens decide and rounded once; ids outside [0, vocab)
  * add nothing, whatever grad holds there.  accumulate = 1: the sum is added
  * to what grad_table holds (the head's gradient, where the head is the
  * embedding), and rows without tokens are left as they are; 0: they become 0.
@@ -639,7 +639,8 @@ int externd_linear_logprobs(const void* x, int64_t x_stride, const void* weight,
  *  workspace  device, >= externd_linear_logprobs_backward_workspace_bytes() with
  *             need_x, need_weight = whether the outputs are given; 256-byte aligned.
  * Sums are fp32; G enters its products in dtype (rounded to bf16, or to fp16
- * below 2^15 with a power of two for each row; fp32 as three bf16 parts).    */
+ * below 2^15 with a power of two for each row, the target's entry with what it
+ * loses; fp32 as three bf16 parts).                                          */
 size_t externd_linear_logprobs_backward_workspace_bytes(int32_t dtype, int64_t rows, int64_t vocab, int64_t width,
                                                         int32_t need_x, int32_t need_weight);  /* 0 on invalid arguments */
 int externd_linear_logprobs_backward(const void* x, int64_t x_stride, const void* weight, int64_t weight_stride,

@@ -868,7 +868,7 @@ def _overlaps(a, b) -> bool:
     wa, wb = a.shape[1] * size, b.shape[1] * size
     if a0 >= b0 + (b.shape[0] - 1) * sb + wb or b0 >= a0 + (a.shape[0] - 1) * sa + wa:
         return False
-    return not (sa == sb and (b0 - a0) % sa >= wa and (b0 - a0) % sa + wb <= sa)      # columns side by side in one buffer
+    return not (sa == sb > 0 and (b0 - a0) % sa >= wa and (b0 - a0) % sa + wb <= sa)      # columns side by side in one buffer
 
 
 def _elsewhere(torch, t, stream):
@@ -1101,8 +1101,8 @@ def _written_twice(ins, ops, nbytes) -> bool:
 def clip_gradients(tensors, max_norm: float = float("inf"), out=None, stream=None, workspace=None):
     """The norm over all entries of ``tensors`` (CUDA, dense, float32, bfloat16
     or float16, mixed), and each of them times min(1, max_norm / norm), in place
-    or into ``out`` (as many tensors of the same sizes and types, and of the same strides where they are not contiguous)
-    (externd_clip_gradients).  With max_norm infinite only the norm.  Returns
+    or into ``out`` (as many tensors of the same sizes and types, and of the same
+    strides where they are not contiguous) (externd_clip_gradients).  With max_norm infinite only the norm.  Returns
     the norm, a float32 CUDA scalar; nothing is copied to the host."""
     torch = _torch()
     tensors = list(tensors)
@@ -1118,6 +1118,8 @@ def clip_gradients(tensors, max_norm: float = float("inf"), out=None, stream=Non
         raise ExterndError(EINVAL, "externd_clip_gradients")
     device = tensors[0].device if tensors else torch.device("cuda", torch.cuda.current_device())
     index = device.index
+    if workspace is not None and workspace.device != device:
+        raise ValueError(f"workspace: expected on {device}, got {workspace.device}")
     if _dtype_codes is None:
         _dtype_code(torch, torch.float32, "")
     # hundreds of tensors are ordinary, so each property is taken of all at once

@@ -110,7 +110,8 @@ __device__ __forceinline__ void cut(const v4u* x, v4u* part) {
 
 // The six products of two operands' parts that are not below 2^-24.  The smaller
 // five are summed by themselves first: c would round each of them at its own size
-// (8 rows of 65537, error of lse 7e-8 to 2.4e-7 of itself for TODO).
+// (8 rows of 65537: the error of lse is 1.2e-8 to 1.0e-7 of itself, and 7e-8 to
+// 2.4e-7 with all six summed into c; 5 % of the time).
 __device__ __forceinline__ f32x16 mfma_cut(const v4u* a, const v4u* b, f32x16 c) {
   f32x16 small = {};
   small = mfma<EXTERND_BF16>(a[1], b[1], small);
