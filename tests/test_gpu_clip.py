@@ -152,3 +152,15 @@ def test_refusals(ext):
         with pytest.raises(ext.ExterndError):
             call()
     assert ext.clip_gradients([t, t]).item() == pytest.approx(math.sqrt(20), rel=2 * U)      # only read: twice is twice
+
+
+def test_a_workspace_of_another_device(ext):
+    class Elsewhere:
+        device, is_cuda = torch.device("cuda", 1), True
+        data_ptr, numel, element_size = (lambda s: 256), (lambda s: 1 << 20), (lambda s: 1)
+
+        def is_contiguous(self):
+            return True
+
+    with pytest.raises(ValueError):
+        ext.clip_gradients([torch.ones(10, device="cuda:0")], workspace=Elsewhere())

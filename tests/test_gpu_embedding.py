@@ -199,3 +199,14 @@ def test_refusals(ext):
                  lambda: ext.embedding_backward(g, ids, 4, workspace=torch.empty(16, device="cuda"))):
         with pytest.raises(ext.ExterndError):
             call()
+
+
+def test_rows_that_are_one(ext):
+    """Expanded rows (a stride of 0) are refused, as table and as output, also where they overlap."""
+    one, ids = torch.ones((1, 8), device="cuda"), torch.zeros((3,), dtype=torch.int64, device="cuda")
+    with pytest.raises(ValueError):
+        ext.embedding(one.expand(4, 8), ids, out=one.expand(3, 8))
+    for call in (lambda: ext.embedding(one.expand(4, 8), ids), lambda: ext.embedding(one, ids, out=torch.ones((1, 8), device="cuda").expand(3, 8)),
+                 lambda: ext.embedding_backward(one.expand(3, 8), ids, 4)):
+        with pytest.raises(ext.ExterndError):
+            call()
