@@ -111,7 +111,8 @@ __device__ __forceinline__ void cut(const v4u* x, v4u* part) {
 // The six products of two operands' parts that are not below 2^-24.  The smaller
 // five are summed by themselves first: c would round each of them at its own size
 // (8 rows of 65537: the error of lse is 1.2e-8 to 1.0e-7 of itself, and 7e-8 to
-// 2.4e-7 with all six summed into c; 5 % of the time).
+// 2.4e-7 with all six summed into c; 5 % of the time).  Few rows hold the smaller
+// ones' sum over all of K beside c (2.5e-8 to 7.5e-8); many have no registers for it.
 __device__ __forceinline__ f32x16 mfma_cut(const v4u* a, const v4u* b, f32x16 c) {
   f32x16 small = {};
   small = mfma<EXTERND_BF16>(a[1], b[1], small);
@@ -128,12 +129,14 @@ __device__ __forceinline__ f32x16 mfma_cut(const v4u* a, const v4u* b, f32x16 c)
 // Loads of operands whose rows begin at multiples of 16 bytes and are whole
 // vectors, straight into LDS.  (Part of a vector would come as zeros where the operand
 // ends.  K is rounded up to whole vectors by rows: zeros in memory.)  The buffer's base moves on with the
-// steps, and what lies past its end, or is no vector of the tile, becomes zeros.
-template <bool COL, int X, int BK, int EV = 8>
+// steps, and what lies past its end becomes zeros.  HELD: rows that are loaded at all.
+template <bool COL, int X, int BK, int EV = 8, int HELD = X>
 struct Direct {
   typedef Tile<COL, X, BK, EV> T;
   static constexpr int B = 16 / EV;                           // bytes of an entry
-  static constexpr int LOADS = T::LOADS ? T::LOADS : 1;      // of a wave, whether or not all of it has one
+  static constexpr int VECTORS = COL ? T::VECTORS : HELD * T::CH;
+  static constexpr int LOADS = (VECTORS + GEMM_THREADS - 1) / GEMM_THREADS;      // of a wave, or one less
+  static_assert(VECTORS % 64 == 0, "a wave has all of a load or none");
   static constexpr unsigned NONE = 0xFFFFFFFFu;
   const char* base;
   int64_t left, k_left;      // bytes from the base to the operand's end; k's from the next step on
@@ -153,25 +156,28 @@ struct Direct {
     for (int i = 0; i < LOADS; i++) {
       int r, v;
       T::place(i * GEMM_THREADS + (int)threadIdx.x, &r, &v);
-      const bool in = i * GEMM_THREADS + (int)threadIdx.x < T::VECTORS && (COL ? v * 16 < width : r < rows);
+      const bool in = i * GEMM_THREADS + (int)threadIdx.x < VECTORS && (COL ? v * 16 < width : r < rows);
       offset[i] = in ? (unsigned)(r * row + v * 16) : NONE;
     }
   }
+  static __device__ __forceinline__ bool has(int i) {      // whether this wave has a load i
+    return (i + 1) * GEMM_THREADS <= VECTORS || i * GEMM_THREADS + (int)(threadIdx.x & ~63u) < VECTORS;
+  }
   // The vectors of the next step, to the tile at `lds`.
   __device__ __forceinline__ void issue(lds_char* lds) {
-    if (T::LOADS == 0 && (int)(threadIdx.x & ~63u) >= T::VECTORS) return;
     const unsigned to = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)lds + (threadIdx.x >> 6) * 1024);
     const i32x4 resource = {__builtin_amdgcn_readfirstlane((int)(uintptr_t)base), __builtin_amdgcn_readfirstlane((int)((uintptr_t)base >> 32)),
                             __builtin_amdgcn_readfirstlane((int)(unsigned)min(max(left, (int64_t)0), (int64_t)0xFFFFFFF0)), 0x00020000};
     if (COL || k_left >= BK) {
 #pragma unroll
-      for (int i = 0; i < LOADS; i++) load(to + i * (GEMM_THREADS * 16), offset[i], resource);
+      for (int i = 0; i < LOADS; i++)
+        if (has(i)) load(to + i * (GEMM_THREADS * 16), offset[i], resource);
     } else {                 // by rows, the last step: the next row's entries are none of this one's
 #pragma unroll
       for (int i = 0; i < LOADS; i++) {
         int r, v;
         T::place(i * GEMM_THREADS + (int)threadIdx.x, &r, &v);
-        load(to + i * (GEMM_THREADS * 16), v * EV < k_left ? offset[i] : NONE, resource);
+        if (has(i)) load(to + i * (GEMM_THREADS * 16), v * EV < k_left ? offset[i] : NONE, resource);
       }
     }
     base += step;
@@ -332,9 +338,10 @@ struct Staged {
 // the tile, and KW over the k of a step (for small tiles, which need many k in
 // flight to keep a CU busy): those are summed at the end, and the first WM x WN
 // waves hold the result.
-template <int DT_, bool DIRECT_, bool ACOL_, bool BCOL_, int BM_, int BN_, int WM_, int STAGES_, int KW_ = 1>
+// HELD: rows of A that there are at most, where their room in LDS is for more stages.
+template <int DT_, bool DIRECT_, bool ACOL_, bool BCOL_, int BM_, int BN_, int WM_, int STAGES_, int KW_ = 1, int HELD_ = BM_>
 struct Product {
-  static constexpr int DT = DT_, BM = BM_, BN = BN_, WM = WM_, KW = KW_, WN = 8 / WM_ / KW_, STAGES = STAGES_;
+  static constexpr int DT = DT_, BM = BM_, BN = BN_, WM = WM_, KW = KW_, WN = 8 / WM_ / KW_, STAGES = STAGES_, HELD = HELD_;
   static constexpr bool DIRECT = DIRECT_, ACOL = ACOL_, BCOL = BCOL_;
   // fp32 by rows: A's entries in LDS, cut as they are read; B comes as its three
   // parts, cut ahead, each BN rows of bf16 behind the other.
@@ -346,7 +353,8 @@ struct Product {
   typedef Tile<BCOL, BROWS, BK, 8> TB;
   // steps in registers ahead, where loads go through them: small tiles wait for memory
   static constexpr int DEPTH = BN > 32 ? 1 : DT == EXTERND_F32 || KW > 1 ? 2 : 4;
-  static constexpr int STAGE = (TA::BYTES + TB::BYTES) * PLANES, LOOP_LDS = STAGE * STAGES, JOIN_LDS = KW > 1 ? KW * BM * BN * 4 : 0;
+  static constexpr int A_BYTES = TA::BYTES / BM * HELD;
+  static constexpr int STAGE = (A_BYTES + TB::BYTES) * PLANES, LOOP_LDS = STAGE * STAGES, JOIN_LDS = KW > 1 ? KW * BM * BN * 4 : 0;
   static constexpr int LDS = LOOP_LDS > JOIN_LDS ? LOOP_LDS : JOIN_LDS;
   static_assert(LDS <= 160 * 1024 && TM >= 1 && TN >= 1 && !(RAW && (ACOL || BCOL || TM > 1 || TN > 1)), "fits");
 
@@ -398,54 +406,54 @@ struct Product {
     if (K <= 0) return;      // before any load: row k0 need not exist
     const int64_t steps = (K + BK - 1) / BK;
     if constexpr (DIRECT) {
-      Direct<ACOL, BM, BK, EV> la;
-      Direct<BCOL, BROWS, BK, 8> lb;
+      typedef Direct<ACOL, BM, BK, EV, HELD> DA;
+      typedef Direct<BCOL, BROWS, BK, 8> DB;
+      static_assert(HELD == BM || !ACOL, "rows of A");
+      DA la;
+      DB lb;
       la.init(A, m0, m_count, k0, K);
       lb.init(B, n0, n_count, k0 + b_k, K);
-      static_assert(TA::LOADS > 0, "every wave loads of A");
-      constexpr int EACH = Direct<ACOL, BM, BK, EV>::LOADS + Direct<BCOL, BROWS, BK, 8>::LOADS;
-      const bool fewer = TB::LOADS == 0 && (int)(threadIdx.x & ~63u) >= TB::VECTORS;      // this wave loads of A only
+      const int absent = !DA::has(DA::LOADS - 1) + !DB::has(DB::LOADS - 1);      // of a step's loads, in this wave
       auto issue = [&](int stage) {
         la.issue(lds + stage * STAGE);
-        lb.issue(lds + stage * STAGE + TA::BYTES);
+        lb.issue(lds + stage * STAGE + A_BYTES);
       };
       auto wait = [&](auto stages) {
-        constexpr int N = decltype(stages)::value;
-        if (fewer) wait_loads<TA::LOADS * N>();
-        else wait_loads<EACH * N>();
+        constexpr int N = decltype(stages)::value, EACH = DA::LOADS + DB::LOADS;
+        if (absent == 0) wait_loads<EACH * N>();
+        else if (absent == 1) wait_loads<(EACH - 1) * N>();
+        else wait_loads<(EACH - 2) * N>();
         barrier();
       };
+      // fp32 by rows is bound by its cuts: of five or six pieces of 32 rows the last
+      // ones are shared by two waves, 16 k of a step each, as their SIMDs have one
+      // of the first four already (8 rows of 65537, tiles of 136: 181 -> 167 us)
+      const int pieces = (int)min((m_count + 31) / 32, (int64_t)8), helped = RAW && (pieces == 5 || pieces == 6) ? pieces - 4 : 0;
+      int turn = -1;                                   // which 16 k of a step are this wave's; -1: all, NK or more: none
+      static_assert(!RAW || (NK == 2 && WM == 8), "two waves and their two halves");
       // Fragments are read 16 k ahead of their products, those of the next step
       // as well: the barrier and the loads of a step stand in front of products
       // whose operands are in registers.
       static_assert(NK % 2 == 0, "two sets of fragments in turn");
-      const int ma = wave() / WN * TM * 32, nb = wave() % WN * TN * 32, k0s = k_wave() * NK;
+      int ma = wave() / WN * TM * 32;
+      const int nb = wave() % WN * TN * 32, k0s = k_wave() * NK;
+      if (RAW && helped && wave() >= 4) {
+        ma = (4 + (wave() - 4) % helped) * 32;
+        turn = (wave() - 4) / helped;
+      }
       // of this wave's 32 x 32 products, how many lie in the operands
-      const int tm = (int)max((int64_t)0, min((m_count - ma + 31) / 32, (int64_t)TM)), tn = (int)max((int64_t)0, min((n_count - nb + 31) / 32, (int64_t)TN));
+      const int tm = turn < NK ? (int)max((int64_t)0, min((m_count - ma + 31) / 32, (int64_t)TM)) : 0, tn = (int)max((int64_t)0, min((n_count - nb + 31) / 32, (int64_t)TN));
       for (int s = 0; s < STAGES; s++) issue(s);      // past the last step: zeros, which nothing reads
       wait(std::integral_constant<int, STAGES - 1>());
       auto loop = [&](auto partial) {
-        v4u fa[2][TM][RAW ? 2 : 1], fb[2][TN][RAW ? 3 : 1];
+        v4u fa[2][TM], fb[2][TN];
         auto read = [&](int set, const lds_char* s, int ks) {
 #pragma unroll
           for (int j = 0; j < TN; j++)
-            if (!partial || j < tn) {
-#pragma unroll
-              for (int p = 0; p < (RAW ? 3 : 1); p++) fb[set][j][p] = TB::fragment(s + TA::BYTES, p * BN + nb + j * 32, k0s + ks);
-            }
+            if (!partial || j < tn) fb[set][j] = TB::fragment(s + A_BYTES, nb + j * 32, k0s + ks);
 #pragma unroll
           for (int i = 0; i < TM; i++)
-            if (!partial || i < tm) {
-              if constexpr (RAW) TA::fragment_f32(s, ma + i * 32, k0s + ks, fa[set][i]);
-              else fa[set][i][0] = TA::fragment(s, ma + i * 32, k0s + ks);
-            }
-        };
-        auto multiply = [&](int set, int i, int j) {
-          if constexpr (RAW) {
-            v4u x[3];
-            cut(fa[set][i], x);
-            acc[i][j] = mfma_cut(x, fb[set][j], acc[i][j]);
-          } else acc[i][j] = mfma<DT>(fa[set][i][0], fb[set][j][0], acc[i][j]);
+            if (!partial || i < tm) fa[set][i] = TA::fragment(s, ma + i * 32, k0s + ks);
         };
         read(0, lds, 0);
         int stage = 0;
@@ -463,17 +471,85 @@ struct Product {
             for (int i = 0; i < TM; i++)
 #pragma unroll
               for (int j = 0; j < TN; j++)
-                if (!partial || (i < tm && j < tn)) multiply(ks & 1, i, j);
+                if (!partial || (i < tm && j < tn)) acc[i][j] = mfma<DT>(fa[ks & 1][i], fb[ks & 1][j], acc[i][j]);
             __builtin_amdgcn_sched_barrier(0);
           }
           stage = next;
         }
       };
+      // The same of fp32 by rows.  The cut of the next 16 k goes between the
+      // products of these, which wait for one another.
+      auto loop_raw = [&](auto partial) {
+        v4u raw[2], part[2][3], fb[2][3];
+        f32x16 small = {};
+        auto mine = [&](int ks) { return !partial || (tm && tn && (turn < 0 || turn == ks)); };
+        auto read = [&](int set, const lds_char* s, int ks) {
+          if (!mine(ks)) return;
+          TA::fragment_f32(s, ma, ks, raw);
+#pragma unroll
+          for (int p = 0; p < 3; p++) fb[set][p] = TB::fragment(s + A_BYTES, p * BN, ks);
+        };
+        read(0, lds, 0);
+        if (mine(0)) cut(raw, part[0]);
+        int stage = 0;
+        for (int64_t t = 0; t < steps; t++) {
+          const int next = stage + 1 == STAGES ? 0 : stage + 1;
+#pragma unroll
+          for (int ks = 0; ks < 2; ks++) {
+            if (ks == 0) read(1, lds + stage * STAGE, 1);
+            else if (t + 1 < steps) {
+              wait(std::integral_constant<int, STAGES - 2>());
+              issue(stage);
+              read(0, lds + next * STAGE, 0);
+            }
+            const v4u *a = part[ks], *b = fb[ks];
+            if (mine(ks)) {
+              small = mfma<EXTERND_BF16>(a[1], b[1], small);
+              small = mfma<EXTERND_BF16>(a[0], b[2], small);
+              small = mfma<EXTERND_BF16>(a[2], b[0], small);
+              acc[0][0] = mfma<EXTERND_BF16>(a[0], b[0], acc[0][0]);
+              small = mfma<EXTERND_BF16>(a[0], b[1], small);
+              small = mfma<EXTERND_BF16>(a[1], b[0], small);
+            }
+            if (mine(ks ^ 1)) cut(raw, part[ks ^ 1]);      // behind the last step: of what was read before
+            if (!partial) {
+#pragma unroll
+              for (int i = 0; i < 6; i++) {
+                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);      // a product,
+                __builtin_amdgcn_sched_group_barrier(0x2, 8, 0);      // vector instructions
+              }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+          }
+          stage = next;
+        }
+#pragma unroll
+        for (int r = 0; r < 16; r++) acc[0][0][r] += small[r];
+      };
       // a tile at the operands' ends costs what it holds: 65537 columns are 256 tiles and a small one
-      if (tm < TM || tn < TN) loop(std::true_type());
+      if constexpr (RAW) {
+        if (tm < TM || tn < TN || turn >= 0) loop_raw(std::true_type());
+        else loop_raw(std::false_type());
+      } else if (tm < TM || tn < TN) loop(std::true_type());
       else loop(std::false_type());
       wait_loads<0>();
       barrier();
+      if (RAW && helped) {
+        typedef __attribute__((address_space(3))) float* floats;
+        floats part = (floats)lds + (ma / 32 - 4) * 16 * 64 + (threadIdx.x & 63);
+        if (turn == 1) {
+#pragma unroll
+          for (int r = 0; r < 16; r++) part[r * 64] = acc[0][0][r];
+        }
+        wait_loads<63>();
+        barrier();
+        if (turn == 0) {
+#pragma unroll
+          for (int r = 0; r < 16; r++) acc[0][0][r] += part[r * 64];
+        }
+        wait_loads<63>();
+        barrier();
+      }
     } else {
       static_assert(DIRECT || STAGES == 2, "two buffers");
       Staged<DT, ACOL, BM, BK, DEPTH> la;

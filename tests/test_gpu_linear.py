@@ -264,6 +264,17 @@ def test_the_targets_entry_is_not_rounded(ext, dtype, rows, width, vocab, one):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("whole", [True, False])
+@pytest.mark.parametrize("vocab,width", [(38000, 96), (38000, 44), (45000, 100), (45000, 260), (32769, 300), (20118, 132), (20148, 40)])
+def test_few_rows_and_pieces_of_a_tile(ext, dtype, whole, vocab, width):
+    """Tiles, or last ones, of five and six pieces of 32 columns, of which waves share the last; odd numbers of steps."""
+    x, w, y = make(9, width, vocab, dtype, 25, whole)
+    y[3], y[4], y[5] = vocab - 1, 130, 165
+    check(ext, x, w, y, whole=whole)
+    check_backward(ext, x, w, y, *gradients(9, y, 26, "ge"), dtype, whole=whole)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("offset,gap", [(1, 0), (0, 1), (3, 5), (2, 6), (8, 8), (5, 11)])
 def test_strides(ext, dtype, offset, gap):
     """Rows that begin anywhere, with gaps that hold NaN; outputs between other columns."""
