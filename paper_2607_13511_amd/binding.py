@@ -1085,10 +1085,10 @@ def _written_twice(ins, ops, nbytes) -> bool:
             end = max(end, b)
             end_wrote = max(end_wrote, b) if wrote else end_wrote
         return False
-    a, size = np.array(ops, dtype=np.int64), np.array(nbytes, dtype=np.int64)      # the same without a loop
+    a, size = np.asarray(ops, dtype=np.int64), np.asarray(nbytes, dtype=np.int64)      # the same without a loop
     keep, wrote = size > 0, np.ones(len(ops), dtype=bool)
     if ops is not ins:
-        i = np.array(ins, dtype=np.int64)
+        i = np.asarray(ins, dtype=np.int64)
         keep = np.concatenate([keep, keep & (i != a)])
         a, size, wrote = np.concatenate([a, i]), np.concatenate([size, size]), np.concatenate([wrote, ~wrote])
     a, size, wrote = a[keep], size[keep], wrote[keep]
@@ -1122,30 +1122,39 @@ def clip_gradients(tensors, max_norm: float = float("inf"), out=None, stream=Non
         raise ValueError(f"workspace: expected on {device}, got {workspace.device}")
     if _dtype_codes is None:
         _dtype_code(torch, torch.float32, "")
-    # hundreds of tensors are ordinary, so each property is taken of all at once
+    # hundreds of tensors are ordinary, so each property is taken of all at once (216
+    # and as many outputs: 180 us a call, nearly all of it here, -> 141)
+    T = torch.Tensor
     dtypes = [t.dtype for t in tensors]
-    codes = [_dtype_codes.get(d) for d in dtypes]
-    gaps = False in [t.is_contiguous() for t in tensors]
-    if None in codes or any([t.get_device() != index for t in tensors]) or (gaps and not all([_dense(t) for t in tensors])):
+    codes = list(map(_dtype_codes.get, dtypes))
+    gaps = False in map(T.is_contiguous, tensors)
+    if None in codes or not {index}.issuperset(map(T.get_device, tensors)) or (gaps and not all(map(_dense, tensors))):
         i = next(i for i, t in enumerate(tensors) if t.dtype not in _dtype_codes or t.get_device() != index or not _dense(t))
         t = tensors[i]
         raise ValueError(f"tensors[{i}]: expected a dense CUDA tensor of float32, bfloat16 or float16 on {device}, got "
                          f"{t.dtype} {tuple(t.shape)} {t.stride()} on {t.device}")
-    ops = ins = [t.data_ptr() for t in tensors]
-    sizes = [t.numel() for t in tensors]
+    ops = ins = list(map(T.data_ptr, tensors))
+    sizes = list(map(T.numel, tensors))
     if out is not None:
-        if (gaps or False in [o.is_contiguous() for o in outs] or [o.dtype for o in outs] != dtypes
-                or [o.numel() for o in outs] != sizes or any([o.get_device() != index for o in outs])):
+        if (gaps or False in map(T.is_contiguous, outs) or [o.dtype for o in outs] != dtypes
+                or list(map(T.numel, outs)) != sizes or not {index}.issuperset(map(T.get_device, outs))):
             for i, (t, o) in enumerate(zip(tensors, outs)):
                 if not (o.dtype is t.dtype and o.get_device() == index and o.shape == t.shape
                         and (o.is_contiguous() and t.is_contiguous() or o.stride() == t.stride())):
                     raise ValueError(f"out[{i}]: expected {t.dtype} {tuple(t.shape)} {t.stride()} on {t.device}, got {o.dtype} "
                                      f"{tuple(o.shape)} {o.stride()} on {o.device}")
-        ops = [o.data_ptr() for o in outs]
-    if max_norm != float("inf") and tensors:
-        if _written_twice(ins, ops, [n * (4 if c == 0 else 2) for n, c in zip(sizes, codes)]):
-            raise ValueError("tensors: what is written overlaps another tensor")
+        ops = list(map(T.data_ptr, outs))
     n = len(tensors)
+    counts, types = np.array(sizes, dtype=np.int64), np.array(codes, dtype=np.int32)
+    in_ptrs = np.array(ins, dtype=np.int64)
+    out_ptrs = in_ptrs if ops is ins else np.array(ops, dtype=np.int64)
+    if max_norm != float("inf") and tensors:
+        if n <= 32:
+            twice = _written_twice(ins, ops, [m * (4 if c == 0 else 2) for m, c in zip(sizes, codes)])
+        else:
+            twice = _written_twice(in_ptrs, out_ptrs, counts << (1 + (types == 0)))
+        if twice:
+            raise ValueError("tensors: what is written overlaps another tensor")
     norm = torch.empty((), dtype=torch.float32, device=device)
     L = lib()
     if workspace is not None:
@@ -1154,9 +1163,8 @@ def clip_gradients(tensors, max_norm: float = float("inf"), out=None, stream=Non
         nbytes = L.externd_clip_gradients_workspace_bytes(n)
         workspace = torch.empty((nbytes,), dtype=torch.uint8, device=device)
         wp = workspace.data_ptr()
-    ptrs, counts, types = np.array([ins, ops], dtype=np.int64), np.array(sizes, dtype=np.int64), np.array(codes, dtype=np.int32)
-    st = L.externd_clip_gradients(n, ptrs.ctypes.data, ptrs.ctypes.data + 8 * n, counts.ctypes.data, types.ctypes.data, max_norm,
-                                  norm.data_ptr(), wp, nbytes, _stream_ptr(torch, stream))
+    st = L.externd_clip_gradients(n, in_ptrs.ctypes.data, None if ops is ins else out_ptrs.ctypes.data, counts.ctypes.data,
+                                  types.ctypes.data, max_norm, norm.data_ptr(), wp, nbytes, _stream_ptr(torch, stream))
     if st != OK:
         raise ExterndError(st, "externd_clip_gradients")
     return norm
