@@ -28,6 +28,7 @@ struct LinearArgs {
   const int64_t* targets;
   float scale;
   int row_tiles, vocab_tiles;      // of this launch
+  int grad_x_tiles;                // k_grads: before those of grad_weight
   int64_t step;                    // vocabulary of a tile
   int64_t v0, v1;                  // vocabulary of this launch
   // forward
@@ -62,9 +63,9 @@ struct LinearArgs {
 // Tiles in an order in which those that run together share operands: an XCD
 // (workgroups go round robin over the eight) takes a stretch of them, eight
 // row tiles of one vocabulary tile after another.
-__device__ __forceinline__ void place_tile(int rows, int others, int* row, int* other) {
-  const int total = rows * others, xcd = blockIdx.x & 7, per = total >> 3, more = total & 7;
-  const int at = xcd * per + min(xcd, more) + (int)(blockIdx.x >> 3);
+__device__ __forceinline__ void place_tile(int block, int rows, int others, int* row, int* other) {
+  const int total = rows * others, xcd = block & 7, per = total >> 3, more = total & 7;
+  const int at = xcd * per + min(xcd, more) + (block >> 3);
   const int panel = at / (8 * others), in = at - panel * 8 * others, w = min(8, rows - panel * 8);
   *row = panel * 8 + in % w;
   *other = in / w;
@@ -133,7 +134,7 @@ __global__ __launch_bounds__(GEMM_THREADS, 2) void k_logits(LinearArgs a) {
   constexpr int DT = P::DT, TM = P::TM, TN = P::TN;
   __shared__ __align__(16) char lds[P::LDS];
   int rt, vt;
-  place_tile(a.row_tiles, a.vocab_tiles, &rt, &vt);
+  place_tile((int)blockIdx.x, a.row_tiles, a.vocab_tiles, &rt, &vt);
   const int64_t m0 = a.v0 + vt * a.step, n0 = (int64_t)rt * P::BN, ms = min(a.step, a.v1 - m0);
   f32x16 acc[TM][TN];
   if constexpr (P::RAW) P::run(a.weight, m0, ms, Operand{a.cut, a.cut_width}, 0, P::BROWS, 0, a.width, (lds_char*)lds, acc);
@@ -382,11 +383,10 @@ __global__ __launch_bounds__(256) void k_cut(LinearArgs a) {
 // G weight of this piece (columns of weight along m, rows of G along n), added to
 // the split's sums so far.
 template <typename P>
-__global__ __launch_bounds__(GEMM_THREADS, 2) void k_grad_x(LinearArgs a) {
-  __shared__ __align__(16) char lds[P::LDS];
+__device__ __forceinline__ void grad_x_tile(const LinearArgs& a, int block, char* lds) {
   const int cols = (int)((a.width + P::BM - 1) / P::BM);
   int rt, other;
-  place_tile(a.row_tiles, cols * a.splits, &rt, &other);
+  place_tile(block, a.row_tiles, cols * a.splits, &rt, &other);
   const int s = other / cols;
   const int64_t m0 = (int64_t)(other - s * cols) * P::BM, n0 = (int64_t)rt * P::BN, k0 = s * a.split, K = min(a.split, a.p1 - a.p0 - k0);
   f32x16 acc[P::TM][P::TN];
@@ -519,11 +519,10 @@ __device__ __forceinline__ void add_rests(const LinearArgs& a, f32x16 (*acc)[P::
 
 // G^T x of this piece: columns of x along m, of G (the vocabulary) along n.
 template <typename P>
-__global__ __launch_bounds__(GEMM_THREADS, 2) void k_grad_weight(LinearArgs a) {
+__device__ __forceinline__ void grad_weight_tile(const LinearArgs& a, int block, char* lds) {
   typedef typename Elem<P::DT>::T T;
-  __shared__ __align__(16) char lds[P::LDS];
   int ct, vt;
-  place_tile((int)((a.width + P::BM - 1) / P::BM), a.vocab_tiles, &ct, &vt);
+  place_tile(block, (int)((a.width + P::BM - 1) / P::BM), a.vocab_tiles, &ct, &vt);
   const int64_t m0 = (int64_t)ct * P::BM, n0 = (int64_t)vt * P::BN, ns = a.v1 - a.v0;
   f32x16 acc[P::TM][P::TN];
   const Operand x = {a.packed, a.packed_width}, G = {(T*)a.G + (a.v0 - a.p0), a.G_width};
@@ -554,6 +553,24 @@ __global__ __launch_bounds__(GEMM_THREADS, 2) void k_grad_weight(LinearArgs a) {
         if (m + e < width) at[e] = Elem<P::DT>::store(y[e]);      // exact: of its type
     }
   });
+}
+
+template <typename P>
+__global__ __launch_bounds__(GEMM_THREADS, 2) void k_grad_x(LinearArgs a) {
+  __shared__ __align__(16) char lds[P::LDS];
+  grad_x_tile<P>(a, (int)blockIdx.x, lds);
+}
+template <typename P>
+__global__ __launch_bounds__(GEMM_THREADS, 2) void k_grad_weight(LinearArgs a) {
+  __shared__ __align__(16) char lds[P::LDS];
+  grad_weight_tile<P>(a, (int)blockIdx.x, lds);
+}
+// Both, where the CUs hold the tiles of both at once.
+template <typename X, typename W>
+__global__ __launch_bounds__(GEMM_THREADS, 2) void k_grads(LinearArgs a) {
+  __shared__ __align__(16) char lds[X::LDS > W::LDS ? X::LDS : W::LDS];
+  if ((int)blockIdx.x < a.grad_x_tiles) grad_x_tile<X>(a, (int)blockIdx.x, lds);
+  else grad_weight_tile<W>(a, (int)blockIdx.x - a.grad_x_tiles, lds);
 }
 
 // grad_weight without rows.
@@ -659,6 +676,10 @@ static LinearWork backward_work(int32_t dtype, int64_t rows, int64_t vocab, int6
   int64_t splits = CUS / (cols * row_tiles);
   const int64_t max_splits = ceil_div(w.G_width, 128);
   splits = splits < 1 ? 1 : splits > max_splits ? max_splits : splits;
+  // fewer, if grad_weight's tiles then run beside them and not after: the longer of both sums for one after the other
+  const int64_t weight_tiles = cols * ceil_div(vocab < w.piece + 255 ? vocab : w.piece + 255, dtype == EXTERND_F32 ? 128 : 256);
+  const int64_t beside = (CUS - weight_tiles) / (cols * row_tiles), sum = beside > 0 ? ceil_div(w.G_width, beside) : 0;
+  if (need_x && need_weight && beside > 0 && beside < splits && (sum > rows ? sum : rows) < rows + ceil_div(w.G_width, splits)) splits = beside;
   w.split = ceil_div(ceil_div(w.G_width, splits), 64) * 64;
   w.splits = (int)ceil_div(w.G_width, w.split);
   size_t at = cut_bytes(dtype, rows, width, &w);
@@ -703,11 +724,6 @@ static void with_tail(LinearArgs a, int64_t other_tiles, L large, S small) {
 }
 
 template <typename P>
-static void launch_grad_x(LinearArgs a, hipStream_t s) {
-  a.row_tiles = (int)ceil_div(a.rows, P::BN);
-  k_grad_x<P><<<(unsigned)(a.row_tiles * ceil_div(a.width, P::BM) * a.splits), GEMM_THREADS, 0, s>>>(a);
-}
-template <typename P>
 static void launch_grad_weight(LinearArgs a, hipStream_t s) {
   a.vocab_tiles = (int)ceil_div(a.v1 - a.v0, P::BN);
   k_grad_weight<P><<<(unsigned)(ceil_div(a.width, P::BM) * a.vocab_tiles), GEMM_THREADS, 0, s>>>(a);
@@ -733,16 +749,32 @@ static void choose_logits(const LinearArgs& a, hipStream_t s) {
                 [&](const LinearArgs& b) { launch_logits<Small, BACK>(b, s); });
   }
 }
-template <int DT, bool DIRECT>
-static void choose_grad_x(const LinearArgs& a, hipStream_t s) {
+// grad_x of this piece, and grad_weight in the same launch if the tiles of both are no
+// more than CUs (58 fp32 rows of 3607, width 521: 52 -> 41 us; 1000 bf16 rows of 5000,
+// width 1024, of which fewer splits make room: 104 -> 83).  Returns whether it was.
+template <typename X, typename W>
+static bool launch_grad_x(LinearArgs a, hipStream_t s) {
+  a.row_tiles = (int)ceil_div(a.rows, X::BN);
+  const int64_t cols = ceil_div(a.width, X::BM), tiles = a.row_tiles * cols * a.splits;
+  a.vocab_tiles = (int)ceil_div(a.v1 - a.v0, W::BN);
+  const bool both = a.grad_weight && tiles + ceil_div(a.width, W::BM) * a.vocab_tiles <= CUS;
+  if (both) {
+    a.grad_x_tiles = (int)tiles;
+    k_grads<X, W><<<(unsigned)(tiles + ceil_div(a.width, W::BM) * a.vocab_tiles), GEMM_THREADS, 0, s>>>(a);
+  } else k_grad_x<X><<<(unsigned)tiles, GEMM_THREADS, 0, s>>>(a);
+  return both;
+}
+template <int DT, bool DIRECT, typename W>
+static bool choose_grad_x(const LinearArgs& a, hipStream_t s) {
   const int n = tile_rows(DT, a.rows);
   if constexpr (DT == EXTERND_F32) {
-    if (n == 32) launch_grad_x<Product<DT, false, true, false, 256, 32, 8, 2>>(a, s);
-    else launch_grad_x<Product<DT, false, true, false, 256, 128, 4, 2>>(a, s);
+    if (n == 32) return launch_grad_x<Product<DT, false, true, false, 256, 32, 8, 2>, W>(a, s);
+    return launch_grad_x<Product<DT, false, true, false, 256, 128, 4, 2>, W>(a, s);
   } else {
-    if (n == 32) launch_grad_x<Product<DT, DIRECT, true, false, 256, 32, 8, DIRECT ? 4 : 2>>(a, s);
-    else if (n == 128 || !DIRECT) launch_grad_x<Product<DT, DIRECT, true, false, 256, 128, 4, DIRECT ? 3 : 2>>(a, s);
-    else if constexpr (DIRECT) launch_grad_x<Product<DT, true, true, false, 256, 256, 2, 2>>(a, s);
+    if (n == 32) return launch_grad_x<Product<DT, DIRECT, true, false, 256, 32, 8, DIRECT ? 4 : 2>, W>(a, s);
+    if constexpr (DIRECT)
+      if (n == 256) return launch_grad_x<Product<DT, true, true, false, 256, 256, 2, 2>, W>(a, s);
+    return launch_grad_x<Product<DT, DIRECT, true, false, 256, 128, 4, DIRECT ? 3 : 2>, W>(a, s);
   }
 }
 
@@ -775,14 +807,13 @@ static void launch_backward(LinearArgs a, bool direct, hipStream_t s) {
     a.v1 = a.p1;
     if (direct) choose_logits<DT, true, true>(a, s);
     else choose_logits<DT, false, true>(a, s);
-    if (a.grad_x) {
-      if (DT != EXTERND_F32 && direct) choose_grad_x<DT, DT != EXTERND_F32>(a, s);
-      else choose_grad_x<DT, false>(a, s);
-    }
-    if (a.grad_weight) {
-      if constexpr (DT == EXTERND_F32) launch_grad_weight<Product<DT, false, true, true, 256, 128, 4, 2>>(a, s);
+    typedef std::conditional_t<DT == EXTERND_F32, Product<DT, false, true, true, 256, 128, 4, 2>, Product<DT, DT != EXTERND_F32, true, true, 256, 256, 2, 2>> W;
+    bool both = false;
+    if (a.grad_x) both = DT != EXTERND_F32 && direct ? choose_grad_x<DT, DT != EXTERND_F32, W>(a, s) : choose_grad_x<DT, false, W>(a, s);
+    if (a.grad_weight && !both) {
+      if constexpr (DT == EXTERND_F32) launch_grad_weight<W>(a, s);
       else
-        with_tail(a, ceil_div(a.width, 256), [&](const LinearArgs& b) { launch_grad_weight<Product<DT, true, true, true, 256, 256, 2, 2>>(b, s); },
+        with_tail(a, ceil_div(a.width, 256), [&](const LinearArgs& b) { launch_grad_weight<W>(b, s); },
                   [&](const LinearArgs& b) { launch_grad_weight<Product<DT, true, true, true, 256, 32, 8, 4>>(b, s); });
     }
   }

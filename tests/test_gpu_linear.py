@@ -264,6 +264,19 @@ def test_the_targets_entry_is_not_rounded(ext, dtype, rows, width, vocab, one):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,width,vocab", [(9, 256, 20000), (58, 521, 3607), (130, 264, 8000), (300, 512, 2000), (700, 1000, 5000)])
+def test_both_gradients_at_once(ext, dtype, rows, width, vocab):
+    """Sizes whose tiles of both products the CUs hold together, and each by itself."""
+    x, w, y = make(rows, width, vocab, dtype, 27)
+    g = gradients(rows, y, 28, "ge")
+    check_backward(ext, x, w, y, *g, dtype)
+    got = ext.linear_logprobs(x, w, y)
+    lse, H = got.lse, got.entropy
+    _, gw = ext.linear_logprobs_backward(x, w, y, lse, H, *g)
+    assert torch.equal(gw, ext.linear_logprobs_backward(x, w, y, lse, H, *g, need_x=False)[1])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("whole", [True, False])
 @pytest.mark.parametrize("vocab,width", [(38000, 96), (38000, 44), (45000, 100), (45000, 260), (32769, 300), (20118, 132), (20148, 40)])
 def test_few_rows_and_pieces_of_a_tile(ext, dtype, whole, vocab, width):
