@@ -299,35 +299,44 @@ __global__ __launch_bounds__(256) void k_logits_join(LinearArgs a) {
   }
 }
 
-// What each row's gradient is made of.  For fp16 one workgroup goes over all
+// What row r's gradient is made of.
+__device__ __forceinline__ RowInfo row_info(const LinearArgs& a, int64_t r, bool fp16, bool fp32) {
+  const int64_t y = a.targets ? a.targets[r] : -1;
+  const bool asked = y >= 0 && y < a.vocab;
+  RowInfo w = {};
+  w.y = asked ? (int32_t)y : -1;
+  const float g = a.g_logprob && asked ? a.g_logprob[r] : 0.f, ge = a.g_entropy ? a.g_entropy[r] : 0.f;
+  const float h = ge == 0.f ? 0.f : a.entropy_in[r], lse = a.lse_in[r];
+  w.present = g != 0.f || ge != 0.f;
+  w.lse = !w.present || lse == -INFINITY ? INFINITY : fp32 ? lse : lse * LOG2E;
+  w.up = 1.f;
+  if (fp16 && w.present) {
+    // |G| <= |g| + |ge| (p |ln p| + p H) < |g| + |ge| (1 + H)
+    const float most = fabsf(g) + (ge == 0.f ? 0.f : fabsf(ge) * (1.f + fabsf(h)));
+    const int k = most <= 3.402823466e38f ? 14 - ilogbf(most) : 0;
+    w.up = ldexpf(1.f, k > 120 ? 120 : k < -120 ? -120 : k);
+  }
+  // -p (g + ge (ln p + H))
+  w.g = g * w.up;
+  w.a = -ge * w.up * (fp32 ? 1.f : LN2);
+  w.b = -fmaf(ge, h, g) * w.up;
+  return w;
+}
+__device__ __forceinline__ void put_row(const LinearArgs& a, int64_t r, const RowInfo& w) {
+  a.info[r] = w;
+  a.target[r] = w.present ? w.y : -1;
+  a.rest[r] = 0.f;
+}
+
+// Of all rows, where k_pack does not do it.  For fp16 one workgroup goes over all
 // rows, as the least `up` scales what the rows' sum is made of.
 __global__ __launch_bounds__(1024) void k_rows(LinearArgs a, int fp16, int fp32) {
   __shared__ float least[16];
   float up_all = 0x1p120f;
   for (int64_t r = (int64_t)blockIdx.x * 1024 + threadIdx.x; r < a.rows; r += (int64_t)gridDim.x * 1024) {
-    const int64_t y = a.targets ? a.targets[r] : -1;
-    const bool asked = y >= 0 && y < a.vocab;
-    RowInfo w = {};
-    w.y = asked ? (int32_t)y : -1;
-    const float g = a.g_logprob && asked ? a.g_logprob[r] : 0.f, ge = a.g_entropy ? a.g_entropy[r] : 0.f;
-    const float h = ge == 0.f ? 0.f : a.entropy_in[r], lse = a.lse_in[r];
-    w.present = g != 0.f || ge != 0.f;
-    w.lse = !w.present || lse == -INFINITY ? INFINITY : fp32 ? lse : lse * LOG2E;
-    w.up = 1.f;
-    if (fp16 && w.present) {
-      // |G| <= |g| + |ge| (p |ln p| + p H) < |g| + |ge| (1 + H)
-      const float most = fabsf(g) + (ge == 0.f ? 0.f : fabsf(ge) * (1.f + fabsf(h)));
-      const int k = most <= 3.402823466e38f ? 14 - ilogbf(most) : 0;
-      w.up = ldexpf(1.f, k > 120 ? 120 : k < -120 ? -120 : k);
-      up_all = fminf(up_all, w.up);
-    }
-    // -p (g + ge (ln p + H))
-    w.g = g * w.up;
-    w.a = -ge * w.up * (fp32 ? 1.f : LN2);
-    w.b = -fmaf(ge, h, g) * w.up;
-    a.info[r] = w;
-    a.target[r] = w.present ? w.y : -1;
-    a.rest[r] = 0.f;
+    const RowInfo w = row_info(a, r, fp16, fp32);
+    if (fp16 && w.present) up_all = fminf(up_all, w.up);
+    put_row(a, r, w);
   }
   if (!fp16) {
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.up_all = 1.f;
@@ -344,7 +353,8 @@ __global__ __launch_bounds__(1024) void k_rows(LinearArgs a, int fp16, int fp32)
 
 // x for its product with G: rows that take no part are zeros whatever they hold,
 // fp16 rows are down by what their G is up beyond the least (a power of two:
-// exact but for entries that it takes below 2^-14).
+// exact but for entries that it takes below 2^-14).  In the other types a row's
+// first thread also writes what k_rows would, a launch less (58 fp32 rows of 3607: 41 -> 39.5 us).
 template <int DT>
 __global__ __launch_bounds__(256) void k_pack(LinearArgs a) {
   typedef typename Elem<DT>::T T;
@@ -352,7 +362,11 @@ __global__ __launch_bounds__(256) void k_pack(LinearArgs a) {
   const int64_t units = a.packed_width / E, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= units * a.rows) return;
   const int64_t r = i / units, c = (i - r * units) * E;
-  const RowInfo w = a.info[r];
+  const RowInfo w = DT == EXTERND_F16 ? a.info[r] : row_info(a, r, false, DT == EXTERND_F32);
+  if (DT != EXTERND_F16 && c == 0) {
+    put_row(a, r, w);
+    if (r == 0) *a.up_all = 1.f;
+  }
   const T* from = (const T*)a.x.p + r * a.x.stride + c;
   float x[E] = {};
   if (w.present) {
@@ -798,7 +812,7 @@ static void launch_backward(LinearArgs a, bool direct, hipStream_t s) {
     k_zero_rows<DT><<<(unsigned)(a.vocab < 4096 ? a.vocab : 4096), 256, 0, s>>>(a);
     return;
   }
-  k_rows<<<DT == EXTERND_F16 ? 1 : (unsigned)ceil_div(a.rows, 1024), 1024, 0, s>>>(a, DT == EXTERND_F16, DT == EXTERND_F32);
+  if (DT == EXTERND_F16 || !a.grad_weight) k_rows<<<DT == EXTERND_F16 ? 1 : (unsigned)ceil_div(a.rows, 1024), 1024, 0, s>>>(a, DT == EXTERND_F16, DT == EXTERND_F32);
   if (direct) launch_cut<DT>(a, s);
   if (a.grad_weight) k_pack<DT><<<(unsigned)ceil_div(a.rows * (a.packed_width / Vec<DT>::E), 256), 256, 0, s>>>(a);
   for (a.p0 = 0; a.p0 < a.vocab; a.p0 = a.p1) {
