@@ -53,16 +53,16 @@ struct Tile {
   static_assert(VECTORS % GEMM_THREADS == 0 || VECTORS < GEMM_THREADS, "whole loads");
   static constexpr int CH = COL ? X / EV : BK / EV;            // vectors of a row in memory
   // Where in the operand the vector at place `i` of the tile is: its row in memory and its vector there.
-  static __device__ __forceinline__ void place(int i, int* row, int* vec) {
+  static __host__ __device__ __forceinline__ void place(int i, int* row, int* vec) {
     *row = i / CH;
     const int v = i % CH;
     if constexpr (COL) *vec = ((v >> 1) ^ spread(*row)) << 1 | (v & 1);
     else *vec = v ^ swap(*row);
   }
   // By rows: the sixteen rows that are read together go to different banks (256 bytes of them).
-  static __device__ __forceinline__ int swap(int row) { return CH >= 16 ? row & 15 : (row / (16 / (CH < 16 ? CH : 16))) & (CH - 1); }
+  static __host__ __device__ __forceinline__ int swap(int row) { return CH >= 16 ? row & 15 : (row / (16 / (CH < 16 ? CH : 16))) & (CH - 1); }
   // By columns: pairs of vectors (16 columns) of four rows of k go to different banks.
-  static __device__ __forceinline__ int spread(int k) { return (2 * (k & 3)) & (X / 16 - 1); }
+  static __host__ __device__ __forceinline__ int spread(int k) { return (2 * (k & 3)) & (X / 16 - 1); }
   // The byte at which a lane reads its fragment of 32 columns from x0 on, without what depends on x0 and on the step of 16 k.
   static __device__ __forceinline__ v4u fragment(const lds_char* t, int x0, int ks) {
     const int lane = threadIdx.x & 63;
@@ -140,25 +140,32 @@ struct Direct {
   static constexpr unsigned NONE = 0xFFFFFFFFu;
   const char* base;
   int64_t left, k_left;      // bytes from the base to the operand's end; k's from the next step on
+  int64_t step;              // bytes: 64 rows of 2^24 entries of G (a piece of few rows) are past 31 bits
   unsigned offset[LOADS];
-  int step;
 
   // count of m (or n) from x0 on, K of k from k0 on.
-  __device__ __forceinline__ void init(const Operand& o, int64_t x0, int64_t count, int64_t k0, int64_t K) {
-    const int64_t row = o.stride * B, cols = min(count, (int64_t)X);
+  __host__ __device__ __forceinline__ void init(const Operand& o, int64_t x0, int64_t count, int64_t k0, int64_t K, int thread) {
+    const int64_t row = o.stride * B, cols = count < X ? count : X;
     if (!COL) K = (K + EV - 1) & ~(int64_t)(EV - 1);
     const int64_t rows = COL ? K : cols, width = (COL ? cols : K) * B;
     base = (const char*)o.p + (COL ? k0 * row + x0 * B : x0 * row + k0 * B);
     left = rows > 0 ? (rows - 1) * row + width : 0;
     k_left = K;
-    step = (int)(COL ? BK * row : BK * B);
+    step = COL ? BK * row : BK * B;
 #pragma unroll
     for (int i = 0; i < LOADS; i++) {
       int r, v;
-      T::place(i * GEMM_THREADS + (int)threadIdx.x, &r, &v);
-      const bool in = i * GEMM_THREADS + (int)threadIdx.x < VECTORS && (COL ? v * 16 < width : r < rows);
+      T::place(i * GEMM_THREADS + thread, &r, &v);
+      const bool in = i * GEMM_THREADS + thread < VECTORS && (COL ? v * 16 < width : r < rows);
       offset[i] = in ? (unsigned)(r * row + v * 16) : NONE;
     }
+  }
+  // Bytes behind the base that are the operand's, as the buffer's size.
+  __host__ __device__ __forceinline__ unsigned room() const { return left <= 0 ? 0u : left < (int64_t)0xFFFFFFF0 ? (unsigned)left : 0xFFFFFFF0u; }
+  __host__ __device__ __forceinline__ void next() {
+    base += step;
+    left -= step;
+    k_left -= BK;
   }
   static __device__ __forceinline__ bool has(int i) {      // whether this wave has a load i
     return (i + 1) * GEMM_THREADS <= VECTORS || i * GEMM_THREADS + (int)(threadIdx.x & ~63u) < VECTORS;
@@ -167,7 +174,7 @@ struct Direct {
   __device__ __forceinline__ void issue(lds_char* lds) {
     const unsigned to = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)lds + (threadIdx.x >> 6) * 1024);
     const i32x4 resource = {__builtin_amdgcn_readfirstlane((int)(uintptr_t)base), __builtin_amdgcn_readfirstlane((int)((uintptr_t)base >> 32)),
-                            __builtin_amdgcn_readfirstlane((int)(unsigned)min(max(left, (int64_t)0), (int64_t)0xFFFFFFF0)), 0x00020000};
+                            __builtin_amdgcn_readfirstlane((int)room()), 0x00020000};
     if (COL || k_left >= BK) {
 #pragma unroll
       for (int i = 0; i < LOADS; i++)
@@ -180,9 +187,7 @@ struct Direct {
         if (has(i)) load(to + i * (GEMM_THREADS * 16), v * EV < k_left ? offset[i] : NONE, resource);
       }
     }
-    base += step;
-    left -= step;
-    k_left -= BK;
+    next();
   }
   // LDS is written behind the compiler's back: whoever reads it waits for it (wait_loads).
   static __device__ __forceinline__ void load(unsigned to, unsigned from, i32x4 resource) {
@@ -411,8 +416,8 @@ struct Product {
       static_assert(HELD == BM || !ACOL, "rows of A");
       DA la;
       DB lb;
-      la.init(A, m0, m_count, k0, K);
-      lb.init(B, n0, n_count, k0 + b_k, K);
+      la.init(A, m0, m_count, k0, K, (int)threadIdx.x);
+      lb.init(B, n0, n_count, k0 + b_k, K, (int)threadIdx.x);
       const int absent = !DA::has(DA::LOADS - 1) + !DB::has(DB::LOADS - 1);      // of a step's loads, in this wave
       auto issue = [&](int stage) {
         la.issue(lds + stage * STAGE);
