@@ -640,7 +640,9 @@ int externd_linear_logprobs(const void* x, int64_t x_stride, const void* weight,
  *             need_x, need_weight = whether the outputs are given; 256-byte aligned.
  * Sums are fp32; G enters its products in dtype (rounded to bf16, or to fp16
  * below 2^15 with a power of two for each row, the target's entry with what it
- * loses; fp32 as three bf16 parts).                                          */
+ * loses; fp32 as three bf16 parts).  In fp16 grad_weight takes x with such
+ * powers as well: of all rows' largest |x| (|g_logprob| + |g_entropy| (1 + entropy)),
+ * times scale, 2^-38 is left out of a row's part.                            */
 size_t externd_linear_logprobs_backward_workspace_bytes(int32_t dtype, int64_t rows, int64_t vocab, int64_t width,
                                                         int32_t need_x, int32_t need_weight);  /* 0 on invalid arguments */
 int externd_linear_logprobs_backward(const void* x, int64_t x_stride, const void* weight, int64_t weight_stride,

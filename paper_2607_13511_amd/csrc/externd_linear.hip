@@ -50,7 +50,12 @@ struct LinearArgs {
   // 1.66e-3, which the rounding of the result alone makes; 1.3 % of the time).
   int32_t* target;                 // of a row that takes part, or -1
   float* rest;
-  float* up_all;                   // the least `up` of the rows that take part
+  // fp16: a row's x is packed times x_up / up, so that G^T x is x_up times too large.
+  // x_up is the power of two that brings the largest of all rows to 2^14 .. 2^15; the
+  // exponents that it follows from are left by ROW_BLOCKS workgroups or fewer.
+  float* x_up;
+  int32_t* row_exponents;
+  int row_blocks;
   void *grad_x, *grad_weight;
   int64_t grad_x_stride, grad_weight_stride, p0, p1;      // this piece of the vocabulary, G's columns
   void *G, *packed;                // rows x G_width; rows x packed_width: x, zero where a row takes no part
@@ -328,44 +333,75 @@ __device__ __forceinline__ void put_row(const LinearArgs& a, int64_t r, const Ro
   a.rest[r] = 0.f;
 }
 
-// Of all rows, where k_pack does not do it.  For fp16 one workgroup goes over all
-// rows, as the least `up` scales what the rows' sum is made of.
+// Of all rows, where k_pack does not do it.
 __global__ __launch_bounds__(1024) void k_rows(LinearArgs a, int fp16, int fp32) {
-  __shared__ float least[16];
-  float up_all = 0x1p120f;
-  for (int64_t r = (int64_t)blockIdx.x * 1024 + threadIdx.x; r < a.rows; r += (int64_t)gridDim.x * 1024) {
-    const RowInfo w = row_info(a, r, fp16, fp32);
-    if (fp16 && w.present) up_all = fminf(up_all, w.up);
-    put_row(a, r, w);
-  }
-  if (!fp16) {
-    if (blockIdx.x == 0 && threadIdx.x == 0) *a.up_all = 1.f;
-    return;
-  }
-  for (int d = 32; d; d >>= 1) up_all = fminf(up_all, __shfl_xor(up_all, d));
-  if ((threadIdx.x & 63) == 0) least[threadIdx.x >> 6] = up_all;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int i = 1; i < 16; i++) up_all = fminf(up_all, least[i]);
-    *a.up_all = up_all;
-  }
+  const int64_t r = (int64_t)blockIdx.x * 1024 + threadIdx.x;
+  if (r < a.rows) put_row(a, r, row_info(a, r, fp16, fp32));
 }
 
-// x for its product with G: rows that take no part are zeros whatever they hold,
-// fp16 rows are down by what their G is up beyond the least (a power of two:
-// exact but for entries that it takes below 2^-14).  In the other types a row's
+// The same before fp16's k_pack, a wave a row, which also looks for the largest
+// finite entry of x: its exponent without that of `up`, the largest of a workgroup's rows.
+constexpr int ROW_BLOCKS = 1024, NO_EXPONENT = -1000;
+__global__ __launch_bounds__(256) void k_rows_of_x(LinearArgs a) {
+  __shared__ int most[4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int exponent = NO_EXPONENT;
+  for (int64_t r = (int64_t)blockIdx.x * 4 + wave; r < a.rows; r += (int64_t)gridDim.x * 4) {
+    const RowInfo w = row_info(a, r, true, false);
+    if (lane == 0) put_row(a, r, w);
+    if (!w.present) continue;
+    const _Float16* x = (const _Float16*)a.x.p + r * a.x.stride;
+    unsigned largest = 0;      // magnitudes order as whole numbers do
+    auto look = [&](unsigned bits) { largest = max(largest, (bits & 0x7FFFu) < 0x7C00u ? bits & 0x7FFFu : 0u); };
+    const int64_t whole = a.width & ~(int64_t)7;
+#pragma unroll 4
+    for (int64_t c = lane * 8; c < whole; c += 512) {
+      const v4u v = load_any(x + c);
+#pragma unroll
+      for (int i = 0; i < 4; i++) {
+        look(v[i]);
+        look(v[i] >> 16);
+      }
+    }
+    if (whole + lane < a.width) look(__builtin_bit_cast(uint16_t, x[whole + lane]));
+    for (int d = 32; d; d >>= 1) largest = max(largest, (unsigned)__shfl_xor((int)largest, d));
+    if (largest) exponent = max(exponent, ilogbf((float)__builtin_bit_cast(_Float16, (uint16_t)largest)) - ilogbf(w.up));
+  }
+  if (lane == 0) most[wave] = exponent;
+  __syncthreads();
+  if (threadIdx.x == 0) a.row_exponents[blockIdx.x] = max(max(most[0], most[1]), max(most[2], most[3]));
+}
+
+// x for its product with G: rows that take no part are zeros whatever they hold.
+// In fp16 G is up by a power of two for each row, and x is down by as much, all of it
+// up by x_up: a product is exact but for entries that this takes below 2^-14, which
+// are rounded by 2^-25, some 2^-39 of the largest.  (Down by the rows' own powers alone, with the
+// largest row's x as it is, 2^-25 of x: of rows 2^10 below the largest no more than seven bits
+// were left of small entries, and none of rows 2^24 below it.)  In the other types a row's
 // first thread also writes what k_rows would, a launch less (58 fp32 rows of 3607: 41 -> 39.5 us).
 template <int DT>
 __global__ __launch_bounds__(256) void k_pack(LinearArgs a) {
   typedef typename Elem<DT>::T T;
   constexpr int E = Vec<DT>::E;
+  int up = 0;
+  if constexpr (DT == EXTERND_F16) {
+    __shared__ int most[4];
+    int exponent = NO_EXPONENT;
+    for (int i = threadIdx.x; i < a.row_blocks; i += 256) exponent = max(exponent, a.row_exponents[i]);
+    for (int d = 32; d; d >>= 1) exponent = max(exponent, __shfl_xor(exponent, d));
+    if ((threadIdx.x & 63) == 0) most[threadIdx.x >> 6] = exponent;
+    __syncthreads();
+    // at least 14 - (15 + 120); at most so that its reciprocal is a normal number
+    up = min(14 - max(max(most[0], most[1]), max(most[2], most[3])), 126);
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.x_up = ldexpf(1.f, up);
+  }
   const int64_t units = a.packed_width / E, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= units * a.rows) return;
   const int64_t r = i / units, c = (i - r * units) * E;
   const RowInfo w = DT == EXTERND_F16 ? a.info[r] : row_info(a, r, false, DT == EXTERND_F32);
   if (DT != EXTERND_F16 && c == 0) {
     put_row(a, r, w);
-    if (r == 0) *a.up_all = 1.f;
+    if (r == 0) *a.x_up = 1.f;
   }
   const T* from = (const T*)a.x.p + r * a.x.stride + c;
   float x[E] = {};
@@ -373,9 +409,11 @@ __global__ __launch_bounds__(256) void k_pack(LinearArgs a) {
     if (c + E <= a.width) Vec<DT>::unpack(load_any(from), x);
     else
       for (int e = 0; e < E; e++) x[e] = c + e < a.width ? Elem<DT>::load(from[e]) : 0.f;
-    const float f = DT == EXTERND_F16 ? *a.up_all / w.up : 1.f;
+    if constexpr (DT == EXTERND_F16) {
+      const int d = up - ilogbf(w.up);
 #pragma unroll
-    for (int e = 0; e < E; e++) x[e] *= f;
+      for (int e = 0; e < E; e++) x[e] = ldexpf(x[e], d);
+    }
   }
   *(v4u*)((T*)a.packed + r * a.packed_width + c) = Vec<DT>::pack(x);
 }
@@ -542,7 +580,7 @@ __device__ __forceinline__ void grad_weight_tile(const LinearArgs& a, int block,
   const Operand x = {a.packed, a.packed_width}, G = {(T*)a.G + (a.v0 - a.p0), a.G_width};
   P::run(x, m0, a.packed_width - m0, G, n0, (ns - n0 + 7) & ~(int64_t)7, 0, a.rows, (lds_char*)lds, acc);      // whole vectors: G's rows have room
   if constexpr (P::DT != EXTERND_F32) add_rests<P>(a, acc, m0, n0, lds);
-  const float f = a.scale, down = 1.f / *a.up_all;
+  const float f = a.scale, down = 1.f / *a.x_up;
 #pragma unroll
   for (int j = 0; j < P::TN; j++)
 #pragma unroll
@@ -635,7 +673,7 @@ static int64_t tile_step(int32_t dtype, int64_t rows, int64_t vocab, bool back) 
 }
 
 struct LinearWork {
-  size_t cut, parts, at_target, info, target, rest, up_all, packed, G, dx, bytes;
+  size_t cut, parts, at_target, info, target, rest, x_up, row_exponents, packed, G, dx, bytes;
   int64_t tiles, step, piece, G_width, packed_width, dx_width, cut_width, split;
   int splits;
 };
@@ -700,7 +738,8 @@ static LinearWork backward_work(int32_t dtype, int64_t rows, int64_t vocab, int6
   w.info = at, at += round256((size_t)rows * sizeof(RowInfo));
   w.target = at, at += round256((size_t)rows * 4);
   w.rest = at, at += round256((size_t)rows * 4);
-  w.up_all = at, at += 256;
+  w.x_up = at, at += 256;
+  w.row_exponents = at, at += dtype == EXTERND_F16 && need_weight ? ROW_BLOCKS * 4 : 0;
   w.packed = at, at += need_weight ? round256((size_t)(rows * w.packed_width) * dtype_bytes(dtype)) : 0;
   w.G = at, at += round256((size_t)(rows * w.G_width) * dtype_bytes(dtype));
   w.dx = at, at += need_x ? round256((size_t)(w.splits * rows * w.dx_width) * 4) : 0;
@@ -812,7 +851,8 @@ static void launch_backward(LinearArgs a, bool direct, hipStream_t s) {
     k_zero_rows<DT><<<(unsigned)(a.vocab < 4096 ? a.vocab : 4096), 256, 0, s>>>(a);
     return;
   }
-  if (DT == EXTERND_F16 || !a.grad_weight) k_rows<<<DT == EXTERND_F16 ? 1 : (unsigned)ceil_div(a.rows, 1024), 1024, 0, s>>>(a, DT == EXTERND_F16, DT == EXTERND_F32);
+  if (!a.grad_weight) k_rows<<<(unsigned)ceil_div(a.rows, 1024), 1024, 0, s>>>(a, DT == EXTERND_F16, DT == EXTERND_F32);
+  else if (DT == EXTERND_F16) k_rows_of_x<<<a.row_blocks, 256, 0, s>>>(a);
   if (direct) launch_cut<DT>(a, s);
   if (a.grad_weight) k_pack<DT><<<(unsigned)ceil_div(a.rows * (a.packed_width / Vec<DT>::E), 256), 256, 0, s>>>(a);
   for (a.p0 = 0; a.p0 < a.vocab; a.p0 = a.p1) {
@@ -931,7 +971,9 @@ int externd_linear_logprobs_backward(const void* x, int64_t x_stride, const void
   a.info = (RowInfo*)(at + w.info);
   a.target = (int32_t*)(at + w.target);
   a.rest = (float*)(at + w.rest);
-  a.up_all = (float*)(at + w.up_all);
+  a.x_up = (float*)(at + w.x_up);
+  a.row_exponents = (int32_t*)(at + w.row_exponents);
+  a.row_blocks = (int)(rows < 4 * ROW_BLOCKS ? ceil_div(rows, 4) : ROW_BLOCKS);
   a.packed = at + w.packed;
   a.G = at + w.G;
   a.dx = (float*)(at + w.dx);
