@@ -6,7 +6,7 @@
 
 namespace externd {
 
-constexpr int64_t FORWARD_ROWS = 8192;                // of a pass, so that the parts stay small
+constexpr int64_t FORWARD_ROWS = 8192;                // of a pass at most (pass_rows)
 constexpr int64_t PIECE_ENTRIES = (int64_t)1 << 26;   // of G in a piece of the vocabulary, where rows allow it
 constexpr int CUS = 256;
 
@@ -658,6 +658,14 @@ static bool small_tiles(int32_t dtype, int64_t rows, int64_t vocab) {
   return ceil_div(vocab, 256) * ceil_div(rows, tile_rows(dtype, rows)) < CUS && small <= CUS * (rows <= 32 ? 1 : 4);
 }
 
+// Rows of a pass of the forward call, so that the parts stay small and the tiles of
+// a launch, of 128 rows at the least here, have fewer than 2^32 threads.
+static int64_t pass_rows(int64_t rows, int64_t vocab) {
+  int64_t most = FORWARD_ROWS;
+  while (most / 128 * ceil_div(vocab, 256) * GEMM_THREADS > MAX_THREADS) most /= 2;
+  return rows < most ? rows : most;
+}
+
 // Vocabulary of a tile of logits: 64 for small tiles; 128 where tiles of 256 are
 // so few that half as large ones still take one round (452 fp32 rows of 7232, 116
 // tiles or 228: the gradients take 630 -> 546 us); else 256.  One row tile of the
@@ -686,7 +694,7 @@ static size_t cut_bytes(int32_t dtype, int64_t rows, int64_t width, LinearWork* 
 
 static LinearWork forward_work(int32_t dtype, int64_t rows, int64_t vocab, int64_t width) {
   LinearWork w = {};
-  const int64_t r = rows < FORWARD_ROWS ? rows : FORWARD_ROWS;
+  const int64_t r = pass_rows(rows, vocab);
   w.step = tile_step(dtype, r, vocab, false);
   w.tiles = ceil_div(vocab, w.step);
   w.parts = cut_bytes(dtype, r, width, &w);
@@ -902,11 +910,12 @@ int externd_linear_logprobs(const void* x, int64_t x_stride, const void* weight,
   const LinearWork w = forward_work(dtype, rows, vocab, width);
   if (!workspace || workspace_bytes < w.bytes) return EXTERND_EWORKSPACE;
   const hipStream_t s = (hipStream_t)stream;
-  for (int64_t r = 0; r < rows; r += FORWARD_ROWS) {
+  const int64_t pass = pass_rows(rows, vocab);
+  for (int64_t r = 0; r < rows; r += pass) {
     LinearArgs a = {};
     a.x = {(const char*)x + r * x_stride * dtype_bytes(dtype), x_stride};
     a.weight = {weight, weight_stride};
-    a.rows = rows - r < FORWARD_ROWS ? rows - r : FORWARD_ROWS;
+    a.rows = rows - r < pass ? rows - r : pass;
     a.vocab = a.v1 = vocab;
     a.all_parts = (int)w.tiles;
     a.width = width;

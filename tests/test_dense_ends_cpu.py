@@ -163,3 +163,15 @@ def test_needs_a_gpu(name):
     args = {"embedding": 2, "embedding_backward": 3, "linear_logprobs": 2, "linear_logprobs_backward": 5, "clip_gradients": 1}[name]
     with pytest.raises(RuntimeError):
         getattr(binding, name)(*[torch.ones(2, 2)] * args)
+
+
+@pytest.mark.parametrize("dtype", [0, 1, 2])
+@pytest.mark.parametrize("vocab", [(1 << 25) - 256, (1 << 25) - 255, 1 << 25])
+@pytest.mark.parametrize("rows", [4097, 8064, 8065, 8192, 100000])
+def test_a_pass_of_rows_is_one_launch(dtype, vocab, rows):
+    """Tiles of 128 rows and 256 columns, 512 threads each, are fewer than 2^32 threads: from the workspace, which holds
+    16 bytes for each of a pass's rows and tiles of columns and 4 for each row."""
+    size = binding.lib().externd_linear_logprobs_workspace_bytes(dtype, rows, vocab, 64)
+    tiles = -(-vocab // 256)
+    of_a_pass = size // (16 * tiles)
+    assert 2048 <= of_a_pass <= rows and -(-of_a_pass // 128) * tiles * 512 < 1 << 32

@@ -116,3 +116,25 @@ def test_rows_of_zeros_and_infinities_in_fp16(ext):
     for rows in (x[4:5], x[4:5] * 0 + math.nan):      # no finite entry but zeros, or none
         gx, gw = ext.linear_logprobs_backward(rows.contiguous(), w, y[:1], far[:1], far[:1], g[:1])
         assert (gw[0] == 0).all() if rows[0, 0] == 0 else gw[0].isnan().all()
+
+
+@pytest.mark.parametrize("dtype,width", [("fp32", 4), ("bf16", 5)])
+def test_the_largest_launch(ext, dtype, width):
+    """8192 rows of 2^25 columns in tiles of 128 rows, which one launch cannot hold.  Logits are exact (whole numbers); lse
+    carries (n / 64 + 40) u + 4 u (1 + Z) of the sum of n exponentials and 2 u of itself: n / 64 u = 2^-5."""
+    vocab, rows = 1 << 25, 8192
+    t = TYPES[dtype][0]
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    w = (torch.randint(-3, 4, (vocab, width), generator=gen, device="cuda") * 0.5).to(t)
+    few = (torch.randint(-3, 4, (4, width), generator=gen, device="cuda") * 0.5).to(t)
+    y = torch.randint(0, vocab, (rows,), generator=gen, device="cuda")
+    y[0], y[rows - 1] = vocab - 1, 0
+    got = ext.linear_logprobs(few.repeat(rows // 4, 1), w, y)
+    torch.cuda.synchronize()
+    total = torch.zeros(4, dtype=torch.float64, device="cuda")
+    for v0 in range(0, vocab, 1 << 22):
+        total += torch.exp(few.double() @ w[v0:v0 + (1 << 22)].double().t().contiguous()).sum(1)
+    lse = torch.log(total).repeat(rows // 4)
+    z = (few.double().repeat(rows // 4, 1) * w[y].double()).sum(1)
+    assert ((got.lse - lse).abs() <= 2.0 ** -5 + 100 * U * (1 + lse.abs())).all()
+    assert ((got.logprob - (z - lse)).abs() <= 2.0 ** -5 + 100 * U * (1 + lse.abs() + z.abs())).all()
