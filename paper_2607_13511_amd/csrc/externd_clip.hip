@@ -138,8 +138,9 @@ __global__ __launch_bounds__(256) void k_scale(ClipList l, const double* partial
   const double ratio = max_norm / total;
   const bool whole = total == 0.0 || ratio >= 1.0 || max_norm == INFINITY;
   // a ratio that fp32 holds with fewer bits is split: half of its exponent, a power of two, is multiplied first, and
-  // what that takes below fp32's normal numbers ends as 0
-  const float before = ratio < 0x1p-100 && ratio > 0.0 ? exp2f((float)(ilogb(ratio) / 2)) : 1.f;
+  // what that takes below fp32's normal numbers ends as 0; so does every product with 2^-280, which is not split
+  // (from 2^-300 on half of the exponent would be none of fp32's powers, and the rest infinite)
+  const float before = ratio < 0x1p-100 && ratio > 0x1p-280 ? exp2f((float)(ilogb(ratio) / 2)) : 1.f;
   const float factor = whole ? 1.f : (float)(ratio / before);      // NaN: it stays
   // from the stretch's end, which k_squares read last and which may still be in the cache
   const uint32_t c0 = blockIdx.x * l.each, c1 = min(c0 + l.each, l.chunks);
