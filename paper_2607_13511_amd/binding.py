@@ -864,8 +864,9 @@ def _overlaps(a, b) -> bool:
     if not a.numel() or not b.numel():
         return False
     size, (a0, b0) = a.element_size(), (a.data_ptr(), b.data_ptr())
-    sa, sb = (t.stride(0) * size if t.shape[0] > 1 else t.shape[1] * size for t in (a, b))
     wa, wb = a.shape[1] * size, b.shape[1] * size
+    sa, sb = (t.stride(0) * size if t.shape[0] > 1 else None for t in (a, b))      # None: a single row, at any distance from the next
+    sa, sb = sa or sb or wa, sb or sa or wb
     if a0 >= b0 + (b.shape[0] - 1) * sb + wb or b0 >= a0 + (a.shape[0] - 1) * sa + wa:
         return False
     return not (sa == sb > 0 and (b0 - a0) % sa >= wa and (b0 - a0) % sa + wb <= sa)      # columns side by side in one buffer

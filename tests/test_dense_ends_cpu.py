@@ -175,3 +175,16 @@ def test_a_pass_of_rows_is_one_launch(dtype, vocab, rows):
     tiles = -(-vocab // 256)
     of_a_pass = size // (16 * tiles)
     assert 2048 <= of_a_pass <= rows and -(-of_a_pass // 128) * tiles * 512 < 1 << 32
+
+
+def test_views_of_one_buffer_overlap_where_bytes_are_shared():
+    """Against the sets of their entries: columns side by side, rows apart, one row or many."""
+    import torch
+    buf = torch.zeros(6, 10)
+    where = torch.arange(60).view(6, 10)
+    cuts = [(r0, r1, c0, c1) for r0 in range(6) for r1 in range(r0, 7) if r1 - r0 in (0, 1, 2, 6) for c0, c1 in ((0, 4), (4, 10), (0, 10), (3, 5), (9, 10))]
+    for a in cuts:
+        for b in cuts:
+            x, y = (buf[r0:r1, c0:c1] for r0, r1, c0, c1 in (a, b))
+            shared = set(where[a[0]:a[1], a[2]:a[3]].flatten().tolist()) & set(where[b[0]:b[1], b[2]:b[3]].flatten().tolist())
+            assert binding._overlaps(x, y) == bool(shared), (a, b)
