@@ -597,7 +597,7 @@ int externd_embedding(const void* table, int32_t dtype, int64_t vocab, int64_t w
  * embedding), and rows without tokens are left as they are; 0: they become 0.
  *  workspace  device, >= externd_embedding_backward_workspace_bytes(), 256-byte
  *             aligned (may be NULL with tokens = 0).
- * tokens <= 2^26, vocab < 2^31, width <= 2^20.                               */
+ * tokens <= 2^26, vocab < 2^31 - 1, width <= 2^20.                           */
 size_t externd_embedding_backward_workspace_bytes(int64_t tokens, int64_t vocab, int64_t width);  /* 0 on invalid arguments */
 int externd_embedding_backward(const void* grad, int32_t dtype, int64_t tokens, int64_t width, int64_t grad_stride,
                                const int64_t* ids, int64_t vocab, float scale, int32_t accumulate, void* grad_table,
@@ -640,7 +640,7 @@ int externd_linear_logprobs(const void* x, int64_t x_stride, const void* weight,
  *             need_x, need_weight = whether the outputs are given; 256-byte aligned.
  * Sums are fp32; G enters its products in dtype (rounded to bf16, or to fp16
  * below 2^15 with a power of two for each row, the target's entry with what it
- * loses; fp32 as three bf16 parts).  In fp16 grad_weight takes x with such
+ * loses; an entry that p makes large keeps its half unit; fp32 as three bf16 parts).  In fp16 grad_weight takes x with such
  * powers as well: of all rows' largest |x| (|g_logprob| + |g_entropy| (1 + entropy)),
  * times scale, 2^-38 is left out of a row's part.                            */
 size_t externd_linear_logprobs_backward_workspace_bytes(int32_t dtype, int64_t rows, int64_t vocab, int64_t width,

@@ -92,7 +92,6 @@ struct SortArgs {
   int64_t tokens, vocab;
   unsigned *keys[2], *places[2];            // sorted so far: the id (vocab where there is none) and the token
   // tokens past RANK_TOKENS: passes over digits of `bits` bits
-  int64_t per_wave;
   int blocks, passes, bits;
   unsigned* counts;                         // blocks x digits of the present pass
   int scanned;                              // counts are those of the blocks before, and one row more of all of them

@@ -7,7 +7,7 @@
 namespace externd {
 
 constexpr int64_t FORWARD_ROWS = 8192;                // of a pass at most (pass_rows)
-constexpr int64_t PIECE_ENTRIES = (int64_t)1 << 26;   // of G in a piece of the vocabulary, where rows allow it
+constexpr int64_t PIECE_ENTRIES = (int64_t)1 << 26;   // of G in a piece of the vocabulary, but eight tiles at least
 constexpr int CUS = 256;
 
 struct Part {
@@ -44,10 +44,12 @@ struct LinearArgs {
   RowInfo* info;
   // G enters its products in the type of x and weight: in bf16 and fp16 that is six
   // times as fast as fp32 parts, and the roundings of p in its many entries average
-  // out.  The target's entry, a row's one large one, does not: its rounding would be
-  // in all of the row's grad_x, and of the target's grad_weight, alike.  What it has
+  // out.  The target's entry, which g makes large in every row, does not: its rounding would
+  // be in all of the row's grad_x, and of the target's grad_weight, alike.  What it has
   // lost is added to both (2048 rows of 65537, bf16: error of the gradients 2.38e-3 ->
-  // 1.66e-3, which the rounding of the result alone makes; 1.3 % of the time).
+  // 1.66e-3, which the rounding of the result alone makes; 1.3 % of the time).  An
+  // entry that p makes large, where a row is sure of another token or of one under an
+  // entropy's gradient, keeps its rounding: half a unit of the type, as the result has.
   int32_t* target;                 // of a row that takes part, or -1
   float* rest;
   // fp16: a row's x is packed times x_up / up, so that G^T x is x_up times too large.
@@ -644,7 +646,9 @@ static bool linear_sizes(int64_t rows, int64_t vocab, int64_t width) {
   return rows <= (1 << 22) && vocab <= (1 << 25) && width <= (1 << 20) && rows * width <= (int64_t)1 << 33 && vocab * width <= (int64_t)1 << 37;
 }
 
-// Rows of a tile; operands that go through registers take 128 at most (256 would not leave enough of them).
+// Rows of a tile, as sizes are planned.  16-bit operands that go through registers have tiles of 128 rows
+// where this says 256 (which would not leave enough of them): twice the tiles that the plan counts, and
+// with a step of 128 columns half of each tile of 256 lies behind its end, masked.
 static int tile_rows(int32_t dtype, int64_t rows) {
   if (rows <= 32) return 32;
   return dtype == EXTERND_F32 || rows <= 128 ? 128 : 256;
@@ -704,8 +708,8 @@ static LinearWork forward_work(int32_t dtype, int64_t rows, int64_t vocab, int64
 }
 
 // Vocabulary of a piece, of which the last takes up to 255 more: G of a piece
-// stays below PIECE_ENTRIES where rows allow it, and among such pieces the one is
-// taken whose tiles leave the fewest rounds of the CUs partly empty (a round of
+// stays below PIECE_ENTRIES or is eight tiles of 256, whichever is more (2^22 rows: 2048
+// columns and the rest, 19 GB of bf16), and among such pieces the one is taken whose tiles leave the fewest rounds of the CUs partly empty (a round of
 // logits costs width, one of grad_weight rows).  2048 rows, 65537 x 2560: two of 32768,
 // 4 and 5 whole rounds, where three equal ones are 3 and 4 each: 2127 -> 2070 us.
 static int64_t choose_piece(int64_t rows, int64_t vocab, int64_t width, int64_t row_tiles, int64_t weight_tiles) {

@@ -188,3 +188,16 @@ def test_views_of_one_buffer_overlap_where_bytes_are_shared():
             x, y = (buf[r0:r1, c0:c1] for r0, r1, c0, c1 in (a, b))
             shared = set(where[a[0]:a[1], a[2]:a[3]].flatten().tolist()) & set(where[b[0]:b[1], b[2]:b[3]].flatten().tolist())
             assert binding._overlaps(x, y) == bool(shared), (a, b)
+
+
+@pytest.mark.parametrize("dtype,size", [(0, 4), (1, 2), (2, 2)])
+@pytest.mark.parametrize("vocab", [300, 2303, 2304, 40000])
+@pytest.mark.parametrize("rows", [1, 3000, 40000, 1 << 20, 1 << 22])
+def test_what_a_piece_of_G_takes(dtype, size, vocab, rows):
+    """A piece is up to 2^26 entries or eight tiles of 256 columns, whichever is more, the last one up to 255 columns more, in
+    rows an odd number of 256 entries apart: 512 more.  Beside it 40 bytes a row, grad_x's sums of up to 256 splits' tiles of
+    rows x 8 columns, and 8 KB."""
+    took = binding.lib().externd_linear_logprobs_backward_workspace_bytes(dtype, rows, vocab, 8, 1, 0)
+    columns = min(max((1 << 26) // rows, 2048), -(-vocab // 256) * 256) + 512
+    splits = max(1, 256 // -(-rows // 256))
+    assert rows * vocab * size * (vocab <= 2303) <= took <= rows * columns * size + rows * 40 + splits * rows * 32 + 8192 + 4 * rows
