@@ -30,6 +30,34 @@ static long columns(int64_t stride, int64_t count, int64_t K, int stages) {
   return wrong;
 }
 
+// The same of an operand by rows of K entries, of which `count` are there: no load past a row's end either.
+template <int X, int BK, int EV>
+static long rows(int64_t stride, int64_t count, int64_t K, int stages) {
+  typedef Direct<false, X, BK, EV> D;
+  const int64_t bytes = 16 / EV, steps = (K + BK - 1) / BK;
+  char* const p = (char*)((int64_t)1 << 44);
+  long wrong = 0;
+  for (int thread = 0; thread < GEMM_THREADS; thread++)
+    for (int64_t x0 : {(int64_t)0, (count - 1) / X * X}) {
+      D d;
+      d.init(Operand{p, stride}, x0, count - x0, 0, K, thread);
+      for (int64_t n = 0; n < stages + steps - 1; n++, d.next()) {
+        if (n == 4 && steps > 16) {      // on to the last steps
+          for (; n < steps - 4; n++) d.next();
+        }
+        for (int i = 0; i < D::LOADS; i++) {
+          int r, v;
+          D::T::place(i * GEMM_THREADS + thread, &r, &v);
+          if (d.k_left < BK && v * EV >= d.k_left) continue;      // as issue() has it
+          if (d.offset[i] > d.room() || d.room() - d.offset[i] < 16) continue;
+          const int64_t at = d.base + d.offset[i] - p, row = at / (stride * bytes), column = at % (stride * bytes);
+          wrong += at < 0 || row >= count || column + 16 > K * bytes || n >= steps;
+        }
+      }
+    }
+  return wrong;
+}
+
 int main() {
   const int64_t most = ((int64_t)1 << 25) + 768;      // the longest row of G
   long wrong = 0;
@@ -44,6 +72,17 @@ int main() {
         wrong += w;
       }
     }
+  for (int64_t stride : {(int64_t)264, (int64_t)4096, ((int64_t)1 << 22) - 8, most})
+    for (int64_t count : {(int64_t)1, (int64_t)3, (int64_t)32, (int64_t)100, (int64_t)300})
+      for (int64_t K : {(int64_t)8, (int64_t)256, (int64_t)264, stride}) {
+        if (K > stride || (stride == most && count > 32)) continue;      // G's rows: no more than a piece holds
+        long w = 0;
+        for (int stages : {2, 3, 4, 6})
+          w += rows<256, 64, 8>(stride, count, K, stages) + rows<128, 64, 8>(stride, count, K, stages) + rows<32, 64, 8>(stride, count, K, stages) +
+               rows<64, 256, 8>(stride, count, K, stages) + rows<256, 32, 4>(stride, count, K, stages);
+        if (w) printf("%lld rows of %lld, %lld k: %ld loads\n", (long long)count, (long long)stride, (long long)K, w);
+        wrong += w;
+      }
   printf("%ld loads outside\n", wrong);
   return wrong != 0;
 }
